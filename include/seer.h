@@ -25,6 +25,10 @@
  *   seer_lm_head_prepack,      synthetic LM head (one-time weight layout;
  *   seer_lm_head_predict,      argmax + confidence) and
  *   seer_remask_step           low-confidence remasking between steps
+ *   seer_page_plan,            paged keys and values: block tables and slot
+ *   seer_kv_store,             maps from the requests' lengths, rows into
+ *   seer_attn_paged,           their pages, attention over the pages, and
+ *   seer_attn_prompt           over packed prompts with grouped heads
  *
  * Conventions shared by every call:
  *   - Buffers are owned by the caller.  Pointers are device pointers unless a
@@ -464,6 +468,149 @@ int seer_lm_head_predict(const seer_dims* dims, const void* w_packed, int32_t vo
 int seer_remask_step(const seer_dims* dims, const int32_t* cu_seqlens, const int32_t* seqused, int32_t batch,
                      int32_t max_used, int32_t steps_left, const int32_t* pred, const float* conf, int32_t* tokens,
                      const void* x0, const void* emb, int32_t vocab, void* x_next, hipStream_t stream);
+
+/* ---- paged keys and values ------------------------------------------------
+ * The prefix cache above holds each sequence in one contiguous range.  For
+ * requests that come, grow, are cut and end beside each other, the keys and
+ * values live in pages of one pool per layer:
+ *   pool  [n_pages][2][n_kv_heads][page_size][head_dim]   K at [.][0], V at [.][1]
+ *   table [batch][table_width] int32: the pages of each request in order
+ * Token t of request b is slot t % page_size of page table[b][t / page_size].
+ * seer_page_plan keeps the table, seer_kv_store fills the pages, and
+ * seer_attn_paged reads them: for the next token of each request, for a tree
+ * of drafted tokens, for a further part of a prompt, or for the window of a
+ * denoising step (every row sees every key, Sec. 3.6).  seer_attn_prompt is
+ * the causal attention of prompts whose keys and values are still packed rows.
+ * Attention only: the projections around it are the caller's. */
+
+/* Pages of a pool.  page_size: 16, 32, 64, 128 or 256 tokens;
+ * n_pages * page_size < 2^31. */
+typedef struct seer_page_desc {
+  int32_t page_size;
+  int32_t n_pages;
+  int32_t table_width;   /* entries of a request's row of the table */
+} seer_page_desc;
+
+/* Heads of the attention calls.  n_heads is a multiple of n_kv_heads: query
+ * head h reads key/value head h / (n_heads / n_kv_heads).  dtype: bf16 with
+ * head_dim 64 or 128, or fp32 with head_dim <= 128 and head_dim % 4 == 0.
+ * scale multiplies q . k; 0 means 1 / sqrt(head_dim). */
+typedef struct seer_attn_desc {
+  int32_t n_heads;
+  int32_t n_kv_heads;
+  int32_t head_dim;
+  int32_t dtype;         /* SEER_DTYPE_* of q, k, v and the output */
+  int32_t flags;         /* SEER_ATTN_* */
+  float scale;
+} seer_attn_desc;
+
+/* seer_attn_desc.flags: V (rows and pages) is fp16 beside bf16 q and k, the
+ * element types of a bf16 layer's qkv rows. */
+#define SEER_ATTN_V_F16 1
+
+/* Which keys a query row sees. */
+#define SEER_MASK_NONE   0   /* every key of its request */
+#define SEER_MASK_CAUSAL 1   /* keys up to its own position */
+#define SEER_MASK_TREE   2   /* the cached context, and the rows of the call that its bits name */
+
+/* seer_page_plan status bits. */
+#define SEER_PAGES_EXHAUSTED 1   /* not enough free pages */
+#define SEER_PAGES_WIDTH     2   /* a request needs more pages than a row of the table has entries */
+#define SEER_PAGES_INVALID   4   /* a length or the free count contradicts another argument */
+
+/* Bytes of one pool (0 for a bad description). */
+size_t seer_page_pool_bytes(const seer_attn_desc* desc, const seer_page_desc* pages);
+
+/* The pages of a step, one launch, nothing read back.  Request b's row of the
+ * table holds the pages of held[b] tokens, of which the first keep[b] stay
+ * (keep[b] <= held[b]: a window cut at its boundary, drafted tokens that were
+ * refused; 0 for a request that has ended), and the call's rows
+ * [cu_seqlens[b], cu_seqlens[b+1]), the first seqused[b] of them real (NULL:
+ * all), are to follow.  With H = ceil(held / page_size) and N = ceil((keep +
+ * real rows) / page_size):
+ *   table[b][N .. H) (N < H) go back to the free pages; those entries keep
+ *                    their values, which mean nothing from then on;
+ *   table[b][H .. N) (N > H) are taken from them;
+ *   kv_len[b] = keep + real rows, the held[b] of the next call;
+ *   slots[r] = page * page_size + slot of row r, -1 for rows that are padding
+ *              and for rows from cu_seqlens[batch] up to rows_ub.
+ * Free pages are a stack free_pages[n_pages] with *free_in entries: all pages
+ * given back are put on it first, in order of request and entry, then pages
+ * are taken off its top in the same order, so a call may take what it gives
+ * back.  *free_out is the new number of entries; entries from there on are
+ * left as they were.
+ * *status: 0, or SEER_PAGES_* bits; then nothing is taken or given back:
+ * table and free_pages stay, *free_out = *free_in, kv_len[b] = held[b], every
+ * slot is -1.
+ * All pointers are device pointers; slots may be NULL where rows_ub is 0.
+ * free_out may not be free_in, kv_len neither held nor keep: a program keeps
+ * two of each and alternates.
+ * Errors: EINVAL (null pointers, batch < 1, rows_ub < 0, bad description, the
+ * aliases above), EUNSUPPORTED (batch > 4096, page_size). */
+int seer_page_plan(const seer_page_desc* pages, const int32_t* held, const int32_t* keep, const int32_t* cu_seqlens,
+                   const int32_t* seqused, int32_t batch, int32_t rows_ub, int32_t* free_pages,
+                   const int32_t* free_in, int32_t* free_out, int32_t* table, int32_t* kv_len, int32_t* slots,
+                   int32_t* status, hipStream_t stream);
+
+/* Copy key and value rows into their pages: row r < rows_ub of k and of v
+ * (n_kv_heads * head_dim elements, rows k_stride and v_stride elements apart)
+ * to slot slots[r] of the pool.  Rows whose slot is negative or past the pool
+ * are skipped.  The slots of one call are distinct (of two rows with one slot
+ * each 16-byte piece is from one or the other).
+ * Errors: EINVAL (null pointers, rows_ub < 1, bad descriptions, rows, strides
+ * or pool not aligned to 16 bytes, a stride below the row), EUNSUPPORTED. */
+int seer_kv_store(const seer_attn_desc* desc, const seer_page_desc* pages, const void* k, int64_t k_stride,
+                  const void* v, int64_t v_stride, int32_t rows_ub, const int32_t* slots, void* pool,
+                  hipStream_t stream);
+
+/* Workspace bytes of the attention calls for up to rows_ub rows in batch
+ * sequences: the partial results of launches that split the keys.  0 for a
+ * bad description. */
+size_t seer_attn_workspace_bytes(const seer_attn_desc* desc, int32_t rows_ub, int32_t batch);
+
+/* Attention of packed prompts: for row i of a sequence and head h
+ *     out = sum_j p_j v_j,  p = softmax_j (scale q . k_j)
+ * over the keys j <= i of the same sequence (SEER_MASK_CAUSAL) or all of them
+ * (SEER_MASK_NONE).  q, out: rows of n_heads * head_dim elements, k and v of
+ * n_kv_heads * head_dim, each with its own row stride in elements, so that
+ * q | k | v rows of one projection are read in place.  seqused: optional; rows
+ * at or past seqused[b] are no keys and get a zero output.  Rows
+ * [0, cu_seqlens[batch]) are read and written, no others.
+ * Precision: products of the given types summed in fp32; the softmax's
+ * statistics and the sums are fp32; the probabilities are rounded to V's type
+ * for the second product (bf16, fp16, or none for fp32).  A key that a row
+ * does not see has no part in it, whatever its k and v hold (NaN, infinity).
+ * workspace: seer_attn_workspace_bytes, 256-byte aligned; it holds nothing
+ * between calls.
+ * Errors: EINVAL (null pointers, batch or rows_ub < 1, an unknown mask or
+ * SEER_MASK_TREE, rows or strides not aligned to 16 bytes, a stride below the
+ * row, out equal to q, k or v), EUNSUPPORTED (desc; rows_ub * n_heads >= 2^31),
+ * EWORKSPACE. */
+int seer_attn_prompt(const seer_attn_desc* desc, int32_t mask, const void* q, int64_t q_stride, const void* k,
+                     int64_t k_stride, const void* v, int64_t v_stride, void* out, int64_t out_stride,
+                     int32_t rows_ub, const int32_t* cu_seqlens, const int32_t* seqused, int32_t batch,
+                     void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* The same over pages: request b's keys are its kv_len[b] cached tokens, the
+ * last n of them those of the call's n real rows (as seer_page_plan and
+ * seer_kv_store leave them): row i stands at position p_i = kv_len[b] - n + i.
+ *   SEER_MASK_NONE    row i sees every key: a denoising step's window
+ *   SEER_MASK_CAUSAL  keys at positions <= p_i: single tokens, parts of a prompt
+ *   SEER_MASK_TREE    positions below kv_len[b] - n, and row j of the call where
+ *                     bit j % 64 of tree_bits[r][j / 64] is set (r: the row's
+ *                     index in the call, tree_words 64-bit words a row); a row
+ *                     sees itself only if its own bit is set.  Rows from
+ *                     64 tree_words on are seen by none.
+ * A row that sees no key gets a zero output.  Keys on a page whose table entry
+ * is outside [0, n_pages) are seen by no row, and kv_len[b] counts up to
+ * table_width * page_size.  tree_bits: NULL unless SEER_MASK_TREE.
+ * Errors: as seer_attn_prompt; EINVAL (pages, tree_bits NULL or tree_words < 1
+ * with SEER_MASK_TREE). */
+int seer_attn_paged(const seer_attn_desc* desc, const seer_page_desc* pages, int32_t mask, const void* q,
+                    int64_t q_stride, void* out, int64_t out_stride, int32_t rows_ub, const int32_t* cu_seqlens,
+                    const int32_t* seqused, int32_t batch, const void* pool, const int32_t* table,
+                    const int32_t* kv_len, const uint64_t* tree_bits, int32_t tree_words, void* workspace,
+                    size_t workspace_bytes, hipStream_t stream);
 
 /* ---- recorded launch sequences (Sec. 3.5) -------------------------------
  * The graph-compatible execution paths replay a fixed launch sequence.  Every

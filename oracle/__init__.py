@@ -15,6 +15,8 @@ Modules (each function cites the passage of the paper it follows):
   pipeline  -- step 0 detection, one-shot truncation, truncated steps
   kvcache   -- truncated steps on the window rows with the prefix's keys and
                values cached (Appendix D, KV-cache compatibility)
+  paged     -- keys and values in pages: the book-keeping of a step, and the
+               attention over pages and prompts (Appendix D, Sec. 3.6)
   rope      -- rotary position embedding of queries and keys (the paper is
                silent on positions; RoFormer's definition, rotate-half pairs)
 

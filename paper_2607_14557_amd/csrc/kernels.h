@@ -280,4 +280,72 @@ int launch_prepack(const PrepackParams& p, hipStream_t s);
 // in the fragment-major order of frag_b_index.
 int launch_pack_frag(const void* src, int N, int K, void* dst, hipStream_t s);
 
+// ---- paged keys and values ---------------------------------------------------
+
+// status bits of the plan (SEER_PAGES_*)
+constexpr int kPagesExhausted = SEER_PAGES_EXHAUSTED;
+constexpr int kPagesWidth = SEER_PAGES_WIDTH;
+constexpr int kPagesInvalid = SEER_PAGES_INVALID;
+constexpr int kPlanMaxBatch = 4096;
+
+struct PagePlanParams {
+  int shift;             // log2 of the tokens of a page
+  int n_pages;
+  int width;             // entries of a row of the table
+  const int* held;
+  const int* keep;
+  const int* cu;
+  const int* used;       // [B] or null
+  int B;
+  int rows_ub;
+  int* free_pages;
+  const int* free_in;
+  int* free_out;
+  int* table;
+  int* kv_len;
+  int* slots;
+  int* status;
+};
+int launch_page_plan(const PagePlanParams& p, hipStream_t s);
+
+struct KvStoreParams {
+  const uint8_t* k;
+  const uint8_t* v;
+  size_t k_stride, v_stride;   // bytes
+  int rows_ub;
+  const int* slots;
+  uint8_t* pool;
+  int shift, n_pages, n_kv;
+  int head_pieces;             // 16-byte pieces of a head's row
+};
+int launch_kv_store(const KvStoreParams& p, hipStream_t s);
+
+constexpr int kMaskNone = SEER_MASK_NONE;
+constexpr int kMaskCausal = SEER_MASK_CAUSAL;
+constexpr int kMaskTree = SEER_MASK_TREE;
+
+// Attention with grouped heads: k and v are rows (k_stride, v_stride) or, with
+// a table, the pool.  Strides in elements.
+struct GqaParams {
+  const void* q;
+  const void* k;
+  const void* v;
+  void* out;
+  long long q_stride, k_stride, v_stride, o_stride;
+  const int* cu;               // [B+1]
+  const int* used;             // [B] or null
+  int B;
+  int rows_ub;
+  int n_heads, n_kv, head_dim;
+  float scale;
+  int mask;                    // kMask*
+  bool bf16, v_f16;
+  const int* table;            // [B][width] or null
+  const int* kv_len;           // [B]
+  int shift, n_pages, width;
+  const unsigned long long* bits;   // [rows][words]
+  int words;
+};
+int launch_gqa(const GqaParams& p, hipStream_t s);
+
 }  // namespace seer

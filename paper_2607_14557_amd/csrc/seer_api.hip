@@ -1,6 +1,6 @@
 // C ABI of the Seer hot path: argument checks, workspace layout and the launch
 // sequence of each entry point.  Kernels live in gemm_bf16.hip, attn_bf16.hip,
-// f32_kernels.hip and rows.hip.
+// f32_kernels.hip, rows.hip, pages.hip and attn_gqa.hip.
 #include <math.h>
 #include <stdarg.h>
 #include <stdio.h>
@@ -662,6 +662,186 @@ int seer_remask_step(const seer_dims* dims, const int32_t* cu_seqlens, const int
   p.x0 = static_cast<const uint16_t*>(x0); p.emb = static_cast<const uint16_t*>(emb); p.vocab = vocab;
   p.x_next = static_cast<uint16_t*>(x_next); p.d = dims->d_model;
   if (seer::launch_remask(p, stream)) return hip_fail("remask launch");
+  return ok();
+}
+
+// ---- paged keys and values ---------------------------------------------------
+
+static int check_heads(const seer_attn_desc* d) {
+  if (!d) return fail(SEER_EINVAL, "desc is NULL");
+  if (d->n_heads < 1 || d->n_kv_heads < 1 || d->head_dim < 1)
+    return fail(SEER_EINVAL, "head counts and head_dim must be positive (got %d, %d, %d)", d->n_heads, d->n_kv_heads,
+                d->head_dim);
+  if (d->n_heads % d->n_kv_heads != 0)
+    return fail(SEER_EINVAL, "n_heads (%d) must be a multiple of n_kv_heads (%d)", d->n_heads, d->n_kv_heads);
+  if (!isfinite(d->scale)) return fail(SEER_EINVAL, "scale must be finite");
+  if (d->flags & ~SEER_ATTN_V_F16) return fail(SEER_EINVAL, "unknown flags %d", d->flags);
+  if (d->dtype == SEER_DTYPE_BF16) {
+    if (d->head_dim != 64 && d->head_dim != 128)
+      return fail(SEER_EUNSUPPORTED, "bf16 attention needs head_dim 64 or 128 (got %d)", d->head_dim);
+  } else if (d->dtype == SEER_DTYPE_F32) {
+    if (d->flags & SEER_ATTN_V_F16) return fail(SEER_EINVAL, "SEER_ATTN_V_F16 goes with bf16");
+    if (d->head_dim > 128 || d->head_dim % 4 != 0)
+      return fail(SEER_EUNSUPPORTED, "fp32 attention needs head_dim <= 128, a multiple of 4 (got %d)", d->head_dim);
+  } else {
+    return fail(SEER_EUNSUPPORTED, "unknown dtype %d", d->dtype);
+  }
+  if ((long long)d->n_heads * d->head_dim > (1 << 24))
+    return fail(SEER_EUNSUPPORTED, "n_heads * head_dim must stay below 2^24");
+  return SEER_OK;
+}
+
+static int check_pages(const seer_page_desc* p) {
+  if (!p) return fail(SEER_EINVAL, "pages is NULL");
+  if (p->n_pages < 1 || p->table_width < 1)
+    return fail(SEER_EINVAL, "n_pages and table_width must be positive (got %d, %d)", p->n_pages, p->table_width);
+  if (p->page_size < 16 || p->page_size > 256 || (p->page_size & (p->page_size - 1)) != 0)
+    return fail(SEER_EUNSUPPORTED, "page_size must be 16, 32, 64, 128 or 256 (got %d)", p->page_size);
+  if ((long long)p->n_pages * p->page_size >= (1ll << 31))
+    return fail(SEER_EINVAL, "n_pages * page_size must stay below 2^31");
+  return SEER_OK;
+}
+
+static int page_shift(const seer_page_desc* p) {
+  int s = 0;
+  while ((1 << s) < p->page_size) ++s;
+  return s;
+}
+
+size_t seer_page_pool_bytes(const seer_attn_desc* desc, const seer_page_desc* pages) {
+  if (check_heads(desc) != SEER_OK || check_pages(pages) != SEER_OK) return 0;
+  return (size_t)pages->n_pages * 2 * desc->n_kv_heads * pages->page_size * desc->head_dim *
+         (desc->dtype == SEER_DTYPE_BF16 ? 2 : 4);
+}
+
+int seer_page_plan(const seer_page_desc* pages, const int32_t* held, const int32_t* keep, const int32_t* cu_seqlens,
+                   const int32_t* seqused, int32_t batch, int32_t rows_ub, int32_t* free_pages,
+                   const int32_t* free_in, int32_t* free_out, int32_t* table, int32_t* kv_len, int32_t* slots,
+                   int32_t* status, hipStream_t stream) {
+  int rc = check_pages(pages);
+  if (rc) return rc;
+  if (!held || !keep || !cu_seqlens || !free_pages || !free_in || !free_out || !table || !kv_len || !status)
+    return fail(SEER_EINVAL, "a required pointer is NULL");
+  if (batch < 1 || batch > seer::kPlanMaxBatch)
+    return fail(batch < 1 ? SEER_EINVAL : SEER_EUNSUPPORTED, "batch must be in [1, %d] (got %d)", seer::kPlanMaxBatch,
+                batch);
+  if (rows_ub < 0) return fail(SEER_EINVAL, "rows_ub must be >= 0");
+  if (rows_ub > 0 && !slots) return fail(SEER_EINVAL, "slots is NULL");
+  if (free_in == free_out || kv_len == held || kv_len == keep)
+    return fail(SEER_EINVAL, "free_out may not be free_in, kv_len neither held nor keep");
+  seer::PagePlanParams p{};
+  p.shift = page_shift(pages); p.n_pages = pages->n_pages; p.width = pages->table_width;
+  p.held = held; p.keep = keep; p.cu = cu_seqlens; p.used = seqused; p.B = batch; p.rows_ub = rows_ub;
+  p.free_pages = free_pages; p.free_in = free_in; p.free_out = free_out;
+  p.table = table; p.kv_len = kv_len; p.slots = slots; p.status = status;
+  if (seer::launch_page_plan(p, stream)) return hip_fail("page plan launch");
+  return ok();
+}
+
+// a row operand: not null, 16-byte aligned, rows of `width` elements `stride` apart
+static int check_rows(const char* name, const void* ptr, int64_t stride, int64_t width, int es) {
+  if (!ptr) return fail(SEER_EINVAL, "%s is NULL", name);
+  if (!aligned(ptr, 16) || stride * es % 16 != 0)
+    return fail(SEER_EINVAL, "%s and its rows must be 16-byte aligned (row stride %lld elements)", name, (long long)stride);
+  if (stride < width || stride > (1ll << 40))
+    return fail(SEER_EINVAL, "the row stride of %s (%lld) is not one of rows of %lld elements", name, (long long)stride,
+                (long long)width);
+  return SEER_OK;
+}
+
+int seer_kv_store(const seer_attn_desc* desc, const seer_page_desc* pages, const void* k, int64_t k_stride,
+                  const void* v, int64_t v_stride, int32_t rows_ub, const int32_t* slots, void* pool,
+                  hipStream_t stream) {
+  int rc = check_heads(desc);
+  if (rc) return rc;
+  rc = check_pages(pages);
+  if (rc) return rc;
+  const int es = desc->dtype == SEER_DTYPE_BF16 ? 2 : 4;
+  const int64_t width = (int64_t)desc->n_kv_heads * desc->head_dim;
+  if ((rc = check_rows("k", k, k_stride, width, es)) || (rc = check_rows("v", v, v_stride, width, es))) return rc;
+  if (rows_ub < 1) return fail(SEER_EINVAL, "rows_ub must be >= 1 (got %d)", rows_ub);
+  if (!slots || !pool) return fail(SEER_EINVAL, "a required pointer is NULL");
+  if (!aligned(pool, 16)) return fail(SEER_EINVAL, "pool must be 16-byte aligned");
+  seer::KvStoreParams p{};
+  p.k = static_cast<const uint8_t*>(k); p.v = static_cast<const uint8_t*>(v);
+  p.k_stride = (size_t)k_stride * es; p.v_stride = (size_t)v_stride * es;
+  p.rows_ub = rows_ub; p.slots = slots; p.pool = static_cast<uint8_t*>(pool);
+  p.shift = page_shift(pages); p.n_pages = pages->n_pages; p.n_kv = desc->n_kv_heads;
+  p.head_pieces = desc->head_dim * es / 16;
+  if (seer::launch_kv_store(p, stream)) return hip_fail("kv store launch");
+  return ok();
+}
+
+size_t seer_attn_workspace_bytes(const seer_attn_desc* desc, int32_t rows_ub, int32_t batch) {
+  if (check_heads(desc) != SEER_OK || rows_ub < 0 || batch < 0) return 0;
+  return 256;
+}
+
+// what both attention calls check and fill in
+static int gqa_params(seer::GqaParams& p, const seer_attn_desc* desc, int32_t mask, const void* q, int64_t q_stride,
+                      void* out, int64_t out_stride, int32_t rows_ub, const int32_t* cu_seqlens,
+                      const int32_t* seqused, int32_t batch, void* workspace, size_t workspace_bytes) {
+  int rc = check_heads(desc);
+  if (rc) return rc;
+  if (mask < SEER_MASK_NONE || mask > SEER_MASK_TREE) return fail(SEER_EINVAL, "unknown mask %d", mask);
+  const int es = desc->dtype == SEER_DTYPE_BF16 ? 2 : 4;
+  const int64_t width = (int64_t)desc->n_heads * desc->head_dim;
+  if ((rc = check_rows("q", q, q_stride, width, es)) || (rc = check_rows("out", out, out_stride, width, es))) return rc;
+  if (q == out) return fail(SEER_EINVAL, "out may not alias an input");
+  if (!cu_seqlens || !workspace) return fail(SEER_EINVAL, "a required pointer is NULL");
+  if (batch < 1) return fail(SEER_EINVAL, "batch must be >= 1 (got %d)", batch);
+  if (rows_ub < 1) return fail(SEER_EINVAL, "rows_ub must be >= 1 (got %d)", rows_ub);
+  if ((long long)rows_ub * desc->n_heads >= (1ll << 31))
+    return fail(SEER_EUNSUPPORTED, "rows_ub * n_heads must stay below 2^31 (got %d * %d)", rows_ub, desc->n_heads);
+  if (!aligned(workspace, 256)) return fail(SEER_EINVAL, "workspace must be 256-byte aligned");
+  const size_t need = seer_attn_workspace_bytes(desc, rows_ub, batch);
+  if (workspace_bytes < need) return fail(SEER_EWORKSPACE, "workspace holds %zu bytes, need %zu", workspace_bytes, need);
+  p.q = q; p.out = out; p.q_stride = q_stride; p.o_stride = out_stride;
+  p.cu = cu_seqlens; p.used = seqused; p.B = batch; p.rows_ub = rows_ub;
+  p.n_heads = desc->n_heads; p.n_kv = desc->n_kv_heads; p.head_dim = desc->head_dim;
+  p.scale = desc->scale != 0.0f ? desc->scale : 1.0f / sqrtf((float)desc->head_dim);
+  p.mask = mask; p.bf16 = desc->dtype == SEER_DTYPE_BF16; p.v_f16 = (desc->flags & SEER_ATTN_V_F16) != 0;
+  return SEER_OK;
+}
+
+int seer_attn_prompt(const seer_attn_desc* desc, int32_t mask, const void* q, int64_t q_stride, const void* k,
+                     int64_t k_stride, const void* v, int64_t v_stride, void* out, int64_t out_stride,
+                     int32_t rows_ub, const int32_t* cu_seqlens, const int32_t* seqused, int32_t batch,
+                     void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  seer::GqaParams p{};
+  int rc = gqa_params(p, desc, mask, q, q_stride, out, out_stride, rows_ub, cu_seqlens, seqused, batch, workspace,
+                      workspace_bytes);
+  if (rc) return rc;
+  if (mask == SEER_MASK_TREE) return fail(SEER_EINVAL, "SEER_MASK_TREE is for seer_attn_paged");
+  const int es = p.bf16 ? 2 : 4;
+  const int64_t width = (int64_t)p.n_kv * p.head_dim;
+  if ((rc = check_rows("k", k, k_stride, width, es)) || (rc = check_rows("v", v, v_stride, width, es))) return rc;
+  if (out == k || out == v) return fail(SEER_EINVAL, "out may not alias an input");
+  p.k = k; p.v = v; p.k_stride = k_stride; p.v_stride = v_stride;
+  if (seer::launch_gqa(p, stream)) return hip_fail("prompt attention launch");
+  return ok();
+}
+
+int seer_attn_paged(const seer_attn_desc* desc, const seer_page_desc* pages, int32_t mask, const void* q,
+                    int64_t q_stride, void* out, int64_t out_stride, int32_t rows_ub, const int32_t* cu_seqlens,
+                    const int32_t* seqused, int32_t batch, const void* pool, const int32_t* table,
+                    const int32_t* kv_len, const uint64_t* tree_bits, int32_t tree_words, void* workspace,
+                    size_t workspace_bytes, hipStream_t stream) {
+  seer::GqaParams p{};
+  int rc = gqa_params(p, desc, mask, q, q_stride, out, out_stride, rows_ub, cu_seqlens, seqused, batch, workspace,
+                      workspace_bytes);
+  if (rc) return rc;
+  rc = check_pages(pages);
+  if (rc) return rc;
+  if (!pool || !table || !kv_len) return fail(SEER_EINVAL, "a required pointer is NULL");
+  if (!aligned(pool, 16)) return fail(SEER_EINVAL, "pool must be 16-byte aligned");
+  if (out == pool) return fail(SEER_EINVAL, "out may not alias an input");
+  if (mask == SEER_MASK_TREE && (!tree_bits || tree_words < 1))
+    return fail(SEER_EINVAL, "SEER_MASK_TREE needs tree_bits and tree_words >= 1");
+  p.k = pool; p.v = pool; p.table = table; p.kv_len = kv_len;
+  p.shift = page_shift(pages); p.n_pages = pages->n_pages; p.width = pages->table_width;
+  p.bits = reinterpret_cast<const unsigned long long*>(tree_bits); p.words = tree_words;
+  if (seer::launch_gqa(p, stream)) return hip_fail("paged attention launch");
   return ok();
 }
 

@@ -18,6 +18,9 @@ SEER_ROUTE_HYBRID, SEER_ROUTE_NAIVE_PAD, SEER_ROUTE_VARLEN_ONLY = 0, 1, 2
 SEER_PATH_STATIC, SEER_PATH_VARLEN, SEER_PATH_EAGER = 0, 1, 2
 SEER_REPACK_WINDOW_ONLY = 1
 SEER_STATUS_V_RANGE = 1
+SEER_ATTN_V_F16 = 1
+SEER_MASK_NONE, SEER_MASK_CAUSAL, SEER_MASK_TREE = 0, 1, 2
+SEER_PAGES_EXHAUSTED, SEER_PAGES_WIDTH, SEER_PAGES_INVALID = 1, 2, 4
 
 EXPORTED = ("seer_prepacked_bytes", "seer_prepack_weights", "seer_layer_workspace_bytes",
             "seer_layer_status_reset", "seer_layer_workspace_offsets", "seer_layer_forward_varlen",
@@ -26,7 +29,9 @@ EXPORTED = ("seer_prepacked_bytes", "seer_prepack_weights", "seer_layer_workspac
             "seer_layer_forward_detect_timed", "seer_batch_repack",
             "seer_layer_forward_cached", "seer_kv_export", "seer_graph_begin", "seer_graph_end",
             "seer_graph_launch", "seer_graph_destroy", "seer_lm_head_workspace_bytes", "seer_lm_head_prepack",
-            "seer_lm_head_predict", "seer_remask_step", "seer_last_error", "seer_abi_version")
+            "seer_lm_head_predict", "seer_remask_step", "seer_page_pool_bytes", "seer_page_plan", "seer_kv_store",
+            "seer_attn_workspace_bytes", "seer_attn_prompt", "seer_attn_paged", "seer_last_error",
+            "seer_abi_version")
 
 
 class SeerError(RuntimeError):
@@ -64,6 +69,15 @@ class seer_route_ctrl(ctypes.Structure):
                 ("n_eager", ctypes.c_int32), ("n_groups", ctypes.c_int32),
                 ("max_alloc", ctypes.c_int32), ("status", ctypes.c_int32),
                 ("ready", ctypes.c_int32), ("reserved", ctypes.c_int32 * 7)]
+
+
+class seer_page_desc(ctypes.Structure):
+    _fields_ = [("page_size", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("table_width", ctypes.c_int32)]
+
+
+class seer_attn_desc(ctypes.Structure):
+    _fields_ = [("n_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("flags", ctypes.c_int32), ("scale", ctypes.c_float)]
 
 
 _lib = None
@@ -137,6 +151,20 @@ def load_library():
     L.seer_graph_launch.restype = ctypes.c_int
     L.seer_graph_destroy.argtypes = [_P]
     L.seer_graph_destroy.restype = ctypes.c_int
+    heads, pages, _L = ctypes.POINTER(seer_attn_desc), ctypes.POINTER(seer_page_desc), ctypes.c_int64
+    L.seer_page_pool_bytes.argtypes = [heads, pages]
+    L.seer_page_pool_bytes.restype = ctypes.c_size_t
+    L.seer_page_plan.argtypes = [pages, _P, _P, _P, _P, _I, _I, _P, _P, _P, _P, _P, _P, _P, _P]
+    L.seer_page_plan.restype = ctypes.c_int
+    L.seer_kv_store.argtypes = [heads, pages, _P, _L, _P, _L, _I, _P, _P, _P]
+    L.seer_kv_store.restype = ctypes.c_int
+    L.seer_attn_workspace_bytes.argtypes = [heads, _I, _I]
+    L.seer_attn_workspace_bytes.restype = ctypes.c_size_t
+    L.seer_attn_prompt.argtypes = [heads, _I, _P, _L, _P, _L, _P, _L, _P, _L, _I, _P, _P, _I, _P, ctypes.c_size_t, _P]
+    L.seer_attn_prompt.restype = ctypes.c_int
+    L.seer_attn_paged.argtypes = [heads, pages, _I, _P, _L, _P, _L, _I, _P, _P, _I, _P, _P, _P, _P, _I, _P,
+                                  ctypes.c_size_t, _P]
+    L.seer_attn_paged.restype = ctypes.c_int
     L.seer_last_error.argtypes = []
     L.seer_last_error.restype = ctypes.c_char_p
     L.seer_abi_version.argtypes = []
@@ -328,3 +356,44 @@ def seer_remask_step(dims, cu_seqlens, seqused, batch, max_used, steps_left, pre
     _check(load_library().seer_remask_step(
         ctypes.byref(dims), _ptr(cu_seqlens), _ptr(seqused), int(batch), int(max_used), int(steps_left),
         _ptr(pred), _ptr(conf), _ptr(tokens), _ptr(x0), _ptr(emb), int(vocab), _ptr(x_next), _stream(stream)))
+
+
+def seer_page_pool_bytes(desc, pages):
+    return load_library().seer_page_pool_bytes(ctypes.byref(desc), ctypes.byref(pages))
+
+
+def seer_page_plan(pages, held, keep, cu_seqlens, seqused, batch, rows_ub, free_pages, free_in, free_out, table,
+                   kv_len, slots, status, stream=None):
+    _check(load_library().seer_page_plan(
+        ctypes.byref(pages), _ptr(held), _ptr(keep), _ptr(cu_seqlens), _ptr(seqused), int(batch), int(rows_ub),
+        _ptr(free_pages), _ptr(free_in), _ptr(free_out), _ptr(table), _ptr(kv_len), _ptr(slots), _ptr(status),
+        _stream(stream)))
+
+
+def seer_kv_store(desc, pages, k, k_stride, v, v_stride, rows_ub, slots, pool, stream=None):
+    """k_stride, v_stride: elements from one row to the next."""
+    _check(load_library().seer_kv_store(
+        ctypes.byref(desc), ctypes.byref(pages), _ptr(k), int(k_stride), _ptr(v), int(v_stride), int(rows_ub),
+        _ptr(slots), _ptr(pool), _stream(stream)))
+
+
+def seer_attn_workspace_bytes(desc, rows_ub, batch):
+    return load_library().seer_attn_workspace_bytes(ctypes.byref(desc), int(rows_ub), int(batch))
+
+
+def seer_attn_prompt(desc, mask, q, q_stride, k, k_stride, v, v_stride, out, out_stride, rows_ub, cu_seqlens,
+                     seqused, batch, workspace, workspace_bytes=None, stream=None):
+    nbytes = workspace_bytes if workspace_bytes is not None else workspace.numel() * workspace.element_size()
+    _check(load_library().seer_attn_prompt(
+        ctypes.byref(desc), int(mask), _ptr(q), int(q_stride), _ptr(k), int(k_stride), _ptr(v), int(v_stride),
+        _ptr(out), int(out_stride), int(rows_ub), _ptr(cu_seqlens), _ptr(seqused), int(batch), _ptr(workspace),
+        nbytes, _stream(stream)))
+
+
+def seer_attn_paged(desc, pages, mask, q, q_stride, out, out_stride, rows_ub, cu_seqlens, seqused, batch, pool, table,
+                    kv_len, tree_bits, tree_words, workspace, workspace_bytes=None, stream=None):
+    nbytes = workspace_bytes if workspace_bytes is not None else workspace.numel() * workspace.element_size()
+    _check(load_library().seer_attn_paged(
+        ctypes.byref(desc), ctypes.byref(pages), int(mask), _ptr(q), int(q_stride), _ptr(out), int(out_stride),
+        int(rows_ub), _ptr(cu_seqlens), _ptr(seqused), int(batch), _ptr(pool), _ptr(table), _ptr(kv_len),
+        _ptr(tree_bits), int(tree_words), _ptr(workspace), nbytes, _stream(stream)))
