@@ -494,7 +494,8 @@ typedef struct seer_page_desc {
 /* Heads of the attention calls.  n_heads is a multiple of n_kv_heads: query
  * head h reads key/value head h / (n_heads / n_kv_heads).  dtype: bf16 with
  * head_dim 64 or 128, or fp32 with head_dim <= 128 and head_dim % 4 == 0.
- * scale multiplies q . k; 0 means 1 / sqrt(head_dim). */
+ * scale >= 0 multiplies q . k; 0 means 1 / sqrt(head_dim).  Row strides are at
+ * most 2^24 elements. */
 typedef struct seer_attn_desc {
   int32_t n_heads;
   int32_t n_kv_heads;

@@ -1,111 +1,661 @@
-// Attention with grouped heads over packed rows or pages.
-#include <math.h>
+// Attention with grouped heads over packed prompts and over pages, bf16 on the
+// gfx950 matrix cores (head_dim 64 and 128; V in bf16 or fp16).
+//
+//   out_i = sum_j p_ij v_j,   p_ij = softmax_j(scale q_i . k_j) over the keys that row i sees
+//
+// in one pass over the keys with a running maximum and sum.  Scores are
+// computed transposed, S^T = K Q^T (32x32x16 MFMA): a lane owns one row of
+// queries, its statistics are per-lane values, its mask is one 64-bit word, and
+// the probabilities already sit in the B-operand layout of O^T += V^T P^T.  K
+// and V come by direct-to-LDS loads, V's operand by the LDS transpose read.
+// Two forms:
+//   gqa_tile_kernel  128 rows a workgroup, 32 a wave, K and V tiles of 64 keys shared by the four waves
+//   gqa_few_kernel   32 rows a workgroup, the keys split over its waves
+// both over all of a tile's keys or, where there are few tiles, over a part of
+// them; gqa_join_kernel then adds the parts.
+#include <type_traits>
 
-#include "common.h"
-#include "kernels.h"
+#include "gqa.h"
 
 namespace seer {
 
 namespace {
-__device__ __forceinline__ float to_f(const float* p) { return *p; }
-__device__ __forceinline__ float to_f(const __bf16* p) { return static_cast<float>(*p); }
-__device__ __forceinline__ float to_f(const _Float16* p) { return static_cast<float>(*p); }
-}  // namespace
 
-// One wave per row and head: 64 keys at a time, a key to a lane for the scores,
-// a dim to a lane for the sums.
-template <typename T, typename VT, bool PAGED>
-__global__ __launch_bounds__(256) void gqa_rows_kernel(GqaParams p) {
-  const int lane = threadIdx.x & (kWave - 1);
-  const long long idx = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int r = (int)(idx / p.n_heads), h = (int)(idx % p.n_heads), hk = h / (p.n_heads / p.n_kv);
-  if (r >= p.rows_ub || r >= p.cu[p.B]) return;
-  int lo = 0, hi = p.B - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
-    if (p.cu[mid + 1] > r) hi = mid;
-    else lo = mid + 1;
-  }
-  const int b = lo, i = r - p.cu[b];
-  if (i < 0) return;
-  int len = p.cu[b + 1] - p.cu[b];
-  int used = p.used ? p.used[b] : len;
-  used = used < 0 ? 0 : (used > len ? len : used);
-  T* out = static_cast<T*>(p.out) + (size_t)r * p.o_stride + (size_t)h * p.head_dim;
-  const int D = p.head_dim;
-  float o[2] = {0.0f, 0.0f}, m = -INFINITY, l = 0.0f;
-  if (i < used) {
-    const int ps = 1 << p.shift;
-    int nk = used;
-    if (PAGED) {
-      const long long most = (long long)p.width << p.shift;
-      nk = p.kv_len[b];
-      nk = nk < 0 ? 0 : (nk > most ? (int)most : nk);
-    }
-    const int past = nk - used, pos = past + i;
-    const T* q = static_cast<const T*>(p.q) + (size_t)r * p.q_stride + (size_t)h * D;
-    auto k_row = [&](int key, int page) {
-      return PAGED ? static_cast<const T*>(p.k) + ((((size_t)page * 2) * p.n_kv + hk) * ps + (key & (ps - 1))) * D
-                   : static_cast<const T*>(p.k) + (size_t)(p.cu[b] + key) * p.k_stride + (size_t)hk * D;
-    };
-    auto v_row = [&](int key, int page) {
-      return PAGED ? static_cast<const VT*>(p.v) + ((((size_t)page * 2 + 1) * p.n_kv + hk) * ps + (key & (ps - 1))) * D
-                   : static_cast<const VT*>(p.v) + (size_t)(p.cu[b] + key) * p.v_stride + (size_t)hk * D;
-    };
-    for (int k0 = 0; k0 < nk; k0 += kWave) {
-      const int key = k0 + lane;
-      int page = 0;
-      bool see = key < nk;
-      if (see && PAGED) {
-        page = p.table[(size_t)b * p.width + (key >> p.shift)];
-        see = page >= 0 && page < p.n_pages;
-      }
-      if (see && p.mask == kMaskCausal) see = key <= pos;
-      if (see && p.mask == kMaskTree && key >= past) {
-        const int j = key - past;
-        see = j < 64 * p.words && (p.bits[(size_t)r * p.words + (j >> 6)] >> (j & 63) & 1);
-      }
-      float s = -INFINITY;
-      if (see) {
-        const T* k = k_row(key, page);
-        float acc = 0.0f;
-        for (int d = 0; d < D; ++d) acc = fmaf(to_f(q + d), to_f(k + d), acc);
-        s = acc * p.scale;
-      }
-      const float m_new = fmaxf(m, wave_max(s));
-      const unsigned long long any = __ballot(see);
-      if (any == 0) continue;
-      const float w = see ? expf(s - m_new) : 0.0f;
-      const float a = m == -INFINITY ? 0.0f : expf(m - m_new);
-      m = m_new;
-      l = l * a + wave_sum(w);
-      o[0] *= a;
-      o[1] *= a;
-      for (int t = 0; t < kWave; ++t) {
-        if (!(any >> t & 1)) continue;
-        const float wt = __shfl(w, t, kWave);
-        const VT* v = v_row(k0 + t, __shfl(page, t, kWave));
-#pragma unroll
-        for (int e = 0; e < 2; ++e)
-          if (lane + 64 * e < D) o[e] = fmaf(wt, to_f(v + lane + 64 * e), o[e]);
-      }
+typedef short v4i16_t __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) v4i16_t lds_v4i16_t;
+
+constexpr int NT = 256;
+
+// LDS tiles hold a key per row of DH * 2 bytes, in 16-byte pieces whose place is
+// exchanged so that the reads of a fragment meet distinct banks: piece c of row r
+// of K at c ^ swz_k(r), of V at c ^ swz_v(r).
+template <int DH>
+__device__ __forceinline__ int swz_k(int r) { return DH == 128 ? r & 15 : (r >> 1) & 7; }
+template <int DH>
+__device__ __forceinline__ int swz_v(int r) { return DH == 128 ? 4 * (r & 3) : 4 * ((r >> 1) & 1); }
+
+// Where 16 consecutive keys (a multiple of 16 on) lie: a page holds them all.
+struct KeyRows {
+  const uint8_t* k;
+  const uint8_t* v;
+  size_t step_k, step_v;       // bytes from key to key
+};
+
+template <int DH, bool PAGED>
+struct KeySource {
+  const uint8_t* k;            // packed: the head's first key; paged: the pool
+  const uint8_t* v;
+  size_t step_k, step_v;
+  const int* table;            // the request's row
+  int shift, n_pages, hk, n_kv;
+
+  __device__ __forceinline__ KeySource(const GqaParams& p, const GqaUnit& u) {
+    if constexpr (PAGED) {
+      k = static_cast<const uint8_t*>(p.k);
+      v = k;
+      step_k = step_v = DH * 2;
+      table = p.table + (size_t)u.b * p.width;
+      shift = p.shift;
+      n_pages = p.n_pages;
+      hk = u.hk;
+      n_kv = p.n_kv;
+    } else {
+      step_k = (size_t)p.k_stride * 2;
+      step_v = (size_t)p.v_stride * 2;
+      k = static_cast<const uint8_t*>(p.k) + (size_t)u.s.s0 * step_k + u.hk * (DH * 2);
+      v = static_cast<const uint8_t*>(p.v) + (size_t)u.s.s0 * step_v + u.hk * (DH * 2);
     }
   }
+  // the page of key g (one below the request's end)
+  __device__ __forceinline__ int page(int g) const { return PAGED ? scalar_load(table, g >> shift) : 0; }
+  __device__ __forceinline__ bool held(int id) const { return !PAGED || (id >= 0 && id < n_pages); }
+  __device__ __forceinline__ KeyRows rows(int g, int id) const {
+    if constexpr (PAGED) {
+      const size_t half = (size_t)n_kv << shift;
+      const size_t r = (size_t)(held(id) ? id : 0) * 2 * half + ((size_t)hk << shift) + (g & ((1 << shift) - 1));
+      return {k + r * (DH * 2), k + (r + half) * (DH * 2), DH * 2, DH * 2};
+    } else {
+      return {k + (size_t)g * step_k, v + (size_t)g * step_v, step_k, step_v};
+    }
+  }
+};
+
+// Loads 16 keys of K and V into their rows of the LDS tiles; keys past `last`
+// are the last one again.
+template <int DH>
+__device__ __forceinline__ void load_keys(const KeyRows& src, int last, uint8_t* kd, uint8_t* vd, int lane) {
+  constexpr int ROW = DH * 2, RPL = 1024 / ROW, LPR = ROW / 16;      // rows of a load, lanes of a row
+  const __amdgpu_buffer_rsrc_t rk = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(src.k), 0, -1, 0x00020000);
+  const __amdgpu_buffer_rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(src.v), 0, -1, 0x00020000);
 #pragma unroll
-  for (int e = 0; e < 2; ++e)
-    if (lane + 64 * e < D) out[lane + 64 * e] = static_cast<T>(l == 0.0f ? 0.0f : o[e] / l);
+  for (int q = 0; q < 16 / RPL; ++q) {
+    const int r = RPL * q + lane / LPR;
+    const int rr = r < last ? r : last;
+    const uint32_t ck = (uint32_t)((lane % LPR) ^ swz_k<DH>(r)) << 4;
+    const uint32_t cv = (uint32_t)((lane % LPR) ^ swz_v<DH>(r)) << 4;
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, (lds_void_t*)(kd + RPL * q * ROW), 16, rr * (uint32_t)src.step_k + ck, 0, 0, 0);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, (lds_void_t*)(vd + RPL * q * ROW), 16, rr * (uint32_t)src.step_v + cv, 0, 0, 0);
+  }
 }
 
-int launch_gqa(const GqaParams& p, hipStream_t s) {
-  const long long waves = (long long)p.rows_ub * p.n_heads;
-  const dim3 grid((unsigned)((waves + 3) / 4)), block(256);
-  auto go = [&](auto t, auto v) {
-    if (p.table) hipLaunchKernelGGL((gqa_rows_kernel<decltype(t), decltype(v), true>), grid, block, 0, s, p);
-    else hipLaunchKernelGGL((gqa_rows_kernel<decltype(t), decltype(v), false>), grid, block, 0, s, p);
+// A wave's 32 rows against NI groups of 32 keys.
+template <int DH, bool VF16, int NI>
+struct Rows32 {
+  static constexpr int ROW = DH * 2, KS = DH / 16, DT = DH / 32;
+  using vfrag_t = typename std::conditional<VF16, f16x8_t, bf16x8_t>::type;
+  bf16x8_t qf[KS];
+  f32x16_t o[DT];
+  float m, l;                  // reference maximum (of unscaled scores) and this lane's half of the sum
+  float c;                     // scale * log2(e)
+
+  __device__ __forceinline__ void init(const GqaParams& p, const uint16_t* q, int lane) {
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+      qf[ks] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4_t*>(q + 16 * ks + 8 * (lane >> 5)));
+#pragma unroll
+    for (int i = 0; i < DT; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[i][r] = 0.0f;
+    m = -INFINITY;
+    l = 0.0f;
+    c = p.scale * 1.4426950408889634f;
+  }
+
+  __device__ __forceinline__ static f32x16_t mfma_v(vfrag_t a, u32x4_t b, f32x16_t acc) {
+    if constexpr (VF16) return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, __builtin_bit_cast(f16x8_t, b), acc, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, __builtin_bit_cast(bf16x8_t, b), acc, 0, 0, 0);
+  }
+
+  // One tile: keys fr and 32 + fr at kl, V at vl.  `masked` (the same for the whole
+  // wave): this lane's row sees the keys of `seen` only.
+  __device__ __forceinline__ void step(const uint8_t* kl, const uint8_t* vl, int lane, bool masked,
+                                       unsigned long long seen) {
+    const int fr = lane & 31, fhalf = lane >> 5;
+    f32x16_t s[NI];
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[i][r] = 0.0f;
+    {
+      const uint8_t* krow = kl + fr * ROW;
+      auto kread = [&](int ks, bf16x8_t* dst) {
+        const int ch = (2 * ks + fhalf) ^ swz_k<DH>(fr);
+#pragma unroll
+        for (int i = 0; i < NI; ++i)
+          dst[i] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4_t*>(krow + i * 32 * ROW + ch * 16));
+      };
+      bf16x8_t kf[2][NI];
+      __builtin_amdgcn_sched_barrier(0);
+      kread(0, kf[0]);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        if (ks + 1 < KS) kread(ks + 1, kf[(ks + 1) & 1]);
+#pragma unroll
+        for (int i = 0; i < NI; ++i)
+          s[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[ks & 1][i], qf[ks], s[i], 0, 0, 0);
+        if (ks + 1 < KS) __builtin_amdgcn_sched_group_barrier(0x100, NI, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, NI, 0);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    // element r of s[i] is key 32 i + 8 (r / 4) + 4 fhalf + r % 4
+    const unsigned long long mine = seen >> (4 * fhalf);
+    if (masked) {
+#pragma unroll
+      for (int i = 0; i < NI; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (!(mine >> (32 * i + 8 * (r >> 2) + (r & 3)) & 1)) s[i][r] = -INFINITY;
+    }
+    // Probabilities against the reference maximum, rounded to V's type (half a step:
+    // bf16 2^-8, fp16 2^-11) as the matrix instruction takes them, and their sum,
+    // over the rounded values and in fp32, so that the weights add up to one.
+    u32x4_t pf[2 * NI];
+    float lsum;
+    auto probs = [&](float ref) {
+      const float mc = ref * c;
+      lsum = 0.0f;
+#pragma unroll
+      for (int sl = 0; sl < 2 * NI; ++sl)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float p0 = __builtin_amdgcn_exp2f(s[sl >> 1][(sl & 1) * 8 + 2 * e] * c - mc);
+          const float p1 = __builtin_amdgcn_exp2f(s[sl >> 1][(sl & 1) * 8 + 2 * e + 1] * c - mc);
+          if constexpr (VF16) {
+            const f16x2_t h = __builtin_convertvector(f32x2_t{p0, p1}, f16x2_t);
+            lsum = __builtin_amdgcn_fdot2(h, f16x2_t{(_Float16)1.0f, (_Float16)1.0f}, lsum, false);
+            pf[sl][e] = __builtin_bit_cast(uint32_t, h);
+          } else {
+            const bf16x2_t h = __builtin_convertvector(f32x2_t{p0, p1}, bf16x2_t);
+            lsum = __builtin_amdgcn_fdot2_f32_bf16(h, bf16x2_t{(__bf16)1.0f, (__bf16)1.0f}, lsum, false);
+            pf[sl][e] = __builtin_bit_cast(uint32_t, h);
+          }
+        }
+    };
+    // The reference is the maximum of the first tile in which the row sees a key,
+    // and moves only where a later tile's probabilities pass 2^16 (fp16's range;
+    // with bf16 it keeps the sums far from fp32's): any reference gives the same
+    // softmax, and the common tile takes no maximum.  While a row has seen no key
+    // its reference is -inf, and the NaN or infinity that this gives (-inf + inf,
+    // x + inf) asks for the tile's maximum too.
+    probs(m);
+    if (__any(!(lsum < (VF16 ? INFINITY : 65536.0f)))) {
+      float mt = s[0][0];
+#pragma unroll
+      for (int i = 0; i < NI; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) mt = fmaxf(mt, s[i][r]);
+      // lanes l and l ^ 32 hold the two halves of a row's keys
+      const u32x2_t sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mt), __float_as_uint(mt), false, false);
+      mt = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+      const float m_new = fmaxf(m, mt);
+      const float alpha = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m - m_new) * c);
+      m = m_new;
+      l *= alpha;
+#pragma unroll
+      for (int i = 0; i < DT; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[i][r] *= alpha;
+      probs(m == -INFINITY ? 0.0f : m);
+    }
+    l += lsum;
+
+    // A operand of step n (16-key slice sl, 32-dim tile dt): lane l needs 8 keys of
+    // dim 32 dt + l % 32, in the order of the P fragment.  In each group of 16 lanes
+    // the transpose read hands lane j element j % 4 of lanes 4 e + j / 4, e < 4.
+    const int il = lane & 15;
+    const int vkey = 4 * fhalf + (il >> 2);
+    const int vc8 = 4 * ((lane >> 4) & 1) + (il & 3);
+    const uint8_t* vrow = vl + vkey * ROW;
+    auto vread = [&](int n) {
+      const int sl = n / DT, dt = n % DT;
+      const uint8_t* a = vrow + 16 * sl * ROW + (((8 * dt + vc8) ^ (2 * swz_v<DH>(vkey))) << 3);
+      const v4i16_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_t*)a);
+      const v4i16_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_t*)(a + 8 * ROW));
+      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+    constexpr int STEPS = 2 * NI * DT;
+    if (masked) {
+      // A value that is no number (NaN, an infinity) would reach the rows that do not
+      // see its key as 0 * value.  Where the tile holds one, the product takes zeros
+      // in their place, and a second one of their kinds (1 for inf, 128 for -inf,
+      // 16384 for NaN: sums of at most 64 each stay apart) with the 0/1 of what each
+      // row sees says which outputs they reach.
+      constexpr uint16_t EXPO = VF16 ? 0x7c00 : 0x7f80, MANT = VF16 ? 0x03ff : 0x007f;
+      constexpr uint16_t ONE = VF16 ? 0x3c00 : 0x3f80;
+      bool odd = false;
+#pragma unroll
+      for (int n = 0; n < STEPS; ++n) {
+        const auto f = vread(n);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) odd |= ((uint16_t)f[e] & EXPO) == EXPO;
+      }
+      if (__any(odd)) {
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+          f32x16_t kinds;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) kinds[r] = 0.0f;
+#pragma unroll
+          for (int sl = 0; sl < 2 * NI; ++sl) {
+            auto f = vread(sl * DT + dt);
+            auto kind = f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const uint16_t b = (uint16_t)f[e];
+              const bool bad = (b & EXPO) == EXPO;
+              const float w = b & MANT ? 16384.0f : (b & 0x8000 ? 128.0f : 1.0f);
+              kind[e] = (short)(bad ? (VF16 ? f2h_bits(w) : f2bf(w)) : 0);
+              f[e] = bad ? 0 : f[e];
+            }
+            u32x4_t sees;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int at = 32 * (sl >> 1) + 16 * (sl & 1) + 8 * (e >> 1) + 2 * (e & 1);
+              sees[e] = (mine >> at & 1 ? ONE : 0u) | (mine >> (at + 1) & 1 ? (uint32_t)ONE << 16 : 0u);
+            }
+            o[dt] = mfma_v(__builtin_bit_cast(vfrag_t, f), pf[sl], o[dt]);
+            kinds = mfma_v(__builtin_bit_cast(vfrag_t, kind), sees, kinds);
+          }
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int t = (int)kinds[r], inf = t & 127, ninf = t >> 7 & 127;
+            if (t) o[dt][r] += t >= 16384 || (inf && ninf) ? NAN : (ninf ? -INFINITY : INFINITY);
+          }
+        }
+        return;
+      }
+    }
+    vfrag_t vf[3];
+    __builtin_amdgcn_sched_barrier(0);
+    vf[0] = __builtin_bit_cast(vfrag_t, vread(0));
+    vf[1] = __builtin_bit_cast(vfrag_t, vread(1));
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int n = 0; n < STEPS; ++n) {
+      if (n + 2 < STEPS) vf[(n + 2) % 3] = __builtin_bit_cast(vfrag_t, vread(n + 2));
+      o[n % DT] = mfma_v(vf[n % 3], pf[n / DT], o[n % DT]);
+      if (n + 2 < STEPS) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  }
+};
+
+// 1 / l, and 0 for a row that saw no key (its sums are zero); a NaN stays one.
+__device__ __forceinline__ float inverse(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
+
+// Where unit (slot) leaves its result: per 32 rows and 32 dims 4 x 64 lanes x 16
+// bytes as the lanes hold them, then the rows' maxima and sums.
+template <int RT, int DH>
+struct Parts {
+  static constexpr size_t FLOATS = RT * (DH + 2);
+  float* base;
+  __device__ __forceinline__ Parts(const GqaParams& p, int slot) : base(p.partial + (size_t)slot * FLOATS) {}
+  __device__ __forceinline__ f32x4_t* sum(int w, int dt, int g, int lane) const {
+    return reinterpret_cast<f32x4_t*>(base) + (((w * (DH / 32) + dt) * 4 + g) * 64 + lane);
+  }
+  __device__ __forceinline__ float* max(int row) const { return base + RT * DH + row; }
+  __device__ __forceinline__ float* div(int row) const { return base + RT * (DH + 1) + row; }
+};
+
+__device__ __forceinline__ uint16_t* out_row(const GqaParams& p, const GqaSeq& s, int hk, int tok, int head, int dh) {
+  return static_cast<uint16_t*>(p.out) + (size_t)(s.s0 + tok) * p.o_stride + (size_t)(hk * p.group + head) * dh;
+}
+
+__device__ __forceinline__ void store4(uint16_t* at, f32x4_t v) {
+  uint2 w;
+  w.x = pack_bf2(v[0], v[1]);
+  w.y = pack_bf2(v[2], v[3]);
+  *reinterpret_cast<uint2*>(at) = w;
+}
+
+}  // namespace
+
+template <int DH, bool VF16, bool PAGED>
+__global__ __launch_bounds__(NT, 2) void gqa_tile_kernel(GqaParams p) {
+  constexpr int ROW = DH * 2, DT = DH / 32;
+  __shared__ __attribute__((aligned(1024))) uint8_t k_lds0[64 * ROW];
+  __shared__ __attribute__((aligned(1024))) uint8_t k_lds1[64 * ROW];
+  __shared__ __attribute__((aligned(1024))) uint8_t v_lds0[64 * ROW];
+  __shared__ __attribute__((aligned(1024))) uint8_t v_lds1[64 * ROW];
+  GqaUnit u;
+  if (!gqa_find<kGqaTile, false>(p, blockIdx.x, u) || u.part >= u.parts) return;
+  const int lane = threadIdx.x & 63;
+  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int fr = lane & 31, fhalf = lane >> 5;
+  const int row = u.t * kGqaTile + wv * 32 + fr;
+  const int src = row < u.s.rows ? row : u.s.rows - 1;
+  const int tok = src / p.group, head = src - tok * p.group;
+  const int pos = u.s.past + tok;
+  // tokens of the wave's first and last row
+  const int first = (u.t * kGqaTile + wv * 32) / p.group;
+  const int last = (u.t * kGqaTile + wv * 32 + 31) / p.group;
+  const int open = gqa_open_end(p, u.hi, u.s.past + first, u.s.past);
+  const int wave_end = p.mask == kMaskCausal && u.s.past + last + 1 < u.hi ? u.s.past + last + 1 : u.hi;
+
+  Rows32<DH, VF16, 2> w;
+  w.init(p, static_cast<const uint16_t*>(p.q) + (size_t)(u.s.s0 + tok) * p.q_stride +
+                (size_t)(u.hk * p.group + head) * DH, lane);
+
+  const KeySource<DH, PAGED> keys(p, u);
+  const int n = (u.hi - u.lo + 63) / 64;
+  // pages of the four 16-key groups of a tile
+  int id[4];
+  auto pages = [&](int kbase) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int g = kbase + 16 * i;
+      id[i] = keys.page(g < u.hi ? g : u.hi - 1);
+    }
   };
-  if (!p.bf16) go(float{}, float{});
-  else if (p.v_f16) go(__bf16{}, _Float16{});
-  else go(__bf16{}, __bf16{});
+  auto load = [&](int kbase, auto buf) {
+    constexpr int B = decltype(buf)::value;
+    // a group past the end is the last one again
+    int g = kbase + 16 * wv;
+    g = g < u.hi ? g : (u.hi - 1) & ~15;
+    const int page = wv == 0 ? id[0] : (wv == 1 ? id[1] : (wv == 2 ? id[2] : id[3]));
+    load_keys<DH>(keys.rows(g, page), u.hi - 1 - g < 15 ? u.hi - 1 - g : 15, (B ? k_lds1 : k_lds0) + 16 * wv * ROW,
+                  (B ? v_lds1 : v_lds0) + 16 * wv * ROW, lane);
+  };
+  unsigned long long held = ~0ull, held_next = ~0ull;
+  auto held_of = [&]() {
+    unsigned long long m = ~0ull;
+    if constexpr (PAGED) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (!keys.held(id[i])) m &= ~(0xffffull << (16 * i));
+    }
+    return m;
+  };
+  if (n > 0) {
+    pages(u.lo);
+    load(u.lo, std::integral_constant<int, 0>{});
+    held = held_of();
+    pages(u.lo + 64 < u.hi ? u.lo + 64 : u.hi - 1);
+  }
+  // every load so far (Q and tile 0) lands before the loop, so that the waits in it
+  // are for the next tile alone
+  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_s_waitcnt(0x0f70);       // vmcnt(0)
+  __builtin_amdgcn_sched_barrier(0);
+  __syncthreads();
+  auto step = [&](int kt, auto buf) {
+    constexpr int B = decltype(buf)::value;
+    const int kbase = u.lo + 64 * kt;
+    if (kt + 1 < n) {
+      load(kbase + 64, std::integral_constant<int, B ^ 1>{});
+      held_next = held_of();
+      if (kt + 2 < n) pages(kbase + 128);
+    }
+    if (kbase < wave_end) {
+      const bool masked = kbase + 64 > open || held != ~0ull;
+      unsigned long long seen = ~0ull;
+      if (masked) seen = held & gqa_seen(p, kbase, u.hi, pos, u.s.past, u.s.s0 + tok);
+      w.step(B ? k_lds1 : k_lds0, B ? v_lds1 : v_lds0, lane, masked, seen);
+    }
+    held = held_next;
+    // this wave's loads of the next tile have landed, then one barrier publishes it
+    __builtin_amdgcn_s_waitcnt(0x0f70);
+    __syncthreads();
+  };
+  for (int kt = 0; kt < n; kt += 2) {
+    step(kt, std::integral_constant<int, 0>{});
+    if (kt + 1 < n) step(kt + 1, std::integral_constant<int, 1>{});
+  }
+
+  const float l = w.l + __shfl_xor(w.l, 32, kWave);
+  if (u.parts > 1) {
+    const Parts<kGqaTile, DH> to(p, u.slot + u.part);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *to.sum(wv, dt, g, lane) = f32x4_t{w.o[dt][4 * g], w.o[dt][4 * g + 1], w.o[dt][4 * g + 2], w.o[dt][4 * g + 3]};
+    if (fhalf == 0) {
+      *to.max(wv * 32 + fr) = w.m;
+      *to.div(wv * 32 + fr) = l;
+    }
+    return;
+  }
+  if (row >= u.s.rows) return;
+  const float inv = tok < u.s.used ? inverse(l) : 0.0f;
+  uint16_t* at = out_row(p, u.s, u.hk, tok, head, DH) + fhalf * 4;
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      f32x4_t v;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = tok < u.s.used ? w.o[dt][4 * g + e] * inv : 0.0f;
+      store4(at + dt * 32 + g * 8, v);
+    }
+}
+
+template <int DH, bool VF16, bool PAGED>
+__global__ __launch_bounds__(NT, DH == 128 ? 1 : 2) void gqa_few_kernel(GqaParams p) {
+  constexpr int ROW = DH * 2, DT = DH / 32, FT = 32 * ROW;      // bytes of a wave's K or V tile
+  __shared__ __attribute__((aligned(1024))) uint8_t k_lds0[4 * FT];
+  __shared__ __attribute__((aligned(1024))) uint8_t k_lds1[4 * FT];
+  __shared__ __attribute__((aligned(1024))) uint8_t v_lds0[4 * FT];
+  __shared__ __attribute__((aligned(1024))) uint8_t v_lds1[4 * FT];
+  __shared__ float m_part[4][32], l_part[4][32];
+  GqaUnit u;
+  if (!gqa_find<kGqaFew, false>(p, blockIdx.x, u) || u.part >= u.parts) return;
+  const int lane = threadIdx.x & 63;
+  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int fr = lane & 31, fhalf = lane >> 5;
+  const int row = u.t * kGqaFew + fr;
+  const int src = row < u.s.rows ? row : u.s.rows - 1;
+  const int tok = src / p.group, head = src - tok * p.group;
+  const int pos = u.s.past + tok;
+  const int open = gqa_open_end(p, u.hi, u.s.past + u.t * kGqaFew / p.group, u.s.past);
+
+  Rows32<DH, VF16, 1> w;
+  w.init(p, static_cast<const uint16_t*>(p.q) + (size_t)(u.s.s0 + tok) * p.q_stride +
+                (size_t)(u.hk * p.group + head) * DH, lane);
+
+  const KeySource<DH, PAGED> keys(p, u);
+  // this wave's tiles: 32 of every 128 keys
+  const int k0 = u.lo + 32 * wv;
+  const int n = u.hi > k0 ? (u.hi - k0 + 127) / 128 : 0;
+  int id[2];
+  auto pages = [&](int kbase) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int g = kbase + 16 * i;
+      id[i] = keys.page(g < u.hi ? g : u.hi - 1);
+    }
+  };
+  auto load = [&](int kbase, auto buf) {
+    constexpr int B = decltype(buf)::value;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      int g = kbase + 16 * i;
+      g = g < u.hi ? g : (u.hi - 1) & ~15;
+      load_keys<DH>(keys.rows(g, id[i]), u.hi - 1 - g < 15 ? u.hi - 1 - g : 15,
+                    (B ? k_lds1 : k_lds0) + wv * FT + 16 * i * ROW, (B ? v_lds1 : v_lds0) + wv * FT + 16 * i * ROW, lane);
+    }
+  };
+  unsigned long long held = ~0ull, held_next = ~0ull;
+  auto held_of = [&]() {
+    unsigned long long m = ~0ull;
+    if constexpr (PAGED) {
+      if (!keys.held(id[0])) m &= ~0xffffull;
+      if (!keys.held(id[1])) m &= ~0xffff0000ull;
+    }
+    return m;
+  };
+  if (n > 0) {
+    pages(k0);
+    load(k0, std::integral_constant<int, 0>{});
+    held = held_of();
+    pages(k0 + 128 < u.hi ? k0 + 128 : u.hi - 1);
+  }
+  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_s_waitcnt(0x0f70);       // vmcnt(0)
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_sched_barrier(0);
+  auto step = [&](int kt, auto buf) {
+    constexpr int B = decltype(buf)::value;
+    const int kbase = k0 + 128 * kt;
+    if (kt + 1 < n) {
+      load(kbase + 128, std::integral_constant<int, B ^ 1>{});
+      held_next = held_of();
+      if (kt + 2 < n) pages(kbase + 256);
+    }
+    const bool masked = kbase + 32 > open || held != ~0ull;
+    unsigned long long seen = ~0ull;
+    if (masked) seen = held & gqa_seen(p, kbase, u.hi, pos, u.s.past, u.s.s0 + tok);
+    w.step((B ? k_lds1 : k_lds0) + wv * FT, (B ? v_lds1 : v_lds0) + wv * FT, lane, masked, seen);
+    held = held_next;
+    // the next tile has landed; this one's fragments are in registers or consumed
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt(0x0070);     // vmcnt(0) and lgkmcnt(0)
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  for (int kt = 0; kt < n; kt += 2) {
+    step(kt, std::integral_constant<int, 0>{});
+    if (kt + 1 < n) step(kt + 1, std::integral_constant<int, 1>{});
+  }
+
+  // join the waves: each leaves its sums in its own K tiles and takes 32 dims
+  const float l_own = w.l + __shfl_xor(w.l, 32, kWave);
+  if (fhalf == 0) {
+    m_part[wv][fr] = w.m;
+    l_part[wv][fr] = l_own;
+  }
+  auto sums = [&](int v, int dt, int g) {
+    const int at = dt * 4 + g;              // of DT * 4 blocks of 1 KiB; a buffer has FT / 1024 of them
+    return reinterpret_cast<f32x4_t*>((at >= FT / 1024 ? k_lds1 : k_lds0) + v * FT + at % (FT / 1024) * 1024 + lane * 16);
+  };
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+      *sums(wv, dt, g) = f32x4_t{w.o[dt][4 * g], w.o[dt][4 * g + 1], w.o[dt][4 * g + 2], w.o[dt][4 * g + 3]};
+  __syncthreads();
+  if (wv >= DT) return;
+  float m = m_part[0][fr];
+#pragma unroll
+  for (int v = 1; v < 4; ++v) m = fmaxf(m, m_part[v][fr]);
+  const float ref = m == -INFINITY ? 0.0f : m;
+  float l = 0.0f;
+  f32x4_t sum[4];
+#pragma unroll
+  for (int g = 0; g < 4; ++g) sum[g] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+  for (int v = 0; v < 4; ++v) {
+    const float a = __builtin_amdgcn_exp2f((m_part[v][fr] - ref) * w.c);
+    if (m_part[v][fr] == -INFINITY && l_part[v][fr] == 0.0f) continue;      // a wave whose keys the row does not see
+    l += l_part[v][fr] * a;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) sum[g] += a * *sums(v, wv, g);
+  }
+  if (u.parts > 1) {
+    const Parts<kGqaFew, DH> to(p, u.slot + u.part);
+#pragma unroll
+    for (int g = 0; g < 4; ++g) *to.sum(0, wv, g, lane) = sum[g];
+    if (wv == 0 && fhalf == 0) {
+      *to.max(fr) = m;
+      *to.div(fr) = l;
+    }
+    return;
+  }
+  if (row >= u.s.rows) return;
+  const bool real = tok < u.s.used;
+  const float inv = inverse(l);
+  uint16_t* at = out_row(p, u.s, u.hk, tok, head, DH) + wv * 32 + fhalf * 4;
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    f32x4_t v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = real ? sum[g][e] * inv : 0.0f;
+    store4(at + g * 8, v);
+  }
+}
+
+// Adds the parts of each tile whose keys were cut: a wave takes 32 rows x 32 dims
+// x a quarter (one 16-byte piece a lane).
+template <int RT, int DH>
+__global__ __launch_bounds__(NT) void gqa_join_kernel(GqaParams p) {
+  constexpr int DT = DH / 32, PIECES = RT / 32 * DT;       // workgroups of a tile
+  GqaUnit u;
+  const int piece = blockIdx.x % PIECES;
+  if (!gqa_find<RT, true>(p, blockIdx.x / PIECES, u) || u.parts < 2) return;
+  const int lane = threadIdx.x & 63, g = threadIdx.x >> 6, fr = lane & 31, fhalf = lane >> 5;
+  const int w = piece / DT, dt = piece % DT;
+  const float c = p.scale * 1.4426950408889634f;
+  float m = -INFINITY;
+  for (int i = 0; i < u.parts; ++i) m = fmaxf(m, *Parts<RT, DH>(p, u.slot + i).max(w * 32 + fr));
+  const float ref = m == -INFINITY ? 0.0f : m;
+  float l = 0.0f;
+  f32x4_t sum = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+  for (int i = 0; i < u.parts; ++i) {
+    const Parts<RT, DH> from(p, u.slot + i);
+    const float mi = *from.max(w * 32 + fr), li = *from.div(w * 32 + fr);
+    const f32x4_t v = *from.sum(w, dt, g, lane);
+    const bool none = mi == -INFINITY && li == 0.0f;
+    const float a = none ? 0.0f : __builtin_amdgcn_exp2f((mi - ref) * c);
+    l += li * a;
+    sum += a * v;
+  }
+  const int row = u.t * RT + w * 32 + fr;
+  if (row >= u.s.rows) return;
+  const int tok = row / p.group, head = row - tok * p.group;
+  const bool real = tok < u.s.used;
+  const float inv = inverse(l);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) sum[e] = real ? sum[e] * inv : 0.0f;
+  store4(out_row(p, u.s, u.hk, tok, head, DH) + dt * 32 + g * 8 + fhalf * 4, sum);
+}
+
+int launch_gqa_bf16(const GqaParams& p, const GqaRule& r, hipStream_t s) {
+  auto go = [&](auto dh, auto vf16, auto paged) {
+    constexpr int DH = decltype(dh)::value;
+    constexpr bool V = decltype(vf16)::value, P = decltype(paged)::value;
+    if (r.rt == kGqaTile) {
+      hipLaunchKernelGGL((gqa_tile_kernel<DH, V, P>), dim3(r.grid), dim3(NT), 0, s, p);
+      if (r.target) hipLaunchKernelGGL((gqa_join_kernel<kGqaTile, DH>), dim3(r.tiles * (4 * DH / 32)), dim3(NT), 0, s, p);
+    } else {
+      hipLaunchKernelGGL((gqa_few_kernel<DH, V, P>), dim3(r.grid), dim3(NT), 0, s, p);
+      if (r.target) hipLaunchKernelGGL((gqa_join_kernel<kGqaFew, DH>), dim3(r.tiles * (DH / 32)), dim3(NT), 0, s, p);
+    }
+  };
+  auto with = [&](auto dh, auto vf16) {
+    if (p.table) go(dh, vf16, std::true_type{});
+    else go(dh, vf16, std::false_type{});
+  };
+  if (p.head_dim == 128) {
+    if (p.v_f16) with(std::integral_constant<int, 128>{}, std::true_type{});
+    else with(std::integral_constant<int, 128>{}, std::false_type{});
+  } else {
+    if (p.v_f16) with(std::integral_constant<int, 64>{}, std::true_type{});
+    else with(std::integral_constant<int, 64>{}, std::false_type{});
+  }
   return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 

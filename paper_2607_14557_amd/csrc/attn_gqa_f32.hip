@@ -1,0 +1,289 @@
+// Attention with grouped heads over packed prompts and over pages, fp32 (any
+// head_dim <= 128 that is a multiple of 4), on the fp32 matrix instruction.
+//
+// A workgroup takes 16 rows; its four waves take 16 keys of every 64 each and
+// join at the end.  Scores are computed transposed (S^T = K Q^T, 16x16x4), so
+// that a lane holds four keys of one row and its probabilities are the B operand
+// of O^T += V^T P^T as they are: instruction i of four takes keys 4 g + i, g the
+// lane's group of 16.  K and V go from memory to the operand registers in
+// 16-byte loads; the order of the head's dims in the products is the one that
+// those loads give.
+#include "gqa.h"
+
+namespace seer {
+
+namespace {
+constexpr int NT = 256;
+
+// A part's result: sums [H][e] of 64 lanes x 16 bytes, maxima and sums of 16 rows.
+template <int H>
+struct Parts {
+  static constexpr size_t FLOATS = 16 * (64 * H + 2);
+  float* base;
+  __device__ __forceinline__ Parts(const GqaParams& p, int slot) : base(p.partial + (size_t)slot * FLOATS) {}
+  __device__ __forceinline__ f32x4_t* sum(int t, int lane) const { return reinterpret_cast<f32x4_t*>(base) + t * 64 + lane; }
+  __device__ __forceinline__ float* max(int row) const { return base + 16 * 64 * H + row; }
+  __device__ __forceinline__ float* div(int row) const { return base + 16 * 64 * H + 16 + row; }
+};
+
+__device__ __forceinline__ float inverse(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
+}  // namespace
+
+// H: halves of 64 dims.
+template <int H, bool PAGED>
+__global__ __launch_bounds__(NT) void gqa_f32_kernel(GqaParams p) {
+  constexpr int C = 4 * H;                                     // 16-dim pieces
+  __shared__ f32x4_t o_part[4][4 * H][64];
+  __shared__ float m_part[4][16], l_part[4][16];
+  GqaUnit u;
+  if (!gqa_find<kGqaF32, false>(p, blockIdx.x, u) || u.part >= u.parts) return;
+  const int lane = threadIdx.x & 63;
+  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int fr = lane & 15, g = lane >> 4;
+  const int D = p.head_dim;
+  const int row = u.t * kGqaF32 + fr;
+  const int src = row < u.s.rows ? row : u.s.rows - 1;
+  const int tok = src / p.group, head = src - tok * p.group;
+  const int pos = u.s.past + tok;
+  const int open = gqa_open_end(p, u.hi, u.s.past + u.t * kGqaF32 / p.group, u.s.past);
+  const float c = p.scale * 1.4426950408889634f;
+  const f32x4_t zero = {0.0f, 0.0f, 0.0f, 0.0f};
+
+  f32x4_t qf[C];
+  {
+    const float* q = static_cast<const float*>(p.q) + (size_t)(u.s.s0 + tok) * p.q_stride + (size_t)(u.hk * p.group + head) * D;
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+      const int d = 16 * i + 4 * g;
+      qf[i] = *reinterpret_cast<const f32x4_t*>(q + (d < D ? d : 0));
+      if (d >= D) qf[i] = zero;
+    }
+  }
+  const float* kp = static_cast<const float*>(p.k);
+  const float* vp = static_cast<const float*>(p.v);
+  const int* table = PAGED ? p.table + (size_t)u.b * p.width : nullptr;
+  const size_t half = PAGED ? ((size_t)p.n_kv << p.shift) * D : 0;
+  if (!PAGED) {
+    kp += (size_t)u.s.s0 * p.k_stride + (size_t)u.hk * D;
+    vp += (size_t)u.s.s0 * p.v_stride + (size_t)u.hk * D;
+  }
+  f32x4_t o[4 * H];
+#pragma unroll
+  for (int i = 0; i < 4 * H; ++i) o[i] = zero;
+  float m = -INFINITY, l = 0.0f;
+
+  for (int k0 = u.lo + 16 * wv; k0 < u.hi; k0 += 64) {
+    const int last = u.hi - 1 - k0 < 15 ? u.hi - 1 - k0 : 15;   // the group's last key: those past it are it again
+    bool held = true;
+    const float *ks = kp, *vs = vp;
+    size_t step_k = p.k_stride, step_v = p.v_stride;
+    if (PAGED) {
+      int id = scalar_load(table, k0 >> p.shift);
+      held = id >= 0 && id < p.n_pages;
+      id = held ? id : 0;
+      ks += (size_t)id * 2 * half + (((size_t)u.hk << p.shift) + (k0 & ((1 << p.shift) - 1))) * D;
+      vs = ks + half;
+      step_k = step_v = D;
+    } else {
+      ks += (size_t)k0 * step_k;
+      vs += (size_t)k0 * step_v;
+    }
+    const float* kr = ks + (fr < last ? fr : last) * step_k;
+    f32x4_t kf[C], vf[4][H];
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+      const int d = 16 * i + 4 * g;
+      kf[i] = *reinterpret_cast<const f32x4_t*>(kr + (d < D ? d : 0));
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int r = 4 * g + i;
+      const float* vr = vs + (r < last ? r : last) * step_v;
+#pragma unroll
+      for (int h = 0; h < H; ++h) {
+        const int d = 64 * h + 4 * fr;
+        vf[i][h] = *reinterpret_cast<const f32x4_t*>(vr + (d < D ? d : 0));
+      }
+    }
+    // two chains, so that one product does not wait for the one before
+    f32x4_t s0 = zero, s1 = zero;
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+      if (16 * i >= D) break;
+      const f32x4_t k = 16 * i + 4 * g < D ? kf[i] : zero;
+#pragma unroll
+      for (int e = 0; e < 4; e += 2) {
+        s0 = __builtin_amdgcn_mfma_f32_16x16x4f32(k[e], qf[i][e], s0, 0, 0, 0);
+        s1 = __builtin_amdgcn_mfma_f32_16x16x4f32(k[e + 1], qf[i][e + 1], s1, 0, 0, 0);
+      }
+    }
+    f32x4_t s = s0 + s1;                                      // key k0 + 4 g + e
+    const bool masked = k0 + 16 > open || !held;
+    unsigned mine = 0xf;
+    if (masked) {
+      const unsigned long long seen = held ? gqa_seen(p, k0, u.hi, pos, u.s.past, u.s.s0 + tok) : 0;
+      mine = (unsigned)(seen >> (4 * g)) & 0xf;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (!(mine >> e & 1)) s[e] = -INFINITY;
+    }
+    float mt = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
+    mt = fmaxf(mt, __shfl_xor(mt, 16, kWave));
+    mt = fmaxf(mt, __shfl_xor(mt, 32, kWave));
+    if (__any(mt > m)) {
+      const float m_new = fmaxf(m, mt);
+      const float alpha = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m - m_new) * c);
+      m = m_new;
+      l *= alpha;
+#pragma unroll
+      for (int i = 0; i < 4 * H; ++i) o[i] *= alpha;
+    }
+    const float mc = m == -INFINITY ? 0.0f : m * c;
+    f32x4_t w;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = __builtin_amdgcn_exp2f(s[e] * c - mc);
+    l += (w[0] + w[1]) + (w[2] + w[3]);
+    bool odd = false;
+    if (masked) {
+      // values that are no numbers would reach the rows that do not see their keys as
+      // 0 * value; see the bf16 kernels for the way round it
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int h = 0; h < H; ++h)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) odd |= !(fabsf(vf[i][h][e]) < INFINITY);
+    }
+    if (masked && __any(odd)) {
+#pragma unroll
+      for (int h = 0; h < H; ++h)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          f32x4_t kinds = zero;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float x = vf[i][h][e];
+            const bool bad = !(fabsf(x) < INFINITY);
+            const float kind = !bad ? 0.0f : (x != x ? 16384.0f : (x < 0.0f ? 128.0f : 1.0f));
+            o[4 * h + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(bad ? 0.0f : x, w[i], o[4 * h + e], 0, 0, 0);
+            kinds = __builtin_amdgcn_mfma_f32_16x16x4f32(kind, mine >> i & 1 ? 1.0f : 0.0f, kinds, 0, 0, 0);
+          }
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int t = (int)kinds[r], inf = t & 127, ninf = t >> 7 & 127;
+            if (t) o[4 * h + e][r] += t >= 16384 || (inf && ninf) ? NAN : (ninf ? -INFINITY : INFINITY);
+          }
+        }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int h = 0; h < H; ++h)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            o[4 * h + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[i][h][e], w[i], o[4 * h + e], 0, 0, 0);
+    }
+  }
+
+  // join the waves: wave w takes sums w, w + 4
+  l += __shfl_xor(l, 16, kWave);
+  l += __shfl_xor(l, 32, kWave);
+#pragma unroll
+  for (int i = 0; i < 4 * H; ++i) o_part[wv][i][lane] = o[i];
+  if (g == 0) {
+    m_part[wv][fr] = m;
+    l_part[wv][fr] = l;
+  }
+  __syncthreads();
+  m = fmaxf(fmaxf(m_part[0][fr], m_part[1][fr]), fmaxf(m_part[2][fr], m_part[3][fr]));
+  const float ref = m == -INFINITY ? 0.0f : m;
+  l = 0.0f;
+  f32x4_t sum[H];
+#pragma unroll
+  for (int h = 0; h < H; ++h) sum[h] = zero;
+#pragma unroll
+  for (int v = 0; v < 4; ++v) {
+    const float mv = m_part[v][fr], lv = l_part[v][fr];
+    if (mv == -INFINITY && lv == 0.0f) continue;              // a wave whose keys the row does not see
+    const float a = __builtin_amdgcn_exp2f((mv - ref) * c);
+    l += lv * a;
+#pragma unroll
+    for (int h = 0; h < H; ++h) sum[h] += a * o_part[v][4 * h + wv][lane];
+  }
+  if (u.parts > 1) {
+    const Parts<H> to(p, u.slot + u.part);
+#pragma unroll
+    for (int h = 0; h < H; ++h) *to.sum(4 * h + wv, lane) = sum[h];
+    if (wv == 0 && g == 0) {
+      *to.max(fr) = m;
+      *to.div(fr) = l;
+    }
+    return;
+  }
+  if (row >= u.s.rows) return;
+  // sum[h][i] is dim 64 h + 16 g + 4 i + wv
+  const bool real = tok < u.s.used;
+  const float inv = inverse(l);
+  float* out = static_cast<float*>(p.out) + (size_t)(u.s.s0 + tok) * p.o_stride + (size_t)(u.hk * p.group + head) * D;
+#pragma unroll
+  for (int h = 0; h < H; ++h)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int d = 64 * h + 16 * g + 4 * i + wv;
+      if (d < D) out[d] = real ? sum[h][i] * inv : 0.0f;
+    }
+}
+
+// Adds the parts of each tile whose keys were cut; wave w as in the kernel above.
+template <int H>
+__global__ __launch_bounds__(NT) void gqa_f32_join_kernel(GqaParams p) {
+  GqaUnit u;
+  if (!gqa_find<kGqaF32, true>(p, blockIdx.x, u) || u.parts < 2) return;
+  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, fr = lane & 15, g = lane >> 4, D = p.head_dim;
+  const float c = p.scale * 1.4426950408889634f;
+  float m = -INFINITY;
+  for (int i = 0; i < u.parts; ++i) m = fmaxf(m, *Parts<H>(p, u.slot + i).max(fr));
+  const float ref = m == -INFINITY ? 0.0f : m;
+  float l = 0.0f;
+  f32x4_t sum[H];
+#pragma unroll
+  for (int h = 0; h < H; ++h) sum[h] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+  for (int i = 0; i < u.parts; ++i) {
+    const Parts<H> from(p, u.slot + i);
+    const float mi = *from.max(fr), li = *from.div(fr);
+    const float a = mi == -INFINITY && li == 0.0f ? 0.0f : __builtin_amdgcn_exp2f((mi - ref) * c);
+    l += li * a;
+#pragma unroll
+    for (int h = 0; h < H; ++h) sum[h] += a * *from.sum(4 * h + wv, lane);
+  }
+  const int row = u.t * kGqaF32 + fr;
+  if (row >= u.s.rows) return;
+  const int tok = row / p.group, head = row - tok * p.group;
+  const bool real = tok < u.s.used;
+  const float inv = inverse(l);
+  float* out = static_cast<float*>(p.out) + (size_t)(u.s.s0 + tok) * p.o_stride + (size_t)(u.hk * p.group + head) * D;
+#pragma unroll
+  for (int h = 0; h < H; ++h)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int d = 64 * h + 16 * g + 4 * i + wv;
+      if (d < D) out[d] = real ? sum[h][i] * inv : 0.0f;
+    }
+}
+
+int launch_gqa_f32(const GqaParams& p, const GqaRule& r, hipStream_t s) {
+  const dim3 grid(r.grid), block(NT);
+  if (p.head_dim > 64) {
+    if (p.table) hipLaunchKernelGGL((gqa_f32_kernel<2, true>), grid, block, 0, s, p);
+    else hipLaunchKernelGGL((gqa_f32_kernel<2, false>), grid, block, 0, s, p);
+    if (r.target) hipLaunchKernelGGL(gqa_f32_join_kernel<2>, dim3(r.tiles), block, 0, s, p);
+  } else {
+    if (p.table) hipLaunchKernelGGL((gqa_f32_kernel<1, true>), grid, block, 0, s, p);
+    else hipLaunchKernelGGL((gqa_f32_kernel<1, false>), grid, block, 0, s, p);
+    if (r.target) hipLaunchKernelGGL(gqa_f32_join_kernel<1>, dim3(r.tiles), block, 0, s, p);
+  }
+  return hipGetLastError() == hipSuccess ? 0 : -1;
+}
+
+}  // namespace seer

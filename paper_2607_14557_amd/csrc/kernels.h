@@ -8,6 +8,8 @@
 
 namespace seer {
 
+struct GqaRule;
+
 // SCALE: C = acc * rs[r]; SCALE_ROPE: SCALE with the rotary embedding of the
 // columns < rope_col1 (bf16 only); RESID: C = R + acc; SWIGLU(_COUNT): gate/up pairs;
 // RESID_SPLIT: v = R + acc, C = bf16(v), C2 = bf16(v - C) (bf16 only);
@@ -337,6 +339,7 @@ struct GqaParams {
   int B;
   int rows_ub;
   int n_heads, n_kv, head_dim;
+  int group;                   // n_heads / n_kv
   float scale;
   int mask;                    // kMask*
   bool bf16, v_f16;
@@ -345,7 +348,13 @@ struct GqaParams {
   int shift, n_pages, width;
   const unsigned long long* bits;   // [rows][words]
   int words;
+  // the launch (gqa_rule): units to cut the keys for (0: not cut), blocks that a
+  // part has at least, and the parts' results
+  int target, min_chunk;
+  int max_units;               // that the grid and the results have room for
+  float* partial;
 };
-int launch_gqa(const GqaParams& p, hipStream_t s);
+int launch_gqa_bf16(const GqaParams& p, const GqaRule& r, hipStream_t s);
+int launch_gqa_f32(const GqaParams& p, const GqaRule& r, hipStream_t s);
 
 }  // namespace seer

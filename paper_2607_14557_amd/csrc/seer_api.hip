@@ -1,6 +1,6 @@
 // C ABI of the Seer hot path: argument checks, workspace layout and the launch
 // sequence of each entry point.  Kernels live in gemm_bf16.hip, attn_bf16.hip,
-// f32_kernels.hip, rows.hip, pages.hip and attn_gqa.hip.
+// attn_gqa.hip, attn_gqa_f32.hip, f32_kernels.hip, rows.hip and pages.hip.
 #include <math.h>
 #include <stdarg.h>
 #include <stdio.h>
@@ -9,6 +9,7 @@
 #include <string>
 
 #include "../../include/seer.h"
+#include "dispatch.h"
 #include "kernels.h"
 
 namespace {
@@ -674,7 +675,7 @@ static int check_heads(const seer_attn_desc* d) {
                 d->head_dim);
   if (d->n_heads % d->n_kv_heads != 0)
     return fail(SEER_EINVAL, "n_heads (%d) must be a multiple of n_kv_heads (%d)", d->n_heads, d->n_kv_heads);
-  if (!isfinite(d->scale)) return fail(SEER_EINVAL, "scale must be finite");
+  if (!(d->scale >= 0.0f) || !isfinite(d->scale)) return fail(SEER_EINVAL, "scale must be finite and >= 0");
   if (d->flags & ~SEER_ATTN_V_F16) return fail(SEER_EINVAL, "unknown flags %d", d->flags);
   if (d->dtype == SEER_DTYPE_BF16) {
     if (d->head_dim != 64 && d->head_dim != 128)
@@ -743,7 +744,7 @@ static int check_rows(const char* name, const void* ptr, int64_t stride, int64_t
   if (!ptr) return fail(SEER_EINVAL, "%s is NULL", name);
   if (!aligned(ptr, 16) || stride * es % 16 != 0)
     return fail(SEER_EINVAL, "%s and its rows must be 16-byte aligned (row stride %lld elements)", name, (long long)stride);
-  if (stride < width || stride > (1ll << 40))
+  if (stride < width || stride > (1 << 24))
     return fail(SEER_EINVAL, "the row stride of %s (%lld) is not one of rows of %lld elements", name, (long long)stride,
                 (long long)width);
   return SEER_OK;
@@ -773,8 +774,14 @@ int seer_kv_store(const seer_attn_desc* desc, const seer_page_desc* pages, const
 }
 
 size_t seer_attn_workspace_bytes(const seer_attn_desc* desc, int32_t rows_ub, int32_t batch) {
-  if (check_heads(desc) != SEER_OK || rows_ub < 0 || batch < 0) return 0;
-  return 256;
+  if (check_heads(desc) != SEER_OK) return 0;
+  if (rows_ub < 1 || batch < 1 || (long long)rows_ub * desc->n_heads >= (1ll << 31)) {
+    fail(SEER_EINVAL, "rows_ub and batch must be positive, rows_ub * n_heads below 2^31");
+    return 0;
+  }
+  const seer::GqaRule r = seer::gqa_rule(desc->dtype == SEER_DTYPE_BF16, desc->n_heads, desc->n_kv_heads,
+                                         desc->head_dim, rows_ub, batch);
+  return 256 + up256(r.bytes);
 }
 
 // what both attention calls check and fill in
@@ -801,7 +808,17 @@ static int gqa_params(seer::GqaParams& p, const seer_attn_desc* desc, int32_t ma
   p.n_heads = desc->n_heads; p.n_kv = desc->n_kv_heads; p.head_dim = desc->head_dim;
   p.scale = desc->scale != 0.0f ? desc->scale : 1.0f / sqrtf((float)desc->head_dim);
   p.mask = mask; p.bf16 = desc->dtype == SEER_DTYPE_BF16; p.v_f16 = (desc->flags & SEER_ATTN_V_F16) != 0;
+  p.group = p.n_heads / p.n_kv;
+  p.partial = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + 256);
   return SEER_OK;
+}
+
+static int launch_gqa(seer::GqaParams& p, hipStream_t stream) {
+  const seer::GqaRule r = seer::gqa_rule(p.bf16, p.n_heads, p.n_kv, p.head_dim, p.rows_ub, p.B);
+  p.target = r.target;
+  p.min_chunk = 1;
+  p.max_units = r.grid;
+  return p.bf16 ? seer::launch_gqa_bf16(p, r, stream) : seer::launch_gqa_f32(p, r, stream);
 }
 
 int seer_attn_prompt(const seer_attn_desc* desc, int32_t mask, const void* q, int64_t q_stride, const void* k,
@@ -818,7 +835,7 @@ int seer_attn_prompt(const seer_attn_desc* desc, int32_t mask, const void* q, in
   if ((rc = check_rows("k", k, k_stride, width, es)) || (rc = check_rows("v", v, v_stride, width, es))) return rc;
   if (out == k || out == v) return fail(SEER_EINVAL, "out may not alias an input");
   p.k = k; p.v = v; p.k_stride = k_stride; p.v_stride = v_stride;
-  if (seer::launch_gqa(p, stream)) return hip_fail("prompt attention launch");
+  if (launch_gqa(p, stream)) return hip_fail("prompt attention launch");
   return ok();
 }
 
@@ -841,7 +858,7 @@ int seer_attn_paged(const seer_attn_desc* desc, const seer_page_desc* pages, int
   p.k = pool; p.v = pool; p.table = table; p.kv_len = kv_len;
   p.shift = page_shift(pages); p.n_pages = pages->n_pages; p.width = pages->table_width;
   p.bits = reinterpret_cast<const unsigned long long*>(tree_bits); p.words = tree_words;
-  if (seer::launch_gqa(p, stream)) return hip_fail("paged attention launch");
+  if (launch_gqa(p, stream)) return hip_fail("paged attention launch");
   return ok();
 }
 

@@ -34,7 +34,7 @@ def test_pool_bytes(S):
     # past 32 bits
     assert S.seer_page_pool_bytes(heads(S, kv=8), pages(S, n=1 << 20)) == (1 << 20) * 2 * 8 * 64 * 128 * 2
     for bad in (heads(S, h=7), heads(S, kv=0), heads(S, h=0), heads(S, d=96), heads(S, d=0), heads(S, t=9),
-                heads(S, flags=2), heads(S, scale=float("nan")), heads(S, scale=float("inf")),
+                heads(S, flags=2), heads(S, scale=float("nan")), heads(S, scale=float("inf")), heads(S, scale=-0.1),
                 heads(S, t=S.SEER_DTYPE_F32, d=132), heads(S, t=S.SEER_DTYPE_F32, d=30),
                 heads(S, t=S.SEER_DTYPE_F32, flags=S.SEER_ATTN_V_F16), heads(S, h=1 << 18, kv=1)):
         assert S.seer_page_pool_bytes(bad, pages(S)) == 0 and S.seer_last_error()
@@ -73,7 +73,7 @@ def test_store_refusals(S):
 
     for kw in (dict(k=None), dict(v=None), dict(slots=None), dict(pool=None), dict(rows=0), dict(k=FAKE + 8),
                dict(v=FAKE + 2), dict(pool=FAKE + 4), dict(ks=255), dict(ks=248), dict(vs=260), dict(vs=-256),
-               dict(ks=1 << 41)):
+               dict(ks=(1 << 24) + 8)):
         assert call(**kw) == S.SEER_EINVAL, kw
     assert call(d=heads(S, d=96)) == S.SEER_EUNSUPPORTED
     assert call(pg=pages(S, size=17)) == S.SEER_EUNSUPPORTED
