@@ -10,7 +10,7 @@
 // and V come by direct-to-LDS loads, V's operand by the LDS transpose read.
 // Two forms:
 //   gqa_tile_kernel  128 rows a workgroup, 32 a wave, K and V tiles of 64 keys shared by the four waves
-//   gqa_few_kernel   32 rows a workgroup, the keys split over its waves
+//   gqa_few_kernel   32 rows a workgroup, the keys split over its two waves
 // both over all of a tile's keys or, where there are few tiles, over a part of
 // them; gqa_join_kernel then adds the parts.
 #include <type_traits>
@@ -24,7 +24,8 @@ namespace {
 typedef short v4i16_t __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) v4i16_t lds_v4i16_t;
 
-constexpr int NT = 256;
+constexpr int NT = 256;          // threads of a workgroup, and of one of the few-row form
+constexpr int NF = 128;
 
 // LDS tiles hold a key per row of DH * 2 bytes, in 16-byte pieces whose place is
 // exchanged so that the reads of a fragment meet distinct banks: piece c of row r
@@ -98,8 +99,36 @@ __device__ __forceinline__ void load_keys(const KeyRows& src, int last, uint8_t*
   }
 }
 
-// A wave's 32 rows against NI groups of 32 keys.
-template <int DH, bool VF16, int NI>
+// Values that are no numbers (NaN, infinities) under a mask: the product would
+// carry them to rows that do not see their keys, as 0 * value.  So the tiles in
+// which some row is blind to a key are swept before they are used (each wave the
+// keys that it loaded itself): such values become zeros there, and after the last
+// tile add_odd adds them to the rows that do see them.  Returns whether there were any.
+template <bool VF16, int BYTES>
+__device__ __forceinline__ bool sweep(uint8_t* tile, int lane) {
+  constexpr uint32_t EXPO = VF16 ? 0x7c007c00u : 0x7f807f80u, LOW = VF16 ? 0x04000400u : 0x00800080u;
+  bool odd = false;
+#pragma unroll
+  for (int i = 0; i < BYTES / 1024; ++i) {
+    u32x4_t* at = reinterpret_cast<u32x4_t*>(tile + i * 1024 + lane * 16);
+    u32x4_t v = *at;
+    bool any = false;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      // an exponent of all ones carries into the bit above it
+      const uint32_t full = ((v[e] & EXPO) + LOW) & 0x80008000u;
+      any |= full != 0;
+      v[e] &= ~((full >> 15) * 0xffffu);
+    }
+    if (any) *at = v;
+    odd |= any;
+  }
+  return __any(odd);
+}
+
+// A wave's 32 rows against NI groups of 32 keys.  FINE: the probabilities as a sum
+// of two bf16 values, for where the matrix instructions are not what bounds.
+template <int DH, bool VF16, int NI, bool FINE>
 struct Rows32 {
   static constexpr int ROW = DH * 2, KS = DH / 16, DT = DH / 32;
   using vfrag_t = typename std::conditional<VF16, f16x8_t, bf16x8_t>::type;
@@ -160,18 +189,20 @@ struct Rows32 {
       __builtin_amdgcn_sched_barrier(0);
     }
     // element r of s[i] is key 32 i + 8 (r / 4) + 4 fhalf + r % 4
-    const unsigned long long mine = seen >> (4 * fhalf);
     if (masked) {
+      const unsigned long long mine = seen >> (4 * fhalf);
+      const uint32_t half[2] = {(uint32_t)mine, (uint32_t)(mine >> 32)};
 #pragma unroll
       for (int i = 0; i < NI; ++i)
 #pragma unroll
         for (int r = 0; r < 16; ++r)
-          if (!(mine >> (32 * i + 8 * (r >> 2) + (r & 3)) & 1)) s[i][r] = -INFINITY;
+          if (!(half[i] >> (8 * (r >> 2) + (r & 3)) & 1)) s[i][r] = -INFINITY;
     }
     // Probabilities against the reference maximum, rounded to V's type (half a step:
-    // bf16 2^-8, fp16 2^-11) as the matrix instruction takes them, and their sum,
-    // over the rounded values and in fp32, so that the weights add up to one.
-    u32x4_t pf[2 * NI];
+    // bf16 2^-8, fp16 2^-11; the two bf16 values of FINE 2^-17) as the matrix
+    // instruction takes them, and their sum in fp32, over the rounded values where
+    // they are coarse, so that the weights add up to one.
+    u32x4_t pf[2 * NI], pl[FINE ? 2 * NI : 1];
     float lsum;
     auto probs = [&](float ref) {
       const float mc = ref * c;
@@ -186,6 +217,11 @@ struct Rows32 {
             const f16x2_t h = __builtin_convertvector(f32x2_t{p0, p1}, f16x2_t);
             lsum = __builtin_amdgcn_fdot2(h, f16x2_t{(_Float16)1.0f, (_Float16)1.0f}, lsum, false);
             pf[sl][e] = __builtin_bit_cast(uint32_t, h);
+          } else if constexpr (FINE) {
+            const uint32_t h = pack_bf2(p0, p1);
+            lsum += p0 + p1;
+            pf[sl][e] = h;
+            pl[sl][e] = pack_bf2(p0 - __uint_as_float(h << 16), p1 - __uint_as_float(h & 0xffff0000u));
           } else {
             const bf16x2_t h = __builtin_convertvector(f32x2_t{p0, p1}, bf16x2_t);
             lsum = __builtin_amdgcn_fdot2_f32_bf16(h, bf16x2_t{(__bf16)1.0f, (__bf16)1.0f}, lsum, false);
@@ -236,57 +272,6 @@ struct Rows32 {
       return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     };
     constexpr int STEPS = 2 * NI * DT;
-    if (masked) {
-      // A value that is no number (NaN, an infinity) would reach the rows that do not
-      // see its key as 0 * value.  Where the tile holds one, the product takes zeros
-      // in their place, and a second one of their kinds (1 for inf, 128 for -inf,
-      // 16384 for NaN: sums of at most 64 each stay apart) with the 0/1 of what each
-      // row sees says which outputs they reach.
-      constexpr uint16_t EXPO = VF16 ? 0x7c00 : 0x7f80, MANT = VF16 ? 0x03ff : 0x007f;
-      constexpr uint16_t ONE = VF16 ? 0x3c00 : 0x3f80;
-      bool odd = false;
-#pragma unroll
-      for (int n = 0; n < STEPS; ++n) {
-        const auto f = vread(n);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) odd |= ((uint16_t)f[e] & EXPO) == EXPO;
-      }
-      if (__any(odd)) {
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt) {
-          f32x16_t kinds;
-#pragma unroll
-          for (int r = 0; r < 16; ++r) kinds[r] = 0.0f;
-#pragma unroll
-          for (int sl = 0; sl < 2 * NI; ++sl) {
-            auto f = vread(sl * DT + dt);
-            auto kind = f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const uint16_t b = (uint16_t)f[e];
-              const bool bad = (b & EXPO) == EXPO;
-              const float w = b & MANT ? 16384.0f : (b & 0x8000 ? 128.0f : 1.0f);
-              kind[e] = (short)(bad ? (VF16 ? f2h_bits(w) : f2bf(w)) : 0);
-              f[e] = bad ? 0 : f[e];
-            }
-            u32x4_t sees;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int at = 32 * (sl >> 1) + 16 * (sl & 1) + 8 * (e >> 1) + 2 * (e & 1);
-              sees[e] = (mine >> at & 1 ? ONE : 0u) | (mine >> (at + 1) & 1 ? (uint32_t)ONE << 16 : 0u);
-            }
-            o[dt] = mfma_v(__builtin_bit_cast(vfrag_t, f), pf[sl], o[dt]);
-            kinds = mfma_v(__builtin_bit_cast(vfrag_t, kind), sees, kinds);
-          }
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int t = (int)kinds[r], inf = t & 127, ninf = t >> 7 & 127;
-            if (t) o[dt][r] += t >= 16384 || (inf && ninf) ? NAN : (ninf ? -INFINITY : INFINITY);
-          }
-        }
-        return;
-      }
-    }
     vfrag_t vf[3];
     __builtin_amdgcn_sched_barrier(0);
     vf[0] = __builtin_bit_cast(vfrag_t, vread(0));
@@ -296,8 +281,9 @@ struct Rows32 {
     for (int n = 0; n < STEPS; ++n) {
       if (n + 2 < STEPS) vf[(n + 2) % 3] = __builtin_bit_cast(vfrag_t, vread(n + 2));
       o[n % DT] = mfma_v(vf[n % 3], pf[n / DT], o[n % DT]);
+      if constexpr (FINE) o[n % DT] = mfma_v(vf[n % 3], pl[n / DT], o[n % DT]);
       if (n + 2 < STEPS) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, FINE ? 2 : 1, 0);
     }
     __builtin_amdgcn_sched_barrier(0);
   }
@@ -305,6 +291,29 @@ struct Rows32 {
 
 // 1 / l, and 0 for a row that saw no key (its sums are zero); a NaN stays one.
 __device__ __forceinline__ float inverse(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
+
+// v (four dims from `dim` on) with what the swept values do to a row: keys from
+// `from` to the unit's end.  Those of tiles that were not swept have done it
+// already; an infinity or a NaN added again changes nothing.
+template <int DH, bool VF16, bool PAGED>
+__device__ __forceinline__ f32x4_t add_odd(f32x4_t v, const KeySource<DH, PAGED>& keys, const GqaUnit& u,
+                                           const GqaSight<PAGED>& sight, int from, int dim) {
+  for (int k0 = from; k0 < u.hi; k0 += 16) {
+    const int id = keys.page(k0);
+    if (!keys.held(id)) continue;
+    const KeyRows src = keys.rows(k0, id);
+    const uint32_t seen = (uint32_t)sight.seen(k0) & 0xffffu;
+    for (int i = 0; i < 16 && k0 + i < u.hi; ++i) {
+      const uint16_t* at = reinterpret_cast<const uint16_t*>(src.v + i * src.step_v) + dim;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float x = VF16 ? (float)__builtin_bit_cast(_Float16, at[e]) : bf2f(at[e]);
+        if ((seen >> i & 1) && !(fabsf(x) < INFINITY)) v[e] += x;
+      }
+    }
+  }
+  return v;
+}
 
 // Where unit (slot) leaves its result: per 32 rows and 32 dims 4 x 64 lanes x 16
 // bytes as the lanes hold them, then the rows' maxima and sums.
@@ -320,8 +329,8 @@ struct Parts {
   __device__ __forceinline__ float* div(int row) const { return base + RT * (DH + 1) + row; }
 };
 
-__device__ __forceinline__ uint16_t* out_row(const GqaParams& p, const GqaSeq& s, int hk, int tok, int head, int dh) {
-  return static_cast<uint16_t*>(p.out) + (size_t)(s.s0 + tok) * p.o_stride + (size_t)(hk * p.group + head) * dh;
+__device__ __forceinline__ uint16_t* out_row(const GqaParams& p, int row, int head, int dh) {
+  return static_cast<uint16_t*>(p.out) + (size_t)row * p.o_stride + (size_t)head * dh;
 }
 
 __device__ __forceinline__ void store4(uint16_t* at, f32x4_t v) {
@@ -340,29 +349,31 @@ __global__ __launch_bounds__(NT, 2) void gqa_tile_kernel(GqaParams p) {
   __shared__ __attribute__((aligned(1024))) uint8_t k_lds1[64 * ROW];
   __shared__ __attribute__((aligned(1024))) uint8_t v_lds0[64 * ROW];
   __shared__ __attribute__((aligned(1024))) uint8_t v_lds1[64 * ROW];
+  __shared__ int odd_from;                   // the first tile that had values to sweep
+  if (threadIdx.x == 0) odd_from = INT_MAX;
   GqaUnit u;
-  if (!gqa_find<kGqaTile, false>(p, blockIdx.x, u) || u.part >= u.parts) return;
+  if (!gqa_find<kGqaTile, NT>(p, u)) return;
   const int lane = threadIdx.x & 63;
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int fr = lane & 31, fhalf = lane >> 5;
   const int row = u.t * kGqaTile + wv * 32 + fr;
   const int src = row < u.s.rows ? row : u.s.rows - 1;
   const int tok = src / p.group, head = src - tok * p.group;
-  const int pos = u.s.past + tok;
-  // tokens of the wave's first and last row
-  const int first = (u.t * kGqaTile + wv * 32) / p.group;
-  const int last = (u.t * kGqaTile + wv * 32 + 31) / p.group;
-  const int open = gqa_open_end(p, u.hi, u.s.past + first, u.s.past);
-  const int wave_end = p.mask == kMaskCausal && u.s.past + last + 1 < u.hi ? u.s.past + last + 1 : u.hi;
+  const GqaSight<PAGED> sight(p, u, tok);
+  // where the workgroup's and the wave's rows begin to be blind to some keys, and
+  // where the wave's last row sees no more
+  const int open_all = gqa_open_end(p, u, u.t * kGqaTile / p.group);
+  const int open = gqa_open_end(p, u, (u.t * kGqaTile + wv * 32) / p.group);
+  int end = u.hi;
+  if (p.mask == kMaskCausal) end = u.s.past + (u.t * kGqaTile + wv * 32 + 31) / p.group + 1;
 
-  Rows32<DH, VF16, 2> w;
+  Rows32<DH, VF16, 2, false> w;
   w.init(p, static_cast<const uint16_t*>(p.q) + (size_t)(u.s.s0 + tok) * p.q_stride +
                 (size_t)(u.hk * p.group + head) * DH, lane);
 
   const KeySource<DH, PAGED> keys(p, u);
   const int n = (u.hi - u.lo + 63) / 64;
-  // pages of the four 16-key groups of a tile
-  int id[4];
+  int id[4];                                 // pages of the four 16-key groups of the next tile
   auto pages = [&](int kbase) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -372,27 +383,33 @@ __global__ __launch_bounds__(NT, 2) void gqa_tile_kernel(GqaParams p) {
   };
   auto load = [&](int kbase, auto buf) {
     constexpr int B = decltype(buf)::value;
-    // a group past the end is the last one again
-    int g = kbase + 16 * wv;
+    int g = kbase + 16 * wv;                 // a group past the end is the last one again
     g = g < u.hi ? g : (u.hi - 1) & ~15;
     const int page = wv == 0 ? id[0] : (wv == 1 ? id[1] : (wv == 2 ? id[2] : id[3]));
     load_keys<DH>(keys.rows(g, page), u.hi - 1 - g < 15 ? u.hi - 1 - g : 15, (B ? k_lds1 : k_lds0) + 16 * wv * ROW,
                   (B ? v_lds1 : v_lds0) + 16 * wv * ROW, lane);
   };
-  unsigned long long held = ~0ull, held_next = ~0ull;
-  auto held_of = [&]() {
-    unsigned long long m = ~0ull;
+  // bits of the keys whose pages are none of the pool's
+  unsigned long long lost = 0, lost_next = 0;
+  auto lost_of = [&]() {
+    unsigned long long m = 0;
     if constexpr (PAGED) {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        if (!keys.held(id[i])) m &= ~(0xffffull << (16 * i));
+        if (!keys.held(id[i])) m |= 0xffffull << (16 * i);
     }
     return m;
+  };
+  // after this wave's part of a tile has landed, before the barrier that publishes it
+  auto check = [&](int kbase, auto buf, unsigned long long lost) {
+    constexpr int B = decltype(buf)::value;
+    if (kbase + 64 <= open_all && lost == 0) return;
+    if (sweep<VF16, 16 * ROW>((B ? v_lds1 : v_lds0) + 16 * wv * ROW, lane) && lane == 0) atomicMin(&odd_from, kbase);
   };
   if (n > 0) {
     pages(u.lo);
     load(u.lo, std::integral_constant<int, 0>{});
-    held = held_of();
+    lost = lost_of();
     pages(u.lo + 64 < u.hi ? u.lo + 64 : u.hi - 1);
   }
   // every load so far (Q and tile 0) lands before the loop, so that the waits in it
@@ -400,24 +417,26 @@ __global__ __launch_bounds__(NT, 2) void gqa_tile_kernel(GqaParams p) {
   __builtin_amdgcn_sched_barrier(0);
   __builtin_amdgcn_s_waitcnt(0x0f70);       // vmcnt(0)
   __builtin_amdgcn_sched_barrier(0);
+  if (n > 0) check(u.lo, std::integral_constant<int, 0>{}, lost);
   __syncthreads();
   auto step = [&](int kt, auto buf) {
     constexpr int B = decltype(buf)::value;
     const int kbase = u.lo + 64 * kt;
     if (kt + 1 < n) {
       load(kbase + 64, std::integral_constant<int, B ^ 1>{});
-      held_next = held_of();
+      lost_next = lost_of();
       if (kt + 2 < n) pages(kbase + 128);
     }
-    if (kbase < wave_end) {
-      const bool masked = kbase + 64 > open || held != ~0ull;
-      unsigned long long seen = ~0ull;
-      if (masked) seen = held & gqa_seen(p, kbase, u.hi, pos, u.s.past, u.s.s0 + tok);
+    if (kbase < end) {
+      const bool masked = kbase + 64 > open || lost != 0;
+      unsigned long long seen = 0;
+      if (masked) seen = ~lost & sight.seen(kbase);
       w.step(B ? k_lds1 : k_lds0, B ? v_lds1 : v_lds0, lane, masked, seen);
     }
-    held = held_next;
+    lost = lost_next;
     // this wave's loads of the next tile have landed, then one barrier publishes it
     __builtin_amdgcn_s_waitcnt(0x0f70);
+    if (kt + 1 < n) check(kbase + 64, std::integral_constant<int, B ^ 1>{}, lost);
     __syncthreads();
   };
   for (int kt = 0; kt < n; kt += 2) {
@@ -425,14 +444,28 @@ __global__ __launch_bounds__(NT, 2) void gqa_tile_kernel(GqaParams p) {
     if (kt + 1 < n) step(kt + 1, std::integral_constant<int, 1>{});
   }
 
+  f32x4_t sum[DT * 4];
+#pragma unroll
+  for (int i = 0; i < DT * 4; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sum[i][e] = w.o[i >> 2][4 * (i & 3) + e];
+  const int odd = __builtin_amdgcn_readfirstlane(odd_from);
+  if (odd < u.hi) {
+#pragma unroll 1
+    for (int i = 0; i < DT * 4; ++i) {
+      // one copy of the code: the quadruples take turns at the front
+      const f32x4_t v = add_odd<DH, VF16, PAGED>(sum[0], keys, u, sight, odd, 32 * (i >> 2) + 8 * (i & 3) + 4 * fhalf);
+#pragma unroll
+      for (int k = 0; k + 1 < DT * 4; ++k) sum[k] = sum[k + 1];
+      sum[DT * 4 - 1] = v;
+    }
+  }
   const float l = w.l + __shfl_xor(w.l, 32, kWave);
   if (u.parts > 1) {
+    if (row >= u.s.rows) return;
     const Parts<kGqaTile, DH> to(p, u.slot + u.part);
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-      for (int g = 0; g < 4; ++g)
-        *to.sum(wv, dt, g, lane) = f32x4_t{w.o[dt][4 * g], w.o[dt][4 * g + 1], w.o[dt][4 * g + 2], w.o[dt][4 * g + 3]};
+    for (int i = 0; i < DT * 4; ++i) *to.sum(wv, i >> 2, i & 3, lane) = sum[i];
     if (fhalf == 0) {
       *to.max(wv * 32 + fr) = w.m;
       *to.div(wv * 32 + fr) = l;
@@ -440,46 +473,41 @@ __global__ __launch_bounds__(NT, 2) void gqa_tile_kernel(GqaParams p) {
     return;
   }
   if (row >= u.s.rows) return;
-  const float inv = tok < u.s.used ? inverse(l) : 0.0f;
-  uint16_t* at = out_row(p, u.s, u.hk, tok, head, DH) + fhalf * 4;
+  const bool real = tok < u.s.used;
+  const float inv = inverse(l);
+  uint16_t* at = out_row(p, u.s.s0 + tok, u.hk * p.group + head, DH) + fhalf * 4;
 #pragma unroll
-  for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      f32x4_t v;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = tok < u.s.used ? w.o[dt][4 * g + e] * inv : 0.0f;
-      store4(at + dt * 32 + g * 8, v);
-    }
+  for (int i = 0; i < DT * 4; ++i) store4(at + (i >> 2) * 32 + (i & 3) * 8, real ? sum[i] * inv : f32x4_t{0, 0, 0, 0});
 }
 
 template <int DH, bool VF16, bool PAGED>
-__global__ __launch_bounds__(NT, DH == 128 ? 1 : 2) void gqa_few_kernel(GqaParams p) {
+__global__ __launch_bounds__(NF, 1) void gqa_few_kernel(GqaParams p) {
   constexpr int ROW = DH * 2, DT = DH / 32, FT = 32 * ROW;      // bytes of a wave's K or V tile
-  __shared__ __attribute__((aligned(1024))) uint8_t k_lds0[4 * FT];
-  __shared__ __attribute__((aligned(1024))) uint8_t k_lds1[4 * FT];
-  __shared__ __attribute__((aligned(1024))) uint8_t v_lds0[4 * FT];
-  __shared__ __attribute__((aligned(1024))) uint8_t v_lds1[4 * FT];
-  __shared__ float m_part[4][32], l_part[4][32];
+  __shared__ __attribute__((aligned(1024))) uint8_t k_lds0[2 * FT];
+  __shared__ __attribute__((aligned(1024))) uint8_t k_lds1[2 * FT];
+  __shared__ __attribute__((aligned(1024))) uint8_t v_lds0[2 * FT];
+  __shared__ __attribute__((aligned(1024))) uint8_t v_lds1[2 * FT];
+  __shared__ float m_part[2][32], l_part[2][32];
+  __shared__ int odd_from[2];
   GqaUnit u;
-  if (!gqa_find<kGqaFew, false>(p, blockIdx.x, u) || u.part >= u.parts) return;
+  if (!gqa_find<kGqaFew, NF>(p, u)) return;
   const int lane = threadIdx.x & 63;
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int fr = lane & 31, fhalf = lane >> 5;
   const int row = u.t * kGqaFew + fr;
   const int src = row < u.s.rows ? row : u.s.rows - 1;
   const int tok = src / p.group, head = src - tok * p.group;
-  const int pos = u.s.past + tok;
-  const int open = gqa_open_end(p, u.hi, u.s.past + u.t * kGqaFew / p.group, u.s.past);
+  const GqaSight<PAGED> sight(p, u, tok);
+  const int open = gqa_open_end(p, u, u.t * kGqaFew / p.group);
 
-  Rows32<DH, VF16, 1> w;
+  Rows32<DH, VF16, 1, !VF16> w;
   w.init(p, static_cast<const uint16_t*>(p.q) + (size_t)(u.s.s0 + tok) * p.q_stride +
                 (size_t)(u.hk * p.group + head) * DH, lane);
 
   const KeySource<DH, PAGED> keys(p, u);
-  // this wave's tiles: 32 of every 128 keys
+  // this wave's tiles: 32 of every 64 keys
   const int k0 = u.lo + 32 * wv;
-  const int n = u.hi > k0 ? (u.hi - k0 + 127) / 128 : 0;
+  const int n = u.hi > k0 ? (u.hi - k0 + 63) / 64 : 0;
   int id[2];
   auto pages = [&](int kbase) {
 #pragma unroll
@@ -498,20 +526,21 @@ __global__ __launch_bounds__(NT, DH == 128 ? 1 : 2) void gqa_few_kernel(GqaParam
                     (B ? k_lds1 : k_lds0) + wv * FT + 16 * i * ROW, (B ? v_lds1 : v_lds0) + wv * FT + 16 * i * ROW, lane);
     }
   };
-  unsigned long long held = ~0ull, held_next = ~0ull;
-  auto held_of = [&]() {
-    unsigned long long m = ~0ull;
+  uint32_t lost = 0, lost_next = 0;
+  auto lost_of = [&]() {
+    uint32_t m = 0;
     if constexpr (PAGED) {
-      if (!keys.held(id[0])) m &= ~0xffffull;
-      if (!keys.held(id[1])) m &= ~0xffff0000ull;
+      if (!keys.held(id[0])) m |= 0xffffu;
+      if (!keys.held(id[1])) m |= 0xffff0000u;
     }
     return m;
   };
+  int odd = INT_MAX;
   if (n > 0) {
     pages(k0);
     load(k0, std::integral_constant<int, 0>{});
-    held = held_of();
-    pages(k0 + 128 < u.hi ? k0 + 128 : u.hi - 1);
+    lost = lost_of();
+    pages(k0 + 64 < u.hi ? k0 + 64 : u.hi - 1);
   }
   __builtin_amdgcn_sched_barrier(0);
   __builtin_amdgcn_s_waitcnt(0x0f70);       // vmcnt(0)
@@ -519,17 +548,21 @@ __global__ __launch_bounds__(NT, DH == 128 ? 1 : 2) void gqa_few_kernel(GqaParam
   __builtin_amdgcn_sched_barrier(0);
   auto step = [&](int kt, auto buf) {
     constexpr int B = decltype(buf)::value;
-    const int kbase = k0 + 128 * kt;
+    const int kbase = k0 + 64 * kt;
+    uint8_t* vl = (B ? v_lds1 : v_lds0) + wv * FT;
     if (kt + 1 < n) {
-      load(kbase + 128, std::integral_constant<int, B ^ 1>{});
-      held_next = held_of();
-      if (kt + 2 < n) pages(kbase + 256);
+      load(kbase + 64, std::integral_constant<int, B ^ 1>{});
+      lost_next = lost_of();
+      if (kt + 2 < n) pages(kbase + 128);
     }
-    const bool masked = kbase + 32 > open || held != ~0ull;
-    unsigned long long seen = ~0ull;
-    if (masked) seen = held & gqa_seen(p, kbase, u.hi, pos, u.s.past, u.s.s0 + tok);
-    w.step((B ? k_lds1 : k_lds0) + wv * FT, (B ? v_lds1 : v_lds0) + wv * FT, lane, masked, seen);
-    held = held_next;
+    const bool masked = kbase + 32 > open || lost != 0;
+    unsigned long long seen = 0;
+    if (masked) {
+      seen = ~lost & sight.seen(kbase);
+      if (sweep<VF16, FT>(vl, lane)) odd = kbase < odd ? kbase : odd;
+    }
+    w.step((B ? k_lds1 : k_lds0) + wv * FT, vl, lane, masked, seen);
+    lost = lost_next;
     // the next tile has landed; this one's fragments are in registers or consumed
     __builtin_amdgcn_sched_barrier(0);
     __builtin_amdgcn_s_waitcnt(0x0070);     // vmcnt(0) and lgkmcnt(0)
@@ -541,12 +574,13 @@ __global__ __launch_bounds__(NT, DH == 128 ? 1 : 2) void gqa_few_kernel(GqaParam
     if (kt + 1 < n) step(kt + 1, std::integral_constant<int, 1>{});
   }
 
-  // join the waves: each leaves its sums in its own K tiles and takes 32 dims
+  // join the waves: each leaves its sums in its own K tiles and takes half the dims
   const float l_own = w.l + __shfl_xor(w.l, 32, kWave);
   if (fhalf == 0) {
     m_part[wv][fr] = w.m;
     l_part[wv][fr] = l_own;
   }
+  if (lane == 0) odd_from[wv] = odd;
   auto sums = [&](int v, int dt, int g) {
     const int at = dt * 4 + g;              // of DT * 4 blocks of 1 KiB; a buffer has FT / 1024 of them
     return reinterpret_cast<f32x4_t*>((at >= FT / 1024 ? k_lds1 : k_lds0) + v * FT + at % (FT / 1024) * 1024 + lane * 16);
@@ -557,65 +591,58 @@ __global__ __launch_bounds__(NT, DH == 128 ? 1 : 2) void gqa_few_kernel(GqaParam
     for (int g = 0; g < 4; ++g)
       *sums(wv, dt, g) = f32x4_t{w.o[dt][4 * g], w.o[dt][4 * g + 1], w.o[dt][4 * g + 2], w.o[dt][4 * g + 3]};
   __syncthreads();
-  if (wv >= DT) return;
-  float m = m_part[0][fr];
-#pragma unroll
-  for (int v = 1; v < 4; ++v) m = fmaxf(m, m_part[v][fr]);
+  const float m = fmaxf(m_part[0][fr], m_part[1][fr]);
   const float ref = m == -INFINITY ? 0.0f : m;
-  float l = 0.0f;
-  f32x4_t sum[4];
+  float a[2];
 #pragma unroll
-  for (int g = 0; g < 4; ++g) sum[g] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-  for (int v = 0; v < 4; ++v) {
-    const float a = __builtin_amdgcn_exp2f((m_part[v][fr] - ref) * w.c);
-    if (m_part[v][fr] == -INFINITY && l_part[v][fr] == 0.0f) continue;      // a wave whose keys the row does not see
-    l += l_part[v][fr] * a;
-#pragma unroll
-    for (int g = 0; g < 4; ++g) sum[g] += a * *sums(v, wv, g);
+  for (int v = 0; v < 2; ++v) {
+    // a wave whose keys the row does not see has no part
+    const bool none = m_part[v][fr] == -INFINITY && l_part[v][fr] == 0.0f;
+    a[v] = none ? 0.0f : __builtin_amdgcn_exp2f((m_part[v][fr] - ref) * w.c);
   }
-  if (u.parts > 1) {
-    const Parts<kGqaFew, DH> to(p, u.slot + u.part);
-#pragma unroll
-    for (int g = 0; g < 4; ++g) *to.sum(0, wv, g, lane) = sum[g];
-    if (wv == 0 && fhalf == 0) {
-      *to.max(fr) = m;
-      *to.div(fr) = l;
-    }
-    return;
-  }
-  if (row >= u.s.rows) return;
+  const float l = l_part[0][fr] * a[0] + l_part[1][fr] * a[1];
+  odd = __builtin_amdgcn_readfirstlane(odd_from[0] < odd_from[1] ? odd_from[0] : odd_from[1]);
+  const Parts<kGqaFew, DH> to(p, u.slot + u.part);
   const bool real = tok < u.s.used;
   const float inv = inverse(l);
-  uint16_t* at = out_row(p, u.s, u.hk, tok, head, DH) + wv * 32 + fhalf * 4;
-#pragma unroll
-  for (int g = 0; g < 4; ++g) {
-    f32x4_t v;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = real ? sum[g][e] * inv : 0.0f;
-    store4(at + g * 8, v);
+  if (u.parts > 1 && wv == 0 && fhalf == 0 && row < u.s.rows) {
+    *to.max(fr) = m;
+    *to.div(fr) = l;
+  }
+#pragma unroll 2
+  for (int i = 0; i < DT * 2; ++i) {
+    const int at = wv * DT * 2 + i, dt = at >> 2, g = at & 3;
+    f32x4_t v = a[0] * *sums(0, dt, g) + a[1] * *sums(1, dt, g);
+    if (odd < u.hi) v = add_odd<DH, VF16, PAGED>(v, keys, u, sight, odd & ~15, 32 * dt + 8 * g + 4 * fhalf);
+    if (row >= u.s.rows) continue;
+    if (u.parts > 1) *to.sum(0, dt, g, lane) = v;
+    else store4(out_row(p, u.s.s0 + tok, u.hk * p.group + head, DH) + dt * 32 + g * 8 + fhalf * 4,
+                real ? v * inv : f32x4_t{0, 0, 0, 0});
   }
 }
 
-// Adds the parts of each tile whose keys were cut: a wave takes 32 rows x 32 dims
-// x a quarter (one 16-byte piece a lane).
+// Adds the parts of each tile whose keys were cut, by the records that its first
+// part left: a wave takes 32 rows x 8 dims (16 bytes a lane).
 template <int RT, int DH>
 __global__ __launch_bounds__(NT) void gqa_join_kernel(GqaParams p) {
-  constexpr int DT = DH / 32, PIECES = RT / 32 * DT;       // workgroups of a tile
-  GqaUnit u;
-  const int piece = blockIdx.x % PIECES;
-  if (!gqa_find<RT, true>(p, blockIdx.x / PIECES, u) || u.parts < 2) return;
+  constexpr int DT = DH / 32, PIECES = RT / 32 * DT;       // workgroups of a slot
+  const int slot = blockIdx.x / PIECES, piece = blockIdx.x % PIECES;
+  const GqaRecord r = static_cast<const GqaRecord*>(p.records)[slot];
+  if (r.parts < 2) return;
   const int lane = threadIdx.x & 63, g = threadIdx.x >> 6, fr = lane & 31, fhalf = lane >> 5;
   const int w = piece / DT, dt = piece % DT;
+  const int row = r.t * RT + w * 32 + fr;
+  if (row >= r.rows) return;
   const float c = p.scale * 1.4426950408889634f;
   float m = -INFINITY;
-  for (int i = 0; i < u.parts; ++i) m = fmaxf(m, *Parts<RT, DH>(p, u.slot + i).max(w * 32 + fr));
+#pragma unroll 8
+  for (int i = 0; i < r.parts; ++i) m = fmaxf(m, *Parts<RT, DH>(p, slot + i).max(w * 32 + fr));
   const float ref = m == -INFINITY ? 0.0f : m;
   float l = 0.0f;
   f32x4_t sum = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 4
-  for (int i = 0; i < u.parts; ++i) {
-    const Parts<RT, DH> from(p, u.slot + i);
+#pragma unroll 8
+  for (int i = 0; i < r.parts; ++i) {
+    const Parts<RT, DH> from(p, slot + i);
     const float mi = *from.max(w * 32 + fr), li = *from.div(w * 32 + fr);
     const f32x4_t v = *from.sum(w, dt, g, lane);
     const bool none = mi == -INFINITY && li == 0.0f;
@@ -623,14 +650,10 @@ __global__ __launch_bounds__(NT) void gqa_join_kernel(GqaParams p) {
     l += li * a;
     sum += a * v;
   }
-  const int row = u.t * RT + w * 32 + fr;
-  if (row >= u.s.rows) return;
   const int tok = row / p.group, head = row - tok * p.group;
-  const bool real = tok < u.s.used;
   const float inv = inverse(l);
-#pragma unroll
-  for (int e = 0; e < 4; ++e) sum[e] = real ? sum[e] * inv : 0.0f;
-  store4(out_row(p, u.s, u.hk, tok, head, DH) + dt * 32 + g * 8 + fhalf * 4, sum);
+  store4(out_row(p, r.s0 + tok, r.hk * p.group + head, DH) + dt * 32 + g * 8 + fhalf * 4,
+         tok < r.used ? sum * inv : f32x4_t{0, 0, 0, 0});
 }
 
 int launch_gqa_bf16(const GqaParams& p, const GqaRule& r, hipStream_t s) {
@@ -639,10 +662,10 @@ int launch_gqa_bf16(const GqaParams& p, const GqaRule& r, hipStream_t s) {
     constexpr bool V = decltype(vf16)::value, P = decltype(paged)::value;
     if (r.rt == kGqaTile) {
       hipLaunchKernelGGL((gqa_tile_kernel<DH, V, P>), dim3(r.grid), dim3(NT), 0, s, p);
-      if (r.target) hipLaunchKernelGGL((gqa_join_kernel<kGqaTile, DH>), dim3(r.tiles * (4 * DH / 32)), dim3(NT), 0, s, p);
+      if (r.target) hipLaunchKernelGGL((gqa_join_kernel<kGqaTile, DH>), dim3(r.grid * (4 * DH / 32)), dim3(NT), 0, s, p);
     } else {
-      hipLaunchKernelGGL((gqa_few_kernel<DH, V, P>), dim3(r.grid), dim3(NT), 0, s, p);
-      if (r.target) hipLaunchKernelGGL((gqa_join_kernel<kGqaFew, DH>), dim3(r.tiles * (DH / 32)), dim3(NT), 0, s, p);
+      hipLaunchKernelGGL((gqa_few_kernel<DH, V, P>), dim3(r.grid), dim3(NF), 0, s, p);
+      if (r.target) hipLaunchKernelGGL((gqa_join_kernel<kGqaFew, DH>), dim3(r.grid * (DH / 32)), dim3(NT), 0, s, p);
     }
   };
   auto with = [&](auto dh, auto vf16) {

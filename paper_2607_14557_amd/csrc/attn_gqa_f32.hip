@@ -35,8 +35,9 @@ __global__ __launch_bounds__(NT) void gqa_f32_kernel(GqaParams p) {
   constexpr int C = 4 * H;                                     // 16-dim pieces
   __shared__ f32x4_t o_part[4][4 * H][64];
   __shared__ float m_part[4][16], l_part[4][16];
+  __shared__ int odd_part[4];
   GqaUnit u;
-  if (!gqa_find<kGqaF32, false>(p, blockIdx.x, u) || u.part >= u.parts) return;
+  if (!gqa_find<kGqaF32, NT>(p, u)) return;
   const int lane = threadIdx.x & 63;
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int fr = lane & 15, g = lane >> 4;
@@ -44,8 +45,8 @@ __global__ __launch_bounds__(NT) void gqa_f32_kernel(GqaParams p) {
   const int row = u.t * kGqaF32 + fr;
   const int src = row < u.s.rows ? row : u.s.rows - 1;
   const int tok = src / p.group, head = src - tok * p.group;
-  const int pos = u.s.past + tok;
-  const int open = gqa_open_end(p, u.hi, u.s.past + u.t * kGqaF32 / p.group, u.s.past);
+  const GqaSight<PAGED> sight(p, u, tok);
+  const int open = gqa_open_end(p, u, u.t * kGqaF32 / p.group);
   const float c = p.scale * 1.4426950408889634f;
   const f32x4_t zero = {0.0f, 0.0f, 0.0f, 0.0f};
 
@@ -72,22 +73,28 @@ __global__ __launch_bounds__(NT) void gqa_f32_kernel(GqaParams p) {
   for (int i = 0; i < 4 * H; ++i) o[i] = zero;
   float m = -INFINITY, l = 0.0f;
 
-  for (int k0 = u.lo + 16 * wv; k0 < u.hi; k0 += 64) {
-    const int last = u.hi - 1 - k0 < 15 ? u.hi - 1 - k0 : 15;   // the group's last key: those past it are it again
-    bool held = true;
-    const float *ks = kp, *vs = vp;
-    size_t step_k = p.k_stride, step_v = p.v_stride;
+  // where the group of keys from k0 on lies (k0 a multiple of 16); false: its page is none of the pool's
+  auto place = [&](int k0, const float*& ks, const float*& vs, size_t& step_k, size_t& step_v) {
     if (PAGED) {
-      int id = scalar_load(table, k0 >> p.shift);
-      held = id >= 0 && id < p.n_pages;
-      id = held ? id : 0;
-      ks += (size_t)id * 2 * half + (((size_t)u.hk << p.shift) + (k0 & ((1 << p.shift) - 1))) * D;
+      const int id = scalar_load(table, k0 >> p.shift);
+      const bool held = id >= 0 && id < p.n_pages;
+      ks = kp + (size_t)(held ? id : 0) * 2 * half + (((size_t)u.hk << p.shift) + (k0 & ((1 << p.shift) - 1))) * D;
       vs = ks + half;
       step_k = step_v = D;
-    } else {
-      ks += (size_t)k0 * step_k;
-      vs += (size_t)k0 * step_v;
+      return held;
     }
+    ks = kp + (size_t)k0 * p.k_stride;
+    vs = vp + (size_t)k0 * p.v_stride;
+    step_k = p.k_stride;
+    step_v = p.v_stride;
+    return true;
+  };
+  int odd_from = INT_MAX;
+  for (int k0 = u.lo + 16 * wv; k0 < u.hi; k0 += 64) {
+    const int last = u.hi - 1 - k0 < 15 ? u.hi - 1 - k0 : 15;   // the group's last key: those past it are it again
+    const float *ks, *vs;
+    size_t step_k, step_v;
+    const bool held = place(k0, ks, vs, step_k, step_v);
     const float* kr = ks + (fr < last ? fr : last) * step_k;
     f32x4_t kf[C], vf[4][H];
 #pragma unroll
@@ -119,13 +126,25 @@ __global__ __launch_bounds__(NT) void gqa_f32_kernel(GqaParams p) {
     }
     f32x4_t s = s0 + s1;                                      // key k0 + 4 g + e
     const bool masked = k0 + 16 > open || !held;
-    unsigned mine = 0xf;
     if (masked) {
-      const unsigned long long seen = held ? gqa_seen(p, k0, u.hi, pos, u.s.past, u.s.s0 + tok) : 0;
-      mine = (unsigned)(seen >> (4 * g)) & 0xf;
+      const uint32_t mine = held ? (uint32_t)(sight.seen(k0) >> (4 * g)) : 0;
 #pragma unroll
       for (int e = 0; e < 4; ++e)
         if (!(mine >> e & 1)) s[e] = -INFINITY;
+      // values that are no numbers would reach the rows that do not see their keys as
+      // 0 * value: zeros here, and added to the rows that see them at the end
+      bool odd = false;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int h = 0; h < H; ++h)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (!(fabsf(vf[i][h][e]) < INFINITY)) {
+              vf[i][h][e] = 0.0f;
+              odd = true;
+            }
+      if (__any(odd)) odd_from = k0 < odd_from ? k0 : odd_from;
     }
     float mt = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
     mt = fmaxf(mt, __shfl_xor(mt, 16, kWave));
@@ -143,46 +162,13 @@ __global__ __launch_bounds__(NT) void gqa_f32_kernel(GqaParams p) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) w[e] = __builtin_amdgcn_exp2f(s[e] * c - mc);
     l += (w[0] + w[1]) + (w[2] + w[3]);
-    bool odd = false;
-    if (masked) {
-      // values that are no numbers would reach the rows that do not see their keys as
-      // 0 * value; see the bf16 kernels for the way round it
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int h = 0; h < H; ++h)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) odd |= !(fabsf(vf[i][h][e]) < INFINITY);
-    }
-    if (masked && __any(odd)) {
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int h = 0; h < H; ++h)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          f32x4_t kinds = zero;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float x = vf[i][h][e];
-            const bool bad = !(fabsf(x) < INFINITY);
-            const float kind = !bad ? 0.0f : (x != x ? 16384.0f : (x < 0.0f ? 128.0f : 1.0f));
-            o[4 * h + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(bad ? 0.0f : x, w[i], o[4 * h + e], 0, 0, 0);
-            kinds = __builtin_amdgcn_mfma_f32_16x16x4f32(kind, mine >> i & 1 ? 1.0f : 0.0f, kinds, 0, 0, 0);
-          }
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int t = (int)kinds[r], inf = t & 127, ninf = t >> 7 & 127;
-            if (t) o[4 * h + e][r] += t >= 16384 || (inf && ninf) ? NAN : (ninf ? -INFINITY : INFINITY);
-          }
-        }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int h = 0; h < H; ++h)
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            o[4 * h + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[i][h][e], w[i], o[4 * h + e], 0, 0, 0);
-    }
+        for (int e = 0; e < 4; ++e)
+          o[4 * h + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[i][h][e], w[i], o[4 * h + e], 0, 0, 0);
   }
 
   // join the waves: wave w takes sums w, w + 4
@@ -194,6 +180,7 @@ __global__ __launch_bounds__(NT) void gqa_f32_kernel(GqaParams p) {
     m_part[wv][fr] = m;
     l_part[wv][fr] = l;
   }
+  if (lane == 0) odd_part[wv] = odd_from;
   __syncthreads();
   m = fmaxf(fmaxf(m_part[0][fr], m_part[1][fr]), fmaxf(m_part[2][fr], m_part[3][fr]));
   const float ref = m == -INFINITY ? 0.0f : m;
@@ -210,7 +197,30 @@ __global__ __launch_bounds__(NT) void gqa_f32_kernel(GqaParams p) {
 #pragma unroll
     for (int h = 0; h < H; ++h) sum[h] += a * o_part[v][4 * h + wv][lane];
   }
+  // sum[h][i] is dim 64 h + 16 g + 4 i + wv
+  odd_from = min(min(odd_part[0], odd_part[1]), min(odd_part[2], odd_part[3]));
+  odd_from = __builtin_amdgcn_readfirstlane(odd_from);
+  if (odd_from < u.hi) {
+    // the values that were left out, for the keys that the row sees (again for those
+    // of other groups, which changes nothing)
+    for (int k0 = odd_from; k0 < u.hi; k0 += 16) {
+      const float *ks, *vs;
+      size_t step_k, step_v;
+      if (!place(k0, ks, vs, step_k, step_v)) continue;
+      const uint32_t seen = (uint32_t)sight.seen(k0);
+      for (int j = 0; j < 16 && k0 + j < u.hi; ++j)
+#pragma unroll
+        for (int h = 0; h < H; ++h)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int d = 64 * h + 16 * g + 4 * i + wv;
+            const float x = vs[j * step_v + (d < D ? d : 0)];
+            if ((seen >> j & 1) && !(fabsf(x) < INFINITY)) sum[h][i] += x;
+          }
+    }
+  }
   if (u.parts > 1) {
+    if (row >= u.s.rows) return;
     const Parts<H> to(p, u.slot + u.part);
 #pragma unroll
     for (int h = 0; h < H; ++h) *to.sum(4 * h + wv, lane) = sum[h];
@@ -221,7 +231,6 @@ __global__ __launch_bounds__(NT) void gqa_f32_kernel(GqaParams p) {
     return;
   }
   if (row >= u.s.rows) return;
-  // sum[h][i] is dim 64 h + 16 g + 4 i + wv
   const bool real = tok < u.s.used;
   const float inv = inverse(l);
   float* out = static_cast<float*>(p.out) + (size_t)(u.s.s0 + tok) * p.o_stride + (size_t)(u.hk * p.group + head) * D;
@@ -237,32 +246,34 @@ __global__ __launch_bounds__(NT) void gqa_f32_kernel(GqaParams p) {
 // Adds the parts of each tile whose keys were cut; wave w as in the kernel above.
 template <int H>
 __global__ __launch_bounds__(NT) void gqa_f32_join_kernel(GqaParams p) {
-  GqaUnit u;
-  if (!gqa_find<kGqaF32, true>(p, blockIdx.x, u) || u.parts < 2) return;
+  const int slot = blockIdx.x;
+  const GqaRecord r = static_cast<const GqaRecord*>(p.records)[slot];
+  if (r.parts < 2) return;
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, fr = lane & 15, g = lane >> 4, D = p.head_dim;
+  const int row = r.t * kGqaF32 + fr;
+  if (row >= r.rows) return;
   const float c = p.scale * 1.4426950408889634f;
   float m = -INFINITY;
-  for (int i = 0; i < u.parts; ++i) m = fmaxf(m, *Parts<H>(p, u.slot + i).max(fr));
+#pragma unroll 8
+  for (int i = 0; i < r.parts; ++i) m = fmaxf(m, *Parts<H>(p, slot + i).max(fr));
   const float ref = m == -INFINITY ? 0.0f : m;
   float l = 0.0f;
   f32x4_t sum[H];
 #pragma unroll
   for (int h = 0; h < H; ++h) sum[h] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 4
-  for (int i = 0; i < u.parts; ++i) {
-    const Parts<H> from(p, u.slot + i);
+#pragma unroll 8
+  for (int i = 0; i < r.parts; ++i) {
+    const Parts<H> from(p, slot + i);
     const float mi = *from.max(fr), li = *from.div(fr);
     const float a = mi == -INFINITY && li == 0.0f ? 0.0f : __builtin_amdgcn_exp2f((mi - ref) * c);
     l += li * a;
 #pragma unroll
     for (int h = 0; h < H; ++h) sum[h] += a * *from.sum(4 * h + wv, lane);
   }
-  const int row = u.t * kGqaF32 + fr;
-  if (row >= u.s.rows) return;
   const int tok = row / p.group, head = row - tok * p.group;
-  const bool real = tok < u.s.used;
+  const bool real = tok < r.used;
   const float inv = inverse(l);
-  float* out = static_cast<float*>(p.out) + (size_t)(u.s.s0 + tok) * p.o_stride + (size_t)(u.hk * p.group + head) * D;
+  float* out = static_cast<float*>(p.out) + (size_t)(r.s0 + tok) * p.o_stride + (size_t)(r.hk * p.group + head) * D;
 #pragma unroll
   for (int h = 0; h < H; ++h)
 #pragma unroll
@@ -277,11 +288,11 @@ int launch_gqa_f32(const GqaParams& p, const GqaRule& r, hipStream_t s) {
   if (p.head_dim > 64) {
     if (p.table) hipLaunchKernelGGL((gqa_f32_kernel<2, true>), grid, block, 0, s, p);
     else hipLaunchKernelGGL((gqa_f32_kernel<2, false>), grid, block, 0, s, p);
-    if (r.target) hipLaunchKernelGGL(gqa_f32_join_kernel<2>, dim3(r.tiles), block, 0, s, p);
+    if (r.target) hipLaunchKernelGGL(gqa_f32_join_kernel<2>, dim3(r.grid), block, 0, s, p);
   } else {
     if (p.table) hipLaunchKernelGGL((gqa_f32_kernel<1, true>), grid, block, 0, s, p);
     else hipLaunchKernelGGL((gqa_f32_kernel<1, false>), grid, block, 0, s, p);
-    if (r.target) hipLaunchKernelGGL(gqa_f32_join_kernel<1>, dim3(r.tiles), block, 0, s, p);
+    if (r.target) hipLaunchKernelGGL(gqa_f32_join_kernel<1>, dim3(r.grid), block, 0, s, p);
   }
   return hipGetLastError() == hipSuccess ? 0 : -1;
 }

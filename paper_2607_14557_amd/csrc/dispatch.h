@@ -189,23 +189,23 @@ struct GqaRule {
   int rt;                // rows of a tile
   int target;            // units to cut the tiles' keys for, 0: not cut
   int grid;              // the most units that can come out
-  int tiles;             // the most tiles, over all heads
-  size_t bytes;          // of the parts' results
+  size_t records;        // bytes of the parts' records
+  size_t bytes;          // of the records and the results
 };
 
 // The form of a launch of up to `rows` rows in `batch` requests.
 inline GqaRule gqa_rule(bool bf16, int heads, int n_kv, int dim, int rows, int batch) {
-  constexpr int kUnits = 512;            // two workgroups for each of 256 CUs
   GqaRule r{};
   const int group = heads / n_kv;
   const long long pairs = (long long)rows * group;
   r.rt = !bf16 ? kGqaF32 : (pairs / batch > 64 ? kGqaTile : kGqaFew);
   const long long tiles = (pairs >= batch ? (pairs - batch) / r.rt + batch : pairs) * n_kv;
-  r.tiles = (int)tiles;
-  r.target = tiles < kUnits ? kUnits : 0;
+  const int units = r.rt == kGqaFew ? 1024 : 512;
+  r.target = tiles < units ? units : 0;
   r.grid = (int)(tiles + (r.target ? r.target + n_kv : 0));
   // a part: the sums of each row, its maximum and its divisor
-  r.bytes = r.target ? (size_t)r.grid * r.rt * ((dim > 64 ? 128 : 64) + 2) * 4 : 0;
+  r.records = r.target ? ((size_t)r.grid * 32 + 255) / 256 * 256 : 0;
+  r.bytes = r.target ? r.records + (size_t)r.grid * r.rt * ((dim > 64 ? 128 : 64) + 2) * 4 : 0;
   return r;
 }
 

@@ -57,6 +57,12 @@ struct GqaUnit {
   GqaSeq s;
 };
 
+// What the joining of a tile's parts has to know, left by the unit of its first
+// part (parts < 2: nothing to join), one per slot.
+struct GqaRecord {
+  int parts, s0, used, rows, t, hk, pad[2];
+};
+
 // The keys that any row of tile t sees end here.
 template <int RT>
 __device__ __forceinline__ int gqa_tile_end(const GqaParams& p, const GqaSeq& s, int t) {
@@ -68,95 +74,104 @@ __device__ __forceinline__ int gqa_tile_end(const GqaParams& p, const GqaSeq& s,
   return end < 0 ? 0 : (end < s.nk ? end : s.nk);
 }
 
-// Finds unit bid of the launch; false past the last one.  Called by all 256
-// threads: each sums its share of the requests, then one scan over the
-// workgroup locates the unit.  p.target > 0: the tiles' keys are cut so that
-// about p.target units come out over all heads, every part the same number of
-// blocks, whatever the requests' lengths.  TILES: bid counts tiles instead (for
-// the joining of their parts).
-template <int RT, bool TILES>
-__device__ __forceinline__ bool gqa_find(const GqaParams& p, int bid, GqaUnit& u) {
-  __shared__ long long wave_sum[4];
-  __shared__ int found[4];
+// Finds the workgroup's unit; false where there is none.  Called by all NT
+// threads: each sums its share of the requests, then one scan over the workgroup
+// locates the unit.  p.target > 0: the tiles' keys are cut so that about p.target
+// units come out over all heads, every part the same number of blocks, whatever
+// the requests' lengths; the workgroup leaves its slot's record.
+template <int RT, int NT>
+__device__ __forceinline__ bool gqa_find(const GqaParams& p, GqaUnit& u) {
+  constexpr int NW = NT / kWave;
+  __shared__ long long wave_sum[2][NW];
+  __shared__ int found[10];
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6;
-  const int per = (p.B + 255) / 256;
+  const int per = (p.B + NT - 1) / NT;
   const int b0 = tid * per < p.B ? tid * per : p.B;
   const int b1 = b0 + per < p.B ? b0 + per : p.B;
+  // with at most one request a thread its lengths are read once
+  GqaSeq mine{};
+  if (per == 1 && b0 < b1) mine = gqa_seq<RT>(p, b0);
+  auto seq = [&](int b) { return per == 1 ? mine : gqa_seq<RT>(p, b); };
   int chunk = INT_MAX;
   if (p.target > 0) {
     long long n = 0;
     for (int b = b0; b < b1; ++b) {
-      const GqaSeq s = gqa_seq<RT>(p, b);
+      const GqaSeq s = seq(b);
       n += (long long)s.tiles * gqa_blocks(s.nk);
     }
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) n += __shfl_xor(n, off, kWave);
-    if (lane == 0) wave_sum[wave] = n;
+    if (lane == 0) wave_sum[0][wave] = n;
     __syncthreads();
-    n = (wave_sum[0] + wave_sum[1] + wave_sum[2] + wave_sum[3]) * p.n_kv;
-    __syncthreads();
-    const long long c = (n + p.target - 1) / p.target;
-    chunk = c < p.min_chunk ? p.min_chunk : (c < INT_MAX ? (int)c : INT_MAX);
+    n = 0;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) n += wave_sum[0][w];
+    const long long c = (n * p.n_kv + p.target - 1) / p.target;
+    chunk = c < 1 ? 1 : (c < INT_MAX ? (int)c : INT_MAX);
   }
-  int units = 0, tiles = 0;
+  int units = 0;
   for (int b = b0; b < b1; ++b) {
-    const GqaSeq s = gqa_seq<RT>(p, b);
+    const GqaSeq s = seq(b);
     units += s.tiles * ((gqa_blocks(s.nk) - 1) / chunk + 1);
-    tiles += s.tiles;
   }
-  // both sums in one scan
-  long long inc = (long long)tiles << 32 | (unsigned)units;
-  const long long own = inc;
+  int inc = units;
 #pragma unroll
   for (int off = 1; off < kWave; off <<= 1) {
-    const long long v = __shfl_up(inc, off, kWave);
+    const int v = __shfl_up(inc, off, kWave);
     if (lane >= off) inc += v;
   }
-  if (lane == kWave - 1) wave_sum[wave] = inc;
+  if (lane == kWave - 1) wave_sum[1][wave] = inc;
   __syncthreads();
-  long long all = 0, before = inc - own;
+  int n = 0, first = inc - units;
 #pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    if (w < wave) before += wave_sum[w];
-    all += wave_sum[w];
+  for (int w = 0; w < NW; ++w) {
+    if (w < wave) first += (int)wave_sum[1][w];
+    n += (int)wave_sum[1][w];
   }
-  const int n = TILES ? (int)(all >> 32) : (int)all;         // of one head
-  if (bid >= n * p.n_kv || (long long)(unsigned)all * p.n_kv > p.max_units) return false;
+  GqaRecord* records = reinterpret_cast<GqaRecord*>(p.records);
+  const int bid = blockIdx.x;
+  if (bid >= (long long)n * p.n_kv || (long long)n * p.n_kv > p.max_units) {
+    if (p.target > 0 && tid == 0) records[bid].parts = 0;
+    return false;
+  }
   // each XCD takes a contiguous range of units, heads slowest: the tiles of one
   // request and head find their keys in its L2
   const int w = xcd_remap(bid, n * p.n_kv);
   u.hk = w / n;
   const int j = w - u.hk * n;
-  int first = TILES ? (int)(before >> 32) : (int)before, unit0 = (int)before;
-  if (j >= first && j < first + (TILES ? tiles : units)) {
+  if (j >= first && j < first + units) {
     int b = b0;
+    GqaSeq s;
+    int m;
     for (;; ++b) {
-      const GqaSeq s = gqa_seq<RT>(p, b);
-      const int parts = (gqa_blocks(s.nk) - 1) / chunk + 1, m = TILES ? s.tiles : s.tiles * parts;
+      s = seq(b);
+      m = s.tiles * ((gqa_blocks(s.nk) - 1) / chunk + 1);
       if (j < first + m) break;
       first += m;
-      unit0 += s.tiles * parts;
     }
-    found[0] = b;
-    found[1] = j - first;
-    found[2] = unit0;
+    found[0] = b; found[1] = j - first; found[2] = first;
+    found[3] = s.s0; found[4] = s.len; found[5] = s.used; found[6] = s.nk; found[7] = s.past; found[8] = s.rows;
+    found[9] = s.tiles;
   }
   __syncthreads();
-  u.b = __builtin_amdgcn_readfirstlane(found[0]);
-  const int rem = __builtin_amdgcn_readfirstlane(found[1]);
-  const int base = __builtin_amdgcn_readfirstlane(found[2]);
-  u.s = gqa_seq<RT>(p, u.b);
+  auto get = [&](int i) { return __builtin_amdgcn_readfirstlane(found[i]); };
+  u.b = get(0);
+  const int rem = get(1), base = get(2);
+  u.s.s0 = get(3); u.s.len = get(4); u.s.used = get(5); u.s.nk = get(6); u.s.past = get(7); u.s.rows = get(8);
+  u.s.tiles = get(9);
   const int most = (gqa_blocks(u.s.nk) - 1) / chunk + 1;       // parts that the request's tiles have room for
-  u.part = TILES ? 0 : rem % most;
+  u.part = rem % most;
   // the tiles of a causal prompt from the last, which has the most keys, to the first
-  u.t = u.s.tiles - 1 - (TILES ? rem : rem / most);
+  u.t = u.s.tiles - 1 - rem / most;
   const int end = gqa_tile_end<RT>(p, u.s, u.t);
   u.parts = (gqa_blocks(end) - 1) / chunk + 1;
-  u.slot = u.hk * (int)all + base + (u.s.tiles - 1 - u.t) * most;
+  u.slot = u.hk * n + base + (u.s.tiles - 1 - u.t) * most;
   const long long lo = (long long)u.part * chunk * kGqaBlock, hi = lo + (long long)chunk * kGqaBlock;
   u.lo = lo < end ? (int)lo : end;
   u.hi = hi < end ? (int)hi : end;
-  return true;
+  if (p.target > 0 && tid == 0)
+    records[u.slot + u.part] = GqaRecord{u.part == 0 ? u.parts : 0, u.s.s0, u.s.used, u.s.rows, u.t, u.hk, {0, 0}};
+  return u.part < u.parts;
 }
 
 // A read that the scalar unit makes where the address is the same for the whole wave.
@@ -164,38 +179,48 @@ __device__ __forceinline__ int scalar_load(const int* p, size_t i) {
   return reinterpret_cast<const __attribute__((address_space(4))) int*>(reinterpret_cast<uintptr_t>(p))[i];
 }
 
-// Which of keys [k0, k0 + 64) row `row` of the call (position pos, own rows from
-// `past`) sees, of the keys before hi; bit i for key k0 + i.
-__device__ __forceinline__ unsigned long long gqa_seen(const GqaParams& p, int k0, int hi, int pos, int past,
-                                                       size_t row) {
-  unsigned long long m = ~0ull;
-  if (hi - k0 < 64) m = hi > k0 ? (1ull << (hi - k0)) - 1 : 0;
-  if (p.mask == kMaskCausal) {
-    const int d = pos - k0;
-    if (d < 63) m &= d < 0 ? 0 : (2ull << d) - 1;
-  } else if (p.mask == kMaskTree) {
-    const int j = k0 - past;                       // the row of the call that key k0 is
-    if (j > -64) {
-      auto word = [&](int w) { return w < p.words ? p.bits[row * p.words + w] : 0ull; };
-      if (j < 0) {
-        m &= word(0) << -j | ((1ull << -j) - 1);
-      } else {
-        const int w = j >> 6, sh = j & 63;
-        unsigned long long x = word(w) >> sh;
-        if (sh) x |= word(w + 1) << (64 - sh);
-        m &= x;
+// What a row sees: the keys before `lim`, and of those from `past` on (the rows of
+// the call), with SEER_MASK_TREE, the ones whose bits are set.
+template <bool PAGED>
+struct GqaSight {
+  int lim, past;
+  const unsigned long long* bits;      // null but for SEER_MASK_TREE
+  int words;
+
+  __device__ __forceinline__ GqaSight(const GqaParams& p, const GqaUnit& u, int tok) {
+    past = u.s.past;
+    lim = u.hi;
+    if (p.mask == kMaskCausal && past + tok + 1 < lim) lim = past + tok + 1;
+    words = p.words;
+    bits = PAGED && p.mask == kMaskTree ? p.bits + (size_t)(u.s.s0 + tok) * p.words : nullptr;
+  }
+  // bit i: key k0 + i, i < 64
+  __device__ __forceinline__ unsigned long long seen(int k0) const {
+    const int n = lim - k0;
+    unsigned long long m = n >= 64 ? ~0ull : (n > 0 ? (1ull << n) - 1 : 0);
+    if (PAGED && bits) {
+      const int j = k0 - past;                       // the row of the call that key k0 is
+      if (j > -64) {
+        auto word = [&](int w) { return w < words ? bits[w] : 0ull; };
+        if (j < 0) {
+          m &= word(0) << -j | ((1ull << -j) - 1);
+        } else {
+          const int w = j >> 6, sh = j & 63;
+          unsigned long long x = word(w) >> sh;
+          if (sh) x |= word(w + 1) << (64 - sh);
+          m &= x;
+        }
       }
     }
+    return m;
   }
-  return m;
-}
+};
 
-// The first key from which on gqa_seen may hide some from a row at position pos
-// or later.
-__device__ __forceinline__ int gqa_open_end(const GqaParams& p, int hi, int pos, int past) {
-  if (p.mask == kMaskCausal) return pos + 1 < hi ? pos + 1 : hi;
-  if (p.mask == kMaskTree) return past < hi ? past : hi;
-  return hi;
+// The first key from which on some row of the unit at token `tok` or later may be
+// blind to one.
+__device__ __forceinline__ int gqa_open_end(const GqaParams& p, const GqaUnit& u, int tok) {
+  const int end = p.mask == kMaskCausal ? u.s.past + tok + 1 : (p.mask == kMaskTree ? u.s.past : u.hi);
+  return end < u.hi ? end : u.hi;
 }
 
 }  // namespace seer

@@ -348,10 +348,11 @@ struct GqaParams {
   int shift, n_pages, width;
   const unsigned long long* bits;   // [rows][words]
   int words;
-  // the launch (gqa_rule): units to cut the keys for (0: not cut), blocks that a
-  // part has at least, and the parts' results
-  int target, min_chunk;
-  int max_units;               // that the grid and the results have room for
+  // the launch (gqa_rule): units to cut the keys for (0: not cut), units that the
+  // grid and the results have room for, and the records and results of the parts
+  int target;
+  int max_units;
+  void* records;
   float* partial;
 };
 int launch_gqa_bf16(const GqaParams& p, const GqaRule& r, hipStream_t s);

@@ -809,15 +809,15 @@ static int gqa_params(seer::GqaParams& p, const seer_attn_desc* desc, int32_t ma
   p.scale = desc->scale != 0.0f ? desc->scale : 1.0f / sqrtf((float)desc->head_dim);
   p.mask = mask; p.bf16 = desc->dtype == SEER_DTYPE_BF16; p.v_f16 = (desc->flags & SEER_ATTN_V_F16) != 0;
   p.group = p.n_heads / p.n_kv;
-  p.partial = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + 256);
+  p.records = workspace;
   return SEER_OK;
 }
 
 static int launch_gqa(seer::GqaParams& p, hipStream_t stream) {
   const seer::GqaRule r = seer::gqa_rule(p.bf16, p.n_heads, p.n_kv, p.head_dim, p.rows_ub, p.B);
   p.target = r.target;
-  p.min_chunk = 1;
   p.max_units = r.grid;
+  p.partial = reinterpret_cast<float*>(static_cast<uint8_t*>(p.records) + r.records);
   return p.bf16 ? seer::launch_gqa_bf16(p, r, stream) : seer::launch_gqa_f32(p, r, stream);
 }
 
