@@ -350,9 +350,12 @@ __global__ __launch_bounds__(NT, 2) void gqa_tile_kernel(GqaParams p) {
   __shared__ __attribute__((aligned(1024))) uint8_t v_lds0[64 * ROW];
   __shared__ __attribute__((aligned(1024))) uint8_t v_lds1[64 * ROW];
   __shared__ int odd_from;                   // the first tile that had values to sweep
-  if (threadIdx.x == 0) odd_from = INT_MAX;
+  __shared__ typename GqaCut<kGqaTile, NT>::Shared cut_lds;
+  GqaCut<kGqaTile, NT> cut(p, cut_lds);
   GqaUnit u;
-  if (!gqa_find<kGqaTile, NT>(p, u)) return;
+  while (cut.next(p, u)) {
+  if (threadIdx.x == 0) odd_from = INT_MAX;
+  __syncthreads();
   const int lane = threadIdx.x & 63;
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int fr = lane & 31, fhalf = lane >> 5;
@@ -461,23 +464,23 @@ __global__ __launch_bounds__(NT, 2) void gqa_tile_kernel(GqaParams p) {
     }
   }
   const float l = w.l + __shfl_xor(w.l, 32, kWave);
-  if (u.parts > 1) {
-    if (row >= u.s.rows) return;
-    const Parts<kGqaTile, DH> to(p, u.slot + u.part);
+  if (row >= u.s.rows) continue;
+  if (!u.whole) {
+    const Parts<kGqaTile, DH> to(p, u.slot);
 #pragma unroll
     for (int i = 0; i < DT * 4; ++i) *to.sum(wv, i >> 2, i & 3, lane) = sum[i];
     if (fhalf == 0) {
       *to.max(wv * 32 + fr) = w.m;
       *to.div(wv * 32 + fr) = l;
     }
-    return;
+    continue;
   }
-  if (row >= u.s.rows) return;
   const bool real = tok < u.s.used;
   const float inv = inverse(l);
   uint16_t* at = out_row(p, u.s.s0 + tok, u.hk * p.group + head, DH) + fhalf * 4;
 #pragma unroll
   for (int i = 0; i < DT * 4; ++i) store4(at + (i >> 2) * 32 + (i & 3) * 8, real ? sum[i] * inv : f32x4_t{0, 0, 0, 0});
+  }
 }
 
 template <int DH, bool VF16, bool PAGED>
@@ -489,8 +492,10 @@ __global__ __launch_bounds__(NF, 1) void gqa_few_kernel(GqaParams p) {
   __shared__ __attribute__((aligned(1024))) uint8_t v_lds1[2 * FT];
   __shared__ float m_part[2][32], l_part[2][32];
   __shared__ int odd_from[2];
+  __shared__ typename GqaCut<kGqaFew, NF>::Shared cut_lds;
+  GqaCut<kGqaFew, NF> cut(p, cut_lds);
   GqaUnit u;
-  if (!gqa_find<kGqaFew, NF>(p, u)) return;
+  while (cut.next(p, u)) {
   const int lane = threadIdx.x & 63;
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int fr = lane & 31, fhalf = lane >> 5;
@@ -526,7 +531,7 @@ __global__ __launch_bounds__(NF, 1) void gqa_few_kernel(GqaParams p) {
                     (B ? k_lds1 : k_lds0) + wv * FT + 16 * i * ROW, (B ? v_lds1 : v_lds0) + wv * FT + 16 * i * ROW, lane);
     }
   };
-  uint32_t lost = 0, lost_next = 0;
+  uint32_t lost[2] = {0, 0};
   auto lost_of = [&]() {
     uint32_t m = 0;
     if constexpr (PAGED) {
@@ -536,38 +541,46 @@ __global__ __launch_bounds__(NF, 1) void gqa_few_kernel(GqaParams p) {
     return m;
   };
   int odd = INT_MAX;
+  constexpr int LOADS = 2 * 32 * ROW / 1024;            // of a tile
   if (n > 0) {
     pages(k0);
     load(k0, std::integral_constant<int, 0>{});
-    lost = lost_of();
-    pages(k0 + 64 < u.hi ? k0 + 64 : u.hi - 1);
+    lost[0] = lost_of();
+    if (n > 1) {
+      pages(k0 + 64);
+      load(k0 + 64, std::integral_constant<int, 1>{});
+      lost[1] = lost_of();
+    }
+    pages(k0 + 128 < u.hi ? k0 + 128 : u.hi - 1);
   }
-  __builtin_amdgcn_sched_barrier(0);
-  __builtin_amdgcn_s_waitcnt(0x0f70);       // vmcnt(0)
-  __builtin_amdgcn_wave_barrier();
-  __builtin_amdgcn_sched_barrier(0);
+  // Both buffers are under way; a tile's buffer is filled again as soon as the tile
+  // is done, so that one to two tiles are in flight all the time.
   auto step = [&](int kt, auto buf) {
     constexpr int B = decltype(buf)::value;
     const int kbase = k0 + 64 * kt;
     uint8_t* vl = (B ? v_lds1 : v_lds0) + wv * FT;
-    if (kt + 1 < n) {
-      load(kbase + 64, std::integral_constant<int, B ^ 1>{});
-      lost_next = lost_of();
-      if (kt + 2 < n) pages(kbase + 128);
-    }
-    const bool masked = kbase + 32 > open || lost != 0;
+    __builtin_amdgcn_sched_barrier(0);
+    if (kt + 1 < n) __builtin_amdgcn_s_waitcnt(0x0f70 | (LOADS & 15) | (LOADS >> 4) << 14);    // vmcnt(LOADS)
+    else __builtin_amdgcn_s_waitcnt(0x0f70);                                                    // vmcnt(0)
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    const bool masked = kbase + 32 > open || lost[B] != 0;
     unsigned long long seen = 0;
     if (masked) {
-      seen = ~lost & sight.seen(kbase);
+      seen = ~lost[B] & sight.seen(kbase);
       if (sweep<VF16, FT>(vl, lane)) odd = kbase < odd ? kbase : odd;
     }
     w.step((B ? k_lds1 : k_lds0) + wv * FT, vl, lane, masked, seen);
-    lost = lost_next;
-    // the next tile has landed; this one's fragments are in registers or consumed
-    __builtin_amdgcn_sched_barrier(0);
-    __builtin_amdgcn_s_waitcnt(0x0070);     // vmcnt(0) and lgkmcnt(0)
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_sched_barrier(0);
+    if (kt + 2 < n) {
+      // this tile's fragments have been read
+      __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_waitcnt(0xc07f);     // lgkmcnt(0)
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_sched_barrier(0);
+      load(kbase + 128, buf);
+      lost[B] = lost_of();
+      if (kt + 3 < n) pages(kbase + 192);
+    }
   };
   for (int kt = 0; kt < n; kt += 2) {
     step(kt, std::integral_constant<int, 0>{});
@@ -602,10 +615,10 @@ __global__ __launch_bounds__(NF, 1) void gqa_few_kernel(GqaParams p) {
   }
   const float l = l_part[0][fr] * a[0] + l_part[1][fr] * a[1];
   odd = __builtin_amdgcn_readfirstlane(odd_from[0] < odd_from[1] ? odd_from[0] : odd_from[1]);
-  const Parts<kGqaFew, DH> to(p, u.slot + u.part);
+  const Parts<kGqaFew, DH> to(p, u.slot);
   const bool real = tok < u.s.used;
   const float inv = inverse(l);
-  if (u.parts > 1 && wv == 0 && fhalf == 0 && row < u.s.rows) {
+  if (!u.whole && wv == 0 && fhalf == 0 && row < u.s.rows) {
     *to.max(fr) = m;
     *to.div(fr) = l;
   }
@@ -615,9 +628,10 @@ __global__ __launch_bounds__(NF, 1) void gqa_few_kernel(GqaParams p) {
     f32x4_t v = a[0] * *sums(0, dt, g) + a[1] * *sums(1, dt, g);
     if (odd < u.hi) v = add_odd<DH, VF16, PAGED>(v, keys, u, sight, odd & ~15, 32 * dt + 8 * g + 4 * fhalf);
     if (row >= u.s.rows) continue;
-    if (u.parts > 1) *to.sum(0, dt, g, lane) = v;
+    if (!u.whole) *to.sum(0, dt, g, lane) = v;
     else store4(out_row(p, u.s.s0 + tok, u.hk * p.group + head, DH) + dt * 32 + g * 8 + fhalf * 4,
                 real ? v * inv : f32x4_t{0, 0, 0, 0});
+  }
   }
 }
 
@@ -626,8 +640,8 @@ __global__ __launch_bounds__(NF, 1) void gqa_few_kernel(GqaParams p) {
 template <int RT, int DH>
 __global__ __launch_bounds__(NT) void gqa_join_kernel(GqaParams p) {
   constexpr int DT = DH / 32, PIECES = RT / 32 * DT;       // workgroups of a slot
-  const int slot = blockIdx.x / PIECES, piece = blockIdx.x % PIECES;
-  const GqaRecord r = static_cast<const GqaRecord*>(p.records)[slot];
+  const int wg = blockIdx.x / PIECES, piece = blockIdx.x % PIECES;
+  const GqaRecord r = static_cast<const GqaRecord*>(p.records)[wg];
   if (r.parts < 2) return;
   const int lane = threadIdx.x & 63, g = threadIdx.x >> 6, fr = lane & 31, fhalf = lane >> 5;
   const int w = piece / DT, dt = piece % DT;
@@ -636,13 +650,13 @@ __global__ __launch_bounds__(NT) void gqa_join_kernel(GqaParams p) {
   const float c = p.scale * 1.4426950408889634f;
   float m = -INFINITY;
 #pragma unroll 8
-  for (int i = 0; i < r.parts; ++i) m = fmaxf(m, *Parts<RT, DH>(p, slot + i).max(w * 32 + fr));
+  for (int i = 0; i < r.parts; ++i) m = fmaxf(m, *Parts<RT, DH>(p, gqa_slot(r, wg, i)).max(w * 32 + fr));
   const float ref = m == -INFINITY ? 0.0f : m;
   float l = 0.0f;
   f32x4_t sum = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 8
   for (int i = 0; i < r.parts; ++i) {
-    const Parts<RT, DH> from(p, slot + i);
+    const Parts<RT, DH> from(p, gqa_slot(r, wg, i));
     const float mi = *from.max(w * 32 + fr), li = *from.div(w * 32 + fr);
     const f32x4_t v = *from.sum(w, dt, g, lane);
     const bool none = mi == -INFINITY && li == 0.0f;
@@ -662,10 +676,10 @@ int launch_gqa_bf16(const GqaParams& p, const GqaRule& r, hipStream_t s) {
     constexpr bool V = decltype(vf16)::value, P = decltype(paged)::value;
     if (r.rt == kGqaTile) {
       hipLaunchKernelGGL((gqa_tile_kernel<DH, V, P>), dim3(r.grid), dim3(NT), 0, s, p);
-      if (r.target) hipLaunchKernelGGL((gqa_join_kernel<kGqaTile, DH>), dim3(r.grid * (4 * DH / 32)), dim3(NT), 0, s, p);
+      if (r.cut) hipLaunchKernelGGL((gqa_join_kernel<kGqaTile, DH>), dim3(r.grid * (4 * DH / 32)), dim3(NT), 0, s, p);
     } else {
       hipLaunchKernelGGL((gqa_few_kernel<DH, V, P>), dim3(r.grid), dim3(NF), 0, s, p);
-      if (r.target) hipLaunchKernelGGL((gqa_join_kernel<kGqaFew, DH>), dim3(r.grid * (DH / 32)), dim3(NT), 0, s, p);
+      if (r.cut) hipLaunchKernelGGL((gqa_join_kernel<kGqaFew, DH>), dim3(r.grid * (DH / 32)), dim3(NT), 0, s, p);
     }
   };
   auto with = [&](auto dh, auto vf16) {

@@ -36,8 +36,10 @@ __global__ __launch_bounds__(NT) void gqa_f32_kernel(GqaParams p) {
   __shared__ f32x4_t o_part[4][4 * H][64];
   __shared__ float m_part[4][16], l_part[4][16];
   __shared__ int odd_part[4];
+  __shared__ typename GqaCut<kGqaF32, NT>::Shared cut_lds;
+  GqaCut<kGqaF32, NT> cut(p, cut_lds);
   GqaUnit u;
-  if (!gqa_find<kGqaF32, NT>(p, u)) return;
+  while (cut.next(p, u)) {
   const int lane = threadIdx.x & 63;
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int fr = lane & 15, g = lane >> 4;
@@ -219,18 +221,17 @@ __global__ __launch_bounds__(NT) void gqa_f32_kernel(GqaParams p) {
           }
     }
   }
-  if (u.parts > 1) {
-    if (row >= u.s.rows) return;
-    const Parts<H> to(p, u.slot + u.part);
+  if (row >= u.s.rows) continue;
+  if (!u.whole) {
+    const Parts<H> to(p, u.slot);
 #pragma unroll
     for (int h = 0; h < H; ++h) *to.sum(4 * h + wv, lane) = sum[h];
     if (wv == 0 && g == 0) {
       *to.max(fr) = m;
       *to.div(fr) = l;
     }
-    return;
+    continue;
   }
-  if (row >= u.s.rows) return;
   const bool real = tok < u.s.used;
   const float inv = inverse(l);
   float* out = static_cast<float*>(p.out) + (size_t)(u.s.s0 + tok) * p.o_stride + (size_t)(u.hk * p.group + head) * D;
@@ -241,13 +242,14 @@ __global__ __launch_bounds__(NT) void gqa_f32_kernel(GqaParams p) {
       const int d = 64 * h + 16 * g + 4 * i + wv;
       if (d < D) out[d] = real ? sum[h][i] * inv : 0.0f;
     }
+  }
 }
 
 // Adds the parts of each tile whose keys were cut; wave w as in the kernel above.
 template <int H>
 __global__ __launch_bounds__(NT) void gqa_f32_join_kernel(GqaParams p) {
-  const int slot = blockIdx.x;
-  const GqaRecord r = static_cast<const GqaRecord*>(p.records)[slot];
+  const int wg = blockIdx.x;
+  const GqaRecord r = static_cast<const GqaRecord*>(p.records)[wg];
   if (r.parts < 2) return;
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, fr = lane & 15, g = lane >> 4, D = p.head_dim;
   const int row = r.t * kGqaF32 + fr;
@@ -255,7 +257,7 @@ __global__ __launch_bounds__(NT) void gqa_f32_join_kernel(GqaParams p) {
   const float c = p.scale * 1.4426950408889634f;
   float m = -INFINITY;
 #pragma unroll 8
-  for (int i = 0; i < r.parts; ++i) m = fmaxf(m, *Parts<H>(p, slot + i).max(fr));
+  for (int i = 0; i < r.parts; ++i) m = fmaxf(m, *Parts<H>(p, gqa_slot(r, wg, i)).max(fr));
   const float ref = m == -INFINITY ? 0.0f : m;
   float l = 0.0f;
   f32x4_t sum[H];
@@ -263,7 +265,7 @@ __global__ __launch_bounds__(NT) void gqa_f32_join_kernel(GqaParams p) {
   for (int h = 0; h < H; ++h) sum[h] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 8
   for (int i = 0; i < r.parts; ++i) {
-    const Parts<H> from(p, slot + i);
+    const Parts<H> from(p, gqa_slot(r, wg, i));
     const float mi = *from.max(fr), li = *from.div(fr);
     const float a = mi == -INFINITY && li == 0.0f ? 0.0f : __builtin_amdgcn_exp2f((mi - ref) * c);
     l += li * a;
@@ -288,11 +290,11 @@ int launch_gqa_f32(const GqaParams& p, const GqaRule& r, hipStream_t s) {
   if (p.head_dim > 64) {
     if (p.table) hipLaunchKernelGGL((gqa_f32_kernel<2, true>), grid, block, 0, s, p);
     else hipLaunchKernelGGL((gqa_f32_kernel<2, false>), grid, block, 0, s, p);
-    if (r.target) hipLaunchKernelGGL(gqa_f32_join_kernel<2>, dim3(r.grid), block, 0, s, p);
+    if (r.cut) hipLaunchKernelGGL(gqa_f32_join_kernel<2>, dim3(r.grid), block, 0, s, p);
   } else {
     if (p.table) hipLaunchKernelGGL((gqa_f32_kernel<1, true>), grid, block, 0, s, p);
     else hipLaunchKernelGGL((gqa_f32_kernel<1, false>), grid, block, 0, s, p);
-    if (r.target) hipLaunchKernelGGL(gqa_f32_join_kernel<1>, dim3(r.grid), block, 0, s, p);
+    if (r.cut) hipLaunchKernelGGL(gqa_f32_join_kernel<1>, dim3(r.grid), block, 0, s, p);
   }
   return hipGetLastError() == hipSuccess ? 0 : -1;
 }

@@ -187,8 +187,8 @@ constexpr int kGqaTile = 128, kGqaFew = 32, kGqaF32 = 16;
 
 struct GqaRule {
   int rt;                // rows of a tile
-  int target;            // units to cut the tiles' keys for, 0: not cut
-  int grid;              // the most units that can come out
+  bool cut;              // whether the tiles' keys are cut, over `grid` workgroups
+  int grid;
   size_t records;        // bytes of the parts' records
   size_t bytes;          // of the records and the results
 };
@@ -200,12 +200,13 @@ inline GqaRule gqa_rule(bool bf16, int heads, int n_kv, int dim, int rows, int b
   const long long pairs = (long long)rows * group;
   r.rt = !bf16 ? kGqaF32 : (pairs / batch > 64 ? kGqaTile : kGqaFew);
   const long long tiles = (pairs >= batch ? (pairs - batch) / r.rt + batch : pairs) * n_kv;
-  const int units = r.rt == kGqaFew ? 1024 : 512;
-  r.target = tiles < units ? units : 0;
-  r.grid = (int)(tiles + (r.target ? r.target + n_kv : 0));
-  // a part: the sums of each row, its maximum and its divisor
-  r.records = r.target ? ((size_t)r.grid * 32 + 255) / 256 * 256 : 0;
-  r.bytes = r.target ? r.records + (size_t)r.grid * r.rt * ((dim > 64 ? 128 : 64) + 2) * 4 : 0;
+  // workgroups that run at once on 256 CUs
+  const int wgs = r.rt == kGqaFew && dim <= 64 ? 1024 : 512;
+  r.cut = r.rt != kGqaTile || tiles < wgs;
+  r.grid = r.cut ? wgs : (int)tiles;
+  // two parts a workgroup: the sums of each row, its maximum and its divisor
+  r.records = r.cut ? (size_t)wgs * 32 : 0;
+  r.bytes = r.cut ? r.records + (size_t)2 * wgs * r.rt * ((dim > 64 ? 128 : 64) + 2) * 4 : 0;
   return r;
 }
 

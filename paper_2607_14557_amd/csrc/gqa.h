@@ -1,5 +1,5 @@
-// What the kernels of the attention with grouped heads share: how a launch is
-// cut into units, where keys lie, which of them a row sees.
+// What the kernels of the attention with grouped heads share: how the work of a
+// launch is cut, and which keys a row sees.
 #pragma once
 
 #include <limits.h>
@@ -49,20 +49,6 @@ __device__ __forceinline__ GqaSeq gqa_seq(const GqaParams& p, int b) {
 
 __device__ __forceinline__ int gqa_blocks(int nk) { return nk > kGqaBlock ? (nk - 1) / kGqaBlock + 1 : 1; }
 
-// One workgroup's share: tile t of request b for key/value head hk, keys
-// [lo, hi); part `part` of the `parts` that the tile's keys are cut into, whose
-// results lie from slot on (slot + part is this one's).
-struct GqaUnit {
-  int b, t, hk, lo, hi, part, parts, slot;
-  GqaSeq s;
-};
-
-// What the joining of a tile's parts has to know, left by the unit of its first
-// part (parts < 2: nothing to join), one per slot.
-struct GqaRecord {
-  int parts, s0, used, rows, t, hk, pad[2];
-};
-
 // The keys that any row of tile t sees end here.
 template <int RT>
 __device__ __forceinline__ int gqa_tile_end(const GqaParams& p, const GqaSeq& s, int t) {
@@ -74,105 +60,172 @@ __device__ __forceinline__ int gqa_tile_end(const GqaParams& p, const GqaSeq& s,
   return end < 0 ? 0 : (end < s.nk ? end : s.nk);
 }
 
-// Finds the workgroup's unit; false where there is none.  Called by all NT
-// threads: each sums its share of the requests, then one scan over the workgroup
-// locates the unit.  p.target > 0: the tiles' keys are cut so that about p.target
-// units come out over all heads, every part the same number of blocks, whatever
-// the requests' lengths; the workgroup leaves its slot's record.
+// A piece of work: keys [lo, hi) for tile t of request b and key/value head hk;
+// all that the tile's rows see (whole), or a part whose result goes to `slot`.
+struct GqaUnit {
+  int b, t, hk, lo, hi, slot;
+  bool whole;
+  GqaSeq s;
+};
+
+// What the joining of a tile's parts has to know: the first part lies in slot
+// `first`, the others in the even slots of the workgroups after it.  One for each
+// workgroup, by the one that has the tile's first key (parts < 2: nothing to join).
+struct GqaRecord {
+  int parts, first, s0, used, rows, t, hk, pad;
+};
+
+// How the work of a launch is cut.
+//   p.cut:     every tile's keys count as blocks of 128, the blocks of all heads,
+//              requests and tiles stand in one line, and each of the p.wgs workgroups
+//              takes an equal stretch of it, whatever the requests' lengths: no
+//              workgroup waits for another, and none starts after the others.  A tile
+//              that lies in several stretches is joined by a second launch.
+//   otherwise: a workgroup for each tile.
+// Every workgroup sums the requests' lengths for itself (each thread its share of
+// the requests, then a scan); with at most one request a thread they are read once.
 template <int RT, int NT>
-__device__ __forceinline__ bool gqa_find(const GqaParams& p, GqaUnit& u) {
-  constexpr int NW = NT / kWave;
-  __shared__ long long wave_sum[2][NW];
-  __shared__ int found[10];
-  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6;
-  const int per = (p.B + NT - 1) / NT;
-  const int b0 = tid * per < p.B ? tid * per : p.B;
-  const int b1 = b0 + per < p.B ? b0 + per : p.B;
-  // with at most one request a thread its lengths are read once
-  GqaSeq mine{};
-  if (per == 1 && b0 < b1) mine = gqa_seq<RT>(p, b0);
-  auto seq = [&](int b) { return per == 1 ? mine : gqa_seq<RT>(p, b); };
-  int chunk = INT_MAX;
-  if (p.target > 0) {
-    long long n = 0;
+struct GqaCut {
+  static constexpr int NW = NT / kWave;
+  struct Shared {
+    long long sums[NW];
+    long long first[NT + 1];     // of each thread's stretch of a head's line
+    GqaSeq seq[NT];              // of each thread's only request
+    int found[12];
+  };
+  Shared& sh;
+  long long n;                   // length of a head's line
+  long long x, x0, x1;           // the next place, and the workgroup's stretch
+  int wg;
+
+  __device__ __forceinline__ static long long uniform(long long v) {
+    return (long long)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32 |
+           (uint32_t)__builtin_amdgcn_readfirstlane((int)v);
+  }
+  __device__ __forceinline__ static long long weight(const GqaParams& p, const GqaSeq& s) {
+    return (long long)s.tiles * (p.cut ? gqa_blocks(s.nk) : 1);
+  }
+
+  __device__ __forceinline__ GqaCut(const GqaParams& p, Shared& shared) : sh(shared) {
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6;
+    const int per = (p.B + NT - 1) / NT;
+    const int b0 = tid * per < p.B ? tid * per : p.B;
+    const int b1 = b0 + per < p.B ? b0 + per : p.B;
+    long long own = 0;
     for (int b = b0; b < b1; ++b) {
-      const GqaSeq s = seq(b);
-      n += (long long)s.tiles * gqa_blocks(s.nk);
+      const GqaSeq s = gqa_seq<RT>(p, b);
+      own += weight(p, s);
+      if (per == 1) sh.seq[tid] = s;
     }
+    long long inc = own;
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1) n += __shfl_xor(n, off, kWave);
-    if (lane == 0) wave_sum[0][wave] = n;
+    for (int off = 1; off < kWave; off <<= 1) {
+      const long long v = __shfl_up(inc, off, kWave);
+      if (lane >= off) inc += v;
+    }
+    if (lane == kWave - 1) sh.sums[wave] = inc;
     __syncthreads();
+    long long first = inc - own;
     n = 0;
 #pragma unroll
-    for (int w = 0; w < NW; ++w) n += wave_sum[0][w];
-    const long long c = (n * p.n_kv + p.target - 1) / p.target;
-    chunk = c < 1 ? 1 : (c < INT_MAX ? (int)c : INT_MAX);
-  }
-  int units = 0;
-  for (int b = b0; b < b1; ++b) {
-    const GqaSeq s = seq(b);
-    units += s.tiles * ((gqa_blocks(s.nk) - 1) / chunk + 1);
-  }
-  int inc = units;
-#pragma unroll
-  for (int off = 1; off < kWave; off <<= 1) {
-    const int v = __shfl_up(inc, off, kWave);
-    if (lane >= off) inc += v;
-  }
-  if (lane == kWave - 1) wave_sum[1][wave] = inc;
-  __syncthreads();
-  int n = 0, first = inc - units;
-#pragma unroll
-  for (int w = 0; w < NW; ++w) {
-    if (w < wave) first += (int)wave_sum[1][w];
-    n += (int)wave_sum[1][w];
-  }
-  GqaRecord* records = reinterpret_cast<GqaRecord*>(p.records);
-  const int bid = blockIdx.x;
-  if (bid >= (long long)n * p.n_kv || (long long)n * p.n_kv > p.max_units) {
-    if (p.target > 0 && tid == 0) records[bid].parts = 0;
-    return false;
-  }
-  // each XCD takes a contiguous range of units, heads slowest: the tiles of one
-  // request and head find their keys in its L2
-  const int w = xcd_remap(bid, n * p.n_kv);
-  u.hk = w / n;
-  const int j = w - u.hk * n;
-  if (j >= first && j < first + units) {
-    int b = b0;
-    GqaSeq s;
-    int m;
-    for (;; ++b) {
-      s = seq(b);
-      m = s.tiles * ((gqa_blocks(s.nk) - 1) / chunk + 1);
-      if (j < first + m) break;
-      first += m;
+    for (int w = 0; w < NW; ++w) {
+      if (w < wave) first += sh.sums[w];
+      n += sh.sums[w];
     }
-    found[0] = b; found[1] = j - first; found[2] = first;
-    found[3] = s.s0; found[4] = s.len; found[5] = s.used; found[6] = s.nk; found[7] = s.past; found[8] = s.rows;
-    found[9] = s.tiles;
+    n = uniform(n);
+    sh.first[tid] = first;
+    if (tid == NT - 1) sh.first[NT] = n;
+    const long long all = n * p.n_kv;
+    const int bid = blockIdx.x;
+    wg = 0;
+    if (p.cut) {
+      const int wgs = all < p.wgs ? (int)all : p.wgs;
+      x0 = x1 = 0;
+      if (bid >= wgs) {
+        if (tid == 0) static_cast<GqaRecord*>(p.records)[bid].parts = 0;
+      } else {
+        // each XCD takes a contiguous part of the line: the tiles of one request and
+        // head find their keys in its L2
+        wg = xcd_remap(bid, wgs);
+        x0 = wg * all / wgs;
+        x1 = (wg + 1) * all / wgs;
+      }
+    } else {
+      x0 = bid < all ? xcd_remap(bid, (int)all) : 0;
+      x1 = bid < all ? x0 + 1 : x0;
+    }
+    x = x0;
   }
-  __syncthreads();
-  auto get = [&](int i) { return __builtin_amdgcn_readfirstlane(found[i]); };
-  u.b = get(0);
-  const int rem = get(1), base = get(2);
-  u.s.s0 = get(3); u.s.len = get(4); u.s.used = get(5); u.s.nk = get(6); u.s.past = get(7); u.s.rows = get(8);
-  u.s.tiles = get(9);
-  const int most = (gqa_blocks(u.s.nk) - 1) / chunk + 1;       // parts that the request's tiles have room for
-  u.part = rem % most;
-  // the tiles of a causal prompt from the last, which has the most keys, to the first
-  u.t = u.s.tiles - 1 - rem / most;
-  const int end = gqa_tile_end<RT>(p, u.s, u.t);
-  u.parts = (gqa_blocks(end) - 1) / chunk + 1;
-  u.slot = u.hk * n + base + (u.s.tiles - 1 - u.t) * most;
-  const long long lo = (long long)u.part * chunk * kGqaBlock, hi = lo + (long long)chunk * kGqaBlock;
-  u.lo = lo < end ? (int)lo : end;
-  u.hi = hi < end ? (int)hi : end;
-  if (p.target > 0 && tid == 0)
-    records[u.slot + u.part] = GqaRecord{u.part == 0 ? u.parts : 0, u.s.s0, u.s.used, u.s.rows, u.t, u.hk, {0, 0}};
-  return u.part < u.parts;
-}
+
+  // The next piece of the workgroup's stretch; false at its end.
+  __device__ __forceinline__ bool next(const GqaParams& p, GqaUnit& u) {
+    if (x >= x1) return false;
+    const int tid = threadIdx.x;
+    u.hk = (int)(x / n);
+    const long long j = x - u.hk * n;
+    __syncthreads();               // the line is written, and the last piece's reads of LDS are done
+    if (j >= sh.first[tid] && j < sh.first[tid + 1]) {
+      const int per = (p.B + NT - 1) / NT;
+      int b = tid * per;
+      long long at = sh.first[tid];
+      GqaSeq s;
+      if (per == 1) {
+        s = sh.seq[tid];
+      } else {
+        for (;; ++b) {
+          s = gqa_seq<RT>(p, b);
+          const long long m = weight(p, s);
+          if (j < at + m) break;
+          at += m;
+        }
+      }
+      const int nb = p.cut ? gqa_blocks(s.nk) : 1;
+      const int rem = (int)(j - at);
+      sh.found[0] = b; sh.found[1] = rem / nb; sh.found[2] = rem % nb; sh.found[3] = nb;
+      sh.found[4] = s.s0; sh.found[5] = s.len; sh.found[6] = s.used; sh.found[7] = s.nk; sh.found[8] = s.past;
+      sh.found[9] = s.rows; sh.found[10] = s.tiles;
+    }
+    __syncthreads();
+    auto get = [&](int i) { return __builtin_amdgcn_readfirstlane(sh.found[i]); };
+    u.b = get(0);
+    u.s.s0 = get(4); u.s.len = get(5); u.s.used = get(6); u.s.nk = get(7); u.s.past = get(8); u.s.rows = get(9);
+    u.s.tiles = get(10);
+    // the tiles of a causal prompt from the last, which has the most keys, to the first
+    u.t = u.s.tiles - 1 - get(1);
+    const int block = get(2), nb = get(3);
+    const int end = gqa_tile_end<RT>(p, u.s, u.t);
+    u.whole = true;
+    u.lo = 0;
+    u.hi = end;
+    u.slot = 0;
+    int take = 1;
+    if (p.cut) {
+      take = nb - block < x1 - x ? nb - block : (int)(x1 - x);
+      u.whole = take == nb;
+      const long long lo = (long long)block * kGqaBlock, hi = lo + (long long)take * kGqaBlock;
+      u.lo = lo < end ? (int)lo : end;
+      u.hi = hi < end ? (int)hi : end;
+      u.slot = 2 * wg + (x == x0 ? 0 : 1);
+      if (tid == 0 && x + take >= x1) {
+        // the last piece: where it opens a tile that goes on, the tile's record
+        GqaRecord r{};
+        if (block == 0 && take < nb) {
+          // the workgroup that has the tile's last block: x0(i) = floor(i all / wgs)
+          const long long all = n * p.n_kv;
+          const int wgs = all < p.wgs ? (int)all : p.wgs;
+          const int last = (int)(((x + nb) * wgs - 1) / all);
+          r = GqaRecord{last - wg + 1, u.slot, u.s.s0, u.s.used, u.s.rows, u.t, u.hk, 0};
+        }
+        static_cast<GqaRecord*>(p.records)[wg] = r;
+      }
+    }
+    x += take;
+    return true;
+  }
+};
+
+// The slot of part i of a record of workgroup wg.
+__device__ __forceinline__ int gqa_slot(const GqaRecord& r, int wg, int i) { return i == 0 ? r.first : 2 * (wg + i); }
 
 // A read that the scalar unit makes where the address is the same for the whole wave.
 __device__ __forceinline__ int scalar_load(const int* p, size_t i) {

@@ -348,10 +348,10 @@ struct GqaParams {
   int shift, n_pages, width;
   const unsigned long long* bits;   // [rows][words]
   int words;
-  // the launch (gqa_rule): units to cut the keys for (0: not cut), units that the
-  // grid and the results have room for, and the records and results of the parts
-  int target;
-  int max_units;
+  // the launch (gqa_rule): whether the tiles' keys are cut, over how many
+  // workgroups, and the records and results of the parts
+  bool cut;
+  int wgs;
   void* records;
   float* partial;
 };

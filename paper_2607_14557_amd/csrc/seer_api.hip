@@ -815,8 +815,8 @@ static int gqa_params(seer::GqaParams& p, const seer_attn_desc* desc, int32_t ma
 
 static int launch_gqa(seer::GqaParams& p, hipStream_t stream) {
   const seer::GqaRule r = seer::gqa_rule(p.bf16, p.n_heads, p.n_kv, p.head_dim, p.rows_ub, p.B);
-  p.target = r.target;
-  p.max_units = r.grid;
+  p.cut = r.cut;
+  p.wgs = r.grid;
   p.partial = reinterpret_cast<float*>(static_cast<uint8_t*>(p.records) + r.records);
   return p.bf16 ? seer::launch_gqa_bf16(p, r, stream) : seer::launch_gqa_f32(p, r, stream);
 }
