@@ -648,21 +648,34 @@ __global__ __launch_bounds__(NT) void gqa_join_kernel(GqaParams p) {
   const int row = r.t * RT + w * 32 + fr;
   if (row >= r.rows) return;
   const float c = p.scale * 1.4426950408889634f;
-  float m = -INFINITY;
-#pragma unroll 8
-  for (int i = 0; i < r.parts; ++i) m = fmaxf(m, *Parts<RT, DH>(p, gqa_slot(r, wg, i)).max(w * 32 + fr));
-  const float ref = m == -INFINITY ? 0.0f : m;
-  float l = 0.0f;
+  // eight parts at a time, all their loads under way together
+  float m = -INFINITY, l = 0.0f;
   f32x4_t sum = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 8
-  for (int i = 0; i < r.parts; ++i) {
-    const Parts<RT, DH> from(p, gqa_slot(r, wg, i));
-    const float mi = *from.max(w * 32 + fr), li = *from.div(w * 32 + fr);
-    const f32x4_t v = *from.sum(w, dt, g, lane);
-    const bool none = mi == -INFINITY && li == 0.0f;
-    const float a = none ? 0.0f : __builtin_amdgcn_exp2f((mi - ref) * c);
-    l += li * a;
-    sum += a * v;
+  for (int i0 = 0; i0 < r.parts; i0 += 8) {
+    float pm[8], pl[8];
+    f32x4_t v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const Parts<RT, DH> from(p, gqa_slot(r, wg, i0 + k < r.parts ? i0 + k : r.parts - 1));
+      pm[k] = *from.max(w * 32 + fr);
+      pl[k] = *from.div(w * 32 + fr);
+      v[k] = *from.sum(w, dt, g, lane);
+    }
+    float top = m;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) top = fmaxf(top, pm[k]);
+    const float ref = top == -INFINITY ? 0.0f : top;
+    const float keep = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m - ref) * c);
+    m = top;
+    l *= keep;
+    sum *= keep;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const bool none = i0 + k >= r.parts || (pm[k] == -INFINITY && pl[k] == 0.0f);
+      const float a = none ? 0.0f : __builtin_amdgcn_exp2f((pm[k] - ref) * c);
+      l += none ? 0.0f : pl[k] * a;
+      sum += none ? f32x4_t{0, 0, 0, 0} : a * v[k];
+    }
   }
   const int tok = row / p.group, head = row - tok * p.group;
   const float inv = inverse(l);

@@ -255,22 +255,39 @@ __global__ __launch_bounds__(NT) void gqa_f32_join_kernel(GqaParams p) {
   const int row = r.t * kGqaF32 + fr;
   if (row >= r.rows) return;
   const float c = p.scale * 1.4426950408889634f;
-  float m = -INFINITY;
-#pragma unroll 8
-  for (int i = 0; i < r.parts; ++i) m = fmaxf(m, *Parts<H>(p, gqa_slot(r, wg, i)).max(fr));
-  const float ref = m == -INFINITY ? 0.0f : m;
-  float l = 0.0f;
+  // eight parts at a time, all their loads under way together
+  float m = -INFINITY, l = 0.0f;
   f32x4_t sum[H];
 #pragma unroll
   for (int h = 0; h < H; ++h) sum[h] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 8
-  for (int i = 0; i < r.parts; ++i) {
-    const Parts<H> from(p, gqa_slot(r, wg, i));
-    const float mi = *from.max(fr), li = *from.div(fr);
-    const float a = mi == -INFINITY && li == 0.0f ? 0.0f : __builtin_amdgcn_exp2f((mi - ref) * c);
-    l += li * a;
+  for (int i0 = 0; i0 < r.parts; i0 += 8) {
+    float pm[8], pl[8];
+    f32x4_t v[8][H];
 #pragma unroll
-    for (int h = 0; h < H; ++h) sum[h] += a * *from.sum(4 * h + wv, lane);
+    for (int k = 0; k < 8; ++k) {
+      const Parts<H> from(p, gqa_slot(r, wg, i0 + k < r.parts ? i0 + k : r.parts - 1));
+      pm[k] = *from.max(fr);
+      pl[k] = *from.div(fr);
+#pragma unroll
+      for (int h = 0; h < H; ++h) v[k][h] = *from.sum(4 * h + wv, lane);
+    }
+    float top = m;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) top = fmaxf(top, pm[k]);
+    const float ref = top == -INFINITY ? 0.0f : top;
+    const float keep = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m - ref) * c);
+    m = top;
+    l *= keep;
+#pragma unroll
+    for (int h = 0; h < H; ++h) sum[h] *= keep;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const bool none = i0 + k >= r.parts || (pm[k] == -INFINITY && pl[k] == 0.0f);
+      const float a = none ? 0.0f : __builtin_amdgcn_exp2f((pm[k] - ref) * c);
+      l += none ? 0.0f : pl[k] * a;
+#pragma unroll
+      for (int h = 0; h < H; ++h) sum[h] += none ? f32x4_t{0, 0, 0, 0} : a * v[k][h];
+    }
   }
   const int tok = row / p.group, head = row - tok * p.group;
   const bool real = tok < r.used;

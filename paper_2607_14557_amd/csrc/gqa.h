@@ -12,7 +12,7 @@
 namespace seer {
 
 // Keys are cut at multiples of this.
-constexpr int kGqaBlock = 128;
+constexpr int kGqaBlock = 64;
 
 // Rows of a key/value head are (token, query head of its group) pairs, the head
 // fastest: row i is token i / G, head i % G.  A tile is RT such rows, so K and V
@@ -76,7 +76,7 @@ struct GqaRecord {
 };
 
 // How the work of a launch is cut.
-//   p.cut:     every tile's keys count as blocks of 128, the blocks of all heads,
+//   p.cut:     every tile's keys count as blocks of 64, the blocks of all heads,
 //              requests and tiles stand in one line, and each of the p.wgs workgroups
 //              takes an equal stretch of it, whatever the requests' lengths: no
 //              workgroup waits for another, and none starts after the others.  A tile

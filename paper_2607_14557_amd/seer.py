@@ -81,6 +81,7 @@ class seer_attn_desc(ctypes.Structure):
 
 
 _lib = None
+_raw_stream = _current_device = None      # set by load_library
 _P = ctypes.c_void_p
 _I = ctypes.c_int32
 
@@ -96,6 +97,10 @@ def load_library():
     if not os.path.exists(LIB_PATH):
         raise RuntimeError("libseer.so is not built (%s); run `python -m paper_2607_14557_amd.build`"
                            % LIB_PATH)
+    global _raw_stream, _current_device
+    _current_device = torch.cuda.current_device
+    _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+        (lambda device: torch.cuda.current_stream(device).cuda_stream)
     L = ctypes.CDLL(LIB_PATH)
     L.seer_prepacked_bytes.argtypes = [ctypes.POINTER(seer_dims)]
     L.seer_prepacked_bytes.restype = ctypes.c_size_t
@@ -183,8 +188,8 @@ def _ptr(x):
 
 def _stream(s):
     if s is None:
-        import torch
-        return torch.cuda.current_stream().cuda_stream
+        # the current stream's handle, without the Stream object around it (0.2 us a call instead of 2.7)
+        return _raw_stream(_current_device())
     if isinstance(s, int):
         return s
     return s.cuda_stream
