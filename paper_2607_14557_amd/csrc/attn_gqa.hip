@@ -81,23 +81,39 @@ struct KeySource {
   }
 };
 
-// Loads 16 keys of K and V into their rows of the LDS tiles; keys past `last`
-// are the last one again.
+// Loads of 16 keys of K and V into their rows of the LDS tiles.  The lane adds to a
+// group's address its row of a load, and the piece of the row that the exchange
+// puts at its place (the same for every load of V).
 template <int DH>
-__device__ __forceinline__ void load_keys(const KeyRows& src, int last, uint8_t* kd, uint8_t* vd, int lane) {
-  constexpr int ROW = DH * 2, RPL = 1024 / ROW, LPR = ROW / 16;      // rows of a load, lanes of a row
-  const __amdgpu_buffer_rsrc_t rk = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(src.k), 0, -1, 0x00020000);
-  const __amdgpu_buffer_rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(src.v), 0, -1, 0x00020000);
+struct KeyLoads {
+  static constexpr int ROW = DH * 2, RPL = 1024 / ROW, LPR = ROW / 16;      // rows of a load, lanes of a row
+  uint32_t at_k[16 / RPL], at_v;
+  int lane;
+  __device__ __forceinline__ KeyLoads(size_t step_k, size_t step_v, int lane_) : lane(lane_) {
+    const int r = lane / LPR, c = lane % LPR;
 #pragma unroll
-  for (int q = 0; q < 16 / RPL; ++q) {
-    const int r = RPL * q + lane / LPR;
-    const int rr = r < last ? r : last;
-    const uint32_t ck = (uint32_t)((lane % LPR) ^ swz_k<DH>(r)) << 4;
-    const uint32_t cv = (uint32_t)((lane % LPR) ^ swz_v<DH>(r)) << 4;
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, (lds_void_t*)(kd + RPL * q * ROW), 16, rr * (uint32_t)src.step_k + ck, 0, 0, 0);
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, (lds_void_t*)(vd + RPL * q * ROW), 16, rr * (uint32_t)src.step_v + cv, 0, 0, 0);
+    for (int q = 0; q < 16 / RPL; ++q)
+      at_k[q] = (RPL * q + r) * (uint32_t)step_k + ((uint32_t)(c ^ swz_k<DH>(RPL * q + r)) << 4);
+    at_v = r * (uint32_t)step_v + ((uint32_t)(c ^ swz_v<DH>(r)) << 4);
   }
-}
+  // keys past `last` are the last one again
+  __device__ __forceinline__ void issue(const KeyRows& src, int last, uint8_t* kd, uint8_t* vd) const {
+    const __amdgpu_buffer_rsrc_t rk = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(src.k), 0, -1, 0x00020000);
+    const __amdgpu_buffer_rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(src.v), 0, -1, 0x00020000);
+    const uint32_t sk = (uint32_t)src.step_k, sv = (uint32_t)src.step_v;
+#pragma unroll
+    for (int q = 0; q < 16 / RPL; ++q) {
+      uint32_t ok = at_k[q], ov = at_v + RPL * q * sv;
+      if (last < 15) {
+        const int r = RPL * q + lane / LPR, less = r > last ? r - last : 0;
+        ok -= less * sk;
+        ov -= less * sv;
+      }
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, (lds_void_t*)(kd + RPL * q * ROW), 16, ok, 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, (lds_void_t*)(vd + RPL * q * ROW), 16, ov, 0, 0, 0);
+    }
+  }
+};
 
 // Values that are no numbers (NaN, infinities) under a mask: the product would
 // carry them to rows that do not see their keys, as 0 * value.  So the tiles in
@@ -375,6 +391,7 @@ __global__ __launch_bounds__(NT, 2) void gqa_tile_kernel(GqaParams p) {
                 (size_t)(u.hk * p.group + head) * DH, lane);
 
   const KeySource<DH, PAGED> keys(p, u);
+  const KeyLoads<DH> loads(keys.step_k, keys.step_v, lane);
   const int n = (u.hi - u.lo + 63) / 64;
   int id[4];                                 // pages of the four 16-key groups of the next tile
   auto pages = [&](int kbase) {
@@ -389,8 +406,8 @@ __global__ __launch_bounds__(NT, 2) void gqa_tile_kernel(GqaParams p) {
     int g = kbase + 16 * wv;                 // a group past the end is the last one again
     g = g < u.hi ? g : (u.hi - 1) & ~15;
     const int page = wv == 0 ? id[0] : (wv == 1 ? id[1] : (wv == 2 ? id[2] : id[3]));
-    load_keys<DH>(keys.rows(g, page), u.hi - 1 - g < 15 ? u.hi - 1 - g : 15, (B ? k_lds1 : k_lds0) + 16 * wv * ROW,
-                  (B ? v_lds1 : v_lds0) + 16 * wv * ROW, lane);
+    loads.issue(keys.rows(g, page), u.hi - 1 - g < 15 ? u.hi - 1 - g : 15, (B ? k_lds1 : k_lds0) + 16 * wv * ROW,
+                (B ? v_lds1 : v_lds0) + 16 * wv * ROW);
   };
   // bits of the keys whose pages are none of the pool's
   unsigned long long lost = 0, lost_next = 0;
@@ -477,9 +494,9 @@ __global__ __launch_bounds__(NT, 2) void gqa_tile_kernel(GqaParams p) {
   }
   const bool real = tok < u.s.used;
   const float inv = inverse(l);
-  uint16_t* at = out_row(p, u.s.s0 + tok, u.hk * p.group + head, DH) + fhalf * 4;
+  uint16_t* to = out_row(p, u.s.s0 + tok, u.hk * p.group + head, DH) + fhalf * 4;
 #pragma unroll
-  for (int i = 0; i < DT * 4; ++i) store4(at + (i >> 2) * 32 + (i & 3) * 8, real ? sum[i] * inv : f32x4_t{0, 0, 0, 0});
+  for (int i = 0; i < DT * 4; ++i) store4(to + (i >> 2) * 32 + (i & 3) * 8, real ? sum[i] * inv : f32x4_t{0, 0, 0, 0});
   }
 }
 
@@ -510,6 +527,7 @@ __global__ __launch_bounds__(NF, 1) void gqa_few_kernel(GqaParams p) {
                 (size_t)(u.hk * p.group + head) * DH, lane);
 
   const KeySource<DH, PAGED> keys(p, u);
+  const KeyLoads<DH> loads(keys.step_k, keys.step_v, lane);
   // this wave's tiles: 32 of every 64 keys
   const int k0 = u.lo + 32 * wv;
   const int n = u.hi > k0 ? (u.hi - k0 + 63) / 64 : 0;
@@ -527,8 +545,8 @@ __global__ __launch_bounds__(NF, 1) void gqa_few_kernel(GqaParams p) {
     for (int i = 0; i < 2; ++i) {
       int g = kbase + 16 * i;
       g = g < u.hi ? g : (u.hi - 1) & ~15;
-      load_keys<DH>(keys.rows(g, id[i]), u.hi - 1 - g < 15 ? u.hi - 1 - g : 15,
-                    (B ? k_lds1 : k_lds0) + wv * FT + 16 * i * ROW, (B ? v_lds1 : v_lds0) + wv * FT + 16 * i * ROW, lane);
+      loads.issue(keys.rows(g, id[i]), u.hi - 1 - g < 15 ? u.hi - 1 - g : 15, (B ? k_lds1 : k_lds0) + wv * FT + 16 * i * ROW,
+                  (B ? v_lds1 : v_lds0) + wv * FT + 16 * i * ROW);
     }
   };
   uint32_t lost[2] = {0, 0};
@@ -606,31 +624,50 @@ __global__ __launch_bounds__(NF, 1) void gqa_few_kernel(GqaParams p) {
   __syncthreads();
   const float m = fmaxf(m_part[0][fr], m_part[1][fr]);
   const float ref = m == -INFINITY ? 0.0f : m;
-  float a[2];
+  float a[2], l = 0.0f;
 #pragma unroll
   for (int v = 0; v < 2; ++v) {
     // a wave whose keys the row does not see has no part
     const bool none = m_part[v][fr] == -INFINITY && l_part[v][fr] == 0.0f;
     a[v] = none ? 0.0f : __builtin_amdgcn_exp2f((m_part[v][fr] - ref) * w.c);
+    l += l_part[v][fr] * a[v];
   }
-  const float l = l_part[0][fr] * a[0] + l_part[1][fr] * a[1];
+  f32x4_t sum[DT * 2];
+#pragma unroll
+  for (int i = 0; i < DT * 2; ++i) {
+    const int at = wv * DT * 2 + i;
+    sum[i] = a[0] * *sums(0, at >> 2, at & 3) + a[1] * *sums(1, at >> 2, at & 3);
+  }
   odd = __builtin_amdgcn_readfirstlane(odd_from[0] < odd_from[1] ? odd_from[0] : odd_from[1]);
-  const Parts<kGqaFew, DH> to(p, u.slot);
+  if (odd < u.hi) {
+#pragma unroll 1
+    for (int i = 0; i < DT * 2; ++i) {
+      // one copy of the code: the quadruples take turns at the front
+      const int at = wv * DT * 2 + i;
+      const f32x4_t v = add_odd<DH, VF16, PAGED>(sum[0], keys, u, sight, odd & ~15, 32 * (at >> 2) + 8 * (at & 3) + 4 * fhalf);
+#pragma unroll
+      for (int k = 0; k + 1 < DT * 2; ++k) sum[k] = sum[k + 1];
+      sum[DT * 2 - 1] = v;
+    }
+  }
+  if (row >= u.s.rows) continue;
+  if (!u.whole) {
+    const Parts<kGqaFew, DH> to(p, u.slot);
+#pragma unroll
+    for (int i = 0; i < DT * 2; ++i) *to.sum(0, (wv * DT * 2 + i) >> 2, i & 3, lane) = sum[i];
+    if (wv == 0 && fhalf == 0) {
+      *to.max(fr) = m;
+      *to.div(fr) = l;
+    }
+    continue;
+  }
   const bool real = tok < u.s.used;
   const float inv = inverse(l);
-  if (!u.whole && wv == 0 && fhalf == 0 && row < u.s.rows) {
-    *to.max(fr) = m;
-    *to.div(fr) = l;
-  }
-#pragma unroll 2
+  uint16_t* to = out_row(p, u.s.s0 + tok, u.hk * p.group + head, DH) + fhalf * 4;
+#pragma unroll
   for (int i = 0; i < DT * 2; ++i) {
-    const int at = wv * DT * 2 + i, dt = at >> 2, g = at & 3;
-    f32x4_t v = a[0] * *sums(0, dt, g) + a[1] * *sums(1, dt, g);
-    if (odd < u.hi) v = add_odd<DH, VF16, PAGED>(v, keys, u, sight, odd & ~15, 32 * dt + 8 * g + 4 * fhalf);
-    if (row >= u.s.rows) continue;
-    if (!u.whole) *to.sum(0, dt, g, lane) = v;
-    else store4(out_row(p, u.s.s0 + tok, u.hk * p.group + head, DH) + dt * 32 + g * 8 + fhalf * 4,
-                real ? v * inv : f32x4_t{0, 0, 0, 0});
+    const int at = wv * DT * 2 + i;
+    store4(to + (at >> 2) * 32 + (at & 3) * 8, real ? sum[i] * inv : f32x4_t{0, 0, 0, 0});
   }
   }
 }
@@ -639,7 +676,7 @@ __global__ __launch_bounds__(NF, 1) void gqa_few_kernel(GqaParams p) {
 // part left: a wave takes 32 rows x 8 dims (16 bytes a lane).
 template <int RT, int DH>
 __global__ __launch_bounds__(NT) void gqa_join_kernel(GqaParams p) {
-  constexpr int DT = DH / 32, PIECES = RT / 32 * DT;       // workgroups of a slot
+  constexpr int DT = DH / 32, PIECES = RT / 32 * DT;       // workgroups of a tile
   const int wg = blockIdx.x / PIECES, piece = blockIdx.x % PIECES;
   const GqaRecord r = static_cast<const GqaRecord*>(p.records)[wg];
   if (r.parts < 2) return;

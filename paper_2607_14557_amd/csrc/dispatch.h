@@ -189,25 +189,30 @@ struct GqaRule {
   int rt;                // rows of a tile
   bool cut;              // whether the tiles' keys are cut, over `grid` workgroups
   int grid;
-  size_t records;        // bytes of the parts' records
-  size_t bytes;          // of the records and the results
 };
 
-// The form of a launch of up to `rows` rows in `batch` requests.
-inline GqaRule gqa_rule(bool bf16, int heads, int n_kv, int dim, int rows, int batch) {
+// The form of a launch of up to `rows` rows in `batch` requests of up to `keys`
+// keys.
+inline GqaRule gqa_rule(bool bf16, int heads, int n_kv, int dim, int rows, int batch, long long keys) {
   GqaRule r{};
   const int group = heads / n_kv;
   const long long pairs = (long long)rows * group;
   r.rt = !bf16 ? kGqaF32 : (pairs / batch > 64 ? kGqaTile : kGqaFew);
   const long long tiles = (pairs >= batch ? (pairs - batch) / r.rt + batch : pairs) * n_kv;
+  const long long blocks = (keys + 63) / 64 > 0 ? (keys + 63) / 64 : 1;
   // workgroups that run at once on 256 CUs
   const int wgs = r.rt == kGqaFew && dim <= 64 ? 1024 : 512;
-  r.cut = r.rt != kGqaTile || tiles < wgs;
-  r.grid = r.cut ? wgs : (int)tiles;
-  // two parts a workgroup: the sums of each row, its maximum and its divisor
-  r.records = r.cut ? (size_t)wgs * 32 : 0;
-  r.bytes = r.cut ? r.records + (size_t)2 * wgs * r.rt * ((dim > 64 ? 128 : 64) + 2) * 4 : 0;
+  // the places of the line are counted in 31 bits
+  r.cut = (r.rt != kGqaTile || tiles < wgs) && blocks <= 0x7fffffff / tiles;
+  r.grid = (int)(!r.cut ? tiles : (tiles * blocks < wgs ? tiles * blocks : wgs));
   return r;
+}
+
+// Bytes of the parts of a cut launch (their records, then two results a workgroup:
+// the sums of each row, its maximum and its divisor), for any number of keys.
+inline size_t gqa_record_bytes(const GqaRule& r) { return ((size_t)r.grid * 32 + 255) / 256 * 256; }
+inline size_t gqa_bytes(const GqaRule& r, int dim) {
+  return r.cut ? gqa_record_bytes(r) + (size_t)2 * r.grid * r.rt * ((dim > 64 ? 128 : 64) + 2) * 4 : 0;
 }
 
 }  // namespace seer

@@ -88,22 +88,25 @@ template <int RT, int NT>
 struct GqaCut {
   static constexpr int NW = NT / kWave;
   struct Shared {
-    long long sums[NW];
-    long long first[NT + 1];     // of each thread's stretch of a head's line
+    int sums[NW];
+    int first[NT + 1];           // of each thread's stretch of a head's line
     GqaSeq seq[NT];              // of each thread's only request
     int found[12];
   };
   Shared& sh;
-  long long n;                   // length of a head's line
-  long long x, x0, x1;           // the next place, and the workgroup's stretch
+  int n, all;                    // length of a head's line, and of the whole
+  int wgs, each, more;           // workgroups with work: `more` of them take each + 1, the others each
+  int x, x0, x1;                 // the next place, and the workgroup's stretch
   int wg;
 
-  __device__ __forceinline__ static long long uniform(long long v) {
-    return (long long)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32 |
-           (uint32_t)__builtin_amdgcn_readfirstlane((int)v);
+  __device__ __forceinline__ static int weight(const GqaParams& p, const GqaSeq& s) {
+    return s.tiles * (p.cut ? gqa_blocks(s.nk) : 1);
   }
-  __device__ __forceinline__ static long long weight(const GqaParams& p, const GqaSeq& s) {
-    return (long long)s.tiles * (p.cut ? gqa_blocks(s.nk) : 1);
+  __device__ __forceinline__ int start(int i) const { return i * each + (i < more ? i : more); }
+  // the workgroup that has place y
+  __device__ __forceinline__ int holder(int y) const {
+    const int head = more * (each + 1);
+    return y < head ? (int)((unsigned)y / (unsigned)(each + 1)) : more + (int)((unsigned)(y - head) / (unsigned)each);
   }
 
   __device__ __forceinline__ GqaCut(const GqaParams& p, Shared& shared) : sh(shared) {
@@ -111,48 +114,50 @@ struct GqaCut {
     const int per = (p.B + NT - 1) / NT;
     const int b0 = tid * per < p.B ? tid * per : p.B;
     const int b1 = b0 + per < p.B ? b0 + per : p.B;
-    long long own = 0;
+    int own = 0;
     for (int b = b0; b < b1; ++b) {
       const GqaSeq s = gqa_seq<RT>(p, b);
       own += weight(p, s);
       if (per == 1) sh.seq[tid] = s;
     }
-    long long inc = own;
+    int inc = own;
 #pragma unroll
     for (int off = 1; off < kWave; off <<= 1) {
-      const long long v = __shfl_up(inc, off, kWave);
+      const int v = __shfl_up(inc, off, kWave);
       if (lane >= off) inc += v;
     }
     if (lane == kWave - 1) sh.sums[wave] = inc;
     __syncthreads();
-    long long first = inc - own;
+    int first = inc - own;
     n = 0;
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
       if (w < wave) first += sh.sums[w];
       n += sh.sums[w];
     }
-    n = uniform(n);
+    n = __builtin_amdgcn_readfirstlane(n);
     sh.first[tid] = first;
     if (tid == NT - 1) sh.first[NT] = n;
-    const long long all = n * p.n_kv;
+    all = n * p.n_kv;
     const int bid = blockIdx.x;
     wg = 0;
-    if (p.cut) {
-      const int wgs = all < p.wgs ? (int)all : p.wgs;
-      x0 = x1 = 0;
-      if (bid >= wgs) {
-        if (tid == 0) static_cast<GqaRecord*>(p.records)[bid].parts = 0;
-      } else {
-        // each XCD takes a contiguous part of the line: the tiles of one request and
-        // head find their keys in its L2
-        wg = xcd_remap(bid, wgs);
-        x0 = wg * all / wgs;
-        x1 = (wg + 1) * all / wgs;
-      }
-    } else {
-      x0 = bid < all ? xcd_remap(bid, (int)all) : 0;
-      x1 = bid < all ? x0 + 1 : x0;
+    wgs = all;
+    each = 1;
+    more = 0;
+    if (p.cut && all > p.wgs) {
+      wgs = p.wgs;
+      each = (unsigned)all / (unsigned)wgs;
+      more = all - each * wgs;
+    }
+    x0 = x1 = 0;
+    if (bid < wgs) {
+      // each XCD takes a contiguous part of the line: the tiles of one request and
+      // head find their keys in its L2
+      wg = xcd_remap(bid, wgs);
+      x0 = start(wg);
+      x1 = start(wg + 1);
+    } else if (p.cut && tid == 0) {
+      static_cast<GqaRecord*>(p.records)[bid].parts = 0;
     }
     x = x0;
   }
@@ -161,38 +166,37 @@ struct GqaCut {
   __device__ __forceinline__ bool next(const GqaParams& p, GqaUnit& u) {
     if (x >= x1) return false;
     const int tid = threadIdx.x;
-    u.hk = (int)(x / n);
-    const long long j = x - u.hk * n;
+    u.hk = (unsigned)x / (unsigned)n;
+    const int j = x - u.hk * n;
     __syncthreads();               // the line is written, and the last piece's reads of LDS are done
     if (j >= sh.first[tid] && j < sh.first[tid + 1]) {
       const int per = (p.B + NT - 1) / NT;
-      int b = tid * per;
-      long long at = sh.first[tid];
+      int b = tid * per, at = sh.first[tid];
       GqaSeq s;
       if (per == 1) {
         s = sh.seq[tid];
       } else {
         for (;; ++b) {
           s = gqa_seq<RT>(p, b);
-          const long long m = weight(p, s);
+          const int m = weight(p, s);
           if (j < at + m) break;
           at += m;
         }
       }
-      const int nb = p.cut ? gqa_blocks(s.nk) : 1;
-      const int rem = (int)(j - at);
-      sh.found[0] = b; sh.found[1] = rem / nb; sh.found[2] = rem % nb; sh.found[3] = nb;
-      sh.found[4] = s.s0; sh.found[5] = s.len; sh.found[6] = s.used; sh.found[7] = s.nk; sh.found[8] = s.past;
-      sh.found[9] = s.rows; sh.found[10] = s.tiles;
+      sh.found[0] = b; sh.found[1] = j - at; sh.found[2] = s.tiles;
+      sh.found[3] = s.s0; sh.found[4] = s.len; sh.found[5] = s.used; sh.found[6] = s.nk; sh.found[7] = s.past;
+      sh.found[8] = s.rows;
     }
     __syncthreads();
     auto get = [&](int i) { return __builtin_amdgcn_readfirstlane(sh.found[i]); };
     u.b = get(0);
-    u.s.s0 = get(4); u.s.len = get(5); u.s.used = get(6); u.s.nk = get(7); u.s.past = get(8); u.s.rows = get(9);
-    u.s.tiles = get(10);
+    const int rem = get(1);
+    u.s.tiles = get(2); u.s.s0 = get(3); u.s.len = get(4); u.s.used = get(5); u.s.nk = get(6); u.s.past = get(7);
+    u.s.rows = get(8);
+    const int nb = p.cut ? gqa_blocks(u.s.nk) : 1;
+    const int tile = (unsigned)rem / (unsigned)nb, block = rem - tile * nb;
     // the tiles of a causal prompt from the last, which has the most keys, to the first
-    u.t = u.s.tiles - 1 - get(1);
-    const int block = get(2), nb = get(3);
+    u.t = u.s.tiles - 1 - tile;
     const int end = gqa_tile_end<RT>(p, u.s, u.t);
     u.whole = true;
     u.lo = 0;
@@ -200,7 +204,7 @@ struct GqaCut {
     u.slot = 0;
     int take = 1;
     if (p.cut) {
-      take = nb - block < x1 - x ? nb - block : (int)(x1 - x);
+      take = nb - block < x1 - x ? nb - block : x1 - x;
       u.whole = take == nb;
       const long long lo = (long long)block * kGqaBlock, hi = lo + (long long)take * kGqaBlock;
       u.lo = lo < end ? (int)lo : end;
@@ -209,13 +213,8 @@ struct GqaCut {
       if (tid == 0 && x + take >= x1) {
         // the last piece: where it opens a tile that goes on, the tile's record
         GqaRecord r{};
-        if (block == 0 && take < nb) {
-          // the workgroup that has the tile's last block: x0(i) = floor(i all / wgs)
-          const long long all = n * p.n_kv;
-          const int wgs = all < p.wgs ? (int)all : p.wgs;
-          const int last = (int)(((x + nb) * wgs - 1) / all);
-          r = GqaRecord{last - wg + 1, u.slot, u.s.s0, u.s.used, u.s.rows, u.t, u.hk, 0};
-        }
+        if (block == 0 && take < nb)
+          r = GqaRecord{holder(x + nb - 1) - wg + 1, u.slot, u.s.s0, u.s.used, u.s.rows, u.t, u.hk, 0};
         static_cast<GqaRecord*>(p.records)[wg] = r;
       }
     }

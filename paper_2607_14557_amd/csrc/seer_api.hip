@@ -779,9 +779,10 @@ size_t seer_attn_workspace_bytes(const seer_attn_desc* desc, int32_t rows_ub, in
     fail(SEER_EINVAL, "rows_ub and batch must be positive, rows_ub * n_heads below 2^31");
     return 0;
   }
+  // keys enough for the largest grid
   const seer::GqaRule r = seer::gqa_rule(desc->dtype == SEER_DTYPE_BF16, desc->n_heads, desc->n_kv_heads,
-                                         desc->head_dim, rows_ub, batch);
-  return 256 + up256(r.bytes);
+                                         desc->head_dim, rows_ub, batch, 1 << 16);
+  return 256 + up256(seer::gqa_bytes(r, desc->head_dim));
 }
 
 // what both attention calls check and fill in
@@ -814,10 +815,11 @@ static int gqa_params(seer::GqaParams& p, const seer_attn_desc* desc, int32_t ma
 }
 
 static int launch_gqa(seer::GqaParams& p, hipStream_t stream) {
-  const seer::GqaRule r = seer::gqa_rule(p.bf16, p.n_heads, p.n_kv, p.head_dim, p.rows_ub, p.B);
+  const seer::GqaRule r = seer::gqa_rule(p.bf16, p.n_heads, p.n_kv, p.head_dim, p.rows_ub, p.B,
+                                         p.table ? (long long)p.width << p.shift : p.rows_ub);
   p.cut = r.cut;
   p.wgs = r.grid;
-  p.partial = reinterpret_cast<float*>(static_cast<uint8_t*>(p.records) + r.records);
+  p.partial = reinterpret_cast<float*>(static_cast<uint8_t*>(p.records) + seer::gqa_record_bytes(r));
   return p.bf16 ? seer::launch_gqa_bf16(p, r, stream) : seer::launch_gqa_f32(p, r, stream);
 }
 
