@@ -10,7 +10,7 @@
 // and V come by direct-to-LDS loads, V's operand by the LDS transpose read.
 // Two forms:
 //   gqa_tile_kernel  128 rows a workgroup, 32 a wave, K and V tiles of 64 keys shared by the four waves
-//   gqa_few_kernel   32 rows a workgroup, the keys split over its two waves
+//   gqa_few_kernel   32 rows a workgroup, the keys split over its two or four waves
 // both over all of a tile's keys or, where there are few tiles, over a part of
 // them; gqa_join_kernel then adds the parts.
 #include <type_traits>
@@ -24,8 +24,7 @@ namespace {
 typedef short v4i16_t __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) v4i16_t lds_v4i16_t;
 
-constexpr int NT = 256;          // threads of a workgroup, and of one of the few-row form
-constexpr int NF = 128;
+constexpr int NT = 256;
 
 // LDS tiles hold a key per row of DH * 2 bytes, in 16-byte pieces whose place is
 // exchanged so that the reads of a fragment meet distinct banks: piece c of row r
@@ -219,6 +218,7 @@ struct Rows32 {
     // instruction takes them, and their sum in fp32, over the rounded values where
     // they are coarse, so that the weights add up to one.
     u32x4_t pf[2 * NI], pl[FINE ? 2 * NI : 1];
+    const float floor = masked ? 0.0f : 7.5e-37f;         // (FINE) 2^-120
     float lsum;
     auto probs = [&](float ref) {
       const float mc = ref * c;
@@ -234,10 +234,13 @@ struct Rows32 {
             lsum = __builtin_amdgcn_fdot2(h, f16x2_t{(_Float16)1.0f, (_Float16)1.0f}, lsum, false);
             pf[sl][e] = __builtin_bit_cast(uint32_t, h);
           } else if constexpr (FINE) {
-            const uint32_t h = pack_bf2(p0, p1);
+            // the upper halves as they are, so that what is left is not negative; it is
+            // kept above zero, as an infinite value times zero would be none
+            const uint32_t b0 = __float_as_uint(p0), b1 = __float_as_uint(p1);
             lsum += p0 + p1;
-            pf[sl][e] = h;
-            pl[sl][e] = pack_bf2(p0 - __uint_as_float(h << 16), p1 - __uint_as_float(h & 0xffff0000u));
+            pf[sl][e] = __builtin_amdgcn_perm(b1, b0, 0x07060302u);
+            pl[sl][e] = pack_bf2(fmaxf(p0 - __uint_as_float(b0 & 0xffff0000u), floor),
+                                 fmaxf(p1 - __uint_as_float(b1 & 0xffff0000u), floor));
           } else {
             const bf16x2_t h = __builtin_convertvector(f32x2_t{p0, p1}, bf16x2_t);
             lsum = __builtin_amdgcn_fdot2_f32_bf16(h, bf16x2_t{(__bf16)1.0f, (__bf16)1.0f}, lsum, false);
@@ -377,14 +380,14 @@ __global__ __launch_bounds__(NT, 2) void gqa_tile_kernel(GqaParams p) {
   const int fr = lane & 31, fhalf = lane >> 5;
   const int row = u.t * kGqaTile + wv * 32 + fr;
   const int src = row < u.s.rows ? row : u.s.rows - 1;
-  const int tok = src / p.group, head = src - tok * p.group;
+  const int tok = gqa_token(p, src), head = src - tok * p.group;
   const GqaSight<PAGED> sight(p, u, tok);
   // where the workgroup's and the wave's rows begin to be blind to some keys, and
   // where the wave's last row sees no more
-  const int open_all = gqa_open_end(p, u, u.t * kGqaTile / p.group);
-  const int open = gqa_open_end(p, u, (u.t * kGqaTile + wv * 32) / p.group);
+  const int open_all = gqa_open_end(p, u, gqa_token(p, u.t * kGqaTile));
+  const int open = gqa_open_end(p, u, gqa_token(p, u.t * kGqaTile + wv * 32));
   int end = u.hi;
-  if (p.mask == kMaskCausal) end = u.s.past + (u.t * kGqaTile + wv * 32 + 31) / p.group + 1;
+  if (p.mask == kMaskCausal) end = u.s.past + gqa_token(p, u.t * kGqaTile + wv * 32 + 31) + 1;
 
   Rows32<DH, VF16, 2, false> w;
   w.init(p, static_cast<const uint16_t*>(p.q) + (size_t)(u.s.s0 + tok) * p.q_stride +
@@ -500,17 +503,18 @@ __global__ __launch_bounds__(NT, 2) void gqa_tile_kernel(GqaParams p) {
   }
 }
 
-template <int DH, bool VF16, bool PAGED>
-__global__ __launch_bounds__(NF, 1) void gqa_few_kernel(GqaParams p) {
+template <int DH, bool VF16, bool PAGED, int NW>
+__global__ __launch_bounds__(64 * NW, 1) void gqa_few_kernel(GqaParams p) {
   constexpr int ROW = DH * 2, DT = DH / 32, FT = 32 * ROW;      // bytes of a wave's K or V tile
-  __shared__ __attribute__((aligned(1024))) uint8_t k_lds0[2 * FT];
-  __shared__ __attribute__((aligned(1024))) uint8_t k_lds1[2 * FT];
-  __shared__ __attribute__((aligned(1024))) uint8_t v_lds0[2 * FT];
-  __shared__ __attribute__((aligned(1024))) uint8_t v_lds1[2 * FT];
-  __shared__ float m_part[2][32], l_part[2][32];
-  __shared__ int odd_from[2];
-  __shared__ typename GqaCut<kGqaFew, NF>::Shared cut_lds;
-  GqaCut<kGqaFew, NF> cut(p, cut_lds);
+  constexpr int PW = DT * 4 / NW;                               // 8-dim pieces that a wave joins
+  __shared__ __attribute__((aligned(1024))) uint8_t k_lds0[NW * FT];
+  __shared__ __attribute__((aligned(1024))) uint8_t k_lds1[NW * FT];
+  __shared__ __attribute__((aligned(1024))) uint8_t v_lds0[NW * FT];
+  __shared__ __attribute__((aligned(1024))) uint8_t v_lds1[NW * FT];
+  __shared__ float m_part[NW][32], l_part[NW][32];
+  __shared__ int odd_from[NW];
+  __shared__ typename GqaCut<kGqaFew, 64 * NW>::Shared cut_lds;
+  GqaCut<kGqaFew, 64 * NW> cut(p, cut_lds);
   GqaUnit u;
   while (cut.next(p, u)) {
   const int lane = threadIdx.x & 63;
@@ -518,9 +522,9 @@ __global__ __launch_bounds__(NF, 1) void gqa_few_kernel(GqaParams p) {
   const int fr = lane & 31, fhalf = lane >> 5;
   const int row = u.t * kGqaFew + fr;
   const int src = row < u.s.rows ? row : u.s.rows - 1;
-  const int tok = src / p.group, head = src - tok * p.group;
+  const int tok = gqa_token(p, src), head = src - tok * p.group;
   const GqaSight<PAGED> sight(p, u, tok);
-  const int open = gqa_open_end(p, u, u.t * kGqaFew / p.group);
+  const int open = gqa_open_end(p, u, gqa_token(p, u.t * kGqaFew));
 
   Rows32<DH, VF16, 1, !VF16> w;
   w.init(p, static_cast<const uint16_t*>(p.q) + (size_t)(u.s.s0 + tok) * p.q_stride +
@@ -528,9 +532,10 @@ __global__ __launch_bounds__(NF, 1) void gqa_few_kernel(GqaParams p) {
 
   const KeySource<DH, PAGED> keys(p, u);
   const KeyLoads<DH> loads(keys.step_k, keys.step_v, lane);
-  // this wave's tiles: 32 of every 64 keys
+  // this wave's tiles: 32 of every 32 NW keys
+  constexpr int STEP = 32 * NW;
   const int k0 = u.lo + 32 * wv;
-  const int n = u.hi > k0 ? (u.hi - k0 + 63) / 64 : 0;
+  const int n = u.hi > k0 ? (u.hi - k0 + STEP - 1) / STEP : 0;
   int id[2];
   auto pages = [&](int kbase) {
 #pragma unroll
@@ -565,17 +570,17 @@ __global__ __launch_bounds__(NF, 1) void gqa_few_kernel(GqaParams p) {
     load(k0, std::integral_constant<int, 0>{});
     lost[0] = lost_of();
     if (n > 1) {
-      pages(k0 + 64);
-      load(k0 + 64, std::integral_constant<int, 1>{});
+      pages(k0 + STEP);
+      load(k0 + STEP, std::integral_constant<int, 1>{});
       lost[1] = lost_of();
     }
-    pages(k0 + 128 < u.hi ? k0 + 128 : u.hi - 1);
+    pages(k0 + 2 * STEP < u.hi ? k0 + 2 * STEP : u.hi - 1);
   }
   // Both buffers are under way; a tile's buffer is filled again as soon as the tile
   // is done, so that one to two tiles are in flight all the time.
   auto step = [&](int kt, auto buf) {
     constexpr int B = decltype(buf)::value;
-    const int kbase = k0 + 64 * kt;
+    const int kbase = k0 + STEP * kt;
     uint8_t* vl = (B ? v_lds1 : v_lds0) + wv * FT;
     __builtin_amdgcn_sched_barrier(0);
     if (kt + 1 < n) __builtin_amdgcn_s_waitcnt(0x0f70 | (LOADS & 15) | (LOADS >> 4) << 14);    // vmcnt(LOADS)
@@ -595,9 +600,9 @@ __global__ __launch_bounds__(NF, 1) void gqa_few_kernel(GqaParams p) {
       __builtin_amdgcn_s_waitcnt(0xc07f);     // lgkmcnt(0)
       __builtin_amdgcn_wave_barrier();
       __builtin_amdgcn_sched_barrier(0);
-      load(kbase + 128, buf);
+      load(kbase + 2 * STEP, buf);
       lost[B] = lost_of();
-      if (kt + 3 < n) pages(kbase + 192);
+      if (kt + 3 < n) pages(kbase + 3 * STEP);
     }
   };
   for (int kt = 0; kt < n; kt += 2) {
@@ -605,56 +610,58 @@ __global__ __launch_bounds__(NF, 1) void gqa_few_kernel(GqaParams p) {
     if (kt + 1 < n) step(kt + 1, std::integral_constant<int, 1>{});
   }
 
-  // join the waves: each leaves its sums in its own K tiles and takes half the dims
+  // join the waves: each leaves its sums in its own K tiles and takes PW pieces
   const float l_own = w.l + __shfl_xor(w.l, 32, kWave);
   if (fhalf == 0) {
     m_part[wv][fr] = w.m;
     l_part[wv][fr] = l_own;
   }
   if (lane == 0) odd_from[wv] = odd;
-  auto sums = [&](int v, int dt, int g) {
-    const int at = dt * 4 + g;              // of DT * 4 blocks of 1 KiB; a buffer has FT / 1024 of them
+  auto sums = [&](int v, int at) {          // piece `at` of DT * 4 blocks of 1 KiB; a buffer has FT / 1024 of them
     return reinterpret_cast<f32x4_t*>((at >= FT / 1024 ? k_lds1 : k_lds0) + v * FT + at % (FT / 1024) * 1024 + lane * 16);
   };
 #pragma unroll
-  for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-    for (int g = 0; g < 4; ++g)
-      *sums(wv, dt, g) = f32x4_t{w.o[dt][4 * g], w.o[dt][4 * g + 1], w.o[dt][4 * g + 2], w.o[dt][4 * g + 3]};
+  for (int at = 0; at < DT * 4; ++at)
+    *sums(wv, at) = f32x4_t{w.o[at >> 2][4 * (at & 3)], w.o[at >> 2][4 * (at & 3) + 1], w.o[at >> 2][4 * (at & 3) + 2],
+                            w.o[at >> 2][4 * (at & 3) + 3]};
   __syncthreads();
-  const float m = fmaxf(m_part[0][fr], m_part[1][fr]);
-  const float ref = m == -INFINITY ? 0.0f : m;
-  float a[2], l = 0.0f;
+  float m = -INFINITY;
 #pragma unroll
-  for (int v = 0; v < 2; ++v) {
+  for (int v = 0; v < NW; ++v) m = fmaxf(m, m_part[v][fr]);
+  const float ref = m == -INFINITY ? 0.0f : m;
+  float l = 0.0f;
+  f32x4_t sum[PW];
+#pragma unroll
+  for (int i = 0; i < PW; ++i) sum[i] = f32x4_t{0, 0, 0, 0};
+#pragma unroll
+  for (int v = 0; v < NW; ++v) {
     // a wave whose keys the row does not see has no part
     const bool none = m_part[v][fr] == -INFINITY && l_part[v][fr] == 0.0f;
-    a[v] = none ? 0.0f : __builtin_amdgcn_exp2f((m_part[v][fr] - ref) * w.c);
-    l += l_part[v][fr] * a[v];
-  }
-  f32x4_t sum[DT * 2];
+    const float a = none ? 0.0f : __builtin_amdgcn_exp2f((m_part[v][fr] - ref) * w.c);
+    l += l_part[v][fr] * a;
 #pragma unroll
-  for (int i = 0; i < DT * 2; ++i) {
-    const int at = wv * DT * 2 + i;
-    sum[i] = a[0] * *sums(0, at >> 2, at & 3) + a[1] * *sums(1, at >> 2, at & 3);
+    for (int i = 0; i < PW; ++i) sum[i] += a * *sums(v, wv * PW + i);
   }
-  odd = __builtin_amdgcn_readfirstlane(odd_from[0] < odd_from[1] ? odd_from[0] : odd_from[1]);
+  odd = odd_from[0];
+#pragma unroll
+  for (int v = 1; v < NW; ++v) odd = odd_from[v] < odd ? odd_from[v] : odd;
+  odd = __builtin_amdgcn_readfirstlane(odd);
   if (odd < u.hi) {
 #pragma unroll 1
-    for (int i = 0; i < DT * 2; ++i) {
+    for (int i = 0; i < PW; ++i) {
       // one copy of the code: the quadruples take turns at the front
-      const int at = wv * DT * 2 + i;
+      const int at = wv * PW + i;
       const f32x4_t v = add_odd<DH, VF16, PAGED>(sum[0], keys, u, sight, odd & ~15, 32 * (at >> 2) + 8 * (at & 3) + 4 * fhalf);
 #pragma unroll
-      for (int k = 0; k + 1 < DT * 2; ++k) sum[k] = sum[k + 1];
-      sum[DT * 2 - 1] = v;
+      for (int k = 0; k + 1 < PW; ++k) sum[k] = sum[k + 1];
+      sum[PW - 1] = v;
     }
   }
   if (row >= u.s.rows) continue;
   if (!u.whole) {
     const Parts<kGqaFew, DH> to(p, u.slot);
 #pragma unroll
-    for (int i = 0; i < DT * 2; ++i) *to.sum(0, (wv * DT * 2 + i) >> 2, i & 3, lane) = sum[i];
+    for (int i = 0; i < PW; ++i) *to.sum(0, (wv * PW + i) >> 2, (wv * PW + i) & 3, lane) = sum[i];
     if (wv == 0 && fhalf == 0) {
       *to.max(fr) = m;
       *to.div(fr) = l;
@@ -665,8 +672,8 @@ __global__ __launch_bounds__(NF, 1) void gqa_few_kernel(GqaParams p) {
   const float inv = inverse(l);
   uint16_t* to = out_row(p, u.s.s0 + tok, u.hk * p.group + head, DH) + fhalf * 4;
 #pragma unroll
-  for (int i = 0; i < DT * 2; ++i) {
-    const int at = wv * DT * 2 + i;
+  for (int i = 0; i < PW; ++i) {
+    const int at = wv * PW + i;
     store4(to + (at >> 2) * 32 + (at & 3) * 8, real ? sum[i] * inv : f32x4_t{0, 0, 0, 0});
   }
   }
@@ -685,14 +692,15 @@ __global__ __launch_bounds__(NT) void gqa_join_kernel(GqaParams p) {
   const int row = r.t * RT + w * 32 + fr;
   if (row >= r.rows) return;
   const float c = p.scale * 1.4426950408889634f;
-  // eight parts at a time, all their loads under way together
+  // the loads of several parts under way together
   float m = -INFINITY, l = 0.0f;
   f32x4_t sum = {0.0f, 0.0f, 0.0f, 0.0f};
-  for (int i0 = 0; i0 < r.parts; i0 += 8) {
-    float pm[8], pl[8];
-    f32x4_t v[8];
+  auto add = [&](int i0, auto width) {
+    constexpr int W = decltype(width)::value;
+    float pm[W], pl[W];
+    f32x4_t v[W];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
+    for (int k = 0; k < W; ++k) {
       const Parts<RT, DH> from(p, gqa_slot(r, wg, i0 + k < r.parts ? i0 + k : r.parts - 1));
       pm[k] = *from.max(w * 32 + fr);
       pl[k] = *from.div(w * 32 + fr);
@@ -700,21 +708,25 @@ __global__ __launch_bounds__(NT) void gqa_join_kernel(GqaParams p) {
     }
     float top = m;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) top = fmaxf(top, pm[k]);
+    for (int k = 0; k < W; ++k) top = fmaxf(top, pm[k]);
     const float ref = top == -INFINITY ? 0.0f : top;
     const float keep = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m - ref) * c);
     m = top;
     l *= keep;
     sum *= keep;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
+    for (int k = 0; k < W; ++k) {
       const bool none = i0 + k >= r.parts || (pm[k] == -INFINITY && pl[k] == 0.0f);
       const float a = none ? 0.0f : __builtin_amdgcn_exp2f((pm[k] - ref) * c);
       l += none ? 0.0f : pl[k] * a;
       sum += none ? f32x4_t{0, 0, 0, 0} : a * v[k];
     }
-  }
-  const int tok = row / p.group, head = row - tok * p.group;
+  };
+  if (r.parts <= 4) add(0, std::integral_constant<int, 4>{});
+  else if (r.parts <= 8) add(0, std::integral_constant<int, 8>{});
+  else
+    for (int i0 = 0; i0 < r.parts; i0 += 16) add(i0, std::integral_constant<int, 16>{});
+  const int tok = gqa_token(p, row), head = row - tok * p.group;
   const float inv = inverse(l);
   store4(out_row(p, r.s0 + tok, r.hk * p.group + head, DH) + dt * 32 + g * 8 + fhalf * 4,
          tok < r.used ? sum * inv : f32x4_t{0, 0, 0, 0});
@@ -727,9 +739,11 @@ int launch_gqa_bf16(const GqaParams& p, const GqaRule& r, hipStream_t s) {
     if (r.rt == kGqaTile) {
       hipLaunchKernelGGL((gqa_tile_kernel<DH, V, P>), dim3(r.grid), dim3(NT), 0, s, p);
       if (r.cut) hipLaunchKernelGGL((gqa_join_kernel<kGqaTile, DH>), dim3(r.grid * (4 * DH / 32)), dim3(NT), 0, s, p);
+    } else if (r.cut) {
+      hipLaunchKernelGGL((gqa_few_kernel<DH, V, P, 2>), dim3(r.grid), dim3(128), 0, s, p);
+      hipLaunchKernelGGL((gqa_join_kernel<kGqaFew, DH>), dim3(r.grid * (DH / 32)), dim3(NT), 0, s, p);
     } else {
-      hipLaunchKernelGGL((gqa_few_kernel<DH, V, P>), dim3(r.grid), dim3(NF), 0, s, p);
-      if (r.cut) hipLaunchKernelGGL((gqa_join_kernel<kGqaFew, DH>), dim3(r.grid * (DH / 32)), dim3(NT), 0, s, p);
+      hipLaunchKernelGGL((gqa_few_kernel<DH, V, P, 4>), dim3(r.grid), dim3(256), 0, s, p);
     }
   };
   auto with = [&](auto dh, auto vf16) {

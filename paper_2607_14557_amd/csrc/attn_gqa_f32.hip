@@ -8,6 +8,8 @@
 // lane's group of 16.  K and V go from memory to the operand registers in
 // 16-byte loads; the order of the head's dims in the products is the one that
 // those loads give.
+#include <type_traits>
+
 #include "gqa.h"
 
 namespace seer {
@@ -46,9 +48,9 @@ __global__ __launch_bounds__(NT) void gqa_f32_kernel(GqaParams p) {
   const int D = p.head_dim;
   const int row = u.t * kGqaF32 + fr;
   const int src = row < u.s.rows ? row : u.s.rows - 1;
-  const int tok = src / p.group, head = src - tok * p.group;
+  const int tok = gqa_token(p, src), head = src - tok * p.group;
   const GqaSight<PAGED> sight(p, u, tok);
-  const int open = gqa_open_end(p, u, u.t * kGqaF32 / p.group);
+  const int open = gqa_open_end(p, u, gqa_token(p, u.t * kGqaF32));
   const float c = p.scale * 1.4426950408889634f;
   const f32x4_t zero = {0.0f, 0.0f, 0.0f, 0.0f};
 
@@ -255,16 +257,17 @@ __global__ __launch_bounds__(NT) void gqa_f32_join_kernel(GqaParams p) {
   const int row = r.t * kGqaF32 + fr;
   if (row >= r.rows) return;
   const float c = p.scale * 1.4426950408889634f;
-  // eight parts at a time, all their loads under way together
+  // the loads of several parts under way together
   float m = -INFINITY, l = 0.0f;
   f32x4_t sum[H];
 #pragma unroll
   for (int h = 0; h < H; ++h) sum[h] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-  for (int i0 = 0; i0 < r.parts; i0 += 8) {
-    float pm[8], pl[8];
-    f32x4_t v[8][H];
+  auto add = [&](int i0, auto width) {
+    constexpr int W = decltype(width)::value;
+    float pm[W], pl[W];
+    f32x4_t v[W][H];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
+    for (int k = 0; k < W; ++k) {
       const Parts<H> from(p, gqa_slot(r, wg, i0 + k < r.parts ? i0 + k : r.parts - 1));
       pm[k] = *from.max(fr);
       pl[k] = *from.div(fr);
@@ -273,7 +276,7 @@ __global__ __launch_bounds__(NT) void gqa_f32_join_kernel(GqaParams p) {
     }
     float top = m;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) top = fmaxf(top, pm[k]);
+    for (int k = 0; k < W; ++k) top = fmaxf(top, pm[k]);
     const float ref = top == -INFINITY ? 0.0f : top;
     const float keep = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m - ref) * c);
     m = top;
@@ -281,15 +284,19 @@ __global__ __launch_bounds__(NT) void gqa_f32_join_kernel(GqaParams p) {
 #pragma unroll
     for (int h = 0; h < H; ++h) sum[h] *= keep;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
+    for (int k = 0; k < W; ++k) {
       const bool none = i0 + k >= r.parts || (pm[k] == -INFINITY && pl[k] == 0.0f);
       const float a = none ? 0.0f : __builtin_amdgcn_exp2f((pm[k] - ref) * c);
       l += none ? 0.0f : pl[k] * a;
 #pragma unroll
       for (int h = 0; h < H; ++h) sum[h] += none ? f32x4_t{0, 0, 0, 0} : a * v[k][h];
     }
-  }
-  const int tok = row / p.group, head = row - tok * p.group;
+  };
+  if (r.parts <= 4) add(0, std::integral_constant<int, 4>{});
+  else if (r.parts <= 8) add(0, std::integral_constant<int, 8>{});
+  else
+    for (int i0 = 0; i0 < r.parts; i0 += 16) add(i0, std::integral_constant<int, 16>{});
+  const int tok = gqa_token(p, row), head = row - tok * p.group;
   const bool real = tok < r.used;
   const float inv = inverse(l);
   float* out = static_cast<float*>(p.out) + (size_t)(r.s0 + tok) * p.o_stride + (size_t)(r.hk * p.group + head) * D;

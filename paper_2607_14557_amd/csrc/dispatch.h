@@ -182,7 +182,7 @@ inline FewRule few_rule(const FewLaunch& g) {
 // ---- attention with grouped heads ---------------------------------------------
 
 // Rows (token, head of the group) of a workgroup: 128 that walk the keys together,
-// 32 whose keys are split over the four waves, 16 likewise (fp32).
+// 32 whose keys are split over the workgroup's waves, 16 likewise (fp32).
 constexpr int kGqaTile = 128, kGqaFew = 32, kGqaF32 = 16;
 
 struct GqaRule {
@@ -191,28 +191,105 @@ struct GqaRule {
   int grid;
 };
 
-// The form of a launch of up to `rows` rows in `batch` requests of up to `keys`
-// keys.
-inline GqaRule gqa_rule(bool bf16, int heads, int n_kv, int dim, int rows, int batch, long long keys) {
-  GqaRule r{};
-  const int group = heads / n_kv;
-  const long long pairs = (long long)rows * group;
-  r.rt = !bf16 ? kGqaF32 : (pairs / batch > 64 ? kGqaTile : kGqaFew);
-  const long long tiles = (pairs >= batch ? (pairs - batch) / r.rt + batch : pairs) * n_kv;
-  const long long blocks = (keys + 63) / 64 > 0 ? (keys + 63) / 64 : 1;
-  // workgroups that run at once on 256 CUs
-  const int wgs = r.rt == kGqaFew && dim <= 64 ? 1024 : 512;
-  // the places of the line are counted in 31 bits
-  r.cut = (r.rt != kGqaTile || tiles < wgs) && blocks <= 0x7fffffff / tiles;
-  r.grid = (int)(!r.cut ? tiles : (tiles * blocks < wgs ? tiles * blocks : wgs));
-  return r;
+struct GqaLaunch {
+  bool bf16;
+  int heads, n_kv, dim;
+  int rows, batch;       // bounds of the call
+  long long keys;        // bound on the keys of a request
+  bool half;             // a causal prompt: its tiles see half the keys on average
+};
+
+// The most tiles, over all key/value heads.
+inline long long gqa_tiles(const GqaLaunch& g, int rt) {
+  const long long pairs = (long long)g.rows * (g.heads / g.n_kv);
+  return (pairs >= g.batch ? (pairs - g.batch) / rt + g.batch : pairs) * g.n_kv;
 }
 
-// Bytes of the parts of a cut launch (their records, then two results a workgroup:
-// the sums of each row, its maximum and its divisor), for any number of keys.
-inline size_t gqa_record_bytes(const GqaRule& r) { return ((size_t)r.grid * 32 + 255) / 256 * 256; }
-inline size_t gqa_bytes(const GqaRule& r, int dim) {
-  return r.cut ? gqa_record_bytes(r) + (size_t)2 * r.grid * r.rt * ((dim > 64 ? 128 : 64) + 2) * 4 : 0;
+// Workgroups that a cut launch has: as many as run at once, but on average at most 32
+// parts a tile (the joining of 128 parts took 20 us), nor more than there are blocks.
+inline int gqa_cut_grid(const GqaLaunch& g, int rt) {
+  const int wgs = rt == kGqaFew && g.dim <= 64 ? 1024 : 512;
+  const long long blocks = (g.keys + 63) / 64 > 0 ? (g.keys + 63) / 64 : 1;
+  const long long most = gqa_tiles(g, rt) * (blocks < 32 ? blocks : 32);
+  return (int)(most < wgs ? most : wgs);
+}
+
+// Expected us of a form, the call's host time included where it is the longer: fits
+// to the measured times of each form alone (bf16: 420 calls of 1 to 256 requests, 1 to
+// 4000 rows and 15 to 40,000 keys each, rms 5 to 13% uncut, 25% cut; fp32: 201 calls,
+// rms 16 to 24%).  Uncut, a tile's keys are one walk, and the tiles run in rounds; cut,
+// all workgroups share the blocks, and a second launch joins.
+inline double gqa_us(const GqaLaunch& g, int rt, bool cut) {
+  struct Uncut { double base, first, step, round, round_step; int slots, keys; };
+  struct Cut { double base, block, tile; };
+  static constexpr Uncut kUncut[3][2] = {             // [form][head_dim > 64]
+      {{7.4, 0.0, 0.94, 1.5, 1.29, 512, 64}, {7.6, 0.7, 1.27, 5.1, 1.79, 512, 64}},
+      {{5.1, 2.3, 0.95, 4.8, 1.18, 512, 128}, {5.3, 3.0, 1.32, 6.3, 1.20, 256, 128}},
+      {{5.8, 1.2, 1.34, 2.8, 1.54, 512, 64}, {4.1, 3.3, 2.93, 7.1, 3.31, 512, 64}}};
+  static constexpr Cut kCut[3][2] = {
+      {{15.3, 1.23, 1.6}, {16.9, 1.93, 4.7}},
+      {{15.1, 1.23, 0.0}, {15.4, 1.34, 2.4}},
+      {{11.3, 1.59, 0.0}, {11.1, 3.02, 4.2}}};
+  const int form = rt == kGqaTile ? 0 : (rt == kGqaFew ? 1 : 2), big = g.dim > 64;
+  const double tiles = (double)gqa_tiles(g, rt);
+  // of packed rows the host knows the sum alone: no request is taken for longer than twice the average
+  double keys = (double)g.keys;
+  if (g.half && keys > 2.0 * g.rows / g.batch) keys = 2.0 * g.rows / g.batch;
+  // what all tiles see together, by the bound: a causal prompt's half; the pages that a table has
+  // room for are seldom all in use (64 requests of 500 to 16,000 keys: 115 us cut, 192 uncut)
+  const double some = g.half ? 0.5 : 0.6;
+  if (!cut) {
+    const Uncut& c = kUncut[form][big];
+    const double steps = keys / c.keys, one = c.first + c.step * steps;
+    const double all = tiles / c.slots * (c.round + c.round_step * steps * some);
+    return c.base + (one > all ? one : all);
+  }
+  const Cut& c = kCut[form][big];
+  const double slots = rt == kGqaFew && !big ? 1024 : 512, share = tiles * keys / 64 / slots * (g.half ? 1.0 : some);
+  return c.base + c.block * (share > 1.0 ? share : 1.0) + c.tile * tiles / slots;
+}
+
+inline GqaRule gqa_rule(const GqaLaunch& g) {
+  GqaRule best{};
+  double least = 0.0;
+  const int forms[2] = {g.bf16 ? kGqaFew : kGqaF32, kGqaTile};
+  for (int f = 0; f < (g.bf16 ? 2 : 1); ++f) {
+    const int rt = forms[f];
+    const long long tiles = gqa_tiles(g, rt), blocks = (g.keys + 63) / 64;
+    for (int cut = 0; cut < 2; ++cut) {
+      // the places of the line are counted in 31 bits; 128-row parts are for more than 32 rows a request
+      if (cut && (blocks > 0x7fffffff / tiles ||
+                  (rt == kGqaTile && (long long)g.rows * (g.heads / g.n_kv) <= 32ll * g.batch)))
+        continue;
+      const double us = gqa_us(g, rt, cut);
+      if (best.rt == 0 || us < least) {
+        best.rt = rt;
+        best.cut = cut;
+        best.grid = cut ? gqa_cut_grid(g, rt) : (int)tiles;
+        least = us;
+      }
+    }
+  }
+  return best;
+}
+
+// Bytes of the parts of a cut launch: their records, then two results a workgroup (the
+// sums of each row, its maximum and its divisor).
+inline size_t gqa_record_bytes(int grid) { return ((size_t)grid * 32 + 255) / 256 * 256; }
+inline size_t gqa_part_bytes(int grid, int rt, int dim) {
+  return gqa_record_bytes(grid) + (size_t)2 * grid * rt * ((dim > 64 ? 128 : 64) + 2) * 4;
+}
+
+// The most that any launch with these rows and requests needs, whatever its keys and mask.
+inline size_t gqa_workspace(GqaLaunch g) {
+  g.keys = 1 << 20;
+  const int few = g.bf16 ? kGqaFew : kGqaF32;
+  size_t most = gqa_part_bytes(gqa_cut_grid(g, few), few, g.dim);
+  if (g.bf16 && (long long)g.rows * (g.heads / g.n_kv) > 32ll * g.batch) {
+    const size_t tile = gqa_part_bytes(gqa_cut_grid(g, kGqaTile), kGqaTile, g.dim);
+    most = tile > most ? tile : most;
+  }
+  return most;
 }
 
 }  // namespace seer

@@ -18,6 +18,12 @@ constexpr int kGqaBlock = 64;
 // fastest: row i is token i / G, head i % G.  A tile is RT such rows, so K and V
 // are read once for all the query heads that share them, whatever G is.
 
+// x / group, x below 2^31, without a division: the host's p.group_mul is
+// floor(2^32 (2^shift - group) / group) + 1 for the shift with 2^shift >= group.
+__device__ __forceinline__ int gqa_token(const GqaParams& p, int x) {
+  return (int)((__umulhi((unsigned)x, p.group_mul) + (unsigned)x) >> p.group_shift);
+}
+
 // A request of the call.
 struct GqaSeq {
   int s0, len, used;       // first row, rows, real rows
@@ -54,7 +60,7 @@ template <int RT>
 __device__ __forceinline__ int gqa_tile_end(const GqaParams& p, const GqaSeq& s, int t) {
   if (s.used == 0) return 0;
   if (p.mask != kMaskCausal) return s.nk;
-  int last = ((t + 1) * RT - 1) / p.group;                 // last token of the tile
+  int last = gqa_token(p, (t + 1) * RT - 1);               // last token of the tile
   last = last < s.used ? last : s.used - 1;
   const int end = s.past + last + 1;
   return end < 0 ? 0 : (end < s.nk ? end : s.nk);
@@ -91,7 +97,6 @@ struct GqaCut {
     int sums[NW];
     int first[NT + 1];           // of each thread's stretch of a head's line
     GqaSeq seq[NT];              // of each thread's only request
-    int found[12];
   };
   Shared& sh;
   int n, all;                    // length of a head's line, and of the whole
@@ -162,39 +167,59 @@ struct GqaCut {
     x = x0;
   }
 
-  // The next piece of the workgroup's stretch; false at its end.
+  // The next piece of the workgroup's stretch; false at its end.  Every wave looks
+  // for itself.
   __device__ __forceinline__ bool next(const GqaParams& p, GqaUnit& u) {
     if (x >= x1) return false;
-    const int tid = threadIdx.x;
+    const int lane = threadIdx.x & (kWave - 1);
+    const int per = (p.B + NT - 1) / NT;
     u.hk = (unsigned)x / (unsigned)n;
     const int j = x - u.hk * n;
     __syncthreads();               // the line is written, and the last piece's reads of LDS are done
-    if (j >= sh.first[tid] && j < sh.first[tid + 1]) {
-      const int per = (p.B + NT - 1) / NT;
-      int b = tid * per, at = sh.first[tid];
-      GqaSeq s;
-      if (per == 1) {
-        s = sh.seq[tid];
-      } else {
-        for (;; ++b) {
-          s = gqa_seq<RT>(p, b);
-          const int m = weight(p, s);
-          if (j < at + m) break;
-          at += m;
-        }
-      }
-      sh.found[0] = b; sh.found[1] = j - at; sh.found[2] = s.tiles;
-      sh.found[3] = s.s0; sh.found[4] = s.len; sh.found[5] = s.used; sh.found[6] = s.nk; sh.found[7] = s.past;
-      sh.found[8] = s.rows;
+    int f = 0;                     // the thread whose stretch has place j
+#pragma unroll
+    for (int c = 0; c < NT; c += kWave) {
+      const unsigned long long hit = __ballot(j >= sh.first[c + lane] && j < sh.first[c + lane + 1]);
+      if (hit) f = c + __builtin_ctzll(hit);
     }
-    __syncthreads();
-    auto get = [&](int i) { return __builtin_amdgcn_readfirstlane(sh.found[i]); };
-    u.b = get(0);
-    const int rem = get(1);
-    u.s.tiles = get(2); u.s.s0 = get(3); u.s.len = get(4); u.s.used = get(5); u.s.nk = get(6); u.s.past = get(7);
-    u.s.rows = get(8);
+    int at = sh.first[f];
+    u.b = f;
+    GqaSeq s;
+    if (per == 1) {
+      s = sh.seq[f];
+    } else {
+      // the thread's requests, one a lane
+      for (int i0 = 0; i0 < per; i0 += kWave) {
+        const int b = f * per + i0 + lane;
+        GqaSeq mine{};
+        if (i0 + lane < per && b < p.B) mine = gqa_seq<RT>(p, b);
+        const int m = weight(p, mine);
+        int inc = m;
+#pragma unroll
+        for (int off = 1; off < kWave; off <<= 1) {
+          const int v = __shfl_up(inc, off, kWave);
+          if (lane >= off) inc += v;
+        }
+        const unsigned long long hit = __ballot(j >= at + inc - m && j < at + inc);
+        if (hit) {
+          const int l = __builtin_ctzll(hit);
+          auto of = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
+          u.b = f * per + i0 + l;
+          at += of(inc - m);
+          s.s0 = of(mine.s0); s.len = of(mine.len); s.used = of(mine.used); s.nk = of(mine.nk); s.past = of(mine.past);
+          s.rows = of(mine.rows); s.tiles = of(mine.tiles);
+          break;
+        }
+        at += __builtin_amdgcn_readlane(inc, kWave - 1);
+      }
+    }
+    auto uni = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+    u.b = uni(u.b);
+    const int rem = uni(j - at);
+    u.s.tiles = uni(s.tiles); u.s.s0 = uni(s.s0); u.s.len = uni(s.len); u.s.used = uni(s.used); u.s.nk = uni(s.nk);
+    u.s.past = uni(s.past); u.s.rows = uni(s.rows);
     const int nb = p.cut ? gqa_blocks(u.s.nk) : 1;
-    const int tile = (unsigned)rem / (unsigned)nb, block = rem - tile * nb;
+    const int tile = p.cut ? (int)((unsigned)rem / (unsigned)nb) : rem, block = p.cut ? rem - tile * nb : 0;
     // the tiles of a causal prompt from the last, which has the most keys, to the first
     u.t = u.s.tiles - 1 - tile;
     const int end = gqa_tile_end<RT>(p, u.s, u.t);
@@ -210,7 +235,7 @@ struct GqaCut {
       u.lo = lo < end ? (int)lo : end;
       u.hi = hi < end ? (int)hi : end;
       u.slot = 2 * wg + (x == x0 ? 0 : 1);
-      if (tid == 0 && x + take >= x1) {
+      if (threadIdx.x == 0 && x + take >= x1) {
         // the last piece: where it opens a tile that goes on, the tile's record
         GqaRecord r{};
         if (block == 0 && take < nb)

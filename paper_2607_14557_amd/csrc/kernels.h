@@ -339,7 +339,9 @@ struct GqaParams {
   int B;
   int rows_ub;
   int n_heads, n_kv, head_dim;
-  int group;                   // n_heads / n_kv
+  int group;                   // n_heads / n_kv, and what divides by it (gqa_token)
+  unsigned group_mul;
+  int group_shift;
   float scale;
   int mask;                    // kMask*
   bool bf16, v_f16;

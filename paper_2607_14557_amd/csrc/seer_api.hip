@@ -773,16 +773,17 @@ int seer_kv_store(const seer_attn_desc* desc, const seer_page_desc* pages, const
   return ok();
 }
 
+static seer::GqaLaunch gqa_launch(const seer_attn_desc* d, int32_t rows_ub, int32_t batch) {
+  return seer::GqaLaunch{d->dtype == SEER_DTYPE_BF16, d->n_heads, d->n_kv_heads, d->head_dim, rows_ub, batch, 0, false};
+}
+
 size_t seer_attn_workspace_bytes(const seer_attn_desc* desc, int32_t rows_ub, int32_t batch) {
   if (check_heads(desc) != SEER_OK) return 0;
   if (rows_ub < 1 || batch < 1 || (long long)rows_ub * desc->n_heads >= (1ll << 31)) {
     fail(SEER_EINVAL, "rows_ub and batch must be positive, rows_ub * n_heads below 2^31");
     return 0;
   }
-  // keys enough for the largest grid
-  const seer::GqaRule r = seer::gqa_rule(desc->dtype == SEER_DTYPE_BF16, desc->n_heads, desc->n_kv_heads,
-                                         desc->head_dim, rows_ub, batch, 1 << 16);
-  return 256 + up256(seer::gqa_bytes(r, desc->head_dim));
+  return 256 + up256(seer::gqa_workspace(gqa_launch(desc, rows_ub, batch)));
 }
 
 // what both attention calls check and fill in
@@ -810,16 +811,20 @@ static int gqa_params(seer::GqaParams& p, const seer_attn_desc* desc, int32_t ma
   p.scale = desc->scale != 0.0f ? desc->scale : 1.0f / sqrtf((float)desc->head_dim);
   p.mask = mask; p.bf16 = desc->dtype == SEER_DTYPE_BF16; p.v_f16 = (desc->flags & SEER_ATTN_V_F16) != 0;
   p.group = p.n_heads / p.n_kv;
+  while ((1ll << p.group_shift) < p.group) ++p.group_shift;
+  p.group_mul = (unsigned)((((1ull << p.group_shift) - p.group) << 32) / p.group + 1);
   p.records = workspace;
   return SEER_OK;
 }
 
-static int launch_gqa(seer::GqaParams& p, hipStream_t stream) {
-  const seer::GqaRule r = seer::gqa_rule(p.bf16, p.n_heads, p.n_kv, p.head_dim, p.rows_ub, p.B,
-                                         p.table ? (long long)p.width << p.shift : p.rows_ub);
+static int launch_gqa(seer::GqaParams& p, const seer_attn_desc* desc, hipStream_t stream) {
+  seer::GqaLaunch g = gqa_launch(desc, p.rows_ub, p.B);
+  g.keys = p.table ? (long long)p.width << p.shift : p.rows_ub;
+  g.half = !p.table && p.mask == SEER_MASK_CAUSAL;
+  const seer::GqaRule r = seer::gqa_rule(g);
   p.cut = r.cut;
   p.wgs = r.grid;
-  p.partial = reinterpret_cast<float*>(static_cast<uint8_t*>(p.records) + seer::gqa_record_bytes(r));
+  p.partial = reinterpret_cast<float*>(static_cast<uint8_t*>(p.records) + seer::gqa_record_bytes(r.grid));
   return p.bf16 ? seer::launch_gqa_bf16(p, r, stream) : seer::launch_gqa_f32(p, r, stream);
 }
 
@@ -837,7 +842,7 @@ int seer_attn_prompt(const seer_attn_desc* desc, int32_t mask, const void* q, in
   if ((rc = check_rows("k", k, k_stride, width, es)) || (rc = check_rows("v", v, v_stride, width, es))) return rc;
   if (out == k || out == v) return fail(SEER_EINVAL, "out may not alias an input");
   p.k = k; p.v = v; p.k_stride = k_stride; p.v_stride = v_stride;
-  if (launch_gqa(p, stream)) return hip_fail("prompt attention launch");
+  if (launch_gqa(p, desc, stream)) return hip_fail("prompt attention launch");
   return ok();
 }
 
@@ -860,7 +865,7 @@ int seer_attn_paged(const seer_attn_desc* desc, const seer_page_desc* pages, int
   p.k = pool; p.v = pool; p.table = table; p.kv_len = kv_len;
   p.shift = page_shift(pages); p.n_pages = pages->n_pages; p.width = pages->table_width;
   p.bits = reinterpret_cast<const unsigned long long*>(tree_bits); p.words = tree_words;
-  if (launch_gqa(p, stream)) return hip_fail("paged attention launch");
+  if (launch_gqa(p, desc, stream)) return hip_fail("paged attention launch");
   return ok();
 }
 
