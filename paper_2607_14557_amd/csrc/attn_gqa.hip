@@ -368,13 +368,13 @@ __global__ __launch_bounds__(NT, 2) void gqa_tile_kernel(GqaParams p) {
   __shared__ __attribute__((aligned(1024))) uint8_t k_lds1[64 * ROW];
   __shared__ __attribute__((aligned(1024))) uint8_t v_lds0[64 * ROW];
   __shared__ __attribute__((aligned(1024))) uint8_t v_lds1[64 * ROW];
-  __shared__ int odd_from;                   // the first tile that had values to sweep
+  __shared__ int odd_at[2];                  // the first tile that had values to sweep; pieces alternate
   __shared__ typename GqaCut<kGqaTile, NT>::Shared cut_lds;
+  if (threadIdx.x < 2) odd_at[threadIdx.x] = INT_MAX;
   GqaCut<kGqaTile, NT> cut(p, cut_lds);
   GqaUnit u;
-  while (cut.next(p, u)) {
-  if (threadIdx.x == 0) odd_from = INT_MAX;
-  __syncthreads();
+  for (int turn = 0; cut.next(p, u); turn ^= 1) {
+  if (threadIdx.x == 0) odd_at[turn ^ 1] = INT_MAX;
   const int lane = threadIdx.x & 63;
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int fr = lane & 31, fhalf = lane >> 5;
@@ -427,7 +427,7 @@ __global__ __launch_bounds__(NT, 2) void gqa_tile_kernel(GqaParams p) {
   auto check = [&](int kbase, auto buf, unsigned long long lost) {
     constexpr int B = decltype(buf)::value;
     if (kbase + 64 <= open_all && lost == 0) return;
-    if (sweep<VF16, 16 * ROW>((B ? v_lds1 : v_lds0) + 16 * wv * ROW, lane) && lane == 0) atomicMin(&odd_from, kbase);
+    if (sweep<VF16, 16 * ROW>((B ? v_lds1 : v_lds0) + 16 * wv * ROW, lane) && lane == 0) atomicMin(&odd_at[turn], kbase);
   };
   if (n > 0) {
     pages(u.lo);
@@ -472,7 +472,7 @@ __global__ __launch_bounds__(NT, 2) void gqa_tile_kernel(GqaParams p) {
   for (int i = 0; i < DT * 4; ++i)
 #pragma unroll
     for (int e = 0; e < 4; ++e) sum[i][e] = w.o[i >> 2][4 * (i & 3) + e];
-  const int odd = __builtin_amdgcn_readfirstlane(odd_from);
+  const int odd = __builtin_amdgcn_readfirstlane(odd_at[turn]);
   if (odd < u.hi) {
 #pragma unroll 1
     for (int i = 0; i < DT * 4; ++i) {

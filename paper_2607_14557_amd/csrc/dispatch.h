@@ -189,6 +189,7 @@ struct GqaRule {
   int rt;                // rows of a tile
   bool cut;              // whether the tiles' keys are cut, over `grid` workgroups
   int grid;
+  bool sort;             // several rounds of 128-row tiles: the longest requests first (up to 64)
 };
 
 struct GqaLaunch {
@@ -198,6 +199,18 @@ struct GqaLaunch {
   long long keys;        // bound on the keys of a request
   bool half;             // a causal prompt: its tiles see half the keys on average
 };
+
+// x / d for x below 2^31 is (mulhi(x, mul) + x) >> shift.
+struct GqaDivisor {
+  unsigned mul;
+  int shift;
+};
+inline GqaDivisor gqa_divisor(int d) {
+  GqaDivisor r{0, 0};
+  while ((1ll << r.shift) < d) ++r.shift;
+  r.mul = (unsigned)((((1ull << r.shift) - d) << 32) / d + 1);
+  return r;
+}
 
 // The most tiles, over all key/value heads.
 inline long long gqa_tiles(const GqaLaunch& g, int rt) {
@@ -266,6 +279,7 @@ inline GqaRule gqa_rule(const GqaLaunch& g) {
         best.rt = rt;
         best.cut = cut;
         best.grid = cut ? gqa_cut_grid(g, rt) : (int)tiles;
+        best.sort = !cut && rt == kGqaTile && g.batch > 1 && g.batch <= 64 && tiles > 512;
         least = us;
       }
     }

@@ -18,8 +18,7 @@ constexpr int kGqaBlock = 64;
 // fastest: row i is token i / G, head i % G.  A tile is RT such rows, so K and V
 // are read once for all the query heads that share them, whatever G is.
 
-// x / group, x below 2^31, without a division: the host's p.group_mul is
-// floor(2^32 (2^shift - group) / group) + 1 for the shift with 2^shift >= group.
+// x / group without a division (gqa_divisor).
 __device__ __forceinline__ int gqa_token(const GqaParams& p, int x) {
   return (int)((__umulhi((unsigned)x, p.group_mul) + (unsigned)x) >> p.group_shift);
 }
@@ -87,7 +86,10 @@ struct GqaRecord {
 //              takes an equal stretch of it, whatever the requests' lengths: no
 //              workgroup waits for another, and none starts after the others.  A tile
 //              that lies in several stretches is joined by a second launch.
-//   otherwise: a workgroup for each tile.
+//   otherwise: a workgroup for each tile, request after request (p.sort: the ones with
+//              the most keys first, so that no long walk starts at the end), in each all heads, in each the tiles from the last, which sees the most,
+//              to the first.  An XCD has heads of its own where their number allows
+//              it, so that a head's keys are in one L2.
 // Every workgroup sums the requests' lengths for itself (each thread its share of
 // the requests, then a scan); with at most one request a thread they are read once.
 template <int RT, int NT>
@@ -96,13 +98,15 @@ struct GqaCut {
   struct Shared {
     int sums[NW];
     int first[NT + 1];           // of each thread's stretch of a head's line
-    GqaSeq seq[NT];              // of each thread's only request
+    GqaSeq seq[NT];              // of each thread's only request, and its index
+    int id[NT];
   };
   Shared& sh;
   int n, all;                    // length of a head's line, and of the whole
   int wgs, each, more;           // workgroups with work: `more` of them take each + 1, the others each
   int x, x0, x1;                 // the next place, and the workgroup's stretch
   int wg;
+  int heads, head0;              // uncut: the heads of this workgroup's XCD
 
   __device__ __forceinline__ static int weight(const GqaParams& p, const GqaSeq& s) {
     return s.tiles * (p.cut ? gqa_blocks(s.nk) : 1);
@@ -120,10 +124,25 @@ struct GqaCut {
     const int b0 = tid * per < p.B ? tid * per : p.B;
     const int b1 = b0 + per < p.B ? b0 + per : p.B;
     int own = 0;
-    for (int b = b0; b < b1; ++b) {
-      const GqaSeq s = gqa_seq<RT>(p, b);
-      own += weight(p, s);
-      if (per == 1) sh.seq[tid] = s;
+    if (per == 1) {
+      GqaSeq s{};
+      if (tid < p.B) s = gqa_seq<RT>(p, tid);
+      own = weight(p, s);
+      int at = tid;
+      if (p.sort && wave == 0) {
+        // the request's rank by its keys
+        int rank = 0;
+        for (int k = 0; k < p.B; ++k) {
+          const int nk = __builtin_amdgcn_readlane(s.nk, k);
+          rank += nk > s.nk || (nk == s.nk && k < lane);
+        }
+        if (tid < p.B) at = rank;
+        own = __builtin_amdgcn_ds_permute(at * 4, own);
+      }
+      sh.seq[at] = s;
+      sh.id[at] = tid;
+    } else {
+      for (int b = b0; b < b1; ++b) own += weight(p, gqa_seq<RT>(p, b));
     }
     int inc = own;
 #pragma unroll
@@ -155,13 +174,24 @@ struct GqaCut {
       more = all - each * wgs;
     }
     x0 = x1 = 0;
-    if (bid < wgs) {
+    heads = p.n_kv;
+    head0 = 0;
+    if (!p.cut) {
+      int i = bid;
+      if (p.n_kv % 8 == 0) {
+        heads = p.n_kv / 8;
+        head0 = (bid & 7) * heads;
+        i = bid >> 3;
+      }
+      x0 = i;
+      x1 = i < n * heads ? i + 1 : i;
+    } else if (bid < wgs) {
       // each XCD takes a contiguous part of the line: the tiles of one request and
       // head find their keys in its L2
       wg = xcd_remap(bid, wgs);
       x0 = start(wg);
       x1 = start(wg + 1);
-    } else if (p.cut && tid == 0) {
+    } else if (tid == 0) {
       static_cast<GqaRecord*>(p.records)[bid].parts = 0;
     }
     x = x0;
@@ -173,8 +203,9 @@ struct GqaCut {
     if (x >= x1) return false;
     const int lane = threadIdx.x & (kWave - 1);
     const int per = (p.B + NT - 1) / NT;
-    u.hk = (unsigned)x / (unsigned)n;
-    const int j = x - u.hk * n;
+    // cut: head after head; otherwise: the requests' tiles times the heads
+    const int q = (unsigned)x / (unsigned)(p.cut ? n : heads);
+    const int j = p.cut ? x - q * n : q;
     __syncthreads();               // the line is written, and the last piece's reads of LDS are done
     int f = 0;                     // the thread whose stretch has place j
 #pragma unroll
@@ -187,6 +218,7 @@ struct GqaCut {
     GqaSeq s;
     if (per == 1) {
       s = sh.seq[f];
+      u.b = sh.id[f];
     } else {
       // the thread's requests, one a lane
       for (int i0 = 0; i0 < per; i0 += kWave) {
@@ -215,11 +247,13 @@ struct GqaCut {
     }
     auto uni = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
     u.b = uni(u.b);
-    const int rem = uni(j - at);
+    const int rem = uni(p.cut ? j - at : x - at * heads);
     u.s.tiles = uni(s.tiles); u.s.s0 = uni(s.s0); u.s.len = uni(s.len); u.s.used = uni(s.used); u.s.nk = uni(s.nk);
     u.s.past = uni(s.past); u.s.rows = uni(s.rows);
-    const int nb = p.cut ? gqa_blocks(u.s.nk) : 1;
-    const int tile = p.cut ? (int)((unsigned)rem / (unsigned)nb) : rem, block = p.cut ? rem - tile * nb : 0;
+    const int nb = gqa_blocks(u.s.nk), line = p.cut ? nb : u.s.tiles;
+    const int quot = (unsigned)rem / (unsigned)line, left = rem - quot * line;
+    u.hk = p.cut ? q : head0 + quot;
+    const int tile = p.cut ? quot : left, block = p.cut ? left : 0;
     // the tiles of a causal prompt from the last, which has the most keys, to the first
     u.t = u.s.tiles - 1 - tile;
     const int end = gqa_tile_end<RT>(p, u.s, u.t);

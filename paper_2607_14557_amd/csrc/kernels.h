@@ -354,6 +354,7 @@ struct GqaParams {
   // workgroups, and the records and results of the parts
   bool cut;
   int wgs;
+  bool sort;                   // the requests by their keys (uncut, at most 64 of them)
   void* records;
   float* partial;
 };

@@ -811,8 +811,9 @@ static int gqa_params(seer::GqaParams& p, const seer_attn_desc* desc, int32_t ma
   p.scale = desc->scale != 0.0f ? desc->scale : 1.0f / sqrtf((float)desc->head_dim);
   p.mask = mask; p.bf16 = desc->dtype == SEER_DTYPE_BF16; p.v_f16 = (desc->flags & SEER_ATTN_V_F16) != 0;
   p.group = p.n_heads / p.n_kv;
-  while ((1ll << p.group_shift) < p.group) ++p.group_shift;
-  p.group_mul = (unsigned)((((1ull << p.group_shift) - p.group) << 32) / p.group + 1);
+  const seer::GqaDivisor div = seer::gqa_divisor(p.group);
+  p.group_mul = div.mul;
+  p.group_shift = div.shift;
   p.records = workspace;
   return SEER_OK;
 }
@@ -824,6 +825,7 @@ static int launch_gqa(seer::GqaParams& p, const seer_attn_desc* desc, hipStream_
   const seer::GqaRule r = seer::gqa_rule(g);
   p.cut = r.cut;
   p.wgs = r.grid;
+  p.sort = r.sort;
   p.partial = reinterpret_cast<float*>(static_cast<uint8_t*>(p.records) + seer::gqa_record_bytes(r.grid));
   return p.bf16 ? seer::launch_gqa_bf16(p, r, stream) : seer::launch_gqa_f32(p, r, stream);
 }

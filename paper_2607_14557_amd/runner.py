@@ -199,6 +199,112 @@ class SyntheticSampler:
                            x0, self.emb, self.vocab, x_next, stream=stream)
 
 
+class PagedCache:
+    """Keys and values of up to max_batch requests in pages, one pool per layer
+    with one table for all: what seer_page_plan, seer_kv_store, seer_attn_paged
+    and seer_attn_prompt work on.  A step of a program is
+
+        slots = cache.plan(cu, rows_ub, keep)      # pages taken and given back
+        for each layer:
+            cache.store(layer, k, v, rows_ub, slots)
+            cache.attend(layer, q, out, cu, rows_ub, mask)
+
+    with the rows of request b at [cu[b], cu[b+1]) (none for a place that is
+    not in use).  keep[b]: tokens of the request that stay from earlier steps
+    (None: all), fewer where a window was cut or drafts were refused, 0 where
+    the request has ended.  Lengths and free pages stay on the device; each plan
+    reads one of two buffers and writes the other, so a recorded sequence has an
+    even number of plans."""
+
+    def __init__(self, n_heads, n_kv_heads, head_dim, n_layers, n_pages, page_size, max_batch, max_len, max_rows,
+                 dtype="bf16", v_f16=False, scale=0.0, device="cuda"):
+        S.load_library()
+        self.desc = S.seer_attn_desc(n_heads, n_kv_heads, head_dim,
+                                     S.SEER_DTYPE_BF16 if dtype == "bf16" else S.SEER_DTYPE_F32,
+                                     S.SEER_ATTN_V_F16 if v_f16 else 0, scale)
+        width = -(-int(max_len) // int(page_size))
+        self.pages = S.seer_page_desc(page_size, n_pages, width)
+        nbytes = S.seer_page_pool_bytes(self.desc, self.pages)
+        self.ws_bytes = S.seer_attn_workspace_bytes(self.desc, max_rows, max_batch)
+        if nbytes == 0 or self.ws_bytes == 0:
+            raise S.SeerError(S.SEER_EUNSUPPORTED, S.seer_last_error())
+        self.max_batch, self.max_rows = int(max_batch), int(max_rows)
+        kind = torch_dtype(dtype)
+        shape = (n_pages, 2, n_kv_heads, page_size, head_dim)
+        self.pools = [torch.zeros(shape, dtype=kind, device=device) for _ in range(n_layers)]
+        i32 = lambda *s: torch.zeros(*s, dtype=torch.int32, device=device)
+        self.table = i32(max_batch, width)
+        # page 0 is the first one taken
+        self.free_pages = torch.arange(n_pages - 1, -1, -1, dtype=torch.int32, device=device)
+        self._free = [torch.full((1,), n_pages, dtype=torch.int32, device=device), i32(1)]
+        self._lens = [i32(max_batch), i32(max_batch)]
+        self.slots = i32(max_rows)
+        self.status = i32(1)
+        self.workspace = torch.empty(self.ws_bytes, dtype=torch.uint8, device=device)
+
+    @property
+    def lens(self):
+        """[max_batch] int32: the tokens that each request has in the cache."""
+        return self._lens[0]
+
+    @property
+    def free(self):
+        """[1] int32: the number of free pages."""
+        return self._free[0]
+
+    def plan(self, cu, rows_ub, keep=None, seqused=None, stream=None):
+        """The pages and slots of a step; returns the slots of its rows."""
+        if rows_ub > self.max_rows:
+            raise ValueError("rows_ub %d exceeds max_rows %d" % (rows_ub, self.max_rows))
+        held = self._lens[0]
+        S.seer_page_plan(self.pages, held, held if keep is None else keep, cu, seqused, self.max_batch, rows_ub,
+                         self.free_pages, self._free[0], self._free[1], self.table, self._lens[1], self.slots,
+                         self.status, stream=stream)
+        self._lens.reverse()
+        self._free.reverse()
+        return self.slots
+
+    def check(self, stream=None):
+        """Raise SeerError if the last plan was refused; waits for `stream`."""
+        (stream or torch.cuda.current_stream(self.status.device)).synchronize()
+        st = int(self.status.item())
+        if st:
+            why = [n for bit, n in ((S.SEER_PAGES_EXHAUSTED, "not enough free pages"),
+                                    (S.SEER_PAGES_WIDTH, "a request longer than max_len"),
+                                    (S.SEER_PAGES_INVALID, "keep exceeds what a request holds")) if st & bit]
+            raise S.SeerError(S.SEER_EWORKSPACE, "; ".join(why))
+
+    def store(self, layer, k, v, rows_ub, slots=None, stream=None):
+        """Rows of k and v ([rows, n_kv_heads * head_dim], any row stride) into the layer's pages."""
+        S.seer_kv_store(self.desc, self.pages, k, k.stride(0), v, v.stride(0), rows_ub,
+                        self.slots if slots is None else slots, self.pools[layer], stream=stream)
+
+    def store_layer(self, layer, stack, rows_ub, slots=None, stream=None):
+        """The K | V columns that the stack's last layer call left in its
+        workspace (made with the same rows_ub) into the layer's pages: the paged
+        counterpart of seer_kv_export.  A bf16 layer leaves V in fp16, so the
+        cache has to have v_f16."""
+        d, bf16 = stack.dims.d_model, stack.dtype == torch.bfloat16
+        flags = S.SEER_ATTN_V_F16 if bf16 else 0
+        if (self.desc.n_kv_heads * self.desc.head_dim, self.desc.dtype, self.desc.flags) != (d, stack.dims.dtype, flags):
+            raise ValueError("the cache's heads and types are not those of the layer's rows")
+        es = 2 if bf16 else 4
+        k = stack.workspace.data_ptr() + S.seer_layer_workspace_offsets(stack.dims, rows_ub)[0] + d * es
+        S.seer_kv_store(self.desc, self.pages, k, 3 * d, k + d * es, 3 * d, rows_ub,
+                        self.slots if slots is None else slots, self.pools[layer], stream=stream)
+
+    def attend(self, layer, q, out, cu, rows_ub, mask=S.SEER_MASK_CAUSAL, tree_bits=None, seqused=None, stream=None):
+        """Attention of the step's rows over their requests' pages."""
+        S.seer_attn_paged(self.desc, self.pages, mask, q, q.stride(0), out, out.stride(0), rows_ub, cu, seqused,
+                          self.max_batch, self.pools[layer], self.table, self._lens[0], tree_bits,
+                          0 if tree_bits is None else tree_bits.shape[1], self.workspace, self.ws_bytes, stream=stream)
+
+    def prompt(self, q, k, v, out, cu, rows_ub, mask=S.SEER_MASK_CAUSAL, seqused=None, stream=None):
+        """Attention of packed prompts over their own rows (no pages)."""
+        S.seer_attn_prompt(self.desc, mask, q, q.stride(0), k, k.stride(0), v, v.stride(0), out, out.stride(0),
+                           rows_ub, cu, seqused, self.max_batch, self.workspace, self.ws_bytes, stream=stream)
+
+
 class SeerStack:
     """A stack of prepacked layers plus the scratch the ABI calls need."""
 
