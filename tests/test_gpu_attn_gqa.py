@@ -459,3 +459,12 @@ def test_on_another_stream_and_recorded(S, kind):
         assert host(a.out).tobytes() == host(ref["a"]).tobytes()
     ga.close()
     gb.close()
+
+
+@pytest.mark.parametrize("kind,H,KV,mask", [("bf16", 32, 32, "causal"), ("v16", 14, 7, "causal"), ("bf16", 32, 8, "none")])
+def test_several_rounds_of_tiles(S, kind, H, KV, mask):
+    """More tiles of 128 rows than run at once: the requests by their length, ties, empty ones, a request of 65 and more."""
+    lens = [700, 0, 300, 300, 129, 1, 1300, 640] if KV == 32 else [900, 2100, 0, 1500, 64, 2100, 128, 1, 777, 3000]
+    p = Prompt(S, kind, H, KV, 128, lens)
+    p.run(S.SEER_MASK_CAUSAL if mask == "causal" else S.SEER_MASK_NONE)
+    p.check(mask, rows=[0, 127, 128, 299, 640, 1299, 2099])
