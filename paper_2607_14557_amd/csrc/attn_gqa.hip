@@ -218,10 +218,11 @@ struct Rows32 {
     // instruction takes them, and their sum in fp32, over the rounded values where
     // they are coarse, so that the weights add up to one.
     u32x4_t pf[2 * NI], pl[FINE ? 2 * NI : 1];
-    const float floor = masked ? 0.0f : 7.5e-37f;         // (FINE) 2^-120
     float lsum;
     auto probs = [&](float ref) {
-      const float mc = ref * c;
+      // fp16: all 2^10 times as large, so that those down to 2^-24 of the reference are
+      // normal numbers (it goes with the division by their sum)
+      const float mc = VF16 ? ref * c - 10.0f : ref * c;
       lsum = 0.0f;
 #pragma unroll
       for (int sl = 0; sl < 2 * NI; ++sl)
@@ -234,13 +235,13 @@ struct Rows32 {
             lsum = __builtin_amdgcn_fdot2(h, f16x2_t{(_Float16)1.0f, (_Float16)1.0f}, lsum, false);
             pf[sl][e] = __builtin_bit_cast(uint32_t, h);
           } else if constexpr (FINE) {
-            // the upper halves as they are, so that what is left is not negative; it is
-            // kept above zero, as an infinite value times zero would be none
+            // the upper halves as they are, so that what is left is not negative; 2^-20 of
+            // the whole keeps it above zero, as an infinite value times zero would be none
             const uint32_t b0 = __float_as_uint(p0), b1 = __float_as_uint(p1);
             lsum += p0 + p1;
             pf[sl][e] = __builtin_amdgcn_perm(b1, b0, 0x07060302u);
-            pl[sl][e] = pack_bf2(fmaxf(p0 - __uint_as_float(b0 & 0xffff0000u), floor),
-                                 fmaxf(p1 - __uint_as_float(b1 & 0xffff0000u), floor));
+            pl[sl][e] = pack_bf2(__builtin_fmaf(p0, 1.0f + 0x1p-20f, -__uint_as_float(b0 & 0xffff0000u)),
+                                 __builtin_fmaf(p1, 1.0f + 0x1p-20f, -__uint_as_float(b1 & 0xffff0000u)));
           } else {
             const bf16x2_t h = __builtin_convertvector(f32x2_t{p0, p1}, bf16x2_t);
             lsum = __builtin_amdgcn_fdot2_f32_bf16(h, bf16x2_t{(__bf16)1.0f, (__bf16)1.0f}, lsum, false);
@@ -249,8 +250,8 @@ struct Rows32 {
         }
     };
     // The reference is the maximum of the first tile in which the row sees a key,
-    // and moves only where a later tile's probabilities pass 2^16 (fp16's range;
-    // with bf16 it keeps the sums far from fp32's): any reference gives the same
+    // and moves only where a later tile's probabilities pass fp16's range (2^6 of the
+    // reference; with bf16 2^16, far from the end of fp32's): any reference gives the same
     // softmax, and the common tile takes no maximum.  While a row has seen no key
     // its reference is -inf, and the NaN or infinity that this gives (-inf + inf,
     // x + inf) asks for the tile's maximum too.

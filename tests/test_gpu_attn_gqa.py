@@ -468,3 +468,40 @@ def test_several_rounds_of_tiles(S, kind, H, KV, mask):
     p = Prompt(S, kind, H, KV, 128, lens)
     p.run(S.SEER_MASK_CAUSAL if mask == "causal" else S.SEER_MASK_NONE)
     p.check(mask, rows=[0, 127, 128, 299, 640, 1299, 2099])
+
+
+def _set_keys(p, k, at=None, v=None):
+    """Every key of request 0 becomes k, but key `at` zeros with the value v."""
+    import torch
+    pool = p.pool.view(p.P, 2, p.shape[1], p.page, p.shape[2])
+    for t in range(p.kv[0]):
+        page, i = p.table[0, t // p.page], t % p.page
+        pool[page, 0, :, i] = torch.zeros_like(k) if t == at else k
+        if t == at:
+            pool.view(p.vt)[page, 1, :, i] = v
+
+
+@pytest.mark.parametrize("new", [1, 40])
+@pytest.mark.parametrize("kind", list(TYPES))
+def test_a_large_value_with_no_weight(S, kind, new):
+    """A value near the type's end whose key lies 120 below the others in score."""
+    p = Paged(S, kind, 1, 1, 64, [200], [new])
+    p.q.copy_(p.q[:1].expand_as(p.q))
+    _set_keys(p, p.q[0] * (120 * 8 / p.q[0].float().square().sum()).to(p.qt), at=7, v=60000.0 if kind == "v16" else 3e38)
+    p.run("none")
+    p.check("none")
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+def test_many_small_weights(S, kind):
+    """A first key with 2^23.5 times the weight of each of the 100,000 that follow, and no value."""
+    p = Paged(S, kind, 1, 1, 64, [100000], [1], page=256)
+    q = p.q[0].float()
+    p.pool[:, 0] = 0
+    page = p.table[0, 0]
+    p.pool[page, 0, :, 0] = (q * (23.5 * np.log(2) * 8 / q.square().sum())).to(p.qt)
+    p.pool.view(p.vt)[page, 1, :, 0] = 0
+    used = dev(np.unique(p.table[p.table >= 0]))
+    p.pool.view(p.vt)[used.long(), 1] = p.pool.view(p.vt)[used.long(), 1].abs().clamp(max=4)
+    p.run("none")
+    p.check("none")
