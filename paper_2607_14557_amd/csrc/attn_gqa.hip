@@ -724,7 +724,9 @@ __global__ __launch_bounds__(NT) void gqa_join_kernel(GqaParams p) {
     }
   };
   if (r.parts <= 4) add(0, std::integral_constant<int, 4>{});
-  else if (r.parts <= 8) add(0, std::integral_constant<int, 8>{});
+  else if (RT == kGqaFew && r.parts <= 8) add(0, std::integral_constant<int, 8>{});
+  else if constexpr (RT == kGqaTile)
+    for (int i0 = 0; i0 < r.parts; i0 += 8) add(i0, std::integral_constant<int, 8>{});
   else
     for (int i0 = 0; i0 < r.parts; i0 += 16) add(i0, std::integral_constant<int, 16>{});
   const int tok = gqa_token(p, row), head = row - tok * p.group;
