@@ -68,8 +68,8 @@ __global__ __launch_bounds__(PLAN_T) void page_plan_kernel(PagePlanParams p) {
   __shared__ long long wave_give[PLAN_T / kWave], wave_take[PLAN_T / kWave];
   __shared__ int err;
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6;
-  const int in = *p.free_in;
-  if (tid == 0) err = in < 0 || in > p.n_pages ? kPagesInvalid : 0;
+  const int in = *p.free_in;         // used after the sums: under way with the lengths
+  if (tid == 0) err = 0;
   __syncthreads();
 
   const int per = (p.B + PLAN_T - 1) / PLAN_T;
@@ -77,8 +77,10 @@ __global__ __launch_bounds__(PLAN_T) void page_plan_kernel(PagePlanParams p) {
   const int b1 = b0 + per < p.B ? b0 + per : p.B;
   long long give = 0, take = 0;
   int bad = 0;
+  Lens first_l{};                    // of b0, read once
   for (int b = b0; b < b1; ++b) {
     const Lens l = lens_of(p, b);
+    if (b == b0) first_l = l;
     const int H = pages_of(l.held, p.shift), N = pages_of((long long)l.keep + l.real, p.shift);
     if (l.bad) bad |= kPagesInvalid;
     if ((long long)l.keep + l.real > (long long)p.width << p.shift || (long long)l.keep + l.real > INT_MAX)
@@ -102,7 +104,7 @@ __global__ __launch_bounds__(PLAN_T) void page_plan_kernel(PagePlanParams p) {
     gave += wave_give[w];
     took += wave_take[w];
   }
-  int e = err;
+  int e = err | (in < 0 || in > p.n_pages ? kPagesInvalid : 0);
   if (e == 0 && in + gave > p.n_pages) e = kPagesInvalid;
   if (e == 0 && took > in + gave) e = kPagesExhausted;
   const int stride = gridDim.x * PLAN_T, first = blockIdx.x * PLAN_T + tid;
@@ -116,7 +118,7 @@ __global__ __launch_bounds__(PLAN_T) void page_plan_kernel(PagePlanParams p) {
     return;
   }
   for (int b = b0; b < b1; ++b) {
-    const Lens l = lens_of(p, b);
+    const Lens l = b == b0 ? first_l : lens_of(p, b);
     const int H = pages_of(l.held, p.shift), N = pages_of((long long)l.keep + l.real, p.shift);
     og += H > N ? H - N : 0;
     ot += N > H ? N - H : 0;
