@@ -118,6 +118,19 @@ struct GqaCut {
     return y < head ? (int)((unsigned)y / (unsigned)(each + 1)) : more + (int)((unsigned)(y - head) / (unsigned)each);
   }
 
+  // How many workgroups share a line of `all` blocks.  Each of them costs its start,
+  // the reads of its queries and up to two parts (66 KB each of 128 rows by 128) written
+  // and joined, so a short line goes to one workgroup a CU instead of all that run at
+  // once: 128 rows at 1280 blocks 29.7 -> 21.7 us, at 1736 33.1 -> 30.1, at 2720 38.1 ->
+  // 35.9, at 3392 40.7 -> 46.4; 32 rows at 600 blocks 21.0 -> 15.2, at 1280 25.3 -> 21.5,
+  // at 2008 26.0 -> 30.2; 32 rows 64 wide with 512 for 1024 at 2576 blocks 26.4 -> 22.5,
+  // at 5672 25.0 -> 28.9.
+  __device__ __forceinline__ static int workgroups(int most, int all) {
+    if (RT == kGqaF32) return most;
+    if (all < (RT == kGqaTile ? 2800 : 1300)) return most < 256 ? most : 256;
+    return all < 5000 && most > 512 ? 512 : most;
+  }
+
   __device__ __forceinline__ GqaCut(const GqaParams& p, Shared& shared) : sh(shared) {
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6;
     const int per = (p.B + NT - 1) / NT;
@@ -168,8 +181,9 @@ struct GqaCut {
     wgs = all;
     each = 1;
     more = 0;
-    if (p.cut && all > p.wgs) {
-      wgs = p.wgs;
+    const int most = p.cut ? workgroups(p.wgs, all) : all;
+    if (all > most) {
+      wgs = most;
       each = (unsigned)all / (unsigned)wgs;
       more = all - each * wgs;
     }
