@@ -585,8 +585,8 @@ size_t seer_attn_workspace_bytes(const seer_attn_desc* desc, int32_t rows_ub, in
  * between calls.
  * Errors: EINVAL (null pointers, batch or rows_ub < 1, an unknown mask or
  * SEER_MASK_TREE, rows or strides not aligned to 16 bytes, a stride below the
- * row, out equal to q, k or v), EUNSUPPORTED (desc; rows_ub * n_heads >= 2^31),
- * EWORKSPACE. */
+ * row, out equal to q, k or v), EUNSUPPORTED (desc; rows_ub * n_heads >= 2^31;
+ * 2^24 workgroups, of 16 (fp32) to 128 rows and heads each), EWORKSPACE. */
 int seer_attn_prompt(const seer_attn_desc* desc, int32_t mask, const void* q, int64_t q_stride, const void* k,
                      int64_t k_stride, const void* v, int64_t v_stride, void* out, int64_t out_stride,
                      int32_t rows_ub, const int32_t* cu_seqlens, const int32_t* seqused, int32_t batch,

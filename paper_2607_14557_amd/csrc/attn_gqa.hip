@@ -13,6 +13,20 @@
 //   gqa_few_kernel   32 rows a workgroup, the keys split over its two or four waves
 // both over all of a tile's keys or, where there are few tiles, over a part of
 // them; gqa_join_kernel then adds the parts.
+//
+// What bounds them, on an MI355X whose large copies reach 4.9 TB/s (5.9 read only)
+// and whose 8192^3 products reach 1225 TFLOP/s in bf16:
+//   many keys a row (14,416 rows, 32 heads on 8, 1500 to 8192 a prompt): the matrix
+//     instructions, 651 us, 1026 TFLOP/s
+//   single tokens (64 requests of 500 to 16,000 keys, 28 heads on 4): the read of the
+//     cache, 114 us, 5.3 TB/s
+//   short prompts and windows: half the time is the tiles' products and keys, half what
+//     each workgroup does once (its place in the call, queries, first keys, results):
+//     9937 rows of 16 prompts, 32 heads, 135 us, 500 TFLOP/s
+//   a few tiles (one token over 793 keys): two launches' latency, 14 us
+// Tried and slower: the join by the last workgroup to arrive in the first launch (one
+// token 16 -> 42 us: the waits for stores to reach the other XCDs), workgroups of 1024
+// for the join, raised wave priority around the products (no change).
 #include <type_traits>
 
 #include "gqa.h"
@@ -362,6 +376,10 @@ __device__ __forceinline__ void store4(uint16_t* at, f32x4_t v) {
 
 }  // namespace
 
+// 128 rows: K and V of 64 keys are in LDS twice (64 KB at head_dim 128), one tile
+// under way while the other is used, two workgroups a CU.  A step of 64 keys takes
+// 1.27 us alone and 1.84 us with both, 0.92 each: 0.86 us of matrix instructions.
+// Longer tiles leave LDS for one workgroup only; 32 keys need twice the barriers.
 template <int DH, bool VF16, bool PAGED>
 __global__ __launch_bounds__(NT, 2) void gqa_tile_kernel(GqaParams p) {
   constexpr int ROW = DH * 2, DT = DH / 32;
@@ -504,6 +522,10 @@ __global__ __launch_bounds__(NT, 2) void gqa_tile_kernel(GqaParams p) {
   }
 }
 
+// 32 rows: each wave walks 32 of every 32 NW keys by itself, its tiles of its own in
+// LDS, without a barrier until the waves are joined, so that its loads never wait for
+// another wave.  Cut lines have two waves, for more independent walks a CU; whole
+// tiles four, for the shorter walk.
 template <int DH, bool VF16, bool PAGED, int NW>
 __global__ __launch_bounds__(64 * NW, 1) void gqa_few_kernel(GqaParams p) {
   constexpr int ROW = DH * 2, DT = DH / 32, FT = 32 * ROW;      // bytes of a wave's K or V tile
@@ -681,7 +703,9 @@ __global__ __launch_bounds__(64 * NW, 1) void gqa_few_kernel(GqaParams p) {
 }
 
 // Adds the parts of each tile whose keys were cut, by the records that its first
-// part left: a wave takes 32 rows x 8 dims (16 bytes a lane).
+// part left: a wave takes 32 rows x 8 dims (16 bytes a lane).  Bound by the latency
+// of two dependent reads, a record and its parts (6 us), with many 128-row parts by
+// their bytes (104 tiles in 256 parts: 7 us).  4, 8 or 16 parts are under way at once.
 template <int RT, int DH>
 __global__ __launch_bounds__(NT) void gqa_join_kernel(GqaParams p) {
   constexpr int DT = DH / 32, PIECES = RT / 32 * DT;       // workgroups of a tile

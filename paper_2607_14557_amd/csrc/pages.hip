@@ -19,7 +19,9 @@ namespace seer {
 // one workgroup writes is read by another: table entries are written from H on
 // and read below H, free_pages is written from `in` on and read below it, and
 // the counts and lengths have two buffers.
-// Bound by latency: one launch, the loads of the lengths, two block-wide sums.
+// Bound by latency: one launch, the loads of the lengths, a block-wide sum, a
+// search in LDS, the read of a page and its use: 6.0 us for the 240 tokens of 256
+// requests, 5.2 us for 39,936 rows of 48 (a call from the host takes 5.6 us).
 namespace {
 constexpr int PLAN_T = 256;
 
@@ -174,29 +176,33 @@ int launch_page_plan(const PagePlanParams& p, hipStream_t s) {
 
 // ---------------------------------------------------------------------------
 // Rows into pages: a wave copies a row's K and V in 16-byte pieces, head after
-// head; a head's piece of a row is contiguous in the page.
+// head; a head's piece of a row is contiguous in the page.  Bound by memory: 20,118
+// rows of 32 heads by 128, 659 MB moved, 132 us, 5.0 TB/s, the rate of a large copy;
+// 256 rows of 8 heads 3.5 us, the latency of a slot, a row and its store.
 __global__ __launch_bounds__(256) void kv_store_kernel(KvStoreParams p) {
   const int lane = threadIdx.x & (kWave - 1);
-  const int r = blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (r >= p.rows_ub) return;
-  const int slot = p.slots[r];
-  if (slot < 0 || (slot >> p.shift) >= p.n_pages) return;
-  const int off = slot & ((1 << p.shift) - 1);
   const size_t half = (size_t)p.n_kv << p.shift;           // head rows of K (or V) in a page
-  const size_t page = (size_t)(slot >> p.shift) * 2 * half;
   const int n = p.n_kv * p.head_pieces;
-  for (int c = lane; c < 2 * n; c += kWave) {
-    const int v = c >= n, j = v ? c - n : c;
-    const int h = j / p.head_pieces, piece = j - h * p.head_pieces;
-    const uint8_t* src = v ? p.v + (size_t)r * p.v_stride : p.k + (size_t)r * p.k_stride;
-    const size_t row = page + v * half + ((size_t)h << p.shift) + off;
-    *reinterpret_cast<u32x4_t*>(p.pool + (row * p.head_pieces + piece) * 16) =
-        *reinterpret_cast<const u32x4_t*>(src + (size_t)j * 16);
+  for (long long r = blockIdx.x * 4 + (threadIdx.x >> 6); r < p.rows_ub; r += 4ll * gridDim.x) {
+    const int slot = p.slots[r];
+    if (slot < 0 || (slot >> p.shift) >= p.n_pages) continue;
+    const int off = slot & ((1 << p.shift) - 1);
+    const size_t page = (size_t)(slot >> p.shift) * 2 * half;
+    for (int c = lane; c < 2 * n; c += kWave) {
+      const int v = c >= n, j = v ? c - n : c;
+      const int h = j / p.head_pieces, piece = j - h * p.head_pieces;
+      const uint8_t* src = v ? p.v + (size_t)r * p.v_stride : p.k + (size_t)r * p.k_stride;
+      const size_t row = page + v * half + ((size_t)h << p.shift) + off;
+      *reinterpret_cast<u32x4_t*>(p.pool + (row * p.head_pieces + piece) * 16) =
+          *reinterpret_cast<const u32x4_t*>(src + (size_t)j * 16);
+    }
   }
 }
 
 int launch_kv_store(const KvStoreParams& p, hipStream_t s) {
-  hipLaunchKernelGGL(kv_store_kernel, dim3((p.rows_ub + 3) / 4), dim3(256), 0, s, p);
+  // a row a wave, up to the threads that one launch may have
+  const int blocks = p.rows_ub / 4 + (p.rows_ub % 4 != 0);
+  hipLaunchKernelGGL(kv_store_kernel, dim3(blocks < 1 << 22 ? blocks : 1 << 22), dim3(256), 0, s, p);
   return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 

@@ -818,16 +818,19 @@ static int gqa_params(seer::GqaParams& p, const seer_attn_desc* desc, int32_t ma
   return SEER_OK;
 }
 
-static int launch_gqa(seer::GqaParams& p, const seer_attn_desc* desc, hipStream_t stream) {
+static int launch_gqa(seer::GqaParams& p, const seer_attn_desc* desc, hipStream_t stream, const char* what) {
   seer::GqaLaunch g = gqa_launch(desc, p.rows_ub, p.B);
   g.keys = p.table ? (long long)p.width << p.shift : p.rows_ub;
   g.half = !p.table && p.mask == SEER_MASK_CAUSAL;
   const seer::GqaRule r = seer::gqa_rule(g);
+  // of 256 threads each, and a launch has less than 2^32
+  if (r.grid >= 1 << 24) return fail(SEER_EUNSUPPORTED, "%s of %d workgroups, at most 2^24 - 1", what, r.grid);
   p.cut = r.cut;
   p.wgs = r.grid;
   p.sort = r.sort;
   p.partial = reinterpret_cast<float*>(static_cast<uint8_t*>(p.records) + seer::gqa_record_bytes(r.grid));
-  return p.bf16 ? seer::launch_gqa_bf16(p, r, stream) : seer::launch_gqa_f32(p, r, stream);
+  if (p.bf16 ? seer::launch_gqa_bf16(p, r, stream) : seer::launch_gqa_f32(p, r, stream)) return hip_fail(what);
+  return ok();
 }
 
 int seer_attn_prompt(const seer_attn_desc* desc, int32_t mask, const void* q, int64_t q_stride, const void* k,
@@ -844,8 +847,7 @@ int seer_attn_prompt(const seer_attn_desc* desc, int32_t mask, const void* q, in
   if ((rc = check_rows("k", k, k_stride, width, es)) || (rc = check_rows("v", v, v_stride, width, es))) return rc;
   if (out == k || out == v) return fail(SEER_EINVAL, "out may not alias an input");
   p.k = k; p.v = v; p.k_stride = k_stride; p.v_stride = v_stride;
-  if (launch_gqa(p, desc, stream)) return hip_fail("prompt attention launch");
-  return ok();
+  return launch_gqa(p, desc, stream, "prompt attention launch");
 }
 
 int seer_attn_paged(const seer_attn_desc* desc, const seer_page_desc* pages, int32_t mask, const void* q,
@@ -867,8 +869,7 @@ int seer_attn_paged(const seer_attn_desc* desc, const seer_page_desc* pages, int
   p.k = pool; p.v = pool; p.table = table; p.kv_len = kv_len;
   p.shift = page_shift(pages); p.n_pages = pages->n_pages; p.width = pages->table_width;
   p.bits = reinterpret_cast<const unsigned long long*>(tree_bits); p.words = tree_words;
-  if (launch_gqa(p, desc, stream)) return hip_fail("paged attention launch");
-  return ok();
+  return launch_gqa(p, desc, stream, "paged attention launch");
 }
 
 // ---- recorded launch sequences (Sec. 3.5, graph-compatible paths) ----------

@@ -214,7 +214,8 @@ class PagedCache:
     (None: all), fewer where a window was cut or drafts were refused, 0 where
     the request has ended.  Lengths and free pages stay on the device; each plan
     reads one of two buffers and writes the other, so a recorded sequence has an
-    even number of plans."""
+    even number of plans.  The calls go to the current stream (or `stream`) of
+    the cache's device, which has to be the current one."""
 
     def __init__(self, n_heads, n_kv_heads, head_dim, n_layers, n_pages, page_size, max_batch, max_len, max_rows,
                  dtype="bf16", v_f16=False, scale=0.0, device="cuda"):
@@ -252,10 +253,20 @@ class PagedCache:
         """[1] int32: the number of free pages."""
         return self._free[0]
 
-    def plan(self, cu, rows_ub, keep=None, seqused=None, stream=None):
-        """The pages and slots of a step; returns the slots of its rows."""
+    def _takes(self, rows_ub, cu=None, keep=None, seqused=None):
+        """Refuse what the kernels would read or write past an end."""
+        if self.table.is_cuda and torch.cuda.current_device() != self.table.get_device():
+            raise ValueError("the cache is on %s, which is not the current device" % (self.table.device,))
         if rows_ub > self.max_rows:
             raise ValueError("rows_ub %d exceeds max_rows %d" % (rows_ub, self.max_rows))
+        for name, x, n in (("cu", cu, self.max_batch + 1), ("keep", keep, self.max_batch),
+                           ("seqused", seqused, self.max_batch)):
+            if x is not None and x.numel() < n:
+                raise ValueError("%s has %d entries, %d needed" % (name, x.numel(), n))
+
+    def plan(self, cu, rows_ub, keep=None, seqused=None, stream=None):
+        """The pages and slots of a step; returns the slots of its rows."""
+        self._takes(rows_ub, cu, keep, seqused)
         held = self._lens[0]
         S.seer_page_plan(self.pages, held, held if keep is None else keep, cu, seqused, self.max_batch, rows_ub,
                          self.free_pages, self._free[0], self._free[1], self.table, self._lens[1], self.slots,
@@ -276,6 +287,7 @@ class PagedCache:
 
     def store(self, layer, k, v, rows_ub, slots=None, stream=None):
         """Rows of k and v ([rows, n_kv_heads * head_dim], any row stride) into the layer's pages."""
+        self._takes(rows_ub)
         S.seer_kv_store(self.desc, self.pages, k, k.stride(0), v, v.stride(0), rows_ub,
                         self.slots if slots is None else slots, self.pools[layer], stream=stream)
 
@@ -288,6 +300,7 @@ class PagedCache:
         flags = S.SEER_ATTN_V_F16 if bf16 else 0
         if (self.desc.n_kv_heads * self.desc.head_dim, self.desc.dtype, self.desc.flags) != (d, stack.dims.dtype, flags):
             raise ValueError("the cache's heads and types are not those of the layer's rows")
+        self._takes(rows_ub)
         es = 2 if bf16 else 4
         k = stack.workspace.data_ptr() + S.seer_layer_workspace_offsets(stack.dims, rows_ub)[0] + d * es
         S.seer_kv_store(self.desc, self.pages, k, 3 * d, k + d * es, 3 * d, rows_ub,
@@ -295,12 +308,14 @@ class PagedCache:
 
     def attend(self, layer, q, out, cu, rows_ub, mask=S.SEER_MASK_CAUSAL, tree_bits=None, seqused=None, stream=None):
         """Attention of the step's rows over their requests' pages."""
+        self._takes(rows_ub, cu, None, seqused)
         S.seer_attn_paged(self.desc, self.pages, mask, q, q.stride(0), out, out.stride(0), rows_ub, cu, seqused,
                           self.max_batch, self.pools[layer], self.table, self._lens[0], tree_bits,
                           0 if tree_bits is None else tree_bits.shape[1], self.workspace, self.ws_bytes, stream=stream)
 
     def prompt(self, q, k, v, out, cu, rows_ub, mask=S.SEER_MASK_CAUSAL, seqused=None, stream=None):
         """Attention of packed prompts over their own rows (no pages)."""
+        self._takes(rows_ub, cu, None, seqused)
         S.seer_attn_prompt(self.desc, mask, q, q.stride(0), k, k.stride(0), v, v.stride(0), out, out.stride(0),
                            rows_ub, cu, seqused, self.max_batch, self.workspace, self.ws_bytes, stream=stream)
 

@@ -194,3 +194,12 @@ def test_pages_beside_the_layer(S, dtype):
         other.store_layer(0, st, rows)
     with pytest.raises(ValueError):
         c.plan(cu, rows + 1)
+
+
+def test_another_current_device(S, monkeypatch):
+    """A cache's calls while another device is current are refused."""
+    import torch
+    p = Program(S, "bf16")
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    with pytest.raises(ValueError, match="current device"):
+        p.c.plan(dev(np.zeros(6, int)), 8)

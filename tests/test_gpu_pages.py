@@ -124,3 +124,18 @@ def test_store(S, kind, KV, D, page):
             want.view(vt)[s // page, 1, :, s % page] = v[r].view(KV, D)
     S.seer_kv_store(d, pages, k, buf.stride(0), v, buf.stride(0), rows, dev(slots), pool)
     assert pool.cpu().view(torch.uint8).equal(want.cpu().view(torch.uint8))
+
+
+def test_store_of_more_rows_than_a_launch_has_waves(S):
+    import torch
+    n = (1 << 24) + 5
+    d, pages = S.seer_attn_desc(1, 1, 4, S.SEER_DTYPE_F32, 0, 0.0), S.seer_page_desc(16, 2, 1)
+    k = torch.zeros(n, 4, device="cuda")
+    k[0], k[n - 1], k[1 << 24] = 1.0, 2.0, 3.0
+    slots = torch.full((n,), -1, dtype=torch.int32, device="cuda")
+    slots[0], slots[n - 1], slots[1 << 24] = 17, 3, 30
+    pool = torch.full((2, 2, 1, 16, 4), 9.0, device="cuda")
+    S.seer_kv_store(d, pages, k, 4, k, 4, n, slots, pool)
+    want = torch.full((2, 2, 1, 16, 4), 9.0)
+    want[1, :, 0, 1], want[0, :, 0, 3], want[1, :, 0, 14] = 1.0, 2.0, 3.0
+    assert torch.equal(pool.cpu(), want)

@@ -123,3 +123,29 @@ def test_attention_refusals(S):
                dict(mask=S.SEER_MASK_TREE), dict(mask=S.SEER_MASK_TREE, bits=FAKE, words=0)):
         assert paged(S, **kw) == S.SEER_EINVAL, kw
     assert paged(S, pg=pages(S, size=8)) == S.SEER_EUNSUPPORTED
+
+
+def test_attention_of_more_workgroups_than_a_launch_has(S):
+    """2^30 rows of one fp32 head are 2^26 workgroups of 16."""
+    d = heads(S, h=1, kv=1, d=4, t=S.SEER_DTYPE_F32)
+    n = S.seer_attn_workspace_bytes(d, 1 << 30, 1)
+    assert n > 0
+    assert S.load_library().seer_attn_prompt(ctypes.byref(d), S.SEER_MASK_CAUSAL, FAKE, 4, FAKE * 2, 4, FAKE * 3, 4,
+                                             FAKE * 4, 4, 1 << 30, FAKE, None, 1, FAKE, n, None) == S.SEER_EUNSUPPORTED
+    assert "workgroups" in S.seer_last_error()
+
+
+def test_cache_refusals(S):
+    """Rows and per-request arrays shorter than what the kernels read."""
+    import torch
+    from paper_2607_14557_amd.runner import PagedCache
+    c = PagedCache(2, 1, 64, 1, 4, 16, 3, 32, 8, device="cpu")
+    cu, three, x = torch.zeros(4, dtype=torch.int32), torch.zeros(3, dtype=torch.int32), torch.zeros(8, 128, dtype=torch.bfloat16)
+    k = x[:, :64]
+    for call in (lambda: c.plan(cu, 9), lambda: c.plan(cu[:3], 8), lambda: c.plan(cu, 8, three[:2]),
+                 lambda: c.plan(cu, 8, None, three[:1]), lambda: c.store(0, k, k, 9),
+                 lambda: c.attend(0, x, x.clone(), cu[:3], 8), lambda: c.attend(0, x, x.clone(), cu, 9),
+                 lambda: c.attend(0, x, x.clone(), cu, 8, seqused=three[:2]),
+                 lambda: c.prompt(x, k, k, x.clone(), cu[:3], 8), lambda: c.prompt(x, k, k, x.clone(), cu, 9)):
+        with pytest.raises(ValueError):
+            call()
