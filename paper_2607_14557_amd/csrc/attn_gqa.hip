@@ -16,17 +16,20 @@
 //
 // What bounds them, on an MI355X whose large copies reach 4.9 TB/s (5.9 read only)
 // and whose 8192^3 products reach 1225 TFLOP/s in bf16:
-//   many keys a row (14,416 rows, 32 heads on 8, 1500 to 8192 a prompt): the matrix
-//     instructions, 651 us, 1026 TFLOP/s
+//   many keys a row (14,416 rows, 32 heads on 8, 1500 to 8192 a prompt): the chain
+//     inside a tile, scores, exponentials, products, with the matrix pipe half busy:
+//     651 us, 1027 TFLOP/s
 //   single tokens (64 requests of 500 to 16,000 keys, 28 heads on 4): the read of the
-//     cache, 114 us, 5.3 TB/s
-//   short prompts and windows: half the time is the tiles' products and keys, half what
-//     each workgroup does once (its place in the call, queries, first keys, results):
-//     9937 rows of 16 prompts, 32 heads, 135 us, 500 TFLOP/s
-//   a few tiles (one token over 793 keys): two launches' latency, 14 us
+//     cache, 115 us, 5.3 TB/s
+//   short prompts and windows: half the time is that chain, half what each workgroup
+//     does once (its place in the call, queries, first keys, results): 9937 rows of 16
+//     prompts, 32 heads, 136 us, 496 TFLOP/s
+//   a few tiles (one token over 794 keys): the latency of two launches, 14 us
 // Tried and slower: the join by the last workgroup to arrive in the first launch (one
 // token 16 -> 42 us: the waits for stores to reach the other XCDs), workgroups of 1024
-// for the join, raised wave priority around the products (no change).
+// for the join, and a join of the records in use alone (their search costs what the
+// empty workgroups do).  Without effect: raised wave priority around the products,
+// the requests summed by lanes instead of through LDS.
 #include <type_traits>
 
 #include "gqa.h"
@@ -378,8 +381,9 @@ __device__ __forceinline__ void store4(uint16_t* at, f32x4_t v) {
 
 // 128 rows: K and V of 64 keys are in LDS twice (64 KB at head_dim 128), one tile
 // under way while the other is used, two workgroups a CU.  A step of 64 keys takes
-// 1.27 us alone and 1.84 us with both, 0.92 each: 0.86 us of matrix instructions.
-// Longer tiles leave LDS for one workgroup only; 32 keys need twice the barriers.
+// 1.27 us alone and 1.84 us with both, 0.92 each, of which the matrix instructions
+// are a half: the other workgroup fills the waits of the chain.  A third buffer
+// would leave LDS for one workgroup only.
 template <int DH, bool VF16, bool PAGED>
 __global__ __launch_bounds__(NT, 2) void gqa_tile_kernel(GqaParams p) {
   constexpr int ROW = DH * 2, DT = DH / 32;
