@@ -229,7 +229,7 @@ inline int gqa_cut_grid(const GqaLaunch& g, int rt) {
 
 // Expected us of a form, the call's host time included where it is the longer: fits
 // to the measured times of each form alone (bf16: 420 calls of 1 to 256 requests, 1 to
-// 4000 rows and 15 to 40,000 keys each, rms 5 to 13% uncut, 25% cut; fp32: 201 calls,
+// 4000 rows and 15 to 40,000 keys each, rms 5 to 11% uncut, 20 to 22% cut; fp32: 201 calls,
 // rms 16 to 24%).  Uncut, a tile's keys are one walk, and the tiles run in rounds; cut,
 // all workgroups share the blocks, and a second launch joins.
 inline double gqa_us(const GqaLaunch& g, int rt, bool cut) {
@@ -240,8 +240,8 @@ inline double gqa_us(const GqaLaunch& g, int rt, bool cut) {
       {{5.1, 2.3, 0.95, 4.8, 1.18, 512, 128}, {5.3, 3.0, 1.32, 6.3, 1.20, 256, 128}},
       {{5.8, 1.2, 1.34, 2.8, 1.54, 512, 64}, {4.1, 3.3, 2.93, 7.1, 3.31, 512, 64}}};
   static constexpr Cut kCut[3][2] = {
-      {{15.3, 1.23, 1.6}, {16.9, 1.93, 4.7}},
-      {{15.1, 1.23, 0.0}, {15.4, 1.34, 2.4}},
+      {{13.4, 1.26, 2.5}, {14.7, 1.92, 5.0}},
+      {{13.7, 1.21, 3.1}, {14.2, 1.34, 3.3}},
       {{11.3, 1.59, 0.0}, {11.1, 3.02, 4.2}}};
   const int form = rt == kGqaTile ? 0 : (rt == kGqaFew ? 1 : 2), big = g.dim > 64;
   const double tiles = (double)gqa_tiles(g, rt);

@@ -85,7 +85,8 @@ struct GqaRecord {
 //              requests and tiles stand in one line, and each of the p.wgs workgroups
 //              takes an equal stretch of it, whatever the requests' lengths: no
 //              workgroup waits for another, and none starts after the others.  A tile
-//              that lies in several stretches is joined by a second launch.
+//              that lies in several stretches is joined by a second launch.  With few
+//              tiles the places of the line are runs of several blocks (below).
 //   otherwise: a workgroup for each tile, request after request (p.sort: the ones with
 //              the most keys first, so that no long walk starts at the end: sixteen
 //              prompts of 200 to 1300 rows 142 -> 135 us), in each all heads, in each the
@@ -103,15 +104,20 @@ struct GqaCut {
     int id[NT];
   };
   Shared& sh;
+  int run;                       // cut: blocks of a place of the line
   int n, all;                    // length of a head's line, and of the whole
   int wgs, each, more;           // workgroups with work: `more` of them take each + 1, the others each
   int x, x0, x1;                 // the next place, and the workgroup's stretch
   int wg;
   int heads, head0;              // uncut: the heads of this workgroup's XCD
 
-  __device__ __forceinline__ static int weight(const GqaParams& p, const GqaSeq& s) {
-    return s.tiles * (p.cut ? gqa_blocks(s.nk) : 1);
+  // places of a tile of request s
+  __device__ __forceinline__ int places(const GqaParams& p, const GqaSeq& s) const {
+    if (!p.cut) return 1;
+    const int nb = gqa_blocks(s.nk);
+    return run == 1 ? nb : (int)((unsigned)(nb + run - 1) / (unsigned)run);
   }
+  __device__ __forceinline__ int weight(const GqaParams& p, const GqaSeq& s) const { return s.tiles * places(p, s); }
   __device__ __forceinline__ int start(int i) const { return i * each + (i < more ? i : more); }
   // the workgroup that has place y
   __device__ __forceinline__ int holder(int y) const {
@@ -132,7 +138,31 @@ struct GqaCut {
     return all < 5000 && most > 512 ? 512 : most;
   }
 
-  __device__ __forceinline__ GqaCut(const GqaParams& p, Shared& shared) : sh(shared) {
+  // The line: the sums of the threads' places before each of them, and of all.
+  __device__ __forceinline__ void scan(const GqaParams& p, int own) {
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6;
+    int inc = own;
+#pragma unroll
+    for (int off = 1; off < kWave; off <<= 1) {
+      const int v = __shfl_up(inc, off, kWave);
+      if (lane >= off) inc += v;
+    }
+    if (lane == kWave - 1) sh.sums[wave] = inc;
+    __syncthreads();
+    int first = inc - own;
+    n = 0;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      if (w < wave) first += sh.sums[w];
+      n += sh.sums[w];
+    }
+    n = __builtin_amdgcn_readfirstlane(n);
+    sh.first[tid] = first;
+    if (tid == NT - 1) sh.first[NT] = n;
+    all = n * p.n_kv;
+  }
+
+  __device__ __forceinline__ GqaCut(const GqaParams& p, Shared& shared) : sh(shared), run(1) {
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6;
     const int per = (p.B + NT - 1) / NT;
     const int b0 = tid * per < p.B ? tid * per : p.B;
@@ -158,31 +188,39 @@ struct GqaCut {
     } else {
       for (int b = b0; b < b1; ++b) own += weight(p, gqa_seq<RT>(p, b));
     }
-    int inc = own;
-#pragma unroll
-    for (int off = 1; off < kWave; off <<= 1) {
-      const int v = __shfl_up(inc, off, kWave);
-      if (lane >= off) inc += v;
+    scan(p, own);
+    const int most = p.cut ? workgroups(p.wgs, all) : all;
+    // Few tiles: an equal stretch that crosses from one tile to the next makes two
+    // pieces, one after the other, and the launch waits for it (5 us, what 2 blocks take
+    // in fp32 and 3 to 4 in bf16).  So a tile's blocks are taken in runs of one length,
+    // a run a workgroup: the least that is not below an equal stretch, or, if those are
+    // more runs than workgroups, the length that leaves room for each tile's odd one,
+    // while it is not too much above an equal stretch.  One token, 32 heads on 8: 3000
+    // keys 26.3 -> 19.7 us, 6000 26.6 -> 22.2; 4 tokens of 16 heads on 1 at 4000 keys 26.0 ->
+    // 19.2; fp32, 4 tokens of 8 heads on 2 at 4000 keys 28.9 -> 21.7.  Runs twice the equal
+    // stretch: 8 tokens of 32 heads on 32 at 4000 keys 64.9 -> 77.6.
+    if (p.cut && all > most && p.tiles > 1 && 2 * p.tiles <= most) {
+      const int blocks = all, fair = (unsigned)(blocks + most - 1) / (unsigned)most;
+      auto lay = [&](int r) {
+        run = r;
+        own = 0;
+        if (per == 1) own = weight(p, sh.seq[tid]);
+        else
+          for (int b = b0; b < b1; ++b) own += weight(p, gqa_seq<RT>(p, b));
+        __syncthreads();
+        scan(p, own);
+      };
+      lay(fair);
+      if (all > most) {
+        const int room = (unsigned)(blocks + most - p.tiles - 1) / (unsigned)(most - p.tiles);
+        lay(room <= fair + (RT == kGqaF32 ? 1 : 2) ? room : 1);
+      }
     }
-    if (lane == kWave - 1) sh.sums[wave] = inc;
-    __syncthreads();
-    int first = inc - own;
-    n = 0;
-#pragma unroll
-    for (int w = 0; w < NW; ++w) {
-      if (w < wave) first += sh.sums[w];
-      n += sh.sums[w];
-    }
-    n = __builtin_amdgcn_readfirstlane(n);
-    sh.first[tid] = first;
-    if (tid == NT - 1) sh.first[NT] = n;
-    all = n * p.n_kv;
     const int bid = blockIdx.x;
     wg = 0;
     wgs = all;
     each = 1;
     more = 0;
-    const int most = p.cut ? workgroups(p.wgs, all) : all;
     if (all > most) {
       wgs = most;
       each = (unsigned)all / (unsigned)wgs;
@@ -265,7 +303,7 @@ struct GqaCut {
     const int rem = uni(p.cut ? j - at : x - at * heads);
     u.s.tiles = uni(s.tiles); u.s.s0 = uni(s.s0); u.s.len = uni(s.len); u.s.used = uni(s.used); u.s.nk = uni(s.nk);
     u.s.past = uni(s.past); u.s.rows = uni(s.rows);
-    const int nb = gqa_blocks(u.s.nk), line = p.cut ? nb : u.s.tiles;
+    const int nb = places(p, u.s), line = p.cut ? nb : u.s.tiles;
     const int quot = (unsigned)rem / (unsigned)line, left = rem - quot * line;
     u.hk = p.cut ? q : head0 + quot;
     const int tile = p.cut ? quot : left, block = p.cut ? left : 0;
@@ -280,7 +318,7 @@ struct GqaCut {
     if (p.cut) {
       take = nb - block < x1 - x ? nb - block : x1 - x;
       u.whole = take == nb;
-      const long long lo = (long long)block * kGqaBlock, hi = lo + (long long)take * kGqaBlock;
+      const long long lo = (long long)block * run * kGqaBlock, hi = lo + (long long)take * run * kGqaBlock;
       u.lo = lo < end ? (int)lo : end;
       u.hi = hi < end ? (int)hi : end;
       u.slot = 2 * wg + (x == x0 ? 0 : 1);

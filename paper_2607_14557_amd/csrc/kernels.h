@@ -353,7 +353,7 @@ struct GqaParams {
   // the launch (gqa_rule): whether the tiles' keys are cut, over how many
   // workgroups, and the records and results of the parts
   bool cut;
-  int wgs;
+  int wgs, tiles;
   bool sort;                   // the requests by their keys (uncut, at most 64 of them)
   void* records;
   float* partial;

@@ -827,6 +827,7 @@ static int launch_gqa(seer::GqaParams& p, const seer_attn_desc* desc, hipStream_
   if (r.grid >= 1 << 24) return fail(SEER_EUNSUPPORTED, "%s of %d workgroups, at most 2^24 - 1", what, r.grid);
   p.cut = r.cut;
   p.wgs = r.grid;
+  p.tiles = (int)seer::gqa_tiles(g, r.rt);
   p.sort = r.sort;
   p.partial = reinterpret_cast<float*>(static_cast<uint8_t*>(p.records) + seer::gqa_record_bytes(r.grid));
   if (p.bf16 ? seer::launch_gqa_bf16(p, r, stream) : seer::launch_gqa_f32(p, r, stream)) return hip_fail(what);

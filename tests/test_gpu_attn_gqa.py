@@ -505,3 +505,13 @@ def test_many_small_weights(S, kind):
     p.pool.view(p.vt)[used.long(), 1] = p.pool.view(p.vt)[used.long(), 1].abs().clamp(max=4)
     p.run("none")
     p.check("none")
+
+
+@pytest.mark.parametrize("past", [[2999], [1216, 1152], [3000, 900, 7, 0], [12000, 4100], [64 * 512, 64]])
+@pytest.mark.parametrize("kind,H,KV,D", [("bf16", 16, 8, 128), ("v16", 14, 2, 64), ("f32", 8, 2, 64), ("bf16", 40, 1, 128)])
+def test_few_tiles_of_many_keys(S, kind, H, KV, D, past):
+    """Keys in runs, a run a workgroup, and lines that cross from tile to tile."""
+    for new, mask in ((1, "causal"), (3, "none")):
+        p = Paged(S, kind, H, KV, D, past, [new] * len(past), page=64)
+        p.run(mask)
+        p.check(mask)
