@@ -351,7 +351,7 @@ struct GqaParams {
   const unsigned long long* bits;   // [rows][words]
   int words;
   // the launch (gqa_rule): whether the tiles' keys are cut, over how many
-  // workgroups, and the records and results of the parts
+  // workgroups, the most tiles that there are, and the records and results of the parts
   bool cut;
   int wgs, tiles;
   bool sort;                   // the requests by their keys (uncut, at most 64 of them)
