@@ -287,6 +287,15 @@ inline GqaRule gqa_rule(const GqaLaunch& g) {
   return best;
 }
 
+// Whether the line of `all` blocks is cut in runs of one length (GqaCut): more blocks than
+// workgroups, and room for two runs a tile.  `tiles` goes up to 2^31 - 1.
+constexpr bool gqa_in_runs(int all, int most, int tiles) { return all > most && tiles > 1 && tiles <= most / 2; }
+
+// The shortest run that leaves room for each tile's odd one.
+constexpr int gqa_run_room(int blocks, int most, int tiles) {
+  return (int)(((unsigned)blocks + most - tiles - 1) / (unsigned)(most - tiles));
+}
+
 // Bytes of the parts of a cut launch: their records, then two results a workgroup (the
 // sums of each row, its maximum and its divisor).
 inline size_t gqa_record_bytes(int grid) { return ((size_t)grid * 32 + 255) / 256 * 256; }

@@ -199,7 +199,7 @@ struct GqaCut {
     // keys 26.3 -> 19.7 us, 6000 26.6 -> 22.2; 4 tokens of 16 heads on 1 at 4000 keys 26.0 ->
     // 19.2; fp32, 4 tokens of 8 heads on 2 at 4000 keys 28.9 -> 21.7.  Runs twice the equal
     // stretch: 8 tokens of 32 heads on 32 at 4000 keys 64.9 -> 77.6.
-    if (p.cut && all > most && p.tiles > 1 && 2 * p.tiles <= most) {
+    if (p.cut && gqa_in_runs(all, most, p.tiles)) {
       const int blocks = all, fair = ((unsigned)blocks + most - 1) / (unsigned)most;
       auto lay = [&](int r) {
         run = r;
@@ -212,7 +212,7 @@ struct GqaCut {
       };
       lay(fair);
       if (all > most) {
-        const int room = ((unsigned)blocks + most - p.tiles - 1) / (unsigned)(most - p.tiles);
+        const int room = gqa_run_room(blocks, most, p.tiles);
         lay(room <= fair + (RT == kGqaF32 ? 1 : 2) ? room : 1);
       }
     }
