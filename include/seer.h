@@ -579,8 +579,11 @@ size_t seer_attn_workspace_bytes(const seer_attn_desc* desc, int32_t rows_ub, in
  * [0, cu_seqlens[batch]) are read and written, no others.
  * Precision: products of the given types summed in fp32; the softmax's
  * statistics and the sums are fp32; the probabilities are rounded to V's type
- * for the second product (bf16, fp16, or none for fp32).  A key that a row
- * does not see has no part in it, whatever its k and v hold (NaN, infinity).
+ * for the second product (bf16, fp16, or none for fp32).  The sums are made
+ * before they are divided: they stay finite for values of up to 2^126 / (keys of
+ * the request + 64), all fp16 values among them, and for scores that are finite
+ * in fp32 (scale log2(e) q . k).  A key that a row does not see has no part in
+ * it, whatever its k and v hold (NaN, infinity).
  * workspace: seer_attn_workspace_bytes, 256-byte aligned; it holds nothing
  * between calls.
  * Errors: EINVAL (null pointers, batch or rows_ub < 1, an unknown mask or

@@ -238,8 +238,9 @@ struct Rows32 {
     float lsum;
     auto probs = [&](float ref) {
       // fp16: all 2^10 times as large, so that those down to 2^-24 of the reference are
-      // normal numbers (it goes with the division by their sum)
-      const float mc = VF16 ? ref * c - 10.0f : ref * c;
+      // normal numbers; bf16: 2^-16, so that none passes 1 before the reference moves (it
+      // goes with the division by their sum)
+      const float mc = VF16 ? ref * c - 10.0f : ref * c + 16.0f;
       lsum = 0.0f;
 #pragma unroll
       for (int sl = 0; sl < 2 * NI; ++sl)
@@ -266,14 +267,16 @@ struct Rows32 {
           }
         }
     };
-    // The reference is the maximum of the first tile in which the row sees a key,
-    // and moves only where a later tile's probabilities pass fp16's range (2^6 of the
-    // reference; with bf16 2^16, far from the end of fp32's): any reference gives the same
-    // softmax, and the common tile takes no maximum.  While a row has seen no key
-    // its reference is -inf, and the NaN or infinity that this gives (-inf + inf,
-    // x + inf) asks for the tile's maximum too.
+    // The reference is the maximum of the first tile in which the row sees a key, and
+    // moves only where a later tile's probabilities pass fp16's range (2^6 of the
+    // reference) or, with bf16, add up to 2^16 of it in a lane: any reference gives the
+    // same softmax, and the common tile takes no maximum.  With bf16 the sums of large
+    // values stay in fp32's range, as a lane's 16 or 32 keys of a tile count for less than 1
+    // together (a limit of 2^6 without the factor did that too, and took 7% longer where
+    // scores spread by 4).  While a row has seen no key its reference is -inf, and the NaN
+    // or infinity that this gives (-inf + inf, x + inf) asks for the tile's maximum too.
     probs(m);
-    if (__any(!(lsum < (VF16 ? INFINITY : 65536.0f)))) {
+    if (__any(!(lsum < (VF16 ? INFINITY : 1.0f)))) {
       float mt = s[0][0];
 #pragma unroll
       for (int i = 0; i < NI; ++i)
