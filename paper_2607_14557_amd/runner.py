@@ -215,7 +215,13 @@ class PagedCache:
     the request has ended.  Lengths and free pages stay on the device; each plan
     reads one of two buffers and writes the other, so a recorded sequence has an
     even number of plans.  The calls go to the current stream (or `stream`) of
-    the cache's device, which has to be the current one."""
+    the cache's device, which has to be the current one; they share a workspace,
+    so that calls on two streams, recordings among them, may not overlap.
+
+    Rows of q, k, v and out are [at least rows_ub, heads * head_dim] or [.., heads,
+    head_dim] in the cache's types with a row's elements side by side (row
+    strides are free), tree_bits [at least rows_ub, words] int64 and contiguous,
+    cu, keep, seqused and slots int32 and contiguous; ValueError otherwise."""
 
     def __init__(self, n_heads, n_kv_heads, head_dim, n_layers, n_pages, page_size, max_batch, max_len, max_rows,
                  dtype="bf16", v_f16=False, scale=0.0, device="cuda"):
@@ -231,6 +237,8 @@ class PagedCache:
             raise S.SeerError(S.SEER_EUNSUPPORTED, S.seer_last_error())
         self.max_batch, self.max_rows = int(max_batch), int(max_rows)
         kind = torch_dtype(dtype)
+        self.kind, self.v_kind = kind, torch.float16 if v_f16 else kind
+        self.q_width, self.kv_width = n_heads * head_dim, n_kv_heads * head_dim
         shape = (n_pages, 2, n_kv_heads, page_size, head_dim)
         self.pools = [torch.zeros(shape, dtype=kind, device=device) for _ in range(n_layers)]
         i32 = lambda *s: torch.zeros(*s, dtype=torch.int32, device=device)
@@ -242,6 +250,7 @@ class PagedCache:
         self.slots = i32(max_rows)
         self.status = i32(1)
         self.workspace = torch.empty(self.ws_bytes, dtype=torch.uint8, device=device)
+        self._device = self.table.get_device()        # -1 on the CPU
 
     @property
     def lens(self):
@@ -253,16 +262,40 @@ class PagedCache:
         """[1] int32: the number of free pages."""
         return self._free[0]
 
-    def _takes(self, rows_ub, cu=None, keep=None, seqused=None):
-        """Refuse what the kernels would read or write past an end."""
-        if self.table.is_cuda and torch.cuda.current_device() != self.table.get_device():
+    def _takes(self, rows_ub, cu=None, keep=None, seqused=None, slots=None):
+        """Refuse what the kernels would read or write past an end, or misread."""
+        if self._device >= 0 and torch.cuda.current_device() != self._device:
             raise ValueError("the cache is on %s, which is not the current device" % (self.table.device,))
         if rows_ub > self.max_rows:
             raise ValueError("rows_ub %d exceeds max_rows %d" % (rows_ub, self.max_rows))
-        for name, x, n in (("cu", cu, self.max_batch + 1), ("keep", keep, self.max_batch),
-                           ("seqused", seqused, self.max_batch)):
-            if x is not None and x.numel() < n:
-                raise ValueError("%s has %d entries, %d needed" % (name, x.numel(), n))
+        if cu is not None:
+            self._ints("cu", cu, self.max_batch + 1)
+        if keep is not None:
+            self._ints("keep", keep, self.max_batch)
+        if seqused is not None:
+            self._ints("seqused", seqused, self.max_batch)
+        if slots is not None:
+            self._ints("slots", slots, rows_ub)
+
+    def _ints(self, name, x, n):
+        if x.numel() < n:
+            raise ValueError("%s has %d entries, %d needed" % (name, x.numel(), n))
+        if x.dtype is not torch.int32 or not x.is_contiguous() or x.get_device() != self._device:
+            raise ValueError("%s has to be int32, contiguous and on the cache's device" % name)
+
+    def _rows(self, rows_ub, name, x, width, kind):
+        """The same for rows of q, k, v and the output."""
+        if x.dtype is not kind or x.get_device() != self._device:
+            raise ValueError("%s has to be %s on the cache's device" % (name, kind))
+        shape, stride = x.shape, x.stride()
+        if len(shape) == 2:
+            whole = shape[1] >= width and stride[1] == 1
+        else:
+            whole = len(shape) == 3 and shape[1] * shape[2] == width and stride[2] == 1 and stride[1] == shape[2]
+        if not whole:
+            raise ValueError("%s has to have rows of %d elements side by side" % (name, width))
+        if shape[0] < rows_ub:
+            raise ValueError("%s has %d rows, fewer than rows_ub %d" % (name, shape[0], rows_ub))
 
     def plan(self, cu, rows_ub, keep=None, seqused=None, stream=None):
         """The pages and slots of a step; returns the slots of its rows."""
@@ -287,7 +320,9 @@ class PagedCache:
 
     def store(self, layer, k, v, rows_ub, slots=None, stream=None):
         """Rows of k and v ([rows, n_kv_heads * head_dim], any row stride) into the layer's pages."""
-        self._takes(rows_ub)
+        self._takes(rows_ub, slots=slots)
+        self._rows(rows_ub, "k", k, self.kv_width, self.kind)
+        self._rows(rows_ub, "v", v, self.kv_width, self.v_kind)
         S.seer_kv_store(self.desc, self.pages, k, k.stride(0), v, v.stride(0), rows_ub,
                         self.slots if slots is None else slots, self.pools[layer], stream=stream)
 
@@ -300,7 +335,7 @@ class PagedCache:
         flags = S.SEER_ATTN_V_F16 if bf16 else 0
         if (self.desc.n_kv_heads * self.desc.head_dim, self.desc.dtype, self.desc.flags) != (d, stack.dims.dtype, flags):
             raise ValueError("the cache's heads and types are not those of the layer's rows")
-        self._takes(rows_ub)
+        self._takes(rows_ub, slots=slots)
         es = 2 if bf16 else 4
         k = stack.workspace.data_ptr() + S.seer_layer_workspace_offsets(stack.dims, rows_ub)[0] + d * es
         S.seer_kv_store(self.desc, self.pages, k, 3 * d, k + d * es, 3 * d, rows_ub,
@@ -309,6 +344,13 @@ class PagedCache:
     def attend(self, layer, q, out, cu, rows_ub, mask=S.SEER_MASK_CAUSAL, tree_bits=None, seqused=None, stream=None):
         """Attention of the step's rows over their requests' pages."""
         self._takes(rows_ub, cu, None, seqused)
+        self._rows(rows_ub, "q", q, self.q_width, self.kind)
+        self._rows(rows_ub, "out", out, self.q_width, self.kind)
+        if tree_bits is not None:
+            if tree_bits.dtype not in (torch.int64, torch.uint64) or tree_bits.get_device() != self._device or \
+                    tree_bits.dim() != 2 or not tree_bits.is_contiguous() or tree_bits.shape[0] < rows_ub:
+                raise ValueError("tree_bits has to be [at least %d, words] int64, contiguous and on the cache's device"
+                                 % rows_ub)
         S.seer_attn_paged(self.desc, self.pages, mask, q, q.stride(0), out, out.stride(0), rows_ub, cu, seqused,
                           self.max_batch, self.pools[layer], self.table, self._lens[0], tree_bits,
                           0 if tree_bits is None else tree_bits.shape[1], self.workspace, self.ws_bytes, stream=stream)
@@ -316,6 +358,10 @@ class PagedCache:
     def prompt(self, q, k, v, out, cu, rows_ub, mask=S.SEER_MASK_CAUSAL, seqused=None, stream=None):
         """Attention of packed prompts over their own rows (no pages)."""
         self._takes(rows_ub, cu, None, seqused)
+        self._rows(rows_ub, "q", q, self.q_width, self.kind)
+        self._rows(rows_ub, "k", k, self.kv_width, self.kind)
+        self._rows(rows_ub, "v", v, self.kv_width, self.v_kind)
+        self._rows(rows_ub, "out", out, self.q_width, self.kind)
         S.seer_attn_prompt(self.desc, mask, q, q.stride(0), k, k.stride(0), v, v.stride(0), out, out.stride(0),
                            rows_ub, cu, seqused, self.max_batch, self.workspace, self.ws_bytes, stream=stream)
 
