@@ -248,6 +248,7 @@ class PagedCache:
         self._free = [torch.full((1,), n_pages, dtype=torch.int32, device=device), i32(1)]
         self._lens = [i32(max_batch), i32(max_batch)]
         self.slots = i32(max_rows)
+        self._planned = 0                             # rows whose slots are the last plan's
         self.status = i32(1)
         self.workspace = torch.empty(self.ws_bytes, dtype=torch.uint8, device=device)
         self._device = self.table.get_device()        # -1 on the CPU
@@ -276,6 +277,14 @@ class PagedCache:
             self._ints("seqused", seqused, self.max_batch)
         if slots is not None:
             self._ints("slots", slots, rows_ub)
+
+    def _slots(self, rows_ub, slots):
+        """The slots of a store; of the cache's own, no more than the last plan wrote."""
+        if slots is None or slots is self.slots:
+            if rows_ub > self._planned:
+                raise ValueError("rows_ub %d exceeds the %d rows of the last plan" % (rows_ub, self._planned))
+            return self.slots
+        return slots
 
     def _ints(self, name, x, n):
         if x.numel() < n:
@@ -306,6 +315,7 @@ class PagedCache:
                          self.status, stream=stream)
         self._lens.reverse()
         self._free.reverse()
+        self._planned = rows_ub
         return self.slots
 
     def check(self, stream=None):
@@ -323,8 +333,8 @@ class PagedCache:
         self._takes(rows_ub, slots=slots)
         self._rows(rows_ub, "k", k, self.kv_width, self.kind)
         self._rows(rows_ub, "v", v, self.kv_width, self.v_kind)
-        S.seer_kv_store(self.desc, self.pages, k, k.stride(0), v, v.stride(0), rows_ub,
-                        self.slots if slots is None else slots, self.pools[layer], stream=stream)
+        S.seer_kv_store(self.desc, self.pages, k, k.stride(0), v, v.stride(0), rows_ub, self._slots(rows_ub, slots),
+                        self.pools[layer], stream=stream)
 
     def store_layer(self, layer, stack, rows_ub, slots=None, stream=None):
         """The K | V columns that the stack's last layer call left in its
@@ -339,7 +349,7 @@ class PagedCache:
         es = 2 if bf16 else 4
         k = stack.workspace.data_ptr() + S.seer_layer_workspace_offsets(stack.dims, rows_ub)[0] + d * es
         S.seer_kv_store(self.desc, self.pages, k, 3 * d, k + d * es, 3 * d, rows_ub,
-                        self.slots if slots is None else slots, self.pools[layer], stream=stream)
+                        self._slots(rows_ub, slots), self.pools[layer], stream=stream)
 
     def attend(self, layer, q, out, cu, rows_ub, mask=S.SEER_MASK_CAUSAL, tree_bits=None, seqused=None, stream=None):
         """Attention of the step's rows over their requests' pages."""

@@ -108,3 +108,18 @@ def test_tree_bits(calls, S):
         _refused(calls, lambda: c.attend(0, q, q.clone(), cu, ROWS, S.SEER_MASK_TREE, bad), "tree_bits")
     c.attend(0, q, q.clone(), cu, ROWS, S.SEER_MASK_TREE, wide)
     assert len(calls) == 1 and calls[0][1][15] == 3
+
+
+def test_a_store_of_more_rows_than_were_planned(calls):
+    """Slots behind the last plan's rows are an earlier plan's: they would overwrite its tokens."""
+    c, k, cu = _cache(), _bf16(ROWS, KV * D), _i32(B + 1)
+    _refused(calls, lambda: c.store(0, k, k, 1), "last plan")
+    c.plan(cu, ROWS)
+    c.store(0, k, k, ROWS)
+    slots = c.plan(cu, 2)
+    for call in (lambda: c.store(0, k, k, 3), lambda: c.store(0, k, k, ROWS, slots), lambda: c.store(0, k, k, 3, c.slots)):
+        _refused(calls, call, "last plan")
+    c.store(0, k, k, 2)
+    c.store(0, k, k, 1, slots)
+    c.store(0, k, k, ROWS, _i32(ROWS))                # slots of the caller's own
+    assert [n for n, _ in calls] == ["seer_page_plan", "seer_kv_store"] * 2 + ["seer_kv_store"] * 2
