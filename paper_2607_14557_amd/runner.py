@@ -320,7 +320,12 @@ class PagedCache:
 
     def check(self, stream=None):
         """Raise SeerError if the last plan was refused; waits for `stream`."""
-        (stream or torch.cuda.current_stream(self.status.device)).synchronize()
+        if stream is None:
+            stream = torch.cuda.current_stream(self.status.device)
+        elif isinstance(stream, int):                 # a raw handle, as the other calls take it
+            stream = torch.cuda.ExternalStream(stream, self.status.device) if stream else \
+                torch.cuda.default_stream(self.status.device)
+        stream.synchronize()
         st = int(self.status.item())
         if st:
             why = [n for bit, n in ((S.SEER_PAGES_EXHAUSTED, "not enough free pages"),

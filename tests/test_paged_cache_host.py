@@ -123,3 +123,26 @@ def test_a_store_of_more_rows_than_were_planned(calls):
     c.store(0, k, k, 1, slots)
     c.store(0, k, k, ROWS, _i32(ROWS))                # slots of the caller's own
     assert [n for n, _ in calls] == ["seer_page_plan", "seer_kv_store"] * 2 + ["seer_kv_store"] * 2
+
+
+def test_check_takes_a_raw_handle(calls, S, monkeypatch):
+    """As every other call does: 0 is the default stream, whatever the current one is."""
+    waited = []
+
+    class Stream:
+        def __init__(self, name):
+            self.name = name
+
+        def synchronize(self):
+            waited.append(self.name)
+
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: Stream("current"))
+    monkeypatch.setattr(torch.cuda, "default_stream", lambda device=None: Stream("default"))
+    monkeypatch.setattr(torch.cuda, "ExternalStream", lambda handle, device=None: Stream(handle))
+    c = _cache()
+    for s in (None, 0, 12345, Stream("own")):
+        c.check(s)
+    assert waited == ["current", "default", 12345, "own"]
+    c.status.fill_(S.SEER_PAGES_WIDTH)
+    with pytest.raises(S.SeerError):
+        c.check(12345)
