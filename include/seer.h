@@ -553,6 +553,15 @@ int seer_page_plan(const seer_page_desc* pages, const int32_t* held, const int32
                    const int32_t* free_in, int32_t* free_out, int32_t* table, int32_t* kv_len, int32_t* slots,
                    int32_t* status, hipStream_t stream);
 
+/* seer_page_plan, where the bits of a plan that is refused are also added to
+ * *refused (device), which no call clears: *status is the last plan's, and of
+ * several plans in one recording, or of plans that nobody looked at, none goes
+ * unseen.  Errors: as seer_page_plan; EINVAL (refused NULL or status). */
+int seer_page_plan_latched(const seer_page_desc* pages, const int32_t* held, const int32_t* keep,
+                           const int32_t* cu_seqlens, const int32_t* seqused, int32_t batch, int32_t rows_ub,
+                           int32_t* free_pages, const int32_t* free_in, int32_t* free_out, int32_t* table,
+                           int32_t* kv_len, int32_t* slots, int32_t* status, int32_t* refused, hipStream_t stream);
+
 /* Copy key and value rows into their pages: row r < rows_ub of k and of v
  * (n_kv_heads * head_dim elements, rows k_stride and v_stride elements apart)
  * to slot slots[r] of the pool.  Rows whose slot is negative or past the pool

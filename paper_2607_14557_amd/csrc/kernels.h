@@ -307,6 +307,7 @@ struct PagePlanParams {
   int* kv_len;
   int* slots;
   int* status;
+  int* refused;          // or null
 };
 int launch_page_plan(const PagePlanParams& p, hipStream_t s);
 

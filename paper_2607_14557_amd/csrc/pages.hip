@@ -112,6 +112,7 @@ __global__ __launch_bounds__(PLAN_T) void page_plan_kernel(PagePlanParams p) {
   const int stride = gridDim.x * PLAN_T, first = blockIdx.x * PLAN_T + tid;
   if (first == 0) {
     *p.status = e;
+    if (e && p.refused) *p.refused |= e;
     *p.free_out = e ? in : (int)(in + gave - took);
   }
   if (e) {

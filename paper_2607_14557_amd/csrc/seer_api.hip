@@ -715,10 +715,10 @@ size_t seer_page_pool_bytes(const seer_attn_desc* desc, const seer_page_desc* pa
          (desc->dtype == SEER_DTYPE_BF16 ? 2 : 4);
 }
 
-int seer_page_plan(const seer_page_desc* pages, const int32_t* held, const int32_t* keep, const int32_t* cu_seqlens,
-                   const int32_t* seqused, int32_t batch, int32_t rows_ub, int32_t* free_pages,
-                   const int32_t* free_in, int32_t* free_out, int32_t* table, int32_t* kv_len, int32_t* slots,
-                   int32_t* status, hipStream_t stream) {
+static int page_plan(const seer_page_desc* pages, const int32_t* held, const int32_t* keep, const int32_t* cu_seqlens,
+                     const int32_t* seqused, int32_t batch, int32_t rows_ub, int32_t* free_pages,
+                     const int32_t* free_in, int32_t* free_out, int32_t* table, int32_t* kv_len, int32_t* slots,
+                     int32_t* status, int32_t* refused, hipStream_t stream) {
   int rc = check_pages(pages);
   if (rc) return rc;
   if (!held || !keep || !cu_seqlens || !free_pages || !free_in || !free_out || !table || !kv_len || !status)
@@ -734,9 +734,26 @@ int seer_page_plan(const seer_page_desc* pages, const int32_t* held, const int32
   p.shift = page_shift(pages); p.n_pages = pages->n_pages; p.width = pages->table_width;
   p.held = held; p.keep = keep; p.cu = cu_seqlens; p.used = seqused; p.B = batch; p.rows_ub = rows_ub;
   p.free_pages = free_pages; p.free_in = free_in; p.free_out = free_out;
-  p.table = table; p.kv_len = kv_len; p.slots = slots; p.status = status;
+  p.table = table; p.kv_len = kv_len; p.slots = slots; p.status = status; p.refused = refused;
   if (seer::launch_page_plan(p, stream)) return hip_fail("page plan launch");
   return ok();
+}
+
+int seer_page_plan(const seer_page_desc* pages, const int32_t* held, const int32_t* keep, const int32_t* cu_seqlens,
+                   const int32_t* seqused, int32_t batch, int32_t rows_ub, int32_t* free_pages,
+                   const int32_t* free_in, int32_t* free_out, int32_t* table, int32_t* kv_len, int32_t* slots,
+                   int32_t* status, hipStream_t stream) {
+  return page_plan(pages, held, keep, cu_seqlens, seqused, batch, rows_ub, free_pages, free_in, free_out, table, kv_len,
+                   slots, status, nullptr, stream);
+}
+
+int seer_page_plan_latched(const seer_page_desc* pages, const int32_t* held, const int32_t* keep,
+                           const int32_t* cu_seqlens, const int32_t* seqused, int32_t batch, int32_t rows_ub,
+                           int32_t* free_pages, const int32_t* free_in, int32_t* free_out, int32_t* table,
+                           int32_t* kv_len, int32_t* slots, int32_t* status, int32_t* refused, hipStream_t stream) {
+  if (!refused || refused == status) return fail(SEER_EINVAL, "refused may be neither NULL nor status");
+  return page_plan(pages, held, keep, cu_seqlens, seqused, batch, rows_ub, free_pages, free_in, free_out, table, kv_len,
+                   slots, status, refused, stream);
 }
 
 // a row operand: not null, 16-byte aligned, rows of `width` elements `stride` apart

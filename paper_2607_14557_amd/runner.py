@@ -250,6 +250,7 @@ class PagedCache:
         self.slots = i32(max_rows)
         self._planned = 0                             # rows whose slots are the last plan's
         self.status = i32(1)
+        self.refused = i32(1)                         # the bits of every refused plan since the last check
         self.workspace = torch.empty(self.ws_bytes, dtype=torch.uint8, device=device)
         self._device = self.table.get_device()        # -1 on the CPU
 
@@ -310,24 +311,27 @@ class PagedCache:
         """The pages and slots of a step; returns the slots of its rows."""
         self._takes(rows_ub, cu, keep, seqused)
         held = self._lens[0]
-        S.seer_page_plan(self.pages, held, held if keep is None else keep, cu, seqused, self.max_batch, rows_ub,
-                         self.free_pages, self._free[0], self._free[1], self.table, self._lens[1], self.slots,
-                         self.status, stream=stream)
+        S.seer_page_plan_latched(self.pages, held, held if keep is None else keep, cu, seqused, self.max_batch, rows_ub,
+                                 self.free_pages, self._free[0], self._free[1], self.table, self._lens[1], self.slots,
+                                 self.status, self.refused, stream=stream)
         self._lens.reverse()
         self._free.reverse()
         self._planned = rows_ub
         return self.slots
 
     def check(self, stream=None):
-        """Raise SeerError if the last plan was refused; waits for `stream`."""
+        """Raise SeerError if a plan since the last check was refused, in a recording too; waits for `stream`."""
         if stream is None:
             stream = torch.cuda.current_stream(self.status.device)
         elif isinstance(stream, int):                 # a raw handle, as the other calls take it
             stream = torch.cuda.ExternalStream(stream, self.status.device) if stream else \
                 torch.cuda.default_stream(self.status.device)
         stream.synchronize()
-        st = int(self.status.item())
+        st = int(self.refused.item())
         if st:
+            self.refused.zero_()
+            if self._device >= 0:
+                torch.cuda.current_stream(self.status.device).synchronize()     # before plans on other streams
             why = [n for bit, n in ((S.SEER_PAGES_EXHAUSTED, "not enough free pages"),
                                     (S.SEER_PAGES_WIDTH, "a request longer than max_len"),
                                     (S.SEER_PAGES_INVALID, "keep exceeds what a request holds")) if st & bit]

@@ -29,7 +29,7 @@ EXPORTED = ("seer_prepacked_bytes", "seer_prepack_weights", "seer_layer_workspac
             "seer_layer_forward_detect_timed", "seer_batch_repack",
             "seer_layer_forward_cached", "seer_kv_export", "seer_graph_begin", "seer_graph_end",
             "seer_graph_launch", "seer_graph_destroy", "seer_lm_head_workspace_bytes", "seer_lm_head_prepack",
-            "seer_lm_head_predict", "seer_remask_step", "seer_page_pool_bytes", "seer_page_plan", "seer_kv_store",
+            "seer_lm_head_predict", "seer_remask_step", "seer_page_pool_bytes", "seer_page_plan", "seer_page_plan_latched", "seer_kv_store",
             "seer_attn_workspace_bytes", "seer_attn_prompt", "seer_attn_paged", "seer_last_error",
             "seer_abi_version")
 
@@ -161,6 +161,8 @@ def load_library():
     L.seer_page_pool_bytes.restype = ctypes.c_size_t
     L.seer_page_plan.argtypes = [pages, _P, _P, _P, _P, _I, _I, _P, _P, _P, _P, _P, _P, _P, _P]
     L.seer_page_plan.restype = ctypes.c_int
+    L.seer_page_plan_latched.argtypes = [pages, _P, _P, _P, _P, _I, _I, _P, _P, _P, _P, _P, _P, _P, _P, _P]
+    L.seer_page_plan_latched.restype = ctypes.c_int
     L.seer_kv_store.argtypes = [heads, pages, _P, _L, _P, _L, _I, _P, _P, _P]
     L.seer_kv_store.restype = ctypes.c_int
     L.seer_attn_workspace_bytes.argtypes = [heads, _I, _I]
@@ -373,6 +375,14 @@ def seer_page_plan(pages, held, keep, cu_seqlens, seqused, batch, rows_ub, free_
         ctypes.byref(pages), _ptr(held), _ptr(keep), _ptr(cu_seqlens), _ptr(seqused), int(batch), int(rows_ub),
         _ptr(free_pages), _ptr(free_in), _ptr(free_out), _ptr(table), _ptr(kv_len), _ptr(slots), _ptr(status),
         _stream(stream)))
+
+
+def seer_page_plan_latched(pages, held, keep, cu_seqlens, seqused, batch, rows_ub, free_pages, free_in, free_out, table,
+                           kv_len, slots, status, refused, stream=None):
+    _check(load_library().seer_page_plan_latched(
+        ctypes.byref(pages), _ptr(held), _ptr(keep), _ptr(cu_seqlens), _ptr(seqused), int(batch), int(rows_ub),
+        _ptr(free_pages), _ptr(free_in), _ptr(free_out), _ptr(table), _ptr(kv_len), _ptr(slots), _ptr(status),
+        _ptr(refused), _stream(stream)))
 
 
 def seer_kv_store(desc, pages, k, k_stride, v, v_stride, rows_ub, slots, pool, stream=None):

@@ -1,5 +1,6 @@
 """What PagedCache takes and refuses (no GPU): types, rows, strides and sizes that the kernels would read past an end
 or take for something else."""
+import ctypes
 import os
 
 import pytest
@@ -20,7 +21,7 @@ def calls(S, monkeypatch):
     """The entry points' names as they are called, with no launch behind them."""
     from paper_2607_14557_amd import runner
     made = []
-    for name in ("seer_page_plan", "seer_kv_store", "seer_attn_paged", "seer_attn_prompt"):
+    for name in ("seer_page_plan_latched", "seer_kv_store", "seer_attn_paged", "seer_attn_prompt"):
         monkeypatch.setattr(runner.S, name, lambda *a, _name=name, **kw: made.append((_name, a)))
     return made
 
@@ -60,7 +61,7 @@ def test_arrays_of_requests(calls):
         _refused(calls, lambda: c.plan(cu, ROWS, None, bad), "seqused")
         _refused(calls, lambda: c.attend(0, q, q.clone(), cu, ROWS, seqused=bad), "seqused")
     c.plan(cu, ROWS, _i32(B), _i32(B + 5))
-    assert [n for n, _ in calls] == ["seer_page_plan"]
+    assert [n for n, _ in calls] == ["seer_page_plan_latched"]
 
 
 def test_slots(calls):
@@ -122,7 +123,7 @@ def test_a_store_of_more_rows_than_were_planned(calls):
     c.store(0, k, k, 2)
     c.store(0, k, k, 1, slots)
     c.store(0, k, k, ROWS, _i32(ROWS))                # slots of the caller's own
-    assert [n for n, _ in calls] == ["seer_page_plan", "seer_kv_store"] * 2 + ["seer_kv_store"] * 2
+    assert [n for n, _ in calls] == ["seer_page_plan_latched", "seer_kv_store"] * 2 + ["seer_kv_store"] * 2
 
 
 def test_check_takes_a_raw_handle(calls, S, monkeypatch):
@@ -143,6 +144,17 @@ def test_check_takes_a_raw_handle(calls, S, monkeypatch):
     for s in (None, 0, 12345, Stream("own")):
         c.check(s)
     assert waited == ["current", "default", 12345, "own"]
-    c.status.fill_(S.SEER_PAGES_WIDTH)
+    c.refused.fill_(S.SEER_PAGES_WIDTH)
     with pytest.raises(S.SeerError):
         c.check(12345)
+    c.check(12345)                                    # raised once
+
+
+def test_latched_plan_refusals(S):
+    fake = 1 << 20
+    args = [fake, fake + 4096, fake, None, 2, 10, fake, fake, fake + 256, fake, fake + 8192, fake, fake]
+    pages = ctypes.byref(S.seer_page_desc(64, 100, 10))
+    call = S.load_library().seer_page_plan_latched
+    assert call(pages, *args, None, None) == S.SEER_EINVAL
+    assert call(pages, *args, fake, None) == S.SEER_EINVAL and "refused" in S.seer_last_error()
+    assert call(pages, *(args[:4] + [0] + args[5:]), fake + 512, None) == S.SEER_EINVAL and "batch" in S.seer_last_error()
