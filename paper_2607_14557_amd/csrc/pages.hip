@@ -110,13 +110,14 @@ __global__ __launch_bounds__(PLAN_T) void page_plan_kernel(PagePlanParams p) {
   if (e == 0 && in + gave > p.n_pages) e = kPagesInvalid;
   if (e == 0 && took > in + gave) e = kPagesExhausted;
   const int stride = gridDim.x * PLAN_T, first = blockIdx.x * PLAN_T + tid;
+  const unsigned rows = p.rows_ub;   // up to 2^31 - 1: a row's index plus the stride passes an int
   if (first == 0) {
     *p.status = e;
     if (e && p.refused) *p.refused |= e;
     *p.free_out = e ? in : (int)(in + gave - took);
   }
   if (e) {
-    for (int r = first; r < p.rows_ub; r += stride) p.slots[r] = -1;
+    for (unsigned r = first; r < rows; r += stride) p.slots[r] = -1;
     for (int b = first; b < p.B; b += stride) p.kv_len[b] = p.held[b];
     return;
   }
@@ -145,7 +146,8 @@ __global__ __launch_bounds__(PLAN_T) void page_plan_kernel(PagePlanParams p) {
     const int s = top - k;
     return s < in ? p.free_pages[s] : given(s - in);
   };
-  for (int r = first; r < p.rows_ub; r += stride) {
+  for (unsigned at = first; at < rows; at += stride) {
+    const int r = at;
     int slot = -1;
     if (r < row_end[p.B - 1]) {
       const int b = first_above(row_end, p.B, r);
@@ -169,8 +171,7 @@ __global__ __launch_bounds__(PLAN_T) void page_plan_kernel(PagePlanParams p) {
 
 int launch_page_plan(const PagePlanParams& p, hipStream_t s) {
   const int n = p.rows_ub > p.B ? p.rows_ub : p.B;
-  int blocks = (n + PLAN_T - 1) / PLAN_T;
-  blocks = blocks > 256 ? 256 : blocks;
+  const int blocks = n > 256 * PLAN_T ? 256 : (n + PLAN_T - 1) / PLAN_T;
   hipLaunchKernelGGL(page_plan_kernel, dim3(blocks), dim3(PLAN_T), 3 * (size_t)p.B * sizeof(int), s, p);
   return hipGetLastError() == hipSuccess ? 0 : -1;
 }
