@@ -616,7 +616,7 @@ int seer_attn_prompt(const seer_attn_desc* desc, int32_t mask, const void* q, in
  *                     64 tree_words on are seen by none.
  * A row that sees no key gets a zero output.  Keys on a page whose table entry
  * is outside [0, n_pages) are seen by no row, and kv_len[b] counts up to
- * table_width * page_size.  tree_bits: NULL unless SEER_MASK_TREE.
+ * table_width * page_size and 2^31 - 1024.  tree_bits: NULL unless SEER_MASK_TREE.
  * Errors: as seer_attn_prompt; EINVAL (pages, tree_bits NULL or tree_words < 1
  * with SEER_MASK_TREE). */
 int seer_attn_paged(const seer_attn_desc* desc, const seer_page_desc* pages, int32_t mask, const void* q,

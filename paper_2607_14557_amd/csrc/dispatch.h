@@ -287,6 +287,14 @@ inline GqaRule gqa_rule(const GqaLaunch& g) {
   return best;
 }
 
+// The keys of a request over pages: no more than its row of the table has, and at most
+// 2^31 - 1024, so that a place up to four tiles behind the last key fits an int.
+constexpr int kGqaMostKeys = 0x7fffffff - 1023;
+constexpr int gqa_keys(int kv_len, int width, int shift) {
+  const long long room = (long long)width << shift, most = room < kGqaMostKeys ? room : kGqaMostKeys;
+  return kv_len < 0 ? 0 : (kv_len > most ? (int)most : kv_len);
+}
+
 // Whether the line of `all` blocks is cut in runs of one length (GqaCut): more blocks than
 // workgroups, and room for two runs a tile.  `tiles` goes up to 2^31 - 1.
 constexpr bool gqa_in_runs(int all, int most, int tiles) { return all > most && tiles > 1 && tiles <= most / 2; }

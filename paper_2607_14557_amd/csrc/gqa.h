@@ -40,9 +40,7 @@ __device__ __forceinline__ GqaSeq gqa_seq(const GqaParams& p, int b) {
   int used = p.used ? p.used[b] : s.len;
   s.used = used < 0 ? 0 : (used > s.len ? s.len : used);
   if (p.table) {
-    const long long most = (long long)p.width << p.shift;
-    const int nk = p.kv_len[b];
-    s.nk = nk < 0 ? 0 : (nk > most ? (int)most : nk);
+    s.nk = gqa_keys(p.kv_len[b], p.width, p.shift);
   } else {
     s.nk = s.used;
   }

@@ -45,3 +45,11 @@ def test_over_the_range(tmp_path):
                      int(2 ** rng.uniform(0, 31)), rng.randint(0, 1), int(bf16)))
     got = _ask(tmp_path, BODY, rows)
     assert set(got) <= {0, 3} and got.count(3) > 500
+
+
+def test_keys_of_a_request(tmp_path):
+    """No more than the table has, and four tiles behind the last key an int still holds their places."""
+    rows = [(n, w, s) for n in (-5, 0, 1, 63, 4096, 2 ** 30, 2 ** 31 - 1025, 2 ** 31 - 1024, 2 ** 31 - 1)
+            for w in (1, 10, 2 ** 23, 2 ** 31 - 1) for s in (4, 6, 8)]
+    got = _ask(tmp_path, "int answer(const long long* v) { return gqa_keys((int)v[0], (int)v[1], (int)v[2]); }", rows)
+    assert got == [max(0, min(n, w << s, 2 ** 31 - 1024)) for n, w, s in rows]
