@@ -573,7 +573,7 @@ int seer_kv_store(const seer_attn_desc* desc, const seer_page_desc* pages, const
                   const void* v, int64_t v_stride, int32_t rows_ub, const int32_t* slots, void* pool,
                   hipStream_t stream);
 
-/* Workspace bytes of the attention calls for up to rows_ub rows in batch
+/* Workspace bytes of the attention calls for up to rows_ub rows in up to batch
  * sequences: the partial results of launches that split the keys.  0 for a
  * bad description. */
 size_t seer_attn_workspace_bytes(const seer_attn_desc* desc, int32_t rows_ub, int32_t batch);

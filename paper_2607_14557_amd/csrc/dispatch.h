@@ -311,12 +311,15 @@ inline size_t gqa_part_bytes(int grid, int rt, int dim) {
   return gqa_record_bytes(grid) + (size_t)2 * grid * rt * ((dim > 64 ? 128 : 64) + 2) * 4;
 }
 
-// The most that any launch with these rows and requests needs, whatever its keys and mask.
+// The most that any launch with up to these rows and requests needs, whatever its keys and mask.
 inline size_t gqa_workspace(GqaLaunch g) {
   g.keys = 1 << 20;
   const int few = g.bf16 ? kGqaFew : kGqaF32;
   size_t most = gqa_part_bytes(gqa_cut_grid(g, few), few, g.dim);
-  if (g.bf16 && (long long)g.rows * (g.heads / g.n_kv) > 32ll * g.batch) {
+  // 128-row parts are for more than 32 rows a request, so the most requests of a call that has them
+  const long long tiled = ((long long)g.rows * (g.heads / g.n_kv) - 1) / 32;
+  if (g.bf16 && tiled > 0) {
+    g.batch = tiled < g.batch ? (int)tiled : g.batch;
     const size_t tile = gqa_part_bytes(gqa_cut_grid(g, kGqaTile), kGqaTile, g.dim);
     most = tile > most ? tile : most;
   }
