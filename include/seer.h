@@ -25,10 +25,11 @@
  *   seer_lm_head_prepack,      synthetic LM head (one-time weight layout;
  *   seer_lm_head_predict,      argmax + confidence) and
  *   seer_remask_step           low-confidence remasking between steps
- *   seer_page_plan,            paged keys and values: block tables and slot
- *   seer_kv_store,             maps from the requests' lengths, rows into
- *   seer_attn_paged,           their pages, attention over the pages, and
- *   seer_attn_prompt           over packed prompts with grouped heads
+ *   seer_page_plan, seer_page_plan_latched,
+ *   seer_kv_store,             paged keys and values: block tables and slot
+ *   seer_attn_paged,           maps from the requests' lengths, rows into
+ *   seer_attn_prompt           their pages, attention over the pages, and
+ *                              over packed prompts with grouped heads
  *
  * Conventions shared by every call:
  *   - Buffers are owned by the caller.  Pointers are device pointers unless a
@@ -534,7 +535,8 @@ size_t seer_page_pool_bytes(const seer_attn_desc* desc, const seer_page_desc* pa
  *   table[b][H .. N) (N > H) are taken from them;
  *   kv_len[b] = keep + real rows, the held[b] of the next call;
  *   slots[r] = page * page_size + slot of row r, -1 for rows that are padding
- *              and for rows from cu_seqlens[batch] up to rows_ub.
+ *              and for rows from cu_seqlens[batch] up to rows_ub, which is no
+ *              less than cu_seqlens[batch].
  * Free pages are a stack free_pages[n_pages] with *free_in entries: all pages
  * given back are put on it first, in order of request and entry, then pages
  * are taken off its top in the same order, so a call may take what it gives
@@ -592,7 +594,11 @@ size_t seer_attn_workspace_bytes(const seer_attn_desc* desc, int32_t rows_ub, in
  * before they are divided: they stay finite for values of up to 2^126 / (keys of
  * the request + 64), all fp16 values among them, and for scores that are finite
  * in fp32 (scale log2(e) q . k).  A key that a row does not see has no part in
- * it, whatever its k and v hold (NaN, infinity).
+ * it, whatever its k and v hold (NaN, infinity); an infinite value that it sees
+ * gives an infinity, or NaN where its probability rounds to zero.  The order of
+ * the sums, and whether a bf16 probability is rounded once or kept as two bf16
+ * values, go by the bounds of the call (rows_ub, batch, table_width): the same
+ * call gives the same bits, with other bounds they may differ by roundings.
  * workspace: seer_attn_workspace_bytes, 256-byte aligned; it holds nothing
  * between calls.
  * Errors: EINVAL (null pointers, batch or rows_ub < 1, an unknown mask or

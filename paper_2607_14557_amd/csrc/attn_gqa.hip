@@ -231,7 +231,7 @@ struct Rows32 {
           if (!(half[i] >> (8 * (r >> 2) + (r & 3)) & 1)) s[i][r] = -INFINITY;
     }
     // Probabilities against the reference maximum, rounded to V's type (half a step:
-    // bf16 2^-8, fp16 2^-11; the two bf16 values of FINE 2^-17) as the matrix
+    // bf16 2^-8, fp16 2^-11; the two bf16 values of FINE 2^-16) as the matrix
     // instruction takes them, and their sum in fp32, over the rounded values where
     // they are coarse, so that the weights add up to one.
     u32x4_t pf[2 * NI], pl[FINE ? 2 * NI : 1];
