@@ -218,9 +218,9 @@ class PagedCache:
     the cache's device, which has to be the current one; they share a workspace,
     so that calls on two streams, recordings among them, may not overlap.
 
-    Rows of q, k, v and out are [at least rows_ub, heads * head_dim] or [.., heads,
-    head_dim] in the cache's types with a row's elements side by side (row
-    strides are free), tree_bits [at least rows_ub, words] int64 and contiguous,
+    Rows of q, k, v and out are [at least rows_ub, heads * head_dim], or more dims
+    with the same elements, in the cache's types, a row's side by side in memory
+    (row strides are free), tree_bits [at least rows_ub, words] int64 and contiguous,
     cu, keep, seqused and slots int32 and contiguous; ValueError otherwise."""
 
     def __init__(self, n_heads, n_kv_heads, head_dim, n_layers, n_pages, page_size, max_batch, max_len, max_rows,
@@ -298,14 +298,21 @@ class PagedCache:
         if x.dtype is not kind or x.get_device() != self._device:
             raise ValueError("%s has to be %s on the cache's device" % (name, kind))
         shape, stride = x.shape, x.stride()
-        if len(shape) == 2:
-            whole = shape[1] >= width and stride[1] == 1
-        else:
-            whole = len(shape) == 3 and shape[1] * shape[2] == width and stride[2] == 1 and stride[1] == shape[2]
-        if not whole:
+        n = shape[1] if len(shape) == 2 and stride[1] == 1 else self._side_by_side(shape, stride)
+        if n < width:
             raise ValueError("%s has to have rows of %d elements side by side" % (name, width))
         if shape[0] < rows_ub:
             raise ValueError("%s has %d rows, fewer than rows_ub %d" % (name, shape[0], rows_ub))
+
+    @staticmethod
+    def _side_by_side(shape, stride):
+        """Elements of a row that lie one after the other in memory, 0 where it has gaps."""
+        n = 1 if len(shape) > 1 else 0
+        for size, step in zip(shape[:0:-1], stride[:0:-1]):
+            if size != 1 and step != n:
+                return 0
+            n *= size
+        return n
 
     def plan(self, cu, rows_ub, keep=None, seqused=None, stream=None):
         """The pages and slots of a step; returns the slots of its rows."""

@@ -80,7 +80,8 @@ def test_rows(calls, v_f16):
     q, k = _bf16(ROWS, H * D), _bf16(ROWS, KV * D)
     v = k.half() if v_f16 else k
     for bad in (q[:ROWS - 1], q[:, :H * D - 8], q.float(), q.half(), _bf16(H * D, ROWS).t(), _bf16(ROWS, 2 * H * D)[:, ::2],
-                q.view(ROWS, D, H).transpose(1, 2), q[0], q.view(ROWS, 2, H // 2, D)):
+                q.view(ROWS, D, H).transpose(1, 2), q[0],
+                q.view(ROWS, H // 2, 2, D).transpose(1, 2), _bf16(ROWS, H, 2 * D)[:, :, :D]):
         _refused(calls, lambda: c.attend(0, bad, q, cu, ROWS), "q ")
         _refused(calls, lambda: c.attend(0, q, bad, cu, ROWS), "out ")
         _refused(calls, lambda: c.prompt(bad, k, v, q, cu, ROWS), "q ")
@@ -99,7 +100,8 @@ def test_rows(calls, v_f16):
     c.attend(0, qkv, q, cu, 1)
     c.store(0, qkv[:, H * D:(H + KV) * D], v.view(ROWS, KV, D), ROWS)
     c.prompt(qkv[:, :H * D], qkv[:, H * D:(H + KV) * D], v, q, cu, ROWS)
-    assert len(calls) == 4
+    c.attend(0, q.view(ROWS, KV, H // KV, D), qkv.view(ROWS + 5, H + 2 * KV, D)[:, :H], cu, ROWS)
+    assert len(calls) == 5
 
 
 def test_tree_bits(calls, S):
