@@ -30,6 +30,11 @@
  *   seer_attn_paged,           maps from the requests' lengths, rows into
  *   seer_attn_prompt           their pages, attention over the pages, and
  *                              over packed prompts with grouped heads
+ *   seer_rope_rows,            rotary positions of rows, alone and on the way
+ *   seer_kv_store_rope,        into pages; the attention weight of each cached
+ *   seer_row_positions,        token, and eviction by it: a paged cache that
+ *   seer_attn_weights,         stays within a budget
+ *   seer_kv_evict
  *
  * Conventions shared by every call:
  *   - Buffers are owned by the caller.  Pointers are device pointers unless a
@@ -630,6 +635,165 @@ int seer_attn_paged(const seer_attn_desc* desc, const seer_page_desc* pages, int
                     const int32_t* seqused, int32_t batch, const void* pool, const int32_t* table,
                     const int32_t* kv_len, const uint64_t* tree_bits, int32_t tree_words, void* workspace,
                     size_t workspace_bytes, hipStream_t stream);
+
+/* ---- a paged cache within a budget -----------------------------------------
+ * A long context need not be kept whole: tokens that hardly any row attends to
+ * can give way.  Beside a layer's pool stand the marks of its tokens,
+ *   weight [n_pages][n_kv_heads][page_size] float: the attention weight that a
+ *          token has had so far, from the rows of its key/value head
+ *   number [n_pages][n_kv_heads][page_size] int32: its position in the request
+ * seer_kv_store_rope sets them for new tokens, seer_attn_weights adds to the
+ * weights, and seer_kv_evict keeps the heaviest tokens, each key/value head its
+ * own or all the same.  Kept tokens move, so that from then on a token's place
+ * in the cache is not its position: positions are counted apart
+ * (seer_row_positions) and turned into the keys before they are stored.  What an
+ * eviction keeps is the `keep` of the next seer_page_plan, which gives the
+ * pages back; attention over the pages needs no change, as it does not depend
+ * on the order of the keys before the call's rows.  A page belongs to one
+ * request. */
+
+/* Rotary positions: the pairs (a, b) of a head's first R = rotary_dim dims turn,
+ *   x'_a = m (x_a cos t - x_b sin t),  x'_b = m (x_b cos t + x_a sin t),
+ *   t = position * f_j,  j < R / 2,
+ * the others stay.  f_j = theta^(-2 j / R), for contexts beyond original_len
+ * (n) tokens by `scaling`, s = factor:
+ *   PLAIN   f_j
+ *   LINEAR  f_j / s
+ *   BASE    theta * s^(R / (R - 2)) in theta's place (R > 2)
+ *   BANDS   k f_j + (1 - k) f_j / s, k = (n f_j / 2 pi - low) / (high - low) in [0, 1]:
+ *           pairs of at least `high` turns within n stay, those of at most `low`
+ *           are stretched
+ *   RAMP    k f_j + (1 - k) f_j / s, k = 1 - (j - a) / (b - a) in [0, 1], with
+ *           d(t) = R ln(n / (2 pi t)) / (2 ln theta), a = max(floor d(high), 0),
+ *           b = min(ceil d(low), R - 1), b = a + 0.001 where it would not be above a
+ * m = magnitude; 0: 0.1 ln s + 1 for RAMP, 1 otherwise. */
+#define SEER_ROPE_HALF   0   /* a = j, b = j + R / 2 */
+#define SEER_ROPE_PAIRS  1   /* a = 2 j, b = 2 j + 1 */
+#define SEER_ROPE_PLAIN  0
+#define SEER_ROPE_LINEAR 1
+#define SEER_ROPE_BASE   2
+#define SEER_ROPE_BANDS  3
+#define SEER_ROPE_RAMP   4
+typedef struct seer_rope_desc {
+  int32_t layout;        /* SEER_ROPE_HALF, _PAIRS */
+  int32_t rotary_dim;    /* even, at most head_dim; 0: head_dim */
+  int32_t scaling;       /* SEER_ROPE_PLAIN ... _RAMP */
+  int32_t original_len;  /* BANDS and RAMP */
+  float theta;           /* > 1 */
+  float factor;          /* > 0, not for PLAIN */
+  float low, high;       /* BANDS and RAMP: 0 < low < high */
+  float magnitude;       /* >= 0 */
+} seer_rope_desc;
+
+/* seer_rope_rows flags: the transposed rotation, m (x_a cos t + x_b sin t) and
+ * m (x_b cos t - x_a sin t): what takes the gradient of a rotated row back, and
+ * where m = 1 the row itself. */
+#define SEER_ROPE_INVERSE 1
+
+/* The frequencies of a description, in turns a position (f_j / 2 pi), to
+ * turns[rotary_dim / 2] (host).  A program copies them to the device once and
+ * hands them to the calls below (or others of its own making).  Runs on the
+ * host.  Errors: EINVAL. */
+int seer_rope_turns(const seer_rope_desc* rope, int32_t head_dim, double* turns);
+
+/* Rotate rows: q (n_heads * head_dim elements, any row stride) to q_out and k
+ * (n_kv_heads * head_dim) to k_out, both or one of them (the other's pointers
+ * NULL).  Row r stands at positions[r] (device), 0 to 2^31 - 1; rows with a
+ * negative position are left as they are, in the outputs too.  q_out may be q and
+ * k_out k (with the same row stride); else outputs overlap no input.  q and k rows may lie in
+ * one buffer beside each other.  turns: device.  The angle is taken in fp64 and
+ * reduced to half a turn, its sine and cosine and the products are fp32, and
+ * the result is rounded once.
+ * Errors: EINVAL (desc, rope, null pointers, rows or strides not aligned to 16
+ * bytes, a stride below the row, rows_ub < 1, flags, the aliases above),
+ * EUNSUPPORTED (desc). */
+int seer_rope_rows(const seer_attn_desc* desc, const seer_rope_desc* rope, const double* turns, int32_t flags,
+                   const void* q, int64_t q_stride, const void* k, int64_t k_stride, void* q_out, int64_t q_out_stride,
+                   void* k_out, int64_t k_out_stride, int32_t rows_ub, const int32_t* positions, hipStream_t stream);
+
+/* seer_kv_store with rotary positions: row r of k, rotated, and of v go to slot
+ * slots[r] of the pool, and q is rotated to q_out as in seer_rope_rows (q and
+ * q_out NULL: no queries).  The token's marks become weight 0 and number
+ * positions[r], in all heads (weight and number NULL: no marks).  Rows with a
+ * negative position, a negative slot or one past the pool are skipped, their q
+ * too.  The slots of one call are distinct.
+ * Errors: as seer_rope_rows and seer_kv_store. */
+int seer_kv_store_rope(const seer_attn_desc* desc, const seer_page_desc* pages, const seer_rope_desc* rope,
+                       const double* turns, const void* q, int64_t q_stride, void* q_out, int64_t q_out_stride,
+                       const void* k, int64_t k_stride, const void* v, int64_t v_stride, int32_t rows_ub,
+                       const int32_t* positions, const int32_t* slots, void* pool, float* weight, int32_t* number,
+                       hipStream_t stream);
+
+/* The positions of a step's rows: row i of request b, one of the first
+ * seqused[b] (NULL: all), stands at base[b] + i (base NULL: seen[b] + i, both
+ * NULL: i); padding and rows from cu_seqlens[batch] up to rows_ub get -1.
+ * next[b] (optional) is base[b] plus the request's real rows, the seen[b] of the
+ * next step.  status (optional) is the plan's: where it was refused, every
+ * position is -1 and next[b] = seen[b].  All pointers are device pointers;
+ * positions may be NULL where rows_ub is 0.
+ * Errors: EINVAL (null pointers, batch < 1, rows_ub < 0, next equal to seen or base). */
+int seer_row_positions(const int32_t* cu_seqlens, const int32_t* seqused, int32_t batch, const int32_t* seen,
+                       const int32_t* base, const int32_t* status, int32_t rows_ub, int32_t* positions, int32_t* next,
+                       hipStream_t stream);
+
+/* Workspace bytes of seer_attn_weights for up to rows_ub rows, whatever `last`;
+ * 0 for a bad description. */
+size_t seer_attn_weights_workspace_bytes(const seer_attn_desc* desc, const seer_page_desc* pages, int32_t rows_ub,
+                                         int32_t batch);
+
+/* The attention weight that the call's rows give to each cached token: for
+ * token j of request b and key/value head g
+ *     weight[j, g] = decay prev[j, g] + sum over rows i and heads h of g of p_ihj,
+ * p the softmax of seer_attn_paged for the same arguments.  Of each request only
+ * the last `last` real rows count (0: all of them).  prev may be weight, NULL (the
+ * sum alone; so it is with decay 0, when prev is not read) or other marks.  The places of
+ * tokens on pages outside the pool, of requests without a row in the call, and those past
+ * kv_len are not written.  A row that sees no key gives nothing; a key that
+ * a row does not see has no part in it, whatever it holds.
+ * Precision: products of the given types summed in fp32; statistics,
+ * probabilities and sums in fp32, nothing rounded to fewer bits.  Each weight is
+ * summed in one order: the same call gives the same bits; with other bounds
+ * (rows_ub, batch, table_width) or another `last` they may differ by roundings.
+ * workspace: seer_attn_weights_workspace_bytes, 256-byte aligned; it holds
+ * nothing between calls.
+ * Errors: as seer_attn_paged; EINVAL (last < 0, decay negative or not finite),
+ * EUNSUPPORTED (batch > 4096; batch * n_kv_heads * table_width * page_size of
+ * 2^35 (bf16), 2^34 (fp32) or more). */
+int seer_attn_weights(const seer_attn_desc* desc, const seer_page_desc* pages, int32_t mask, const void* q,
+                      int64_t q_stride, int32_t rows_ub, const int32_t* cu_seqlens, const int32_t* seqused,
+                      int32_t batch, int32_t last, const void* pool, const int32_t* table, const int32_t* kv_len,
+                      const uint64_t* tree_bits, int32_t tree_words, float decay, const float* prev, float* weight,
+                      void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* seer_kv_evict flags: one choice for all key/value heads of a request, by the sum of
+ * the heads' weights (taken in fp64, rounded to fp32) and head 0's numbers. */
+#define SEER_EVICT_SHARED 1
+
+/* Workspace bytes of seer_kv_evict; 0 for a bad description. */
+size_t seer_kv_evict_workspace_bytes(const seer_attn_desc* desc, const seer_page_desc* pages, int32_t batch);
+
+/* Cut request b's cache of kv_len[b] tokens to N = min(budget[b], kv_len[b]), for
+ * each key/value head.  Tokens whose number is below `first`, or at least
+ * seen[b] - recent (seen[b]: tokens that the request has had so far), are
+ * protected: they are kept before any other.  Of either kind those with the
+ * larger weight are kept (NaN above all), of equal ones those in the lower
+ * places.  Kept tokens in places from N on move, in order, into the places below N
+ * that are given up: K and V in the pool, weight and number to weight_out and
+ * number_out.  These may be weight and number (in place: nothing else is
+ * written), or other marks, which then get all of the N kept tokens'.
+ * kept[b] = N: the `keep` of the next seer_page_plan.  Places on a page outside the pool hold
+ * nothing: they count as unprotected and lighter than any weight, and nothing
+ * is read from or written to them.
+ * workspace: seer_kv_evict_workspace_bytes, 256-byte aligned; it holds nothing
+ * between calls.
+ * Errors: EINVAL (descriptions, null pointers, flags, batch < 1, first or recent
+ * < 0, only one of weight_out and number_out in place, kept equal to kv_len or
+ * seen, alignment), EUNSUPPORTED (desc, page_size, batch * n_kv_heads >= 2^20),
+ * EWORKSPACE. */
+int seer_kv_evict(const seer_attn_desc* desc, const seer_page_desc* pages, int32_t flags, const int32_t* kv_len,
+                  const int32_t* budget, const int32_t* seen, int32_t batch, int32_t first, int32_t recent,
+                  const int32_t* table, void* pool, const float* weight, const int32_t* number, float* weight_out,
+                  int32_t* number_out, int32_t* kept, void* workspace, size_t workspace_bytes, hipStream_t stream);
 
 /* ---- recorded launch sequences (Sec. 3.5) -------------------------------
  * The graph-compatible execution paths replay a fixed launch sequence.  Every

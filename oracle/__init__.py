@@ -17,6 +17,8 @@ Modules (each function cites the passage of the paper it follows):
                values cached (Appendix D, KV-cache compatibility)
   paged     -- keys and values in pages: the book-keeping of a step, and the
                attention over pages and prompts (Appendix D, Sec. 3.6)
+  budget    -- rotary positions of any layout and scaling, the attention weight
+               of cached tokens, eviction by it (the paper is silent on them)
   rope      -- rotary position embedding of queries and keys (the paper is
                silent on positions; RoFormer's definition, rotate-half pairs)
 

@@ -326,4 +326,22 @@ inline size_t gqa_workspace(GqaLaunch g) {
   return most;
 }
 
+// ---- attention weight of cached tokens --------------------------------------------
+
+// Parts that a request's keys are cut in for the rows' statistics: what fills the chip
+// with waves, a tile of rows and a part each, but no more than 32 to join.
+constexpr int kWeightsWaves = 4096, kWeightsParts = 32;
+inline int weights_parts(long long rows, int batch, int heads, int n_kv, int tile) {
+  const long long tiles = ((rows * (heads / n_kv) + tile - 1) / tile + batch - 1) * n_kv;
+  const long long parts = kWeightsWaves / tiles;
+  return parts < 1 ? 1 : (parts > kWeightsParts ? kWeightsParts : (int)parts);
+}
+
+// The most (row, head, part) that any call with up to so many rows has: as tiles are at
+// least rows * heads / tile, rows * heads * parts is at most waves * tile where it is cut at all.
+inline long long weights_stats(long long rows, int heads, int tile) {
+  const long long all = rows * heads, cut = all > (long long)kWeightsWaves * tile ? all : (long long)kWeightsWaves * tile;
+  return cut < all * kWeightsParts ? cut : all * kWeightsParts;
+}
+
 }  // namespace seer

@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "common.h"
 #include "seer.h"
 
 namespace seer {
@@ -361,5 +362,100 @@ struct GqaParams {
 };
 int launch_gqa_bf16(const GqaParams& p, const GqaRule& r, hipStream_t s);
 int launch_gqa_f32(const GqaParams& p, const GqaRule& r, hipStream_t s);
+
+// ---- a cache within a budget ---------------------------------------------------
+
+// Rotary positions of rows; with a pool, k and v go into their pages.  Strides in bytes.
+struct RopeParams {
+  const uint8_t* q;            // or null
+  const uint8_t* k;
+  const uint8_t* v;
+  uint8_t* q_out;
+  uint8_t* k_out;
+  size_t q_stride, k_stride, v_stride, q_out_stride, k_out_stride;
+  int es;                      // bytes of an element
+  int n_heads, n_kv, dim;
+  int rot;                     // dims that turn
+  bool pairs, inverse;
+  float magnitude;
+  const double* turns;         // [rot / 2] turns a position
+  const int* positions;
+  int rows_ub;
+  const int* slots;
+  uint8_t* pool;               // or null
+  float* weight;               // the marks of the tokens, or null
+  int* number;
+  int shift, n_pages;
+};
+int launch_rope(const RopeParams& p, hipStream_t s);
+
+struct RowPositionsParams {
+  const int* cu;
+  const int* used;             // [B] or null
+  int B;
+  const int* seen;             // [B] or null
+  const int* base;             // [B] or null: seen
+  const int* status;           // of the plan, or null
+  int rows_ub;
+  int* positions;
+  int* next;                   // [B] or null
+};
+int launch_row_positions(const RowPositionsParams& p, hipStream_t s);
+
+constexpr int kWeightsMaxBatch = 4096;
+
+// Attention weight of cached tokens.
+struct WeightsParams {
+  const void* q;
+  long long q_stride;          // elements
+  const int* cu;
+  const int* used;             // [B] or null
+  int B, rows_ub;
+  int last;                    // rows of a request that count, 0: all
+  int n_heads, n_kv, head_dim;
+  int group;                   // n_heads / n_kv, and what divides by it
+  unsigned group_mul;
+  int group_shift;
+  float scale;
+  int mask;                    // kMask*
+  bool bf16;
+  const void* pool;
+  const int* table;
+  const int* kv_len;
+  int shift, n_pages, width;
+  const unsigned long long* bits;
+  int words;
+  float decay;
+  const float* prev;           // or null
+  float* weight;
+  int parts;                   // of a request's keys, whose statistics are joined
+  f32x2_t* stats;              // [rows that count][n_heads][parts] maximum, sum
+  float* lse;                  // [rows that count][n_heads] log2 of the sum
+};
+int launch_weights(const WeightsParams& p, hipStream_t s);
+
+// Eviction.  A list is what one head keeps, or all of them (shared).
+struct EvictParams {
+  int shift, n_pages, width;
+  const int* kv_len;
+  const int* budget;
+  const int* seen;
+  int B, first, recent;
+  bool shared;
+  int lists;                   // of a request: n_kv, or 1
+  const int* table;
+  int n_kv, head_pieces;       // 16-byte pieces of a head's row
+  uint8_t* pool;
+  const float* weight;
+  const int* number;
+  float* weight_out;
+  int* number_out;
+  int* kept;
+  int* counts;                 // [B * lists] moves
+  int* moves;                  // [B * lists][2][room] from, to
+  size_t room;
+  int parts;                   // workgroups of a list's moves
+};
+int launch_evict(const EvictParams& p, hipStream_t s);
 
 }  // namespace seer

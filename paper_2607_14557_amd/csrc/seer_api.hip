@@ -1,6 +1,7 @@
 // C ABI of the Seer hot path: argument checks, workspace layout and the launch
 // sequence of each entry point.  Kernels live in gemm_bf16.hip, attn_bf16.hip,
-// attn_gqa.hip, attn_gqa_f32.hip, f32_kernels.hip, rows.hip and pages.hip.
+// attn_gqa.hip, attn_gqa_f32.hip, f32_kernels.hip, rows.hip, pages.hip, rope.hip,
+// attn_weights.hip and evict.hip.
 #include <math.h>
 #include <stdarg.h>
 #include <stdio.h>
@@ -888,6 +889,257 @@ int seer_attn_paged(const seer_attn_desc* desc, const seer_page_desc* pages, int
   p.shift = page_shift(pages); p.n_pages = pages->n_pages; p.width = pages->table_width;
   p.bits = reinterpret_cast<const unsigned long long*>(tree_bits); p.words = tree_words;
   return launch_gqa(p, desc, stream, "paged attention launch");
+}
+
+// ---- a cache within a budget --------------------------------------------------
+
+static int check_rope(const seer_rope_desc* r, int head_dim) {
+  if (!r) return fail(SEER_EINVAL, "rope is NULL");
+  if (r->layout != SEER_ROPE_HALF && r->layout != SEER_ROPE_PAIRS) return fail(SEER_EINVAL, "unknown layout %d", r->layout);
+  if (r->rotary_dim < 0 || r->rotary_dim > head_dim || r->rotary_dim % 2 != 0)
+    return fail(SEER_EINVAL, "rotary_dim must be even and in [0, head_dim %d] (got %d)", head_dim, r->rotary_dim);
+  if (r->rotary_dim == 0 && head_dim % 2 != 0) return fail(SEER_EINVAL, "a whole head that turns has an even head_dim");
+  if (r->scaling < SEER_ROPE_PLAIN || r->scaling > SEER_ROPE_RAMP) return fail(SEER_EINVAL, "unknown scaling %d", r->scaling);
+  if (!(r->theta > 1.0f) || !isfinite(r->theta)) return fail(SEER_EINVAL, "theta must be finite and > 1");
+  if (!(r->magnitude >= 0.0f) || !isfinite(r->magnitude)) return fail(SEER_EINVAL, "magnitude must be finite and >= 0");
+  if (r->scaling != SEER_ROPE_PLAIN && (!(r->factor > 0.0f) || !isfinite(r->factor)))
+    return fail(SEER_EINVAL, "factor must be finite and > 0");
+  if (r->scaling == SEER_ROPE_BANDS || r->scaling == SEER_ROPE_RAMP) {
+    if (!(r->low > 0.0f) || !(r->high > r->low) || !isfinite(r->high))
+      return fail(SEER_EINVAL, "low and high must be finite, 0 < low < high");
+    if (r->original_len < 1) return fail(SEER_EINVAL, "original_len must be >= 1 (got %d)", r->original_len);
+  }
+  return SEER_OK;
+}
+
+static int rope_dims(const seer_rope_desc* r, int head_dim) { return r->rotary_dim ? r->rotary_dim : head_dim; }
+
+int seer_rope_turns(const seer_rope_desc* rope, int32_t head_dim, double* turns) {
+  if (head_dim < 2 || head_dim > 128) return fail(SEER_EINVAL, "head_dim must be in [2, 128] (got %d)", head_dim);
+  int rc = check_rope(rope, head_dim);
+  if (rc) return rc;
+  if (!turns) return fail(SEER_EINVAL, "turns is NULL");
+  const double two_pi = 6.283185307179586476925, R = rope_dims(rope, head_dim), s = rope->factor, len = rope->original_len;
+  double theta = rope->theta, lo = 0.0, hi = 0.0;
+  if (rope->scaling == SEER_ROPE_BASE && R > 2) theta *= pow(s, R / (R - 2.0));
+  if (rope->scaling == SEER_ROPE_RAMP) {
+    // the pair that makes so many turns in the trained length
+    auto pair_of = [&](double turns_made) { return R * log(len / (two_pi * turns_made)) / (2.0 * log(theta)); };
+    lo = fmax(floor(pair_of(rope->high)), 0.0);
+    hi = fmin(ceil(pair_of(rope->low)), R - 1.0);
+    if (hi <= lo) hi = lo + 0.001;
+  }
+  for (int j = 0; j < (int)R / 2; ++j) {
+    double f = pow(theta, -2.0 * j / R) / two_pi, keep = 1.0;      // keep: the share that is not stretched
+    if (rope->scaling == SEER_ROPE_LINEAR) keep = 0.0;
+    if (rope->scaling == SEER_ROPE_BANDS)
+      keep = fmin(fmax((len * f - rope->low) / ((double)rope->high - rope->low), 0.0), 1.0);
+    if (rope->scaling == SEER_ROPE_RAMP) keep = 1.0 - fmin(fmax((j - lo) / (hi - lo), 0.0), 1.0);
+    turns[j] = keep == 1.0 ? f : f * keep + f / s * (1.0 - keep);
+  }
+  return ok();
+}
+
+// what both rotary calls check and fill in; q may be NULL
+static int rope_params(seer::RopeParams& p, const seer_attn_desc* desc, const seer_rope_desc* rope, const double* turns,
+                       const void* q, int64_t q_stride, void* q_out, int64_t q_out_stride, int32_t rows_ub,
+                       const int32_t* positions) {
+  int rc = check_heads(desc);
+  if (rc) return rc;
+  if ((rc = check_rope(rope, desc->head_dim))) return rc;
+  const int es = desc->dtype == SEER_DTYPE_BF16 ? 2 : 4;
+  const int64_t width = (int64_t)desc->n_heads * desc->head_dim;
+  if (!q != !q_out) return fail(SEER_EINVAL, "q and q_out go together");
+  if (q && ((rc = check_rows("q", q, q_stride, width, es)) || (rc = check_rows("q_out", q_out, q_out_stride, width, es))))
+    return rc;
+  if (q && q == q_out && q_stride != q_out_stride) return fail(SEER_EINVAL, "q_out in q's place needs its row stride");
+  if (rows_ub < 1) return fail(SEER_EINVAL, "rows_ub must be >= 1 (got %d)", rows_ub);
+  if (!turns || !positions) return fail(SEER_EINVAL, "a required pointer is NULL");
+  p.q = static_cast<const uint8_t*>(q); p.q_out = static_cast<uint8_t*>(q_out);
+  p.q_stride = (size_t)q_stride * es; p.q_out_stride = (size_t)q_out_stride * es;
+  p.es = es; p.n_heads = desc->n_heads; p.n_kv = desc->n_kv_heads; p.dim = desc->head_dim;
+  p.rot = rope_dims(rope, desc->head_dim); p.pairs = rope->layout == SEER_ROPE_PAIRS;
+  p.magnitude = rope->magnitude != 0.0f ? rope->magnitude
+                : rope->scaling == SEER_ROPE_RAMP ? (float)(0.1 * log((double)rope->factor) + 1.0) : 1.0f;
+  p.turns = turns; p.positions = positions; p.rows_ub = rows_ub;
+  return SEER_OK;
+}
+
+int seer_rope_rows(const seer_attn_desc* desc, const seer_rope_desc* rope, const double* turns, int32_t flags,
+                   const void* q, int64_t q_stride, const void* k, int64_t k_stride, void* q_out, int64_t q_out_stride,
+                   void* k_out, int64_t k_out_stride, int32_t rows_ub, const int32_t* positions, hipStream_t stream) {
+  seer::RopeParams p{};
+  int rc = rope_params(p, desc, rope, turns, q, q_stride, q_out, q_out_stride, rows_ub, positions);
+  if (rc) return rc;
+  if (flags & ~SEER_ROPE_INVERSE) return fail(SEER_EINVAL, "unknown flags %d", flags);
+  if (!k != !k_out) return fail(SEER_EINVAL, "k and k_out go together");
+  if (!q && !k) return fail(SEER_EINVAL, "neither q nor k");
+  const int64_t width = (int64_t)p.n_kv * p.dim;
+  if (k && ((rc = check_rows("k", k, k_stride, width, p.es)) || (rc = check_rows("k_out", k_out, k_out_stride, width, p.es))))
+    return rc;
+  if (k && k == k_out && k_stride != k_out_stride) return fail(SEER_EINVAL, "k_out in k's place needs its row stride");
+  if (q && k && q_out == k_out) return fail(SEER_EINVAL, "q_out may not be k_out");
+  if (q && k && (q_out == k || k_out == q)) return fail(SEER_EINVAL, "q_out may not be k, nor k_out q");
+  p.k = static_cast<const uint8_t*>(k); p.k_out = static_cast<uint8_t*>(k_out);
+  p.k_stride = (size_t)k_stride * p.es; p.k_out_stride = (size_t)k_out_stride * p.es;
+  p.inverse = (flags & SEER_ROPE_INVERSE) != 0;
+  if (seer::launch_rope(p, stream)) return hip_fail("rope launch");
+  return ok();
+}
+
+int seer_kv_store_rope(const seer_attn_desc* desc, const seer_page_desc* pages, const seer_rope_desc* rope,
+                       const double* turns, const void* q, int64_t q_stride, void* q_out, int64_t q_out_stride,
+                       const void* k, int64_t k_stride, const void* v, int64_t v_stride, int32_t rows_ub,
+                       const int32_t* positions, const int32_t* slots, void* pool, float* weight, int32_t* number,
+                       hipStream_t stream) {
+  seer::RopeParams p{};
+  int rc = rope_params(p, desc, rope, turns, q, q_stride, q_out, q_out_stride, rows_ub, positions);
+  if (rc) return rc;
+  if ((rc = check_pages(pages))) return rc;
+  const int64_t width = (int64_t)p.n_kv * p.dim;
+  if ((rc = check_rows("k", k, k_stride, width, p.es)) || (rc = check_rows("v", v, v_stride, width, p.es))) return rc;
+  if (!slots || !pool) return fail(SEER_EINVAL, "a required pointer is NULL");
+  if (!aligned(pool, 16)) return fail(SEER_EINVAL, "pool must be 16-byte aligned");
+  if (!weight != !number) return fail(SEER_EINVAL, "weight and number go together");
+  if (q && (q_out == k || q_out == v || q_out == pool)) return fail(SEER_EINVAL, "q_out may not be k, v or the pool");
+  p.k = static_cast<const uint8_t*>(k); p.v = static_cast<const uint8_t*>(v);
+  p.k_stride = (size_t)k_stride * p.es; p.v_stride = (size_t)v_stride * p.es;
+  p.slots = slots; p.pool = static_cast<uint8_t*>(pool); p.weight = weight; p.number = number;
+  p.shift = page_shift(pages); p.n_pages = pages->n_pages;
+  if (seer::launch_rope(p, stream)) return hip_fail("rope store launch");
+  return ok();
+}
+
+int seer_row_positions(const int32_t* cu_seqlens, const int32_t* seqused, int32_t batch, const int32_t* seen,
+                       const int32_t* base, const int32_t* status, int32_t rows_ub, int32_t* positions, int32_t* next,
+                       hipStream_t stream) {
+  if (!cu_seqlens || (rows_ub > 0 && !positions)) return fail(SEER_EINVAL, "a required pointer is NULL");
+  if (batch < 1 || rows_ub < 0) return fail(SEER_EINVAL, "batch must be >= 1, rows_ub >= 0 (got %d, %d)", batch, rows_ub);
+  if (next && (next == seen || next == base)) return fail(SEER_EINVAL, "next may be neither seen nor base");
+  if (rows_ub == 0 && !next) return ok();
+  seer::RowPositionsParams p{};
+  p.cu = cu_seqlens; p.used = seqused; p.B = batch; p.seen = seen; p.base = base; p.status = status;
+  p.rows_ub = rows_ub; p.positions = positions; p.next = next;
+  if (seer::launch_row_positions(p, stream)) return hip_fail("row positions launch");
+  return ok();
+}
+
+static int weights_tile(const seer_attn_desc* d) { return d->dtype == SEER_DTYPE_BF16 ? 32 : 16; }
+
+size_t seer_attn_weights_workspace_bytes(const seer_attn_desc* desc, const seer_page_desc* pages, int32_t rows_ub,
+                                         int32_t batch) {
+  if (check_heads(desc) != SEER_OK || check_pages(pages) != SEER_OK) return 0;
+  if (rows_ub < 1 || batch < 1 || (long long)rows_ub * desc->n_heads >= (1ll << 31)) {
+    fail(SEER_EINVAL, "rows_ub and batch must be positive, rows_ub * n_heads below 2^31");
+    return 0;
+  }
+  return up256((size_t)seer::weights_stats(rows_ub, desc->n_heads, weights_tile(desc)) * 8) +
+         up256((size_t)rows_ub * desc->n_heads * 4);
+}
+
+int seer_attn_weights(const seer_attn_desc* desc, const seer_page_desc* pages, int32_t mask, const void* q,
+                      int64_t q_stride, int32_t rows_ub, const int32_t* cu_seqlens, const int32_t* seqused,
+                      int32_t batch, int32_t last, const void* pool, const int32_t* table, const int32_t* kv_len,
+                      const uint64_t* tree_bits, int32_t tree_words, float decay, const float* prev, float* weight,
+                      void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  int rc = check_heads(desc);
+  if (rc) return rc;
+  if ((rc = check_pages(pages))) return rc;
+  if (mask < SEER_MASK_NONE || mask > SEER_MASK_TREE) return fail(SEER_EINVAL, "unknown mask %d", mask);
+  const int es = desc->dtype == SEER_DTYPE_BF16 ? 2 : 4;
+  if ((rc = check_rows("q", q, q_stride, (int64_t)desc->n_heads * desc->head_dim, es))) return rc;
+  if (batch < 1 || batch > seer::kWeightsMaxBatch)
+    return fail(batch < 1 ? SEER_EINVAL : SEER_EUNSUPPORTED, "batch must be in [1, %d] (got %d)", seer::kWeightsMaxBatch,
+                batch);
+  if (rows_ub < 1) return fail(SEER_EINVAL, "rows_ub must be >= 1 (got %d)", rows_ub);
+  if (last < 0) return fail(SEER_EINVAL, "last must be >= 0 (got %d)", last);
+  if (!cu_seqlens || !pool || !table || !kv_len || !weight || !workspace)
+    return fail(SEER_EINVAL, "a required pointer is NULL");
+  if (!aligned(pool, 16)) return fail(SEER_EINVAL, "pool must be 16-byte aligned");
+  if (mask == SEER_MASK_TREE && (!tree_bits || tree_words < 1))
+    return fail(SEER_EINVAL, "SEER_MASK_TREE needs tree_bits and tree_words >= 1");
+  if (!(decay >= 0.0f) || !isfinite(decay)) return fail(SEER_EINVAL, "decay must be finite and >= 0");
+  if ((long long)rows_ub * desc->n_heads >= (1ll << 31))
+    return fail(SEER_EUNSUPPORTED, "rows_ub * n_heads must stay below 2^31 (got %d * %d)", rows_ub, desc->n_heads);
+  const int T = weights_tile(desc);
+  // tiles of keys are counted in 31 bits
+  if ((((long long)pages->table_width * pages->page_size + T - 1) / T) * desc->n_kv_heads * batch >= (1ll << 30))
+    return fail(SEER_EUNSUPPORTED, "batch * n_kv_heads * table_width * page_size must stay below 2^30 * %d", T);
+  if (!aligned(workspace, 256)) return fail(SEER_EINVAL, "workspace must be 256-byte aligned");
+  const size_t need = seer_attn_weights_workspace_bytes(desc, pages, rows_ub, batch);
+  if (workspace_bytes < need) return fail(SEER_EWORKSPACE, "workspace holds %zu bytes, need %zu", workspace_bytes, need);
+  seer::WeightsParams p{};
+  p.q = q; p.q_stride = q_stride; p.cu = cu_seqlens; p.used = seqused; p.B = batch; p.rows_ub = rows_ub; p.last = last;
+  p.n_heads = desc->n_heads; p.n_kv = desc->n_kv_heads; p.head_dim = desc->head_dim; p.group = p.n_heads / p.n_kv;
+  const seer::GqaDivisor div = seer::gqa_divisor(p.group);
+  p.group_mul = div.mul; p.group_shift = div.shift;
+  p.scale = desc->scale != 0.0f ? desc->scale : 1.0f / sqrtf((float)desc->head_dim);
+  p.mask = mask; p.bf16 = desc->dtype == SEER_DTYPE_BF16;
+  p.pool = pool; p.table = table; p.kv_len = kv_len;
+  p.shift = page_shift(pages); p.n_pages = pages->n_pages; p.width = pages->table_width;
+  p.bits = reinterpret_cast<const unsigned long long*>(tree_bits); p.words = tree_words;
+  p.decay = decay; p.prev = decay != 0.0f ? prev : nullptr; p.weight = weight;
+  long long rows = rows_ub;
+  if (last > 0 && (long long)last * batch < rows) rows = (long long)last * batch;
+  p.parts = seer::weights_parts(rows, batch, p.n_heads, p.n_kv, T);
+  p.stats = static_cast<seer::f32x2_t*>(workspace);
+  p.lse = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) +
+                                   up256((size_t)seer::weights_stats(rows_ub, p.n_heads, T) * 8));
+  if (seer::launch_weights(p, stream)) return hip_fail("attention weights launch");
+  return ok();
+}
+
+static size_t evict_room(const seer_page_desc* pages) {
+  return ((size_t)pages->table_width * pages->page_size / 2 + 63) / 64 * 64;
+}
+
+size_t seer_kv_evict_workspace_bytes(const seer_attn_desc* desc, const seer_page_desc* pages, int32_t batch) {
+  if (check_heads(desc) != SEER_OK || check_pages(pages) != SEER_OK) return 0;
+  if (batch < 1) {
+    fail(SEER_EINVAL, "batch must be >= 1 (got %d)", batch);
+    return 0;
+  }
+  const size_t lists = (size_t)batch * desc->n_kv_heads;
+  return up256(lists * 4) + lists * 2 * evict_room(pages) * 4;
+}
+
+int seer_kv_evict(const seer_attn_desc* desc, const seer_page_desc* pages, int32_t flags, const int32_t* kv_len,
+                  const int32_t* budget, const int32_t* seen, int32_t batch, int32_t first, int32_t recent,
+                  const int32_t* table, void* pool, const float* weight, const int32_t* number, float* weight_out,
+                  int32_t* number_out, int32_t* kept, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  int rc = check_heads(desc);
+  if (rc) return rc;
+  if ((rc = check_pages(pages))) return rc;
+  if (flags & ~SEER_EVICT_SHARED) return fail(SEER_EINVAL, "unknown flags %d", flags);
+  if (batch < 1) return fail(SEER_EINVAL, "batch must be >= 1 (got %d)", batch);
+  if (first < 0 || recent < 0) return fail(SEER_EINVAL, "first and recent must be >= 0 (got %d, %d)", first, recent);
+  if (!kv_len || !budget || !seen || !table || !pool || !weight || !number || !weight_out || !number_out || !kept || !workspace)
+    return fail(SEER_EINVAL, "a required pointer is NULL");
+  if (!aligned(pool, 16)) return fail(SEER_EINVAL, "pool must be 16-byte aligned");
+  if ((weight == weight_out) != (number == number_out))
+    return fail(SEER_EINVAL, "weight_out and number_out are both in place or neither is");
+  if (kept == kv_len || kept == seen) return fail(SEER_EINVAL, "kept may be neither kv_len nor seen");
+  if (!aligned(workspace, 256)) return fail(SEER_EINVAL, "workspace must be 256-byte aligned");
+  const size_t need = seer_kv_evict_workspace_bytes(desc, pages, batch);
+  if (workspace_bytes < need) return fail(SEER_EWORKSPACE, "workspace holds %zu bytes, need %zu", workspace_bytes, need);
+  seer::EvictParams p{};
+  p.shift = page_shift(pages); p.n_pages = pages->n_pages; p.width = pages->table_width;
+  p.kv_len = kv_len; p.budget = budget; p.seen = seen; p.B = batch; p.first = first; p.recent = recent;
+  p.shared = (flags & SEER_EVICT_SHARED) != 0;
+  p.lists = p.shared ? 1 : desc->n_kv_heads;
+  if ((long long)batch * p.lists >= 1 << 20)
+    return fail(SEER_EUNSUPPORTED, "batch * n_kv_heads must stay below 2^20 (got %d * %d)", batch, p.lists);
+  p.table = table; p.n_kv = desc->n_kv_heads;
+  p.head_pieces = desc->head_dim * (desc->dtype == SEER_DTYPE_BF16 ? 2 : 4) / 16;
+  p.pool = static_cast<uint8_t*>(pool); p.weight = weight; p.number = number;
+  p.weight_out = weight_out; p.number_out = number_out; p.kept = kept;
+  p.counts = static_cast<int*>(workspace);
+  p.moves = reinterpret_cast<int*>(static_cast<uint8_t*>(workspace) + up256((size_t)batch * desc->n_kv_heads * 4));
+  p.room = evict_room(pages);
+  const int lists = batch * p.lists;
+  p.parts = lists >= 2048 ? 1 : 2048 / lists > 64 ? 64 : 2048 / lists;
+  if (seer::launch_evict(p, stream)) return hip_fail("eviction launch");
+  return ok();
 }
 
 // ---- recorded launch sequences (Sec. 3.5, graph-compatible paths) ----------

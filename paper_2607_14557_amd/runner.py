@@ -304,6 +304,13 @@ class PagedCache:
         if shape[0] < rows_ub:
             raise ValueError("%s has %d rows, fewer than rows_ub %d" % (name, shape[0], rows_ub))
 
+    def _bits(self, rows_ub, tree_bits):
+        if tree_bits is not None:
+            if tree_bits.dtype not in (torch.int64, torch.uint64) or tree_bits.get_device() != self._device or \
+                    tree_bits.dim() != 2 or not tree_bits.is_contiguous() or tree_bits.shape[0] < rows_ub:
+                raise ValueError("tree_bits has to be [at least %d, words] int64, contiguous and on the cache's device"
+                                 % rows_ub)
+
     @staticmethod
     def _side_by_side(shape, stride):
         """Elements of a row that lie one after the other in memory, 0 where it has gaps."""
@@ -357,26 +364,26 @@ class PagedCache:
         workspace (made with the same rows_ub) into the layer's pages: the paged
         counterpart of seer_kv_export.  A bf16 layer leaves V in fp16, so the
         cache has to have v_f16."""
+        k, d, es = self._layer_rows(layer, stack, rows_ub, slots)
+        S.seer_kv_store(self.desc, self.pages, k, 3 * d, k + d * es, 3 * d, rows_ub,
+                        self._slots(rows_ub, slots), self.pools[layer], stream=stream)
+
+    def _layer_rows(self, layer, stack, rows_ub, slots):
+        """(address of the K columns in the stack's workspace, their number, bytes of an element)."""
         d, bf16 = stack.dims.d_model, stack.dtype == torch.bfloat16
         flags = S.SEER_ATTN_V_F16 if bf16 else 0
         if (self.desc.n_kv_heads * self.desc.head_dim, self.desc.dtype, self.desc.flags) != (d, stack.dims.dtype, flags):
             raise ValueError("the cache's heads and types are not those of the layer's rows")
         self._takes(rows_ub, slots=slots)
         es = 2 if bf16 else 4
-        k = stack.workspace.data_ptr() + S.seer_layer_workspace_offsets(stack.dims, rows_ub)[0] + d * es
-        S.seer_kv_store(self.desc, self.pages, k, 3 * d, k + d * es, 3 * d, rows_ub,
-                        self._slots(rows_ub, slots), self.pools[layer], stream=stream)
+        return stack.workspace.data_ptr() + S.seer_layer_workspace_offsets(stack.dims, rows_ub)[0] + d * es, d, es
 
     def attend(self, layer, q, out, cu, rows_ub, mask=S.SEER_MASK_CAUSAL, tree_bits=None, seqused=None, stream=None):
         """Attention of the step's rows over their requests' pages."""
         self._takes(rows_ub, cu, None, seqused)
         self._rows(rows_ub, "q", q, self.q_width, self.kind)
         self._rows(rows_ub, "out", out, self.q_width, self.kind)
-        if tree_bits is not None:
-            if tree_bits.dtype not in (torch.int64, torch.uint64) or tree_bits.get_device() != self._device or \
-                    tree_bits.dim() != 2 or not tree_bits.is_contiguous() or tree_bits.shape[0] < rows_ub:
-                raise ValueError("tree_bits has to be [at least %d, words] int64, contiguous and on the cache's device"
-                                 % rows_ub)
+        self._bits(rows_ub, tree_bits)
         S.seer_attn_paged(self.desc, self.pages, mask, q, q.stride(0), out, out.stride(0), rows_ub, cu, seqused,
                           self.max_batch, self.pools[layer], self.table, self._lens[0], tree_bits,
                           0 if tree_bits is None else tree_bits.shape[1], self.workspace, self.ws_bytes, stream=stream)
@@ -390,6 +397,166 @@ class PagedCache:
         self._rows(rows_ub, "out", out, self.q_width, self.kind)
         S.seer_attn_prompt(self.desc, mask, q, q.stride(0), k, k.stride(0), v, v.stride(0), out, out.stride(0),
                            rows_ub, cu, seqused, self.max_batch, self.workspace, self.ws_bytes, stream=stream)
+
+
+class BudgetCache(PagedCache):
+    """A PagedCache that stays within a budget: keys carry rotary positions, every
+    token the attention weight that it has had, and evict() keeps the heaviest
+    (seer_kv_store_rope, seer_row_positions, seer_attn_weights, seer_kv_evict).
+    A step of a program is
+
+        cache.plan(cu, rows_ub)                    # pages, slots, positions
+        for each layer:
+            cache.store(layer, k, v, rows_ub, q=q)            # q and k rotated
+            cache.attend(layer, q, out, cu, rows_ub, mask)
+            cache.weigh(layer, q, cu, rows_ub, mask)
+        for each layer:                            # now and then
+            cache.evict(layer, budget)             # the next plan gives the pages back
+
+    rope: a seer_rope_desc, or None for keys that are stored as they are.  seen
+    counts the tokens that each request has had; plan() goes on from it, or from
+    `base` where drafts were refused (with the `keep` that goes with them) or a
+    request has ended (0).  After evict() has cut every layer alike, plan() keeps
+    what it kept; a `keep` of the caller's may keep less, not more.  A cut layer
+    takes no other call before that plan, and no plan comes between the layers of
+    one cut: ValueError.  Calls after a refused plan mean nothing until check()
+    has raised it.
+
+    rows, types and streams as for PagedCache; budget, base int32 [max_batch]."""
+
+    def __init__(self, n_heads, n_kv_heads, head_dim, n_layers, n_pages, page_size, max_batch, max_len, max_rows,
+                 rope=None, dtype="bf16", v_f16=False, scale=0.0, device="cuda"):
+        super().__init__(n_heads, n_kv_heads, head_dim, n_layers, n_pages, page_size, max_batch, max_len, max_rows,
+                         dtype=dtype, v_f16=v_f16, scale=scale, device=device)
+        self._still = S.seer_rope_desc(S.SEER_ROPE_HALF, 2, S.SEER_ROPE_PLAIN, 0, 10000.0, 1.0, 0.0, 0.0, 0.0)
+        self._still_turns = torch.zeros(1, dtype=torch.float64, device=device)      # by no angle
+        self.rope, self.turns = self._still, self._still_turns
+        if rope is not None:
+            self.rope = rope
+            self.turns = torch.tensor(S.seer_rope_turns(rope, head_dim), dtype=torch.float64, device=device)
+        marks = (n_pages, n_kv_heads, page_size)
+        self.weights = [torch.zeros(marks, dtype=torch.float32, device=device) for _ in range(n_layers)]
+        self.numbers = [torch.zeros(marks, dtype=torch.int32, device=device) for _ in range(n_layers)]
+        self._seen = [torch.zeros(max_batch, dtype=torch.int32, device=device) for _ in range(2)]
+        self.positions = torch.zeros(max_rows, dtype=torch.int32, device=device)
+        self.kept = torch.zeros(max_batch, dtype=torch.int32, device=device)
+        self._cut = set()                             # layers that are cut since the last plan
+        self._cut_before = set()                      # and before it
+        need = max(S.seer_attn_weights_workspace_bytes(self.desc, self.pages, max_rows, max_batch),
+                   S.seer_kv_evict_workspace_bytes(self.desc, self.pages, max_batch), self.ws_bytes)
+        if need > self.ws_bytes:
+            self.ws_bytes = need
+            self.workspace = torch.empty(need, dtype=torch.uint8, device=device)
+
+    @property
+    def seen(self):
+        """[max_batch] int32: the tokens that each request has had, the position of its next."""
+        return self._seen[0]
+
+    def _whole(self, layer):
+        if layer in self._cut:
+            raise ValueError("layer %d is cut: the next call is plan()" % layer)
+
+    def plan(self, cu, rows_ub, keep=None, seqused=None, base=None, stream=None):
+        """The pages, slots and positions of a step; returns the slots of its rows."""
+        if base is not None:
+            self._ints("base", base, self.max_batch)
+            if base is self._seen[1]:
+                raise ValueError("base may not be the buffer that the plan writes")
+        if self._cut:
+            if len(self._cut) < len(self.pools):
+                raise ValueError("%d of %d layers are cut: a plan comes after all or none" % (len(self._cut), len(self.pools)))
+            keep = self.kept if keep is None else keep
+        slots = super().plan(cu, rows_ub, keep, seqused, stream=stream)
+        self._cut_before, self._cut = self._cut, set()
+        S.seer_row_positions(cu, seqused, self.max_batch, self._seen[0], base, self.status, rows_ub, self.positions,
+                             self._seen[1], stream=stream)
+        self._seen.reverse()
+        return slots
+
+    def check(self, stream=None):
+        """As PagedCache.check; where the last plan was refused, what was cut before it still is."""
+        try:
+            super().check(stream)
+        except S.SeerError:
+            self._cut |= self._cut_before
+            raise
+
+    def _positions(self, rows_ub, positions):
+        if positions is None or positions is self.positions:
+            if rows_ub > self._planned:
+                raise ValueError("rows_ub %d exceeds the %d rows of the last plan" % (rows_ub, self._planned))
+            return self.positions
+        self._ints("positions", positions, rows_ub)
+        return positions
+
+    def rotate(self, q, k, rows_ub, q_out=None, k_out=None, positions=None, inverse=False, stream=None):
+        """Rotary positions of rows of q and k (None: not these), in place or to q_out and k_out: for prompt()."""
+        self._takes(rows_ub)
+        positions = self._positions(rows_ub, positions)
+        q_out, k_out = q if q_out is None else q_out, k if k_out is None else k_out
+        for name, x, width in (("q", q, self.q_width), ("q_out", q_out, self.q_width), ("k", k, self.kv_width),
+                               ("k_out", k_out, self.kv_width)):
+            if x is not None:
+                self._rows(rows_ub, name, x, width, self.kind)
+        row = lambda x: 0 if x is None else x.stride(0)
+        S.seer_rope_rows(self.desc, self.rope, self.turns, S.SEER_ROPE_INVERSE if inverse else 0, q, row(q), k, row(k),
+                         q_out, row(q_out), k_out, row(k_out), rows_ub, positions, stream=stream)
+
+    def store(self, layer, k, v, rows_ub, slots=None, stream=None, q=None, q_out=None, positions=None):
+        """Rows of k, rotated, and v into the layer's pages, with new marks; q, if given, rotated in place or to q_out."""
+        self._takes(rows_ub, slots=slots)
+        self._whole(layer)
+        self._rows(rows_ub, "k", k, self.kv_width, self.kind)
+        self._rows(rows_ub, "v", v, self.kv_width, self.v_kind)
+        q_out = q if q_out is None else q_out
+        for name, x in (("q", q), ("q_out", q_out)):
+            if x is not None:
+                self._rows(rows_ub, name, x, self.q_width, self.kind)
+        row = lambda x: 0 if x is None else x.stride(0)
+        S.seer_kv_store_rope(self.desc, self.pages, self.rope, self.turns, q, row(q), q_out, row(q_out), k, k.stride(0),
+                             v, v.stride(0), rows_ub, self._positions(rows_ub, positions), self._slots(rows_ub, slots),
+                             self.pools[layer], self.weights[layer], self.numbers[layer], stream=stream)
+
+    def store_layer(self, layer, stack, rows_ub, slots=None, stream=None):
+        """As PagedCache.store_layer, with new marks: the layer's keys carry its own positions and are not rotated again."""
+        self._whole(layer)
+        k, d, es = self._layer_rows(layer, stack, rows_ub, slots)
+        S.seer_kv_store_rope(self.desc, self.pages, self._still, self._still_turns, None, 0, None, 0, k, 3 * d, k + d * es,
+                             3 * d, rows_ub, self._positions(rows_ub, None), self._slots(rows_ub, slots), self.pools[layer],
+                             self.weights[layer], self.numbers[layer], stream=stream)
+
+    def attend(self, layer, q, out, cu, rows_ub, mask=S.SEER_MASK_CAUSAL, tree_bits=None, seqused=None, stream=None):
+        """Attention of the step's rows over their requests' pages."""
+        self._whole(layer)
+        super().attend(layer, q, out, cu, rows_ub, mask, tree_bits, seqused, stream=stream)
+
+    def weigh(self, layer, q, cu, rows_ub, mask=S.SEER_MASK_CAUSAL, tree_bits=None, seqused=None, last=0, decay=1.0,
+              stream=None):
+        """Add the attention weight that the step's rows (of each request the last `last`, 0: all) give to the
+        cached tokens, whose weights so far count `decay` times."""
+        self._takes(rows_ub, cu, None, seqused)
+        self._whole(layer)
+        self._rows(rows_ub, "q", q, self.q_width, self.kind)
+        self._bits(rows_ub, tree_bits)
+        w = self.weights[layer]
+        S.seer_attn_weights(self.desc, self.pages, mask, q, q.stride(0), rows_ub, cu, seqused, self.max_batch, last,
+                            self.pools[layer], self.table, self._lens[0], tree_bits,
+                            0 if tree_bits is None else tree_bits.shape[1], decay, w, w, self.workspace, self.ws_bytes,
+                            stream=stream)
+
+    def evict(self, layer, budget, first=0, recent=0, shared=False, stream=None):
+        """Cut each request's cache in this layer to budget[b] tokens; returns the lengths kept.  Takes effect with the
+        next plan, and all layers are cut alike before it."""
+        self._takes(0)
+        self._whole(layer)
+        self._ints("budget", budget, self.max_batch)
+        w, n = self.weights[layer], self.numbers[layer]
+        S.seer_kv_evict(self.desc, self.pages, S.SEER_EVICT_SHARED if shared else 0, self._lens[0], budget, self._seen[0],
+                        self.max_batch, first, recent, self.table, self.pools[layer], w, n, w, n, self.kept,
+                        self.workspace, self.ws_bytes, stream=stream)
+        self._cut.add(layer)
+        return self.kept
 
 
 class SeerStack:

@@ -21,6 +21,10 @@ SEER_STATUS_V_RANGE = 1
 SEER_ATTN_V_F16 = 1
 SEER_MASK_NONE, SEER_MASK_CAUSAL, SEER_MASK_TREE = 0, 1, 2
 SEER_PAGES_EXHAUSTED, SEER_PAGES_WIDTH, SEER_PAGES_INVALID = 1, 2, 4
+SEER_ROPE_HALF, SEER_ROPE_PAIRS = 0, 1
+SEER_ROPE_PLAIN, SEER_ROPE_LINEAR, SEER_ROPE_BASE, SEER_ROPE_BANDS, SEER_ROPE_RAMP = 0, 1, 2, 3, 4
+SEER_ROPE_INVERSE = 1
+SEER_EVICT_SHARED = 1
 
 EXPORTED = ("seer_prepacked_bytes", "seer_prepack_weights", "seer_layer_workspace_bytes",
             "seer_layer_status_reset", "seer_layer_workspace_offsets", "seer_layer_forward_varlen",
@@ -30,7 +34,9 @@ EXPORTED = ("seer_prepacked_bytes", "seer_prepack_weights", "seer_layer_workspac
             "seer_layer_forward_cached", "seer_kv_export", "seer_graph_begin", "seer_graph_end",
             "seer_graph_launch", "seer_graph_destroy", "seer_lm_head_workspace_bytes", "seer_lm_head_prepack",
             "seer_lm_head_predict", "seer_remask_step", "seer_page_pool_bytes", "seer_page_plan", "seer_page_plan_latched", "seer_kv_store",
-            "seer_attn_workspace_bytes", "seer_attn_prompt", "seer_attn_paged", "seer_last_error",
+            "seer_attn_workspace_bytes", "seer_attn_prompt", "seer_attn_paged", "seer_rope_turns", "seer_rope_rows",
+            "seer_kv_store_rope", "seer_row_positions", "seer_attn_weights_workspace_bytes", "seer_attn_weights",
+            "seer_kv_evict_workspace_bytes", "seer_kv_evict", "seer_last_error",
             "seer_abi_version")
 
 
@@ -78,6 +84,12 @@ class seer_page_desc(ctypes.Structure):
 class seer_attn_desc(ctypes.Structure):
     _fields_ = [("n_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
                 ("dtype", ctypes.c_int32), ("flags", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+class seer_rope_desc(ctypes.Structure):
+    _fields_ = [("layout", ctypes.c_int32), ("rotary_dim", ctypes.c_int32), ("scaling", ctypes.c_int32),
+                ("original_len", ctypes.c_int32), ("theta", ctypes.c_float), ("factor", ctypes.c_float),
+                ("low", ctypes.c_float), ("high", ctypes.c_float), ("magnitude", ctypes.c_float)]
 
 
 _lib = None
@@ -172,6 +184,25 @@ def load_library():
     L.seer_attn_paged.argtypes = [heads, pages, _I, _P, _L, _P, _L, _I, _P, _P, _I, _P, _P, _P, _P, _I, _P,
                                   ctypes.c_size_t, _P]
     L.seer_attn_paged.restype = ctypes.c_int
+    rope = ctypes.POINTER(seer_rope_desc)
+    L.seer_rope_turns.argtypes = [rope, _I, ctypes.POINTER(ctypes.c_double)]
+    L.seer_rope_turns.restype = ctypes.c_int
+    L.seer_rope_rows.argtypes = [heads, rope, _P, _I, _P, _L, _P, _L, _P, _L, _P, _L, _I, _P, _P]
+    L.seer_rope_rows.restype = ctypes.c_int
+    L.seer_kv_store_rope.argtypes = [heads, pages, rope, _P, _P, _L, _P, _L, _P, _L, _P, _L, _I, _P, _P, _P, _P, _P, _P]
+    L.seer_kv_store_rope.restype = ctypes.c_int
+    L.seer_row_positions.argtypes = [_P, _P, _I, _P, _P, _P, _I, _P, _P, _P]
+    L.seer_row_positions.restype = ctypes.c_int
+    L.seer_attn_weights_workspace_bytes.argtypes = [heads, pages, _I, _I]
+    L.seer_attn_weights_workspace_bytes.restype = ctypes.c_size_t
+    L.seer_attn_weights.argtypes = [heads, pages, _I, _P, _L, _I, _P, _P, _I, _I, _P, _P, _P, _P, _I, ctypes.c_float, _P,
+                                    _P, _P, ctypes.c_size_t, _P]
+    L.seer_attn_weights.restype = ctypes.c_int
+    L.seer_kv_evict_workspace_bytes.argtypes = [heads, pages, _I]
+    L.seer_kv_evict_workspace_bytes.restype = ctypes.c_size_t
+    L.seer_kv_evict.argtypes = [heads, pages, _I, _P, _P, _P, _I, _I, _I, _P, _P, _P, _P, _P, _P, _P, _P, ctypes.c_size_t,
+                                _P]
+    L.seer_kv_evict.restype = ctypes.c_int
     L.seer_last_error.argtypes = []
     L.seer_last_error.restype = ctypes.c_char_p
     L.seer_abi_version.argtypes = []
@@ -412,3 +443,59 @@ def seer_attn_paged(desc, pages, mask, q, q_stride, out, out_stride, rows_ub, cu
         ctypes.byref(desc), ctypes.byref(pages), int(mask), _ptr(q), int(q_stride), _ptr(out), int(out_stride),
         int(rows_ub), _ptr(cu_seqlens), _ptr(seqused), int(batch), _ptr(pool), _ptr(table), _ptr(kv_len),
         _ptr(tree_bits), int(tree_words), _ptr(workspace), nbytes, _stream(stream)))
+
+
+def seer_rope_turns(rope, head_dim):
+    """The frequencies as a list of turns a position; runs on the host."""
+    out = (ctypes.c_double * 64)()
+    _check(load_library().seer_rope_turns(ctypes.byref(rope), int(head_dim), out))
+    return list(out)[:(rope.rotary_dim or int(head_dim)) // 2]
+
+
+def seer_rope_rows(desc, rope, turns, flags, q, q_stride, k, k_stride, q_out, q_out_stride, k_out, k_out_stride, rows_ub,
+                   positions, stream=None):
+    """turns: fp64 device tensor of seer_rope_turns."""
+    _check(load_library().seer_rope_rows(
+        ctypes.byref(desc), ctypes.byref(rope), _ptr(turns), int(flags), _ptr(q), int(q_stride), _ptr(k), int(k_stride),
+        _ptr(q_out), int(q_out_stride), _ptr(k_out), int(k_out_stride), int(rows_ub), _ptr(positions), _stream(stream)))
+
+
+def seer_kv_store_rope(desc, pages, rope, turns, q, q_stride, q_out, q_out_stride, k, k_stride, v, v_stride, rows_ub,
+                       positions, slots, pool, weight, number, stream=None):
+    _check(load_library().seer_kv_store_rope(
+        ctypes.byref(desc), ctypes.byref(pages), ctypes.byref(rope), _ptr(turns), _ptr(q), int(q_stride), _ptr(q_out),
+        int(q_out_stride), _ptr(k), int(k_stride), _ptr(v), int(v_stride), int(rows_ub), _ptr(positions), _ptr(slots),
+        _ptr(pool), _ptr(weight), _ptr(number), _stream(stream)))
+
+
+def seer_row_positions(cu_seqlens, seqused, batch, seen, base, status, rows_ub, positions, next, stream=None):
+    _check(load_library().seer_row_positions(
+        _ptr(cu_seqlens), _ptr(seqused), int(batch), _ptr(seen), _ptr(base), _ptr(status), int(rows_ub), _ptr(positions),
+        _ptr(next), _stream(stream)))
+
+
+def seer_attn_weights_workspace_bytes(desc, pages, rows_ub, batch):
+    return load_library().seer_attn_weights_workspace_bytes(ctypes.byref(desc), ctypes.byref(pages), int(rows_ub),
+                                                            int(batch))
+
+
+def seer_attn_weights(desc, pages, mask, q, q_stride, rows_ub, cu_seqlens, seqused, batch, last, pool, table, kv_len,
+                      tree_bits, tree_words, decay, prev, weight, workspace, workspace_bytes=None, stream=None):
+    nbytes = workspace_bytes if workspace_bytes is not None else workspace.numel() * workspace.element_size()
+    _check(load_library().seer_attn_weights(
+        ctypes.byref(desc), ctypes.byref(pages), int(mask), _ptr(q), int(q_stride), int(rows_ub), _ptr(cu_seqlens),
+        _ptr(seqused), int(batch), int(last), _ptr(pool), _ptr(table), _ptr(kv_len), _ptr(tree_bits), int(tree_words),
+        float(decay), _ptr(prev), _ptr(weight), _ptr(workspace), nbytes, _stream(stream)))
+
+
+def seer_kv_evict_workspace_bytes(desc, pages, batch):
+    return load_library().seer_kv_evict_workspace_bytes(ctypes.byref(desc), ctypes.byref(pages), int(batch))
+
+
+def seer_kv_evict(desc, pages, flags, kv_len, budget, seen, batch, first, recent, table, pool, weight, number, weight_out,
+                  number_out, kept, workspace, workspace_bytes=None, stream=None):
+    nbytes = workspace_bytes if workspace_bytes is not None else workspace.numel() * workspace.element_size()
+    _check(load_library().seer_kv_evict(
+        ctypes.byref(desc), ctypes.byref(pages), int(flags), _ptr(kv_len), _ptr(budget), _ptr(seen), int(batch), int(first),
+        int(recent), _ptr(table), _ptr(pool), _ptr(weight), _ptr(number), _ptr(weight_out), _ptr(number_out), _ptr(kept),
+        _ptr(workspace), nbytes, _stream(stream)))
