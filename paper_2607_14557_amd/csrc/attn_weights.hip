@@ -12,9 +12,9 @@
 // that adds in one order: no atomics, the same bits every time.
 #include <limits.h>
 
-#include "common.h"
-#include "dispatch.h"
-#include "kernels.h"
+#include <type_traits>
+
+#include "gqa.h"
 
 namespace seer {
 
@@ -200,7 +200,360 @@ __device__ __forceinline__ int token_of(const WeightsParams& p, int x) {
   return (int)((__umulhi((unsigned)x, p.group_mul) + (unsigned)x) >> p.group_shift);
 }
 
+// Where the statistics of a request's rows for a key/value head begin: request after request, in each head
+// after head, in each row after row.
+__device__ __forceinline__ long long stat_row(const WeightsParams& p, const Line& l, const Seq& s, int b, int hk) {
+  return (long long)(l.rows[b] - s.used) * p.n_heads + (long long)hk * s.rows;
+}
+
+// ---- tiles of 64 in LDS, for requests of many rows (bf16) -------------------------
+// Both launches keep one operand in registers and pass the other by it in tiles of 64
+// rows, which the four waves share: two buffers in LDS, filled by direct loads.  Rows
+// lie in 16-byte pieces whose place is exchanged so that the reads of a fragment meet
+// distinct banks: piece c of row r at c ^ swz(r).
+constexpr int TILE = 64;
+template <int DH>
+__device__ __forceinline__ int swz(int r) { return DH == 128 ? r & 15 : (r >> 1) & 7; }
+
+template <int DH>
+struct Stream {
+  static constexpr int ROW = DH * 2, RPL = 1024 / ROW, LPR = ROW / 16, LOADS = 16 / RPL;
+  // 16 rows from `base` on, the lane's row of load q at off(RPL * q + lane / LPR) bytes
+  template <typename Off>
+  __device__ __forceinline__ static void load(const void* base, uint8_t* to, int lane, Off off) {
+    const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, -1, 0x00020000);
+#pragma unroll
+    for (int q = 0; q < LOADS; ++q) {
+      const int row = RPL * q + lane / LPR;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void_t*)(to + RPL * q * ROW), 16,
+                                               off(row) + ((uint32_t)((lane % LPR) ^ swz<DH>(row)) << 4), 0, 0, 0);
+    }
+  }
+  // products of the tile's rows 32 i .. 32 i + 31 with SETS sets of 32 rows in registers
+  template <int SETS>
+  __device__ __forceinline__ static void mul(f32x16_t (&a)[SETS], const uint8_t* tile, int i,
+                                             const bf16x8_t (&st)[SETS][DH / 16], int lane) {
+    const int fr = lane & 31;
+    const uint8_t* row = tile + (32 * i + fr) * ROW;
+#pragma unroll
+    for (int s = 0; s < SETS; ++s)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) a[s][r] = 0.0f;
+#pragma unroll
+    for (int ks = 0; ks < DH / 16; ++ks) {
+      const int c = (2 * ks + (lane >> 5)) ^ swz<DH>(fr);
+      const bf16x8_t f = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4_t*>(row + c * 16));
+#pragma unroll
+      for (int s = 0; s < SETS; ++s) a[s] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, st[s][ks], a[s], 0, 0, 0);
+    }
+  }
+};
+
+template <int DH>
+__device__ __forceinline__ void load_row(bf16x8_t (&f)[DH / 16], const uint16_t* at, int lane) {
+#pragma unroll
+  for (int ks = 0; ks < DH / 16; ++ks)
+    f[ks] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4_t*>(at + 16 * ks + 8 * (lane >> 5)));
+}
+
 }  // namespace
+
+// Maximum and sum of 128 SETS rows over a part of the keys, which pass by: a lane owns
+// SETS rows, half of each tile's keys, and needs no other lane before the end.  The
+// reference of a row's exponentials is the maximum of the first tile in which it sees a
+// key and moves only where a later tile adds up to 2^40 of it: any reference gives the
+// same sum, and the common tile takes no maximum.
+template <int DH, int SETS>
+__global__ __launch_bounds__(NT, 2) void weights_stats_tile_kernel(WeightsParams p) {
+  extern __shared__ int lds[];
+  __shared__ __attribute__((aligned(1024))) uint8_t tile0[TILE * DH * 2];
+  __shared__ __attribute__((aligned(1024))) uint8_t tile1[TILE * DH * 2];
+  constexpr int RT = 128 * SETS;
+  auto units = [&](const Seq& s) { return s.nk > 0 ? (s.rows + RT - 1) / RT * p.n_kv * p.parts : 0; };
+  const Line line = line_of(p, lds, units);
+  const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const float c = p.scale * 1.4426950408889634f;
+  const uint16_t* q = static_cast<const uint16_t*>(p.q);
+  const uint8_t* pool = static_cast<const uint8_t*>(p.pool);
+  for (int u = blockIdx.x; u < line.all; u += gridDim.x) {
+    int at;
+    const int b = __builtin_amdgcn_readfirstlane(request_of(line, p.B, u, at));
+    at = __builtin_amdgcn_readfirstlane(at);
+    const Seq s = seq_of(p, b);
+    const int tiles = (s.rows + RT - 1) / RT;
+    const int t = at % tiles, part = at / tiles % p.parts, hk = at / tiles / p.parts;
+    const int row0 = t * RT + wave * 32 * SETS;
+    bf16x8_t st[SETS][DH / 16];
+    int index[SETS];                             // of the lane's rows among the request's rows of the call
+    float m[SETS], l[SETS];
+#pragma unroll
+    for (int e = 0; e < SETS; ++e) {
+      const int row = row0 + 32 * e + (lane & 31), src = row < s.rows ? row : s.rows - 1;
+      const int tok = token_of(p, src), head = hk * p.group + src - tok * p.group;
+      load_row<DH>(st[e], q + (long long)(s.row0 + tok) * p.q_stride + (long long)head * DH, lane);
+      index[e] = s.index0 + tok;
+      m[e] = -INFINITY;
+      l[e] = 0.0f;
+    }
+    const int keys = part_keys(p, s.nk);
+    const long long begin = (long long)part * keys, end = begin + keys;
+    const int lo = begin < s.nk ? (int)begin : s.nk;
+    int hi = end < s.nk ? (int)end : s.nk;
+    // where the tile's rows see no more, and where the first one begins to be blind
+    const int last = token_of(p, t * RT + RT < s.rows ? t * RT + RT - 1 : s.rows - 1);
+    if (p.mask == kMaskCausal) {
+      const int stop = s.past + s.index0 + last + 1;
+      hi = stop < hi ? (stop > lo ? stop : lo) : hi;
+    }
+    const int first = s.past + s.index0 + token_of(p, row0 < s.rows ? row0 : s.rows - 1) + 1;
+    const int open = p.mask == kMaskCausal ? first : (p.mask == kMaskTree ? s.past : hi);
+    const int* table = p.table + (size_t)b * p.width;
+    const int n = (hi - lo + TILE - 1) / TILE;
+    int id[4];
+    auto pages = [&](int k0) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int key = k0 + 16 * i;
+        id[i] = scalar_load(table, (key < hi ? key : hi - 1) >> p.shift);
+      }
+    };
+    auto held = [&](int i) { return i >= 0 && i < p.n_pages; };
+    auto lost_of = [&]() {
+      unsigned long long x = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (!held(id[i])) x |= 0xffffull << (16 * i);
+      return x;
+    };
+    auto load = [&](int k0, uint8_t* to) {
+      int key = k0 + 16 * wave;                  // a group past the end is the last one again, as are keys past it
+      key = key < hi ? key : (hi - 1) & ~15;
+      const int mine = wave == 0 ? id[0] : (wave == 1 ? id[1] : (wave == 2 ? id[2] : id[3]));
+      const int most = hi - 1 - key < 15 ? hi - 1 - key : 15;
+      const long long row = ((held(mine) ? (long long)mine : 0) * 2 * p.n_kv << p.shift) + ((long long)hk << p.shift) +
+                            (key & ((1 << p.shift) - 1));
+      Stream<DH>::load(pool + row * (DH * 2), to + 16 * wave * DH * 2, lane,
+                       [&](int r) { return (uint32_t)((r < most ? r : most) * DH * 2); });
+    };
+    unsigned long long lost = 0, lost_next = 0;
+    if (n > 0) {
+      pages(lo);
+      load(lo, tile0);
+      lost = lost_of();
+      if (n > 1) pages(lo + TILE);
+    }
+    __builtin_amdgcn_s_waitcnt(0x0f70);          // vmcnt(0)
+    __syncthreads();
+    auto step = [&](int kt, auto buf) {
+      constexpr int B = decltype(buf)::value;
+      const int k0 = lo + TILE * kt;
+      if (kt + 1 < n) {
+        load(k0 + TILE, B ? tile0 : tile1);
+        lost_next = lost_of();
+        if (kt + 2 < n) pages(k0 + 2 * TILE);
+      }
+      if (row0 < s.rows) {
+        const bool masked = k0 + TILE > open || k0 + TILE > hi || lost != 0;
+        float x[SETS][2][16];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          f32x16_t a[SETS];
+          Stream<DH>::template mul<SETS>(a, B ? tile1 : tile0, i, st, lane);
+#pragma unroll
+          for (int e = 0; e < SETS; ++e)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) x[e][i][r] = a[e][r];
+        }
+        if (masked) {
+#pragma unroll
+          for (int e = 0; e < SETS; ++e) {
+            int lim = hi;
+            if (p.mask == kMaskCausal && s.past + index[e] + 1 < lim) lim = s.past + index[e] + 1;
+            const GqaSight<true> sight(lim, s.past, p.mask == kMaskTree ? p.bits + (size_t)(s.row0 - s.index0 + index[e]) * p.words
+                                                                       : nullptr, p.words);
+            const unsigned long long seen = (sight.seen(k0) & ~lost) >> (4 * (lane >> 5));
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const uint32_t half = (uint32_t)(seen >> (32 * i));
+#pragma unroll
+              for (int r = 0; r < 16; ++r)
+                if (!(half >> (8 * (r >> 2) + (r & 3)) & 1)) x[e][i][r] = -INFINITY;
+            }
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < SETS; ++e) {
+          float sum;
+          auto add = [&](float ref) {
+            float s0 = 0.0f, s1 = 0.0f;
+            const float mc = ref * c;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              s0 += __builtin_amdgcn_exp2f(__builtin_fmaf(x[e][0][r], c, -mc));
+              s1 += __builtin_amdgcn_exp2f(__builtin_fmaf(x[e][1][r], c, -mc));
+            }
+            sum = s0 + s1;
+          };
+          add(m[e]);
+          // (no key seen yet: the reference is -inf, and -inf + inf or x + inf ask for a maximum too)
+          if (__any(!(sum < 0x1p40f))) {
+            float top = m[e];
+#pragma unroll
+            for (int r = 0; r < 16; ++r) top = fmaxf(top, fmaxf(x[e][0][r], x[e][1][r]));
+            l[e] *= m[e] == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m[e] - top) * c);
+            m[e] = top;
+            add(top == -INFINITY ? 0.0f : top);
+          }
+          l[e] += sum;
+        }
+      }
+      lost = lost_next;
+      __builtin_amdgcn_s_waitcnt(0x0f70);
+      __syncthreads();
+    };
+    for (int kt = 0; kt < n; kt += 2) {
+      step(kt, std::integral_constant<int, 0>{});
+      if (kt + 1 < n) step(kt + 1, std::integral_constant<int, 1>{});
+    }
+#pragma unroll
+    for (int e = 0; e < SETS; ++e) {
+      const int row = row0 + 32 * e + (lane & 31);
+      const float top = fmaxf(m[e], __shfl_xor(m[e], 32, kWave)), ref = top == -INFINITY ? 0.0f : top;
+      const float part_l = l[e] * __builtin_amdgcn_exp2f((m[e] - ref) * c);
+      const float all = part_l + __shfl_xor(part_l, 32, kWave);
+      if (row < s.rows && lane < 32) {
+        const long long r = stat_row(p, line, s, b, hk) + row;
+        if (p.parts == 1) p.lse[r] = top * c + __builtin_amdgcn_logf(all);
+        else p.stats[r * p.parts + part] = f32x2_t{top * c, all};
+      }
+    }
+  }
+}
+
+// The weights of 128 SETS keys, which stay, from all rows, which pass by.
+template <int DH, int SETS>
+__global__ __launch_bounds__(NT, 2) void weights_sum_tile_kernel(WeightsParams p) {
+  extern __shared__ int lds[];
+  __shared__ __attribute__((aligned(1024))) uint8_t tile0[TILE * DH * 2];
+  __shared__ __attribute__((aligned(1024))) uint8_t tile1[TILE * DH * 2];
+  __shared__ __attribute__((aligned(16))) float lse_lds[2][TILE];
+  __shared__ __attribute__((aligned(16))) int lim_lds[2][TILE];        // the keys before it are seen
+  constexpr int KT = 128 * SETS;
+  auto units = [&](const Seq& s) { return s.used > 0 ? (s.nk + KT - 1) / KT * p.n_kv : 0; };
+  const Line line = line_of(p, lds, units);
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const float c = p.scale * 1.4426950408889634f;
+  const uint8_t* q = static_cast<const uint8_t*>(p.q);
+  const uint16_t* pool = static_cast<const uint16_t*>(p.pool);
+  for (int u = blockIdx.x; u < line.all; u += gridDim.x) {
+    int at;
+    const int b = __builtin_amdgcn_readfirstlane(request_of(line, p.B, u, at));
+    at = __builtin_amdgcn_readfirstlane(at);
+    const Seq s = seq_of(p, b);
+    const int tiles = (s.nk + KT - 1) / KT;
+    const int hk = at / tiles, key0 = (at - hk * tiles) * KT, k0 = key0 + wave * 32 * SETS;
+    const int* table = p.table + (size_t)b * p.width;
+    bf16x8_t st[SETS][DH / 16];
+    long long mark[SETS];                        // where the lane's keys' weights are, -1: nowhere
+    float sum[SETS];
+#pragma unroll
+    for (int e = 0; e < SETS; ++e) {
+      const int key = k0 + 32 * e + (lane & 31), src = key < s.nk ? key : s.nk - 1;
+      bool held;
+      load_row<DH>(st[e], pool + key_row(p, table, hk, src, held), lane);
+      const long long id = table[src >> p.shift];
+      mark[e] = key < s.nk && held ? (((id * p.n_kv) + hk) << p.shift) + (key & ((1 << p.shift) - 1)) : -1;
+      sum[e] = 0.0f;
+    }
+    // the first row that sees a key of the workgroup's, in whole tiles
+    int from = 0;
+    if (p.mask == kMaskCausal) {
+      const int token = key0 - s.past - s.index0;
+      if (token > 0) from = token < s.used ? token * p.group / TILE * TILE : s.rows;
+    }
+    const float* lse = p.lse + stat_row(p, line, s, b, hk);
+    const int n = (s.rows - from + TILE - 1) / TILE;
+    float next_lse = 0.0f;
+    int next_lim = 0;
+    auto load = [&](int r0, uint8_t* to) {
+      int row = r0 + 16 * wave;
+      row = row < s.rows ? row : s.rows - 1;     // rows past the end are the last one again
+      const int base = token_of(p, row);
+      const uint8_t* at = q + ((long long)(s.row0 + base) * p.q_stride + (long long)hk * p.group * DH) * 2;
+      const int most = s.rows - 1 - row < 15 ? s.rows - 1 - row : 15;
+      Stream<DH>::load(at, to + 16 * wave * DH * 2, lane, [&](int r) {
+        const int i = row + (r < most ? r : most), tok = token_of(p, i);
+        return (uint32_t)(tok - base) * (uint32_t)(p.q_stride * 2) + (uint32_t)(i - tok * p.group) * (DH * 2);
+      });
+      if (wave == 0) {
+        const int i = r0 + lane;
+        next_lse = i < s.rows ? lse[i] : INFINITY;
+        next_lim = p.mask == kMaskCausal ? s.past + s.index0 + token_of(p, i < s.rows ? i : s.rows - 1) + 1 : s.nk;
+      }
+    };
+    auto keep = [&](int B) {
+      if (wave == 0) {
+        lse_lds[B][lane] = next_lse;
+        lim_lds[B][lane] = next_lim;
+      }
+    };
+    if (n > 0) {
+      load(from, tile0);
+      keep(0);
+    }
+    __builtin_amdgcn_s_waitcnt(0x0f70);
+    __syncthreads();
+    auto step = [&](int rt, auto buf) {
+      constexpr int B = decltype(buf)::value;
+      const int r0 = from + TILE * rt;
+      if (rt + 1 < n) load(r0 + TILE, B ? tile0 : tile1);
+      if (k0 < s.nk) {
+        const int sure = p.mask == kMaskCausal ? s.past + s.index0 + token_of(p, r0) + 1
+                                               : (p.mask == kMaskTree ? s.past : s.nk);
+        const bool masked = p.mask != kMaskNone && k0 + 32 * SETS > sure;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          f32x16_t a[SETS];
+          Stream<DH>::template mul<SETS>(a, B ? tile1 : tile0, i, st, lane);
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            const int at = 32 * i + 8 * g + 4 * (lane >> 5);
+            const f32x4_t x = *reinterpret_cast<const f32x4_t*>(&lse_lds[B][at]);
+#pragma unroll
+            for (int e = 0; e < SETS; ++e)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) {
+                float w = __builtin_amdgcn_exp2f(__builtin_fmaf(a[e][4 * g + r], c, -x[r]));
+                if (masked) {
+                  const int key = k0 + 32 * e + (lane & 31);
+                  bool see = key < lim_lds[B][at + r];
+                  if (p.mask == kMaskTree && key >= s.past) {
+                    const int j = key - s.past, tok = token_of(p, r0 + at + r < s.rows ? r0 + at + r : s.rows - 1);
+                    see = j >> 6 < p.words && (p.bits[(size_t)(s.row0 + tok) * p.words + (j >> 6)] >> (j & 63) & 1);
+                  }
+                  w = see ? w : 0.0f;
+                }
+                sum[e] += w;
+              }
+          }
+        }
+      }
+      if (rt + 1 < n) keep(B ^ 1);
+      __builtin_amdgcn_s_waitcnt(0x0f70);
+      __syncthreads();
+    };
+    for (int rt = 0; rt < n; rt += 2) {
+      step(rt, std::integral_constant<int, 0>{});
+      if (rt + 1 < n) step(rt + 1, std::integral_constant<int, 1>{});
+    }
+#pragma unroll
+    for (int e = 0; e < SETS; ++e) {
+      const float all = sum[e] + __shfl_xor(sum[e], 32, kWave);
+      if (lane < 32 && mark[e] >= 0)
+        p.weight[mark[e]] = p.prev ? __builtin_fmaf(p.decay, p.prev[mark[e]], all) : all;
+    }
+  }
+}
 
 // Maximum and sum of the rows of a tile over a part of the keys: a wave a unit.
 template <typename Tile>
@@ -250,10 +603,7 @@ __global__ __launch_bounds__(NT) void weights_stats_kernel(WeightsParams p) {
     }
     const float top = Tile::max(m), ref = top == -INFINITY ? 0.0f : top;
     l = Tile::sum(l * __builtin_amdgcn_exp2f(m - ref));
-    if (row < s.rows && lane < T) {
-      const long long r = (line.rows[b] - s.used + tok) * (long long)p.n_heads + head;
-      p.stats[r * p.parts + part] = f32x2_t{top, l};
-    }
+    if (row < s.rows && lane < T) p.stats[(stat_row(p, line, s, b, hk) + row) * p.parts + part] = f32x2_t{top, l};
   }
 }
 
@@ -293,7 +643,7 @@ __global__ __launch_bounds__(NT) void weights_sum_kernel(WeightsParams p) {
     typename Tile::Frag k, q;
     const long long krow = key_row(p, table, hk, src, held);
     Tile::load(k, p.pool, krow, p.head_dim, lane);
-    const float* lse = p.lse + (long long)(line.rows[b] - s.used) * p.n_heads + hk * p.group;
+    const float* lse = p.lse + stat_row(p, line, s, b, hk);
     float sum = 0.0f;
     for (int r0 = 0; r0 < s.rows; r0 += T) {
       const int row = r0 + Tile::row(lane) < s.rows ? r0 + Tile::row(lane) : s.rows - 1;
@@ -306,9 +656,9 @@ __global__ __launch_bounds__(NT) void weights_sum_kernel(WeightsParams p) {
       for (int r = 0; r < Tile::ACC; ++r) {
         const int i = r0 + Tile::of(lane, r);
         if (i >= s.rows) continue;
-        const int it = token_of(p, i), ih = i - it * p.group;
+        const int it = token_of(p, i);
         if (!sees(p, s, s.row0 + it, s.index0 + it, key)) continue;
-        sum += __builtin_amdgcn_exp2f(a[r] * c - lse[(long long)it * p.n_heads + ih]);
+        sum += __builtin_amdgcn_exp2f(a[r] * c - lse[i]);
       }
     }
     sum = Tile::sum(sum);
@@ -328,9 +678,15 @@ int launch_weights(const WeightsParams& p, hipStream_t s) {
     hipLaunchKernelGGL(weights_lse_kernel, dim3(256), dim3(NT), lds, s, p);
     hipLaunchKernelGGL((weights_sum_kernel<Tile>), dim3(2048), dim3(NT), lds, s, p);
   };
+  auto tiles = [&](auto dh) {
+    constexpr int DH = decltype(dh)::value;
+    hipLaunchKernelGGL((weights_stats_tile_kernel<DH, 1>), dim3(1024), dim3(NT), lds, s, p);
+    if (p.parts > 1) hipLaunchKernelGGL(weights_lse_kernel, dim3(256), dim3(NT), lds, s, p);
+    hipLaunchKernelGGL((weights_sum_tile_kernel<DH, 1>), dim3(1024), dim3(NT), lds, s, p);
+  };
   if (p.bf16) {
-    if (p.head_dim == 128) go(TileBf16<128>{});
-    else go(TileBf16<64>{});
+    if (p.head_dim == 128) tiles(std::integral_constant<int, 128>{});
+    else tiles(std::integral_constant<int, 64>{});
   } else {
     if (p.head_dim > 64) go(TileF32<2>{});
     else go(TileF32<1>{});

@@ -328,19 +328,25 @@ inline size_t gqa_workspace(GqaLaunch g) {
 
 // ---- attention weight of cached tokens --------------------------------------------
 
+// Rows (token, head of the group) of a workgroup that makes their statistics (bf16) or of a wave (fp32).
+inline int weights_tile(bool bf16) { return bf16 ? 128 : 16; }
+
 // Parts that a request's keys are cut in for the rows' statistics: what fills the chip
-// with waves, a tile of rows and a part each, but no more than 32 to join.
-constexpr int kWeightsWaves = 4096, kWeightsParts = 32;
-inline int weights_parts(long long rows, int batch, int heads, int n_kv, int tile) {
+// with tiles, but no more than 32 to join.
+inline int weights_want(bool bf16) { return bf16 ? 2048 : 4096; }
+constexpr int kWeightsParts = 32;
+inline int weights_parts(long long rows, int batch, int heads, int n_kv, bool bf16) {
+  const int tile = weights_tile(bf16);
   const long long tiles = ((rows * (heads / n_kv) + tile - 1) / tile + batch - 1) * n_kv;
-  const long long parts = kWeightsWaves / tiles;
+  const long long parts = weights_want(bf16) / tiles;
   return parts < 1 ? 1 : (parts > kWeightsParts ? kWeightsParts : (int)parts);
 }
 
 // The most (row, head, part) that any call with up to so many rows has: as tiles are at
-// least rows * heads / tile, rows * heads * parts is at most waves * tile where it is cut at all.
-inline long long weights_stats(long long rows, int heads, int tile) {
-  const long long all = rows * heads, cut = all > (long long)kWeightsWaves * tile ? all : (long long)kWeightsWaves * tile;
+// least rows * heads / tile, there are at most want * tile of them where the keys are cut at all.
+inline long long weights_stats(long long rows, int heads, bool bf16) {
+  const long long all = rows * heads, most = (long long)weights_want(bf16) * weights_tile(bf16);
+  const long long cut = all > most ? all : most;
   return cut < all * kWeightsParts ? cut : all * kWeightsParts;
 }
 

@@ -356,6 +356,8 @@ struct GqaSight {
     words = p.words;
     bits = PAGED && p.mask == kMaskTree ? p.bits + (size_t)(u.s.s0 + tok) * p.words : nullptr;
   }
+  __device__ __forceinline__ GqaSight(int lim_, int past_, const unsigned long long* bits_, int words_)
+      : lim(lim_), past(past_), bits(bits_), words(words_) {}
   // bit i: key k0 + i, i < 64
   __device__ __forceinline__ unsigned long long seen(int k0) const {
     const int n = lim - k0;

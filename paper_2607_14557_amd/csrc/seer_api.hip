@@ -1024,8 +1024,6 @@ int seer_row_positions(const int32_t* cu_seqlens, const int32_t* seqused, int32_
   return ok();
 }
 
-static int weights_tile(const seer_attn_desc* d) { return d->dtype == SEER_DTYPE_BF16 ? 32 : 16; }
-
 size_t seer_attn_weights_workspace_bytes(const seer_attn_desc* desc, const seer_page_desc* pages, int32_t rows_ub,
                                          int32_t batch) {
   if (check_heads(desc) != SEER_OK || check_pages(pages) != SEER_OK) return 0;
@@ -1033,7 +1031,7 @@ size_t seer_attn_weights_workspace_bytes(const seer_attn_desc* desc, const seer_
     fail(SEER_EINVAL, "rows_ub and batch must be positive, rows_ub * n_heads below 2^31");
     return 0;
   }
-  return up256((size_t)seer::weights_stats(rows_ub, desc->n_heads, weights_tile(desc)) * 8) +
+  return up256((size_t)seer::weights_stats(rows_ub, desc->n_heads, desc->dtype == SEER_DTYPE_BF16) * 8) +
          up256((size_t)rows_ub * desc->n_heads * 4);
 }
 
@@ -1061,7 +1059,7 @@ int seer_attn_weights(const seer_attn_desc* desc, const seer_page_desc* pages, i
   if (!(decay >= 0.0f) || !isfinite(decay)) return fail(SEER_EINVAL, "decay must be finite and >= 0");
   if ((long long)rows_ub * desc->n_heads >= (1ll << 31))
     return fail(SEER_EUNSUPPORTED, "rows_ub * n_heads must stay below 2^31 (got %d * %d)", rows_ub, desc->n_heads);
-  const int T = weights_tile(desc);
+  const int T = desc->dtype == SEER_DTYPE_BF16 ? 32 : 16;
   // tiles of keys are counted in 31 bits
   if ((((long long)pages->table_width * pages->page_size + T - 1) / T) * desc->n_kv_heads * batch >= (1ll << 30))
     return fail(SEER_EUNSUPPORTED, "batch * n_kv_heads * table_width * page_size must stay below 2^30 * %d", T);
@@ -1081,10 +1079,10 @@ int seer_attn_weights(const seer_attn_desc* desc, const seer_page_desc* pages, i
   p.decay = decay; p.prev = decay != 0.0f ? prev : nullptr; p.weight = weight;
   long long rows = rows_ub;
   if (last > 0 && (long long)last * batch < rows) rows = (long long)last * batch;
-  p.parts = seer::weights_parts(rows, batch, p.n_heads, p.n_kv, T);
+  p.parts = seer::weights_parts(rows, batch, p.n_heads, p.n_kv, p.bf16);
   p.stats = static_cast<seer::f32x2_t*>(workspace);
   p.lse = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) +
-                                   up256((size_t)seer::weights_stats(rows_ub, p.n_heads, T) * 8));
+                                   up256((size_t)seer::weights_stats(rows_ub, p.n_heads, p.bf16) * 8));
   if (seer::launch_weights(p, stream)) return hip_fail("attention weights launch");
   return ok();
 }
