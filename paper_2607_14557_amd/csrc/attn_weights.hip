@@ -164,6 +164,20 @@ __device__ __forceinline__ Line line_of(const WeightsParams& p, int* lds, Units 
   return l;
 }
 
+// The line of a launch on tiles: where the heads divide by the 8 XCDs, each XCD has heads
+// of its own and a line of them, so that the units of a head, which read the same keys or
+// rows, run side by side and find them in its L2; otherwise all workgroups share one line.
+struct Share {
+  int heads, head0, first, step;
+  __device__ __forceinline__ Share(int n_kv) {
+    const bool own = n_kv % 8 == 0;              // (the grid is a multiple of 8)
+    heads = own ? n_kv / 8 : n_kv;
+    head0 = own ? (blockIdx.x & 7) * heads : 0;
+    first = own ? blockIdx.x >> 3 : blockIdx.x;
+    step = own ? gridDim.x >> 3 : gridDim.x;
+  }
+};
+
 // The request of unit u, and the unit's place there.
 __device__ __forceinline__ int request_of(const Line& l, int B, int u, int& at) {
   int lo = 0, hi = B - 1;
@@ -229,23 +243,36 @@ struct Stream {
                                                off(row) + ((uint32_t)((lane % LPR) ^ swz<DH>(row)) << 4), 0, 0, 0);
     }
   }
-  // products of the tile's rows 32 i .. 32 i + 31 with SETS sets of 32 rows in registers
+  // products of the tile's rows 32 i .. 32 i + 31 with SETS sets of 32 rows in registers; the
+  // fragments are read AHEAD products before they are used
   template <int SETS>
   __device__ __forceinline__ static void mul(f32x16_t (&a)[SETS], const uint8_t* tile, int i,
                                              const bf16x8_t (&st)[SETS][DH / 16], int lane) {
+    constexpr int KS = DH / 16, AHEAD = 3;
     const int fr = lane & 31;
     const uint8_t* row = tile + (32 * i + fr) * ROW;
+    auto read = [&](int ks) {
+      const int c = (2 * ks + (lane >> 5)) ^ swz<DH>(fr);
+      return __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4_t*>(row + c * 16));
+    };
+    bf16x8_t f[AHEAD + 1];
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int ks = 0; ks < AHEAD; ++ks) f[ks] = read(ks);
 #pragma unroll
     for (int s = 0; s < SETS; ++s)
 #pragma unroll
       for (int r = 0; r < 16; ++r) a[s][r] = 0.0f;
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int ks = 0; ks < DH / 16; ++ks) {
-      const int c = (2 * ks + (lane >> 5)) ^ swz<DH>(fr);
-      const bf16x8_t f = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4_t*>(row + c * 16));
+    for (int ks = 0; ks < KS; ++ks) {
+      if (ks + AHEAD < KS) f[(ks + AHEAD) % (AHEAD + 1)] = read(ks + AHEAD);
 #pragma unroll
-      for (int s = 0; s < SETS; ++s) a[s] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, st[s][ks], a[s], 0, 0, 0);
+      for (int s = 0; s < SETS; ++s) a[s] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[ks % (AHEAD + 1)], st[s][ks], a[s], 0, 0, 0);
+      if (ks + AHEAD < KS) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, SETS, 0);
     }
+    __builtin_amdgcn_sched_barrier(0);
   }
 };
 
@@ -264,24 +291,25 @@ __device__ __forceinline__ void load_row(bf16x8_t (&f)[DH / 16], const uint16_t*
 // key and moves only where a later tile adds up to 2^40 of it: any reference gives the
 // same sum, and the common tile takes no maximum.
 template <int DH, int SETS>
-__global__ __launch_bounds__(NT, 2) void weights_stats_tile_kernel(WeightsParams p) {
+__global__ __launch_bounds__(NT, 4) void weights_stats_tile_kernel(WeightsParams p) {
   extern __shared__ int lds[];
   __shared__ __attribute__((aligned(1024))) uint8_t tile0[TILE * DH * 2];
   __shared__ __attribute__((aligned(1024))) uint8_t tile1[TILE * DH * 2];
   constexpr int RT = 128 * SETS;
-  auto units = [&](const Seq& s) { return s.nk > 0 ? (s.rows + RT - 1) / RT * p.n_kv * p.parts : 0; };
+  const Share share(p.n_kv);
+  auto units = [&](const Seq& s) { return s.nk > 0 ? (s.rows + RT - 1) / RT * share.heads * p.parts : 0; };
   const Line line = line_of(p, lds, units);
   const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const float c = p.scale * 1.4426950408889634f;
   const uint16_t* q = static_cast<const uint16_t*>(p.q);
   const uint8_t* pool = static_cast<const uint8_t*>(p.pool);
-  for (int u = blockIdx.x; u < line.all; u += gridDim.x) {
+  for (int u = share.first; u < line.all; u += share.step) {
     int at;
     const int b = __builtin_amdgcn_readfirstlane(request_of(line, p.B, u, at));
     at = __builtin_amdgcn_readfirstlane(at);
     const Seq s = seq_of(p, b);
     const int tiles = (s.rows + RT - 1) / RT;
-    const int t = at % tiles, part = at / tiles % p.parts, hk = at / tiles / p.parts;
+    const int t = at % tiles, part = at / tiles % p.parts, hk = share.head0 + at / tiles / p.parts;
     const int row0 = t * RT + wave * 32 * SETS;
     bf16x8_t st[SETS][DH / 16];
     int index[SETS];                             // of the lane's rows among the request's rows of the call
@@ -432,26 +460,27 @@ __global__ __launch_bounds__(NT, 2) void weights_stats_tile_kernel(WeightsParams
 
 // The weights of 128 SETS keys, which stay, from all rows, which pass by.
 template <int DH, int SETS>
-__global__ __launch_bounds__(NT, 2) void weights_sum_tile_kernel(WeightsParams p) {
+__global__ __launch_bounds__(NT, 4) void weights_sum_tile_kernel(WeightsParams p) {
   extern __shared__ int lds[];
   __shared__ __attribute__((aligned(1024))) uint8_t tile0[TILE * DH * 2];
   __shared__ __attribute__((aligned(1024))) uint8_t tile1[TILE * DH * 2];
   __shared__ __attribute__((aligned(16))) float lse_lds[2][TILE];
   __shared__ __attribute__((aligned(16))) int lim_lds[2][TILE];        // the keys before it are seen
   constexpr int KT = 128 * SETS;
-  auto units = [&](const Seq& s) { return s.used > 0 ? (s.nk + KT - 1) / KT * p.n_kv : 0; };
+  const Share share(p.n_kv);
+  auto units = [&](const Seq& s) { return s.used > 0 ? (s.nk + KT - 1) / KT * share.heads : 0; };
   const Line line = line_of(p, lds, units);
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const float c = p.scale * 1.4426950408889634f;
   const uint8_t* q = static_cast<const uint8_t*>(p.q);
   const uint16_t* pool = static_cast<const uint16_t*>(p.pool);
-  for (int u = blockIdx.x; u < line.all; u += gridDim.x) {
+  for (int u = share.first; u < line.all; u += share.step) {
     int at;
     const int b = __builtin_amdgcn_readfirstlane(request_of(line, p.B, u, at));
     at = __builtin_amdgcn_readfirstlane(at);
     const Seq s = seq_of(p, b);
     const int tiles = (s.nk + KT - 1) / KT;
-    const int hk = at / tiles, key0 = (at - hk * tiles) * KT, k0 = key0 + wave * 32 * SETS;
+    const int quot = at / tiles, hk = share.head0 + quot, key0 = (at - quot * tiles) * KT, k0 = key0 + wave * 32 * SETS;
     const int* table = p.table + (size_t)b * p.width;
     bf16x8_t st[SETS][DH / 16];
     long long mark[SETS];                        // where the lane's keys' weights are, -1: nowhere
