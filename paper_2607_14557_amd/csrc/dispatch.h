@@ -350,4 +350,24 @@ inline long long weights_stats(long long rows, int heads, bool bf16) {
   return cut < all * kWeightsParts ? cut : all * kWeightsParts;
 }
 
+// ---- eviction ---------------------------------------------------------------------
+
+struct EvictRule {
+  int places;            // the most of a list that a workgroup keeps in registers; 0: any number, read again
+  bool fused;            // whether it moves the list's rows too, instead of a second launch
+  int parts;             // workgroups of a list in that
+};
+inline EvictRule evict_rule(int lists, bool shared, long long places) {
+  EvictRule r{};
+  r.places = places <= 2048 ? 2048 : (places <= 8192 ? 8192 : (places <= 16384 ? 16384 : 0));
+  r.fused = !shared && (r.places == 2048 || r.places == 8192) && lists >= 512;
+  r.parts = lists >= 4096 ? 1 : (4096 / lists > 128 ? 128 : 4096 / lists);
+  return r;
+}
+
+// Moves that a list has room for: half its places, in whole 64.
+inline size_t evict_room(long long places) { return (size_t)(places / 2 + 63) / 64 * 64; }
+// Bytes of a list: slots from and to, and a bit of each place.
+inline size_t evict_list_bytes(long long places) { return evict_room(places) * 8 + evict_room(places) / 32 * 8; }
+
 }  // namespace seer

@@ -4,7 +4,12 @@
 // are given up are filled with the kept tokens from N on, the i-th with the i-th, so
 // that no more rows move than have to; where they come from and where they go never
 // overlap, so all move at once.
+//
+// A list is what one head keeps of a request, or all of them together.  A workgroup
+// reads a list's marks once, into registers, finds the order of the last token that
+// stays by histograms of 11, 11 and 10 bits, and ranks what moves by ballots.
 #include "common.h"
+#include "dispatch.h"
 #include "kernels.h"
 
 namespace seer {
@@ -33,108 +38,333 @@ __device__ __forceinline__ Request request(const EvictParams& p, int b) {
   return r;
 }
 
-// Index of head 0 of place j in the marks; -1 on a page that is none of the pool's.
-__device__ __forceinline__ long long mark_of(const EvictParams& p, const Request& r, int j) {
+// The slot of place j in the pool; -1 on a page that is none of it.
+__device__ __forceinline__ int slot_of(const EvictParams& p, const Request& r, int j) {
   const int id = r.table[j >> p.shift];
-  if (id < 0 || id >= p.n_pages) return -1;
-  return (((long long)id * p.n_kv) << p.shift) + (j & ((1 << p.shift) - 1));
+  return id < 0 || id >= p.n_pages ? -1 : (id << p.shift) + (j & ((1 << p.shift) - 1));
+}
+// Where a slot's marks for head h are.
+__device__ __forceinline__ long long mark_of(const EvictParams& p, int slot, int h) {
+  return (((long long)(slot >> p.shift) * p.n_kv + h) << p.shift) + (slot & ((1 << p.shift) - 1));
+}
+
+struct Mark {
+  float w;               // the head's weight, or the heads' sum
+  int number, slot;
+};
+
+__device__ __forceinline__ Mark look(const EvictParams& p, const Request& r, int h, int j) {
+  Mark m{0.0f, 0, slot_of(p, r, j)};
+  if (m.slot < 0) return m;
+  const long long at = mark_of(p, m.slot, h);
+  if (p.shared) {
+    double sum = 0.0;
+    int i = 0;
+    for (; i + 8 <= p.n_kv; i += 8) {
+      float w[8];                                // on their way together
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w[e] = p.weight[at + ((long long)(i + e) << p.shift)];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum += (double)w[e];
+    }
+    for (; i < p.n_kv; ++i) sum += (double)p.weight[at + ((long long)i << p.shift)];
+    m.w = (float)sum;
+  } else {
+    m.w = p.weight[at];
+  }
+  m.number = p.number[at];
+  return m;
+}
+
+// Order and kind of a place: without a page lighter than any weight, and not protected.
+__device__ __forceinline__ uint32_t order_of(const Mark& m) { return m.slot < 0 ? 0u : order_of(m.w); }
+__device__ __forceinline__ bool guarded(const EvictParams& p, const Mark& m, int seen) {
+  return m.slot >= 0 && (m.number < p.first || (long long)m.number >= (long long)seen - p.recent);
+}
+
+template <int NT>
+struct Shared {
+  static constexpr int NW = NT / kWave;
+  uint32_t hist[3][2048];
+  int part[NW];
+  int guarded, digit, left;
+};
+
+// The order from which on the members of a kind stay, and how many of those with exactly
+// it do: the `left` largest of them.  each(f) calls f(order) for the thread's members.
+template <int NT, typename Each>
+__device__ __forceinline__ uint32_t threshold(Shared<NT>& sh, int& left, Each each) {
+  constexpr int PER = 2048 / NT, NW = NT / kWave;
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6;
+  uint32_t prefix = 0, mask = 0;
+#pragma unroll 1
+  for (int pass = 0; pass < 3; ++pass) {
+    const int shift = pass == 0 ? 21 : (pass == 1 ? 10 : 0), bins = pass == 2 ? 1024 : 2048;
+    uint32_t* hist = sh.hist[pass];
+    each([&](uint32_t key) {
+      // the largest first
+      if ((key & mask) == prefix) atomicAdd(&hist[bins - 1 - (key >> shift & (bins - 1))], 1u);
+    });
+    __syncthreads();
+    int n[PER], own = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      n[i] = hist[tid * PER + i];
+      own += n[i];
+    }
+    int inc = own;
+#pragma unroll
+    for (int off = 1; off < kWave; off <<= 1) {
+      const int v = __shfl_up(inc, off, kWave);
+      if (lane >= off) inc += v;
+    }
+    if (lane == kWave - 1) sh.part[wave] = inc;
+    __syncthreads();
+    int before = inc - own;
+#pragma unroll
+    for (int w = 0; w < NW; ++w)
+      if (w < wave) before += sh.part[w];
+    if (before < left && left <= before + own) {
+      int need = left - before, d = 0;
+#pragma unroll
+      for (int i = 0; i < PER - 1; ++i)
+        if (d == i && need > n[i]) { need -= n[i]; d = i + 1; }
+      sh.digit = bins - 1 - (tid * PER + d);
+      sh.left = need;
+    }
+    __syncthreads();
+    prefix |= (uint32_t)sh.digit << shift;
+    mask |= (uint32_t)(bins - 1) << shift;
+    left = sh.left;
+  }
+  return prefix;
+}
+
+// A move's K and V rows and marks: pieces [i, end) of those of n moves of `heads` heads
+// from h0 on, 16 bytes each, in steps.
+__device__ __forceinline__ void move_rows(const EvictParams& p, const int* from, const int* to, int n, int h0, int heads,
+                                          long long first, long long step) {
+  const int pieces = 2 * p.head_pieces;
+  const size_t row = (size_t)p.head_pieces * 16;
+  const long long page = (long long)p.n_kv << p.shift;
+  for (long long i = first; i < (long long)n * heads * pieces; i += step) {
+    const int mh = (int)(i / pieces), c = (int)(i - (long long)mh * pieces);
+    const int m = mh / heads, h = h0 + mh - m * heads;
+    const int src = from[m], dst = to[m];
+    if (src < 0 || dst < 0) continue;
+    const long long s = mark_of(p, src, h), d = mark_of(p, dst, h);
+    // K of a page lies before its V
+    const int v = c >= p.head_pieces, piece = v ? c - p.head_pieces : c;
+    const long long sr = s + (src >> p.shift) * page + v * page, dr = d + (dst >> p.shift) * page + v * page;
+    *reinterpret_cast<u32x4_t*>(p.pool + dr * row + piece * 16) =
+        *reinterpret_cast<const u32x4_t*>(p.pool + sr * row + piece * 16);
+    if (c == 0) {
+      const float w = p.weight[s];
+      const int number = p.number[s];
+      p.weight_out[d] = w;
+      p.number_out[d] = number;
+    }
+  }
 }
 
 }  // namespace
 
-constexpr int NT = 1024, NW = NT / kWave;
-
-// What a request keeps, for one head or for all: a workgroup finds the weight of the
-// last token that stays, eight bits of it at a time by their histogram, and lists the
-// moves in the order of the places.
-__global__ __launch_bounds__(NT) void evict_select_kernel(EvictParams p) {
-  __shared__ uint32_t hist[256];
-  __shared__ int part[4][NW];
-  __shared__ uint32_t digit_lds;
-  __shared__ int left_lds, guarded_lds;
+// Lists of at most NT * K places.  p.fused: the workgroup moves its list's rows too;
+// otherwise it leaves the slots of what moves, and of shared lists which places below N
+// are given up, for evict_move_kernel.
+template <int NT, int K>
+__global__ __launch_bounds__(NT) void evict_kernel(EvictParams p) {
+  constexpr int NW = NT / kWave, MOST = NT * K <= 8192 ? NT * K / 2 : 1;
+  __shared__ Shared<NT> sh;
+  __shared__ int counts[K][NW];                  // of what moves, per 64 places, then their sums before
+  __shared__ int from_lds[MOST], to_lds[MOST];
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6;
   const int b = blockIdx.x / p.lists, h = blockIdx.x % p.lists;
   const Request r = request(p, b);
   const int seen = p.seen[b];
-  if (tid == 0) guarded_lds = 0;
-  __syncthreads();
-
-  // order and kind of place j
-  auto look = [&](int j, uint32_t& key, bool& guarded) {
-    const long long at = mark_of(p, r, j);
-    key = 0;
-    guarded = false;
-    if (at < 0) return;
-    const long long head = at + ((long long)h << p.shift);
-    float w;
-    if (p.shared) {
-      double sum = 0.0;
-      for (int i = 0; i < p.n_kv; ++i) sum += (double)p.weight[at + ((long long)i << p.shift)];
-      w = (float)sum;
-    } else {
-      w = p.weight[head];
-    }
-    const int number = p.number[head];
-    key = order_of(w);
-    guarded = number < p.first || (long long)number >= (long long)seen - p.recent;
-  };
-  int mine = 0;
-  for (int j = tid; j < r.L; j += NT) {
-    uint32_t key;
-    bool guarded;
-    look(j, key, guarded);
-    mine += guarded;
+  for (int i = tid; i < 3 * 2048; i += NT) (&sh.hist[0][0])[i] = 0;
+  if (tid == 0) sh.guarded = 0;
+  Mark m[K];
+  uint32_t kinds = 0;                            // bit k: place k * NT + tid is protected
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const int j = k * NT + tid;
+    m[k] = Mark{0.0f, 0, -1};
+    if (j < r.L) m[k] = look(p, r, h, j);
   }
-  if (mine) atomicAdd(&guarded_lds, mine);
+  __syncthreads();
+  int mine = 0;
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const bool g = k * NT + tid < r.L && guarded(p, m[k], seen);
+    kinds |= (uint32_t)g << k;
+    mine += __popcll(__ballot(g));
+  }
+  if (lane == 0 && mine) atomicAdd(&sh.guarded, mine);
   __syncthreads();
   // the kind of which some stay, and how many of them
-  const int guarded_all = guarded_lds;
+  const int guarded_all = sh.guarded;
   const bool of_guarded = guarded_all >= r.N;
+  const int members = of_guarded ? guarded_all : r.L - guarded_all;
   int left = of_guarded ? r.N : r.N - guarded_all;
-  uint32_t prefix = 0, mask = 0;
-  if (left > 0) {
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      if (tid < 256) hist[tid] = 0;
-      __syncthreads();
-      for (int j = tid; j < r.L; j += NT) {
-        uint32_t key;
-        bool guarded;
-        look(j, key, guarded);
-        if (guarded == of_guarded && (key & mask) == prefix) atomicAdd(&hist[key >> shift & 255], 1u);
+  const bool some = left > 0 && left < members;
+  uint32_t least = 0;
+  if (some)
+    least = threshold<NT>(sh, left, [&](auto f) {
+#pragma unroll
+      for (int k = 0; k < K; ++k)
+        if (k * NT + tid < r.L && (kinds >> k & 1) == of_guarded) f(order_of(m[k]));
+    });
+  // which stay: of the places with exactly the least order, the first `left`
+  uint32_t stays = 0, ties = 0;
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const bool in = k * NT + tid < r.L, member = (kinds >> k & 1) == of_guarded;
+    const uint32_t order = order_of(m[k]);
+    const bool stay = in && (member ? (some ? order > least : left > 0) : !of_guarded);
+    const bool tie = in && member && some && order == least;
+    stays |= (uint32_t)stay << k;
+    ties |= (uint32_t)tie << k;
+  }
+  // ranks in the order of the places: counts of each 64, their sums, and the ballots
+  auto rank = [&](uint32_t bits, auto use) {
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const unsigned long long set = __ballot(bits >> k & 1);
+      if (lane == 0) counts[k][wave] = __popcll(set);
+    }
+    __syncthreads();
+    if (wave == 0) {
+      int* c = &counts[0][0];
+      int base = 0;
+#pragma unroll
+      for (int i = 0; i < K * NW; i += kWave) {
+        const int own = i + lane < K * NW ? c[i + lane] : 0;
+        int inc = own;
+#pragma unroll
+        for (int off = 1; off < kWave; off <<= 1) {
+          const int v = __shfl_up(inc, off, kWave);
+          if (lane >= off) inc += v;
+        }
+        if (i + lane < K * NW) c[i + lane] = base + inc - own;
+        base += __builtin_amdgcn_readlane(inc, kWave - 1);
       }
-      __syncthreads();
-      if (tid == 0) {
-        int n = left, d = 255;
-        for (; d > 0 && (int)hist[d] < n; --d) n -= hist[d];
-        digit_lds = d;
-        left_lds = n;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const unsigned long long set = __ballot(bits >> k & 1);
+      if (bits >> k & 1) use(k, counts[k][wave] + __popcll(set & ((1ull << lane) - 1)));
+    }
+  };
+  if (some) {
+    rank(ties, [&](int k, int at) {
+      if (at < left) stays |= 1u << k;
+    });
+  }
+  // places below N that are given up, and kept ones from N on: as many of either
+  uint32_t moves = 0;
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const int j = k * NT + tid;
+    if (j < r.L) moves |= (uint32_t)((j < r.N) != (bool)(stays >> k & 1)) << k;
+  }
+  int gone = 0;
+#pragma unroll
+  for (int k = 0; k < K; ++k) gone += __popcll(__ballot((moves >> k & 1) && k * NT + tid < r.N));
+  __syncthreads();
+  if (lane == 0) sh.part[wave] = gone;
+  __syncthreads();
+  int n = 0;
+#pragma unroll
+  for (int w = 0; w < NW; ++w) n += sh.part[w];
+  int* from = p.fused ? from_lds : p.moves + (size_t)blockIdx.x * 2 * p.room;
+  int* to = p.fused ? to_lds : from + p.room;
+  if (n > 0)
+    rank(moves, [&](int k, int at) {
+      if (at < n) to[at] = m[k].slot;
+      else from[at - n] = m[k].slot;
+    });
+  if (p.weight_out != p.weight) {
+    if (!p.shared) {
+      // marks that stay where they are, in another pool
+#pragma unroll
+      for (int k = 0; k < K; ++k)
+        if (k * NT + tid < r.N && (stays >> k & 1) && m[k].slot >= 0) {
+          const long long at = mark_of(p, m[k].slot, h);
+          p.weight_out[at] = m[k].w;
+          p.number_out[at] = m[k].number;
+        }
+    } else {
+      unsigned long long* gone_bits = p.bits + (size_t)blockIdx.x * (p.room / 32);
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        const unsigned long long set = __ballot(!(stays >> k & 1));
+        if (lane == 0 && k * NT + wave * kWave < r.N) gone_bits[(k * NT >> 6) + wave] = set;
       }
-      __syncthreads();
-      prefix |= digit_lds << shift;
-      mask |= 255u << shift;
-      left = left_lds;
-      __syncthreads();
     }
   }
-  // `left` of the places with exactly this order stay (none at all where left is 0)
+  if (tid == 0) {
+    if (h == 0) p.kept[b] = r.N;
+    if (!p.fused) p.counts[blockIdx.x] = n;
+  }
+  if (p.fused && n > 0) {
+    __syncthreads();
+    move_rows(p, from, to, n, h, 1, tid, NT);
+  }
+}
+
+// Lists of any length, whose marks are read again for each histogram.
+__global__ __launch_bounds__(1024) void evict_long_kernel(EvictParams p) {
+  constexpr int NT = 1024, NW = NT / kWave;
+  __shared__ Shared<NT> sh;
+  __shared__ int part[3][NW];
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6;
+  const int b = blockIdx.x / p.lists, h = blockIdx.x % p.lists;
+  const Request r = request(p, b);
+  const int seen = p.seen[b];
+  for (int i = tid; i < 3 * 2048; i += NT) (&sh.hist[0][0])[i] = 0;
+  if (tid == 0) sh.guarded = 0;
+  __syncthreads();
+  int mine = 0;
+  for (int j = tid; j < r.L; j += NT) mine += guarded(p, look(p, r, h, j), seen);
+  if (mine) atomicAdd(&sh.guarded, mine);
+  __syncthreads();
+  const int guarded_all = sh.guarded;
+  const bool of_guarded = guarded_all >= r.N;
+  const int members = of_guarded ? guarded_all : r.L - guarded_all;
+  int left = of_guarded ? r.N : r.N - guarded_all;
+  const bool some = left > 0 && left < members;
+  uint32_t least = 0;
+  if (some)
+    least = threshold<NT>(sh, left, [&](auto f) {
+      for (int j = tid; j < r.L; j += NT) {
+        const Mark m = look(p, r, h, j);
+        if (guarded(p, m, seen) == of_guarded) f(order_of(m));
+      }
+    });
   int* from = p.moves + (size_t)blockIdx.x * 2 * p.room;
   int* to = from + p.room;
+  unsigned long long* gone_bits = p.bits + (size_t)blockIdx.x * (p.room / 32);
   int ties = 0, holes = 0, sources = 0;          // before this stretch of places
   for (int j0 = 0; j0 < r.L; j0 += NT) {
     const int j = j0 + tid;
-    uint32_t key = 0;
-    bool guarded = false, tie = false, stays = false;
+    Mark m{0.0f, 0, -1};
+    bool tie = false, stays = false;
     if (j < r.L) {
-      look(j, key, guarded);
-      if (guarded != of_guarded) stays = guarded;
-      else if (left > 0) {
-        tie = key == prefix;
-        stays = key > prefix;
+      m = look(p, r, h, j);
+      if (guarded(p, m, seen) != of_guarded) stays = !of_guarded;
+      else if (!some) stays = left > 0;
+      else {
+        const uint32_t order = order_of(m);
+        tie = order == least;
+        stays = order > least;
       }
     }
     auto rank = [&](bool is, int k, int& total) {
-      const unsigned long long m = __ballot(is);
-      if (lane == 0) part[k][wave] = __popcll(m);
+      const unsigned long long set = __ballot(is);
+      if (lane == 0) part[k][wave] = __popcll(set);
       __syncthreads();
       int before = 0;
       total = 0;
@@ -143,7 +373,7 @@ __global__ __launch_bounds__(NT) void evict_select_kernel(EvictParams p) {
         if (w < wave) before += n;
         total += n;
       }
-      return before + __popcll(m & ((1ull << lane) - 1));
+      return before + __popcll(set & ((1ull << lane) - 1));
     };
     int all;
     const int tie_at = ties + rank(tie, 0, all);
@@ -154,17 +384,19 @@ __global__ __launch_bounds__(NT) void evict_select_kernel(EvictParams p) {
     holes += all;
     const int source_at = sources + rank(source, 2, all);
     sources += all;
-    if (hole) to[hole_at] = j;
-    if (source) from[source_at] = j;
-    if (j < r.N && stays && p.weight_out != p.weight) {
-      // marks that stay where they are, in another pool
-      const long long at = mark_of(p, r, j);
-      if (at >= 0)
-        for (int i = 0; i < (p.shared ? p.n_kv : 1); ++i) {
-          const long long m = at + ((long long)(p.shared ? i : h) << p.shift);
-          p.weight_out[m] = p.weight[m];
-          p.number_out[m] = p.number[m];
+    if (hole) to[hole_at] = m.slot;
+    if (source) from[source_at] = m.slot;
+    if (p.weight_out != p.weight) {
+      if (!p.shared) {
+        if (j < r.N && stays && m.slot >= 0) {
+          const long long at = mark_of(p, m.slot, h);
+          p.weight_out[at] = m.w;
+          p.number_out[at] = m.number;
         }
+      } else {
+        const unsigned long long set = __ballot(!stays);
+        if (lane == 0 && j < r.N) gone_bits[j >> 6] = set;
+      }
     }
     __syncthreads();
   }
@@ -174,41 +406,34 @@ __global__ __launch_bounds__(NT) void evict_select_kernel(EvictParams p) {
   }
 }
 
-// The moves: a wave takes a token and head, its K, V and marks.
+// The moves of all lists, p.parts workgroups each, and of shared lists the marks that
+// stay where they are, in another pool.
 __global__ __launch_bounds__(256) void evict_move_kernel(EvictParams p) {
-  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6;
   const int list = blockIdx.x / p.parts, part = blockIdx.x % p.parts;
-  const int b = list / p.lists, h0 = p.shared ? 0 : list % p.lists, heads = p.shared ? p.n_kv : 1;
-  const Request r = request(p, b);
-  const int n = p.counts[list];
+  const int h0 = p.shared ? 0 : list % p.lists, heads = p.shared ? p.n_kv : 1;
   const int* from = p.moves + (size_t)list * 2 * p.room;
-  const int* to = from + p.room;
-  const size_t row = (size_t)p.head_pieces * 16;
-  for (long long i = (long long)part * 4 + wave; i < (long long)n * heads; i += 4ll * p.parts) {
-    const int m = (int)(i / heads), h = h0 + (int)(i - (long long)m * heads);
-    const long long src = mark_of(p, r, from[m]), dst = mark_of(p, r, to[m]);
-    if (src < 0 || dst < 0) continue;
-    const long long s = src + ((long long)h << p.shift), d = dst + ((long long)h << p.shift);
-    if (lane == 0) {
-      const float w = p.weight[s];
-      const int number = p.number[s];
-      p.weight_out[d] = w;
-      p.number_out[d] = number;
-    }
-    // K of a page lies before its V
-    const long long page = (long long)p.n_kv << p.shift;
-    const size_t sk = (size_t)(src / page * page + s), dk = (size_t)(dst / page * page + d);
-    for (int c = lane; c < 2 * p.head_pieces; c += kWave) {
-      const int v = c >= p.head_pieces, piece = v ? c - p.head_pieces : c;
-      *reinterpret_cast<u32x4_t*>(p.pool + (dk + v * page) * row + piece * 16) =
-          *reinterpret_cast<const u32x4_t*>(p.pool + (sk + v * page) * row + piece * 16);
-    }
+  const long long first = (long long)part * 256 + threadIdx.x, step = 256ll * p.parts;
+  move_rows(p, from, from + p.room, p.counts[list], h0, heads, first, step);
+  if (!p.shared || p.weight_out == p.weight) return;
+  const Request r = request(p, list);
+  const unsigned long long* gone = p.bits + (size_t)list * (p.room / 32);
+  for (long long i = first; i < (long long)r.N * heads; i += step) {
+    const int h = (int)(i / r.N), j = (int)(i - (long long)h * r.N);
+    const int slot = slot_of(p, r, j);
+    if (slot < 0 || (gone[j >> 6] >> (j & 63) & 1)) continue;
+    const long long at = mark_of(p, slot, h);
+    p.weight_out[at] = p.weight[at];
+    p.number_out[at] = p.number[at];
   }
 }
 
-int launch_evict(const EvictParams& p, hipStream_t s) {
-  hipLaunchKernelGGL(evict_select_kernel, dim3(p.B * p.lists), dim3(NT), 0, s, p);
-  hipLaunchKernelGGL(evict_move_kernel, dim3(p.B * p.lists * p.parts), dim3(256), 0, s, p);
+int launch_evict(const EvictParams& p, const EvictRule& r, hipStream_t s) {
+  const dim3 grid(p.B * p.lists);
+  if (r.places == 2048) hipLaunchKernelGGL((evict_kernel<256, 8>), grid, dim3(256), 0, s, p);
+  else if (r.places == 8192) hipLaunchKernelGGL((evict_kernel<512, 16>), grid, dim3(512), 0, s, p);
+  else if (r.places == 16384) hipLaunchKernelGGL((evict_kernel<1024, 16>), grid, dim3(1024), 0, s, p);
+  else hipLaunchKernelGGL(evict_long_kernel, grid, dim3(1024), 0, s, p);
+  if (!p.fused) hipLaunchKernelGGL(evict_move_kernel, dim3(p.B * p.lists * p.parts), dim3(256), 0, s, p);
   return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 

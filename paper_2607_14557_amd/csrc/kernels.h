@@ -10,6 +10,7 @@
 namespace seer {
 
 struct GqaRule;
+struct EvictRule;
 
 // SCALE: C = acc * rs[r]; SCALE_ROPE: SCALE with the rotary embedding of the
 // columns < rope_col1 (bf16 only); RESID: C = R + acc; SWIGLU(_COUNT): gate/up pairs;
@@ -451,11 +452,13 @@ struct EvictParams {
   float* weight_out;
   int* number_out;
   int* kept;
+  bool fused;
   int* counts;                 // [B * lists] moves
-  int* moves;                  // [B * lists][2][room] from, to
+  int* moves;                  // [B * lists][2][room] slots from, to
+  unsigned long long* bits;    // [B * lists][room / 32] places that are given up (shared)
   size_t room;
   int parts;                   // workgroups of a list's moves
 };
-int launch_evict(const EvictParams& p, hipStream_t s);
+int launch_evict(const EvictParams& p, const EvictRule& r, hipStream_t s);
 
 }  // namespace seer

@@ -1087,9 +1087,7 @@ int seer_attn_weights(const seer_attn_desc* desc, const seer_page_desc* pages, i
   return ok();
 }
 
-static size_t evict_room(const seer_page_desc* pages) {
-  return ((size_t)pages->table_width * pages->page_size / 2 + 63) / 64 * 64;
-}
+static long long evict_places(const seer_page_desc* pages) { return (long long)pages->table_width * pages->page_size; }
 
 size_t seer_kv_evict_workspace_bytes(const seer_attn_desc* desc, const seer_page_desc* pages, int32_t batch) {
   if (check_heads(desc) != SEER_OK || check_pages(pages) != SEER_OK) return 0;
@@ -1098,7 +1096,7 @@ size_t seer_kv_evict_workspace_bytes(const seer_attn_desc* desc, const seer_page
     return 0;
   }
   const size_t lists = (size_t)batch * desc->n_kv_heads;
-  return up256(lists * 4) + lists * 2 * evict_room(pages) * 4;
+  return up256(lists * 4) + lists * seer::evict_list_bytes(evict_places(pages));
 }
 
 int seer_kv_evict(const seer_attn_desc* desc, const seer_page_desc* pages, int32_t flags, const int32_t* kv_len,
@@ -1131,12 +1129,15 @@ int seer_kv_evict(const seer_attn_desc* desc, const seer_page_desc* pages, int32
   p.head_pieces = desc->head_dim * (desc->dtype == SEER_DTYPE_BF16 ? 2 : 4) / 16;
   p.pool = static_cast<uint8_t*>(pool); p.weight = weight; p.number = number;
   p.weight_out = weight_out; p.number_out = number_out; p.kept = kept;
+  const size_t lists = (size_t)batch * p.lists;
+  const seer::EvictRule rule = seer::evict_rule((int)lists, p.shared, evict_places(pages));
+  p.fused = rule.fused;
+  p.parts = rule.parts;
+  p.room = seer::evict_room(evict_places(pages));
   p.counts = static_cast<int*>(workspace);
-  p.moves = reinterpret_cast<int*>(static_cast<uint8_t*>(workspace) + up256((size_t)batch * desc->n_kv_heads * 4));
-  p.room = evict_room(pages);
-  const int lists = batch * p.lists;
-  p.parts = lists >= 2048 ? 1 : 2048 / lists > 64 ? 64 : 2048 / lists;
-  if (seer::launch_evict(p, stream)) return hip_fail("eviction launch");
+  p.moves = reinterpret_cast<int*>(static_cast<uint8_t*>(workspace) + up256(lists * 4));
+  p.bits = reinterpret_cast<unsigned long long*>(p.moves + lists * 2 * p.room);
+  if (seer::launch_evict(p, rule, stream)) return hip_fail("eviction launch");
   return ok();
 }
 
