@@ -354,12 +354,14 @@ inline long long weights_stats(long long rows, int heads, bool bf16) {
 
 struct EvictRule {
   int places;            // the most of a list that a workgroup keeps in registers; 0: any number, read again
+  bool few;              // fewer lists than CUs: more threads each
   bool fused;            // whether it moves the list's rows too, instead of a second launch
   int parts;             // workgroups of a list in that
 };
 inline EvictRule evict_rule(int lists, bool shared, long long places) {
   EvictRule r{};
   r.places = places <= 2048 ? 2048 : (places <= 8192 ? 8192 : (places <= 16384 ? 16384 : 0));
+  r.few = lists < 256;
   r.fused = !shared && (r.places == 2048 || r.places == 8192) && lists >= 512;
   r.parts = lists >= 4096 ? 1 : (4096 / lists > 128 ? 128 : 4096 / lists);
   return r;

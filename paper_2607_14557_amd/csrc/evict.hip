@@ -90,8 +90,9 @@ struct Shared {
   int guarded, digit, left;
 };
 
-// The order from which on the members of a kind stay, and how many of those with exactly
-// it do: the `left` largest of them.  each(f) calls f(order) for the thread's members.
+// The `left` largest members of a kind stay: those above the order that is returned, and
+// the first `left` (now) of those with exactly it; -1: all of those, or of those that share
+// the bits that were looked at.  each(f) calls f(order) for the thread's members.
 template <int NT, typename Each>
 __device__ __forceinline__ uint32_t threshold(Shared<NT>& sh, int& left, Each each) {
   constexpr int PER = 2048 / NT, NW = NT / kWave;
@@ -129,13 +130,17 @@ __device__ __forceinline__ uint32_t threshold(Shared<NT>& sh, int& left, Each ea
 #pragma unroll
       for (int i = 0; i < PER - 1; ++i)
         if (d == i && need > n[i]) { need -= n[i]; d = i + 1; }
+      int same = n[0];
+#pragma unroll
+      for (int i = 1; i < PER; ++i) same = d == i ? n[i] : same;
       sh.digit = bins - 1 - (tid * PER + d);
-      sh.left = need;
+      sh.left = need == same ? -1 : need;
     }
     __syncthreads();
     prefix |= (uint32_t)sh.digit << shift;
     mask |= (uint32_t)(bins - 1) << shift;
     left = sh.left;
+    if (left < 0) break;                         // the whole bin stays
   }
   return prefix;
 }
@@ -221,8 +226,8 @@ __global__ __launch_bounds__(NT) void evict_kernel(EvictParams p) {
   for (int k = 0; k < K; ++k) {
     const bool in = k * NT + tid < r.L, member = (kinds >> k & 1) == of_guarded;
     const uint32_t order = order_of(m[k]);
-    const bool stay = in && (member ? (some ? order > least : left > 0) : !of_guarded);
-    const bool tie = in && member && some && order == least;
+    const bool stay = in && (member ? (some ? order > least || (left < 0 && order == least) : left > 0) : !of_guarded);
+    const bool tie = in && member && some && left > 0 && order == least;
     stays |= (uint32_t)stay << k;
     ties |= (uint32_t)tie << k;
   }
@@ -258,7 +263,7 @@ __global__ __launch_bounds__(NT) void evict_kernel(EvictParams p) {
       if (bits >> k & 1) use(k, counts[k][wave] + __popcll(set & ((1ull << lane) - 1)));
     }
   };
-  if (some) {
+  if (some && left > 0) {
     rank(ties, [&](int k, int at) {
       if (at < left) stays |= 1u << k;
     });
@@ -358,8 +363,8 @@ __global__ __launch_bounds__(1024) void evict_long_kernel(EvictParams p) {
       else if (!some) stays = left > 0;
       else {
         const uint32_t order = order_of(m);
-        tie = order == least;
-        stays = order > least;
+        tie = left > 0 && order == least;
+        stays = order > least || (left < 0 && order == least);
       }
     }
     auto rank = [&](bool is, int k, int& total) {
@@ -429,7 +434,9 @@ __global__ __launch_bounds__(256) void evict_move_kernel(EvictParams p) {
 
 int launch_evict(const EvictParams& p, const EvictRule& r, hipStream_t s) {
   const dim3 grid(p.B * p.lists);
-  if (r.places == 2048) hipLaunchKernelGGL((evict_kernel<256, 8>), grid, dim3(256), 0, s, p);
+  if (r.places == 2048 && r.few) hipLaunchKernelGGL((evict_kernel<1024, 2>), grid, dim3(1024), 0, s, p);
+  else if (r.places == 2048) hipLaunchKernelGGL((evict_kernel<256, 8>), grid, dim3(256), 0, s, p);
+  else if (r.places == 8192 && r.few) hipLaunchKernelGGL((evict_kernel<1024, 8>), grid, dim3(1024), 0, s, p);
   else if (r.places == 8192) hipLaunchKernelGGL((evict_kernel<512, 16>), grid, dim3(512), 0, s, p);
   else if (r.places == 16384) hipLaunchKernelGGL((evict_kernel<1024, 16>), grid, dim3(1024), 0, s, p);
   else hipLaunchKernelGGL(evict_long_kernel, grid, dim3(1024), 0, s, p);
