@@ -111,32 +111,64 @@ __device__ __forceinline__ Seq seq_of(const WeightsParams& p, int b) {
   return s;
 }
 
-// Keys of a part: the parts of a request are equal, whole tiles of 64 keys.
-__device__ __forceinline__ int part_keys(const WeightsParams& p, int nk) {
-  const int blocks = (nk + 63) / 64;
-  return ((blocks + p.parts - 1) / p.parts) * 64;
+// Keys of a part: the parts of a request are equal, whole blocks of 64 keys, `least` or more.
+__device__ __forceinline__ int part_keys(const WeightsParams& p, int nk, int least = 1) {
+  const int blocks = ((nk + 63) / 64 + p.parts - 1) / p.parts;
+  return (blocks > least ? blocks : least) * 64;
 }
 
 // The units of a launch: those of request after request in one line, whose ends each
-// workgroup finds for itself.
+// workgroup finds for itself.  Where there are few requests, what is known of each is kept
+// with them.
+constexpr int kKept = 128;
 struct Line {
   int* end;              // [B] inclusive sums of the requests' units
   int* rows;             // [B] and of their rows that count
+  Seq* kept;             // [B], B <= kKept
   int all;
+  int chunk;             // blocks of 64 keys of a unit of the scores, at least
+  __device__ __forceinline__ Seq seq(const WeightsParams& p, int b) const {
+    Seq s;
+    if (p.B <= kKept) s = kept[b];
+    else s = seq_of(p, b);
+    auto uni = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+    return Seq{uni(s.row0), uni(s.rows), uni(s.index0), uni(s.used), uni(s.nk), uni(s.past)};
+  }
 };
 
-template <typename Units>
+// units(seq, chunk): units of a request.  CHUNK: whether all blocks of keys are counted
+// first, so that units of `chunk` of them are about two for each workgroup that runs at once.
+template <bool CHUNK, typename Units>
 __device__ __forceinline__ Line line_of(const WeightsParams& p, int* lds, Units units) {
   __shared__ int sums[2][WAVES];
-  Line l{lds, lds + p.B, 0};
+  __shared__ float blocks_lds[WAVES];
+  Line l{lds, lds + p.B, reinterpret_cast<Seq*>(lds + 2 * p.B), 0, 2};
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6;
   const int per = (p.B + NT - 1) / NT;
   const int b0 = tid * per < p.B ? tid * per : p.B;
   const int b1 = b0 + per < p.B ? b0 + per : p.B;
-  int n = 0, m = 0;
+  Seq only{};                                    // of the thread's first request, read once
+  float blocks = 0.0f;
   for (int b = b0; b < b1; ++b) {
     const Seq s = seq_of(p, b);
-    n += units(s);
+    if (b == b0) only = s;
+    if (p.B <= kKept) l.kept[b] = s;
+    blocks += (float)((s.rows + 31) / 32) * (float)((s.nk + 63) / 64);
+  }
+  if (CHUNK) {
+    blocks = wave_sum(blocks);
+    if (lane == 0) blocks_lds[wave] = blocks;
+    __syncthreads();
+    float all = 0.0f;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) all += blocks_lds[w];
+    const float want = all * p.n_kv * (1.0f / 2048.0f);
+    if (want > 2.0f) l.chunk = __builtin_amdgcn_readfirstlane((int)want + 1);
+  }
+  int n = 0, m = 0;
+  for (int b = b0; b < b1; ++b) {
+    const Seq s = b == b0 ? only : seq_of(p, b);
+    n += units(s, l.chunk);
     m += s.used;
   }
   int in = n, im = m;
@@ -154,8 +186,8 @@ __device__ __forceinline__ Line line_of(const WeightsParams& p, int* lds, Units 
     l.all += sums[0][w];
   }
   for (int b = b0; b < b1; ++b) {
-    const Seq s = seq_of(p, b);
-    on += units(s);
+    const Seq s = b == b0 ? only : seq_of(p, b);
+    on += units(s, l.chunk);
     om += s.used;
     l.end[b] = on;
     l.rows[b] = om;
@@ -210,6 +242,8 @@ __device__ __forceinline__ bool sees(const WeightsParams& p, const Seq& s, int b
   return true;
 }
 
+__device__ __forceinline__ float scale_of(const WeightsParams& p) { return p.scale * 1.4426950408889634f; }
+
 __device__ __forceinline__ int token_of(const WeightsParams& p, int x) {
   return (int)((__umulhi((unsigned)x, p.group_mul) + (unsigned)x) >> p.group_shift);
 }
@@ -242,6 +276,19 @@ struct Stream {
       __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void_t*)(to + RPL * q * ROW), 16,
                                                off(row) + ((uint32_t)((lane % LPR) ^ swz<DH>(row)) << 4), 0, 0, 0);
     }
+  }
+  // products of 32 rows in registers with those of a tile
+  __device__ __forceinline__ static void mul_by(f32x16_t& a, const uint8_t* tile, const bf16x8_t (&st)[DH / 16], int lane) {
+    const int fr = lane & 31;
+    bf16x8_t f[DH / 16];
+#pragma unroll
+    for (int ks = 0; ks < DH / 16; ++ks)
+      f[ks] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4_t*>(
+                                               tile + fr * ROW + (((2 * ks + (lane >> 5)) ^ swz<DH>(fr & 15)) << 4)));
+#pragma unroll
+    for (int r = 0; r < 16; ++r) a[r] = 0.0f;
+#pragma unroll
+    for (int ks = 0; ks < DH / 16; ++ks) a = __builtin_amdgcn_mfma_f32_32x32x16_bf16(st[ks], f[ks], a, 0, 0, 0);
   }
   // products of the tile's rows 32 i .. 32 i + 31 with SETS sets of 32 rows in registers; the
   // fragments are read AHEAD products before they are used
@@ -297,17 +344,17 @@ __global__ __launch_bounds__(NT, 4) void weights_stats_tile_kernel(WeightsParams
   __shared__ __attribute__((aligned(1024))) uint8_t tile1[TILE * DH * 2];
   constexpr int RT = 128 * SETS;
   const Share share(p.n_kv);
-  auto units = [&](const Seq& s) { return s.nk > 0 ? (s.rows + RT - 1) / RT * share.heads * p.parts : 0; };
-  const Line line = line_of(p, lds, units);
+  auto units = [&](const Seq& s, int) { return s.nk > 0 ? (s.rows + RT - 1) / RT * share.heads * p.parts : 0; };
+  const Line line = line_of<false>(p, lds, units);
   const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const float c = p.scale * 1.4426950408889634f;
+  const float c = scale_of(p);
   const uint16_t* q = static_cast<const uint16_t*>(p.q);
   const uint8_t* pool = static_cast<const uint8_t*>(p.pool);
   for (int u = share.first; u < line.all; u += share.step) {
     int at;
     const int b = __builtin_amdgcn_readfirstlane(request_of(line, p.B, u, at));
     at = __builtin_amdgcn_readfirstlane(at);
-    const Seq s = seq_of(p, b);
+    const Seq s = line.seq(p, b);
     const int tiles = (s.rows + RT - 1) / RT;
     const int t = at % tiles, part = at / tiles % p.parts, hk = share.head0 + at / tiles / p.parts;
     const int row0 = t * RT + wave * 32 * SETS;
@@ -468,17 +515,17 @@ __global__ __launch_bounds__(NT, 4) void weights_sum_tile_kernel(WeightsParams p
   __shared__ __attribute__((aligned(16))) int lim_lds[2][TILE];        // the keys before it are seen
   constexpr int KT = 128 * SETS;
   const Share share(p.n_kv);
-  auto units = [&](const Seq& s) { return s.used > 0 ? (s.nk + KT - 1) / KT * share.heads : 0; };
-  const Line line = line_of(p, lds, units);
+  auto units = [&](const Seq& s, int) { return s.used > 0 ? (s.nk + KT - 1) / KT * share.heads : 0; };
+  const Line line = line_of<false>(p, lds, units);
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const float c = p.scale * 1.4426950408889634f;
+  const float c = scale_of(p);
   const uint8_t* q = static_cast<const uint8_t*>(p.q);
   const uint16_t* pool = static_cast<const uint16_t*>(p.pool);
   for (int u = share.first; u < line.all; u += share.step) {
     int at;
     const int b = __builtin_amdgcn_readfirstlane(request_of(line, p.B, u, at));
     at = __builtin_amdgcn_readfirstlane(at);
-    const Seq s = seq_of(p, b);
+    const Seq s = line.seq(p, b);
     const int tiles = (s.nk + KT - 1) / KT;
     const int quot = at / tiles, hk = share.head0 + quot, key0 = (at - quot * tiles) * KT, k0 = key0 + wave * 32 * SETS;
     const int* table = p.table + (size_t)b * p.width;
@@ -584,19 +631,180 @@ __global__ __launch_bounds__(NT, 4) void weights_sum_tile_kernel(WeightsParams p
   }
 }
 
+// Requests of few rows (bf16): 32 of them against a part of the keys, whose scores are
+// kept.  Each wave walks every fourth 32 keys by itself, its tiles of its own in LDS, two
+// of them on their way, without a barrier before the end.  S = Q K^T: a lane owns a key,
+// its registers are rows, 8 for each group of four, so that only the groups with rows are
+// looked at and a row's scores go to memory 128 bytes at a time.  Bound by the read of the
+// keys.
+template <int DH>
+__global__ __launch_bounds__(NT) void weights_scores_kernel(WeightsParams p) {
+  extern __shared__ int lds[];
+  constexpr int FT = 32 * DH * 2, LOADS = 2 * Stream<DH>::LOADS;
+  __shared__ __attribute__((aligned(1024))) uint8_t tile0[WAVES * FT];
+  __shared__ __attribute__((aligned(1024))) uint8_t tile1[WAVES * FT];
+  __shared__ f32x2_t found[WAVES][32];
+  const Line line = line_of<true>(p, lds, [&](const Seq& s, int chunk) {
+    const int keys = part_keys(p, s.nk, chunk);
+    return s.nk > 0 ? (s.rows + 31) / 32 * p.n_kv * ((s.nk + keys - 1) / keys) : 0;
+  });
+  const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+  const float c = scale_of(p);
+  const uint8_t* pool = static_cast<const uint8_t*>(p.pool);
+  for (int u = blockIdx.x; u < line.all; u += gridDim.x) {
+    int at;
+    const int b = __builtin_amdgcn_readfirstlane(request_of(line, p.B, u, at));
+    at = __builtin_amdgcn_readfirstlane(at);
+    const Seq s = line.seq(p, b);
+    const int keys = part_keys(p, s.nk, line.chunk), tiles = (s.rows + 31) / 32, parts = (s.nk + keys - 1) / keys;
+    const int quot = at / tiles, r0 = (at - quot * tiles) * 32, hk = quot / parts, part = quot - hk * parts;
+    const int lo = part * keys, hi = s.nk - lo < keys ? s.nk : lo + keys;
+    const int n = hi - lo > 32 * wave ? (hi - lo - 32 * wave + 127) / 128 : 0;       // the wave's tiles
+    const int* table = p.table + (size_t)b * p.width;
+    const long long stat = stat_row(p, line, s, b, hk) + r0;
+    const int left = s.rows - r0 < 32 ? s.rows - r0 : 32;
+    // the first key to which some row may be blind
+    int open = hi;
+    if (p.mask == kMaskCausal) open = s.past + s.index0 + token_of(p, r0) + 1;
+    if (p.mask == kMaskTree) open = s.past;
+    open = open < hi ? open : hi;
+
+    // pages of the groups of 16 keys of 32 tiles, one a lane
+    auto page = [&](int k) {
+      const long long key = lo + (long long)(k + (lane >> 1)) * 128 + 32 * wave + 16 * (lane & 1);
+      return table[(int)(key < hi ? key : hi - 1) >> p.shift];
+    };
+    int id = page(0);
+    bf16x8_t st[DH / 16];
+    {
+      const int row = r0 + ((lane & 31) < left ? (lane & 31) : left - 1), tok = token_of(p, row);
+      load_row<DH>(st, static_cast<const uint16_t*>(p.q) + (long long)(s.row0 + tok) * p.q_stride +
+                           (long long)(hk * p.group + row - tok * p.group) * DH, lane);
+    }
+    bool lost[2] = {false, false};               // whether the lane's key of each buffer is on no page
+    auto load = [&](int k, auto buf) {
+      constexpr int B = decltype(buf)::value;
+      if ((k & 31) == 0 && k > 0) {
+        id = page(k);
+        __builtin_amdgcn_s_waitcnt(0x0f70);      // here, and not before each step's use of it
+      }
+      const int key = lo + k * 128 + 32 * wave;
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        const int mine = __builtin_amdgcn_readlane(id, 2 * (k & 31) + g);
+        const bool held = mine >= 0 && mine < p.n_pages;
+        int first = key + 16 * g;                // a group past the end is the last one again, as are keys past it
+        first = first < hi ? first : (hi - 1) & ~15;
+        const int most = hi - 1 - first;
+        const long long row = (((held ? (long long)mine : 0) * 2 * p.n_kv + hk) << p.shift) + (first & ((1 << p.shift) - 1));
+        Stream<DH>::load(pool + row * (DH * 2), (B ? tile1 : tile0) + wave * FT + 16 * g * DH * 2, lane,
+                         [&](int r) { return (uint32_t)((r < most ? r : most) * DH * 2); });
+        if ((lane >> 4 & 1) == g) lost[B] = !held;
+      }
+    };
+    // NG groups of 8 rows
+    auto walk = [&](auto groups) {
+      constexpr int NG = decltype(groups)::value, NR = 4 * NG;
+      float m[NR], l[NR];
+#pragma unroll
+      for (int r = 0; r < NR; ++r) {
+        m[r] = -INFINITY;
+        l[r] = 0.0f;
+      }
+      if (n > 0) load(0, std::integral_constant<int, 0>{});
+      if (n > 1) load(1, std::integral_constant<int, 1>{});
+      __builtin_amdgcn_s_waitcnt(0x0f70);        // vmcnt(0): the rows too
+      auto step = [&](int k, auto buf) {
+        constexpr int B = decltype(buf)::value;
+        // newer than this tile's loads: the other buffer's, and what the tile before has stored
+        // (rows past the last are the last again, so that the number of stores is known)
+        constexpr int NEWER = LOADS + NR;
+        __builtin_amdgcn_sched_barrier(0);
+        if (k > 0 && k + 1 < n) __builtin_amdgcn_s_waitcnt(0x0f70 | (NEWER & 15) | (NEWER >> 4) << 14);
+        else if (k + 1 < n) __builtin_amdgcn_s_waitcnt(0x0f70 | (LOADS & 15) | (LOADS >> 4) << 14);
+        else __builtin_amdgcn_s_waitcnt(0x0f70);
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+        const int k0 = lo + k * 128 + 32 * wave, key = k0 + (lane & 31);
+        f32x16_t a;
+        Stream<DH>::mul_by(a, (B ? tile1 : tile0) + wave * FT, st, lane);
+        if (k0 + 32 > open || __any(lost[B])) {
+          uint32_t own = 0;                      // bit r: the row of element r sees the key
+#pragma unroll 1
+          for (int r = 0; r < NR; ++r) {
+            const int i = r0 + 8 * (r >> 2) + 4 * half + (r & 3), tok = token_of(p, i < s.rows ? i : s.rows - 1);
+            own |= (uint32_t)(!lost[B] && sees(p, s, s.row0 + tok, s.index0 + tok, key)) << r;
+          }
+#pragma unroll
+          for (int r = 0; r < NR; ++r) a[r] = own >> r & 1 ? a[r] : -INFINITY;
+        }
+#pragma unroll
+        for (int r = 0; r < NR; ++r) {
+          const int row = 8 * (r >> 2) + 4 * half + (r & 3);
+          // past the caches: 2 to 3% of a large launch
+          __builtin_nontemporal_store(a[r], &p.scores[(stat + (row < left ? row : left - 1)) * p.places + key]);
+        }
+        if (k + 2 < n) {
+          // this tile's fragments have been read
+          __builtin_amdgcn_sched_barrier(0);
+          __builtin_amdgcn_s_waitcnt(0xc07f);    // lgkmcnt(0)
+          __builtin_amdgcn_wave_barrier();
+          __builtin_amdgcn_sched_barrier(0);
+          load(k + 2, buf);
+        }
+#pragma unroll
+        for (int r = 0; r < NR; ++r) {
+          const float x = a[r] * c, to = fmaxf(m[r], x), ref = to == -INFINITY ? 0.0f : to;
+          l[r] = l[r] * __builtin_amdgcn_exp2f(m[r] - ref) + __builtin_amdgcn_exp2f(x - ref);
+          m[r] = to;
+        }
+      };
+      for (int k = 0; k < n; k += 2) {
+        step(k, std::integral_constant<int, 0>{});
+        if (k + 1 < n) step(k + 1, std::integral_constant<int, 1>{});
+      }
+      // over the 32 keys of a half of the wave
+#pragma unroll
+      for (int r = 0; r < NR; ++r) {
+        float top = m[r];
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, kWave));
+        const float ref = top == -INFINITY ? 0.0f : top;
+        float sum = l[r] * __builtin_amdgcn_exp2f(m[r] - ref);
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor(sum, off, kWave);
+        if ((lane & 31) == 0) found[wave][8 * (r >> 2) + 4 * half + (r & 3)] = f32x2_t{top, sum};
+      }
+    };
+    if (left <= 8) walk(std::integral_constant<int, 1>{});
+    else walk(std::integral_constant<int, 4>{});
+    __syncthreads();
+    if (threadIdx.x < (unsigned)left) {
+      float top = -INFINITY, sum = 0.0f;
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) top = fmaxf(top, found[w][threadIdx.x][0]);
+      const float ref = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) sum += found[w][threadIdx.x][1] * __builtin_amdgcn_exp2f(found[w][threadIdx.x][0] - ref);
+      p.stats[(stat + threadIdx.x) * p.parts + part] = f32x2_t{top, sum};
+    }
+    __syncthreads();
+  }
+}
+
 // Maximum and sum of the rows of a tile over a part of the keys: a wave a unit.
 template <typename Tile>
 __global__ __launch_bounds__(NT) void weights_stats_kernel(WeightsParams p) {
   extern __shared__ int lds[];
   constexpr int T = Tile::T;
-  auto units = [&](const Seq& s) { return s.nk > 0 ? (s.rows + T - 1) / T * p.n_kv * p.parts : 0; };
-  const Line line = line_of(p, lds, units);
+  auto units = [&](const Seq& s, int) { return s.nk > 0 ? (s.rows + T - 1) / T * p.n_kv * p.parts : 0; };
+  const Line line = line_of<false>(p, lds, units);
   const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6;
-  const float c = p.scale * 1.4426950408889634f;
+  const float c = scale_of(p);
   for (int u = blockIdx.x * WAVES + wave; u < line.all; u += gridDim.x * WAVES) {
     int at;
     const int b = request_of(line, p.B, u, at);
-    const Seq s = seq_of(p, b);
+    const Seq s = line.seq(p, b);
     const int tiles = (s.rows + T - 1) / T;
     const int t = at % tiles, part = at / tiles % p.parts, hk = at / tiles / p.parts;
     const int row = t * T + Tile::row(lane), src = row < s.rows ? row : s.rows - 1;
@@ -636,18 +844,80 @@ __global__ __launch_bounds__(NT) void weights_stats_kernel(WeightsParams p) {
   }
 }
 
-// log2 of each row's sum, from its parts: a thread a row and head.
+// log2 of a row's sum, from its parts.
+__device__ __forceinline__ float join(const WeightsParams& p, long long r, int parts) {
+  const f32x2_t* from = p.stats + r * p.parts;
+  float top = -INFINITY, sum = 0.0f;
+  for (int k0 = 0; k0 < parts; k0 += 8) {
+    f32x2_t x[8];                                // on their way together
+#pragma unroll
+    for (int k = 0; k < 8; ++k) x[k] = from[k0 + k < parts ? k0 + k : parts - 1];
+    float to = top;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) to = fmaxf(to, x[k][0]);
+    const float ref = to == -INFINITY ? 0.0f : to;
+    sum *= __builtin_amdgcn_exp2f(top - ref);
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (k0 + k < parts) sum += x[k][1] * __builtin_amdgcn_exp2f(x[k][0] - ref);
+    top = to;
+  }
+  return top + __builtin_amdgcn_logf(sum);
+}
+
+// ... of all rows: a thread a row and head.
 __global__ __launch_bounds__(NT) void weights_lse_kernel(WeightsParams p) {
   extern __shared__ int lds[];
-  const Line line = line_of(p, lds, [&](const Seq& s) { return s.nk > 0 ? s.used : 0; });
+  const Line line = line_of<false>(p, lds, [&](const Seq& s, int) { return s.nk > 0 ? s.used : 0; });
   const long long all = (long long)line.rows[p.B - 1] * p.n_heads;
-  for (long long r = (long long)blockIdx.x * NT + threadIdx.x; r < all; r += (long long)gridDim.x * NT) {
-    const f32x2_t* from = p.stats + r * p.parts;
-    float top = -INFINITY, sum = 0.0f;
-    for (int i = 0; i < p.parts; ++i) top = fmaxf(top, from[i][0]);
-    const float ref = top == -INFINITY ? 0.0f : top;
-    for (int i = 0; i < p.parts; ++i) sum += from[i][1] * __builtin_amdgcn_exp2f(from[i][0] - ref);
-    p.lse[r] = top + __builtin_amdgcn_logf(sum);
+  for (long long r = (long long)blockIdx.x * NT + threadIdx.x; r < all; r += (long long)gridDim.x * NT) p.lse[r] = join(p, r, p.parts);
+}
+
+// The weights from scores that the statistics' launch has left: where a request has few
+// rows, those are fewer bytes than its keys.  A workgroup takes 1024 keys of a head and
+// all rows, whose logarithms it makes for itself.
+__global__ __launch_bounds__(NT) void weights_few_kernel(WeightsParams p) {
+  extern __shared__ int lds[];
+  __shared__ float lse[NT];
+  constexpr int KT = 4 * NT;
+  const Line line = line_of<true>(p, lds, [&](const Seq& s, int) { return s.used > 0 ? (s.nk + KT - 1) / KT * p.n_kv : 0; });
+  const int tid = threadIdx.x;
+  for (int u = blockIdx.x; u < line.all; u += gridDim.x) {
+    int at;
+    const int b = request_of(line, p.B, u, at);
+    const Seq s = line.seq(p, b);
+    const int tiles = (s.nk + KT - 1) / KT, hk = at / tiles, key = (at - hk * tiles) * KT + 4 * tid;
+    const long long first = stat_row(p, line, s, b, hk);
+    const int keys = part_keys(p, s.nk, line.chunk), parts = (s.nk + keys - 1) / keys;
+    f32x4_t sum = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int r0 = 0; r0 < s.rows; r0 += NT) {
+      const int n = s.rows - r0 < NT ? s.rows - r0 : NT;
+      if (tid < n) {
+        const float x = join(p, first + r0 + tid, parts);
+        lse[tid] = x == -INFINITY ? INFINITY : x;          // a row that sees no key
+      }
+      __syncthreads();
+      if (key < s.nk) {
+        const float* from = p.scores + (first + r0) * p.places + key;
+        for (int r = 0; r < n; ++r, from += p.places) {
+          f32x4_t x = *reinterpret_cast<const f32x4_t*>(from);
+          const float l = lse[r];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sum[e] += __builtin_amdgcn_exp2f(x[e] * scale_of(p) - l);
+        }
+      }
+      __syncthreads();
+    }
+    if (key < s.nk) {
+      // a page holds all four
+      const int id = p.table[(size_t)b * p.width + (key >> p.shift)];
+      if (id >= 0 && id < p.n_pages) {
+        const long long mark = (((long long)id * p.n_kv + hk) << p.shift) + (key & ((1 << p.shift) - 1));
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (key + e < s.nk) p.weight[mark + e] = p.prev ? __builtin_fmaf(p.decay, p.prev[mark + e], sum[e]) : sum[e];
+      }
+    }
   }
 }
 
@@ -656,14 +926,14 @@ template <typename Tile>
 __global__ __launch_bounds__(NT) void weights_sum_kernel(WeightsParams p) {
   extern __shared__ int lds[];
   constexpr int T = Tile::T;
-  auto units = [&](const Seq& s) { return s.used > 0 ? (s.nk + T - 1) / T * p.n_kv : 0; };
-  const Line line = line_of(p, lds, units);
+  auto units = [&](const Seq& s, int) { return s.used > 0 ? (s.nk + T - 1) / T * p.n_kv : 0; };
+  const Line line = line_of<false>(p, lds, units);
   const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6;
-  const float c = p.scale * 1.4426950408889634f;
+  const float c = scale_of(p);
   for (int u = blockIdx.x * WAVES + wave; u < line.all; u += gridDim.x * WAVES) {
     int at;
     const int b = request_of(line, p.B, u, at);
-    const Seq s = seq_of(p, b);
+    const Seq s = line.seq(p, b);
     const int tiles = (s.nk + T - 1) / T;
     const int hk = at / tiles, k0 = (at - hk * tiles) * T;
     const int* table = p.table + (size_t)b * p.width;
@@ -700,7 +970,7 @@ __global__ __launch_bounds__(NT) void weights_sum_kernel(WeightsParams p) {
 }
 
 int launch_weights(const WeightsParams& p, hipStream_t s) {
-  const size_t lds = 2 * (size_t)p.B * sizeof(int);
+  const size_t lds = 2 * (size_t)p.B * sizeof(int) + (p.B <= kKept ? p.B * sizeof(Seq) : 0);
   auto go = [&](auto tile) {
     using Tile = decltype(tile);
     hipLaunchKernelGGL((weights_stats_kernel<Tile>), dim3(2048), dim3(NT), lds, s, p);
@@ -709,6 +979,11 @@ int launch_weights(const WeightsParams& p, hipStream_t s) {
   };
   auto tiles = [&](auto dh) {
     constexpr int DH = decltype(dh)::value;
+    if (p.scores) {
+      hipLaunchKernelGGL((weights_scores_kernel<DH>), dim3(2048), dim3(NT), lds, s, p);
+      hipLaunchKernelGGL(weights_few_kernel, dim3(2048), dim3(NT), lds, s, p);
+      return;
+    }
     hipLaunchKernelGGL((weights_stats_tile_kernel<DH, 1>), dim3(1024), dim3(NT), lds, s, p);
     if (p.parts > 1) hipLaunchKernelGGL(weights_lse_kernel, dim3(256), dim3(NT), lds, s, p);
     hipLaunchKernelGGL((weights_sum_tile_kernel<DH, 1>), dim3(1024), dim3(NT), lds, s, p);

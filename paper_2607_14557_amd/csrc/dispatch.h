@@ -335,10 +335,10 @@ inline int weights_tile(bool bf16) { return bf16 ? 128 : 16; }
 // with tiles, but no more than 32 to join.
 inline int weights_want(bool bf16) { return bf16 ? 2048 : 4096; }
 constexpr int kWeightsParts = 32;
-inline int weights_parts(long long rows, int batch, int heads, int n_kv, bool bf16) {
-  const int tile = weights_tile(bf16);
+inline int weights_parts(long long rows, int batch, int heads, int n_kv, bool bf16, bool few) {
+  const int tile = few ? 32 : weights_tile(bf16);
   const long long tiles = ((rows * (heads / n_kv) + tile - 1) / tile + batch - 1) * n_kv;
-  const long long parts = weights_want(bf16) / tiles;
+  const long long parts = (few ? 4096 : weights_want(bf16)) / tiles;
   return parts < 1 ? 1 : (parts > kWeightsParts ? kWeightsParts : (int)parts);
 }
 
@@ -348,6 +348,20 @@ inline long long weights_stats(long long rows, int heads, bool bf16) {
   const long long all = rows * heads, most = (long long)weights_want(bf16) * weights_tile(bf16);
   const long long cut = all > most ? all : most;
   return cut < all * kWeightsParts ? cut : all * kWeightsParts;
+}
+
+// Whether the scores of the statistics' launch are kept for the sums (bf16): 8 bytes a row,
+// head and key, written and read, instead of the head's key again, 2 * head_dim; not for more
+// than 32 rows of a head on average, nor for more scores than this in all.
+constexpr long long kWeightsScores = 1 << 25;
+inline bool weights_few(long long rows, int batch, int heads, int n_kv, long long places, bool bf16) {
+  return bf16 && rows * (heads / n_kv) <= 32ll * batch && rows * heads <= kWeightsScores / places;
+}
+// The most that a call with up to so many rows and requests keeps.
+inline long long weights_scores(long long rows, int batch, int heads, int n_kv, long long places, bool bf16) {
+  const long long few = 32ll * batch / (heads / n_kv);       // rows of that many requests
+  const long long most = (rows < few ? rows : few) * heads;
+  return bf16 ? (most < kWeightsScores / places ? most : kWeightsScores / places) * places : 0;
 }
 
 // ---- eviction ---------------------------------------------------------------------

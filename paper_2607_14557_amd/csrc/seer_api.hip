@@ -1024,6 +1024,20 @@ int seer_row_positions(const int32_t* cu_seqlens, const int32_t* seqused, int32_
   return ok();
 }
 
+// places of a request, in whole tiles of 64
+static long long weights_places(const seer_page_desc* pages) {
+  return ((long long)pages->table_width * pages->page_size + 63) / 64 * 64;
+}
+
+// bytes of a call's statistics, their logarithms and its scores
+static size_t weights_bytes(const seer_attn_desc* d, const seer_page_desc* pages, int32_t rows_ub, int32_t batch, size_t* lse,
+                            size_t* scores) {
+  const bool bf16 = d->dtype == SEER_DTYPE_BF16;
+  *lse = up256((size_t)seer::weights_stats(rows_ub, d->n_heads, bf16) * 8);
+  *scores = *lse + up256((size_t)rows_ub * d->n_heads * 4);
+  return *scores + (size_t)seer::weights_scores(rows_ub, batch, d->n_heads, d->n_kv_heads, weights_places(pages), bf16) * 4;
+}
+
 size_t seer_attn_weights_workspace_bytes(const seer_attn_desc* desc, const seer_page_desc* pages, int32_t rows_ub,
                                          int32_t batch) {
   if (check_heads(desc) != SEER_OK || check_pages(pages) != SEER_OK) return 0;
@@ -1031,8 +1045,8 @@ size_t seer_attn_weights_workspace_bytes(const seer_attn_desc* desc, const seer_
     fail(SEER_EINVAL, "rows_ub and batch must be positive, rows_ub * n_heads below 2^31");
     return 0;
   }
-  return up256((size_t)seer::weights_stats(rows_ub, desc->n_heads, desc->dtype == SEER_DTYPE_BF16) * 8) +
-         up256((size_t)rows_ub * desc->n_heads * 4);
+  size_t lse, scores;
+  return weights_bytes(desc, pages, rows_ub, batch, &lse, &scores);
 }
 
 int seer_attn_weights(const seer_attn_desc* desc, const seer_page_desc* pages, int32_t mask, const void* q,
@@ -1079,10 +1093,15 @@ int seer_attn_weights(const seer_attn_desc* desc, const seer_page_desc* pages, i
   p.decay = decay; p.prev = decay != 0.0f ? prev : nullptr; p.weight = weight;
   long long rows = rows_ub;
   if (last > 0 && (long long)last * batch < rows) rows = (long long)last * batch;
-  p.parts = seer::weights_parts(rows, batch, p.n_heads, p.n_kv, p.bf16);
-  p.stats = static_cast<seer::f32x2_t*>(workspace);
-  p.lse = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) +
-                                   up256((size_t)seer::weights_stats(rows_ub, p.n_heads, p.bf16) * 8));
+  p.places = weights_places(pages);
+  const bool few = seer::weights_few(rows, batch, p.n_heads, p.n_kv, p.places, p.bf16);
+  p.parts = seer::weights_parts(rows, batch, p.n_heads, p.n_kv, p.bf16, few);
+  size_t lse, scores;
+  weights_bytes(desc, pages, rows_ub, batch, &lse, &scores);
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  p.stats = reinterpret_cast<seer::f32x2_t*>(ws);
+  p.lse = reinterpret_cast<float*>(ws + lse);
+  if (few) p.scores = reinterpret_cast<float*>(ws + scores);
   if (seer::launch_weights(p, stream)) return hip_fail("attention weights launch");
   return ok();
 }
