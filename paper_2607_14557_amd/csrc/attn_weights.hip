@@ -111,6 +111,35 @@ __device__ __forceinline__ Seq seq_of(const WeightsParams& p, int b) {
   return s;
 }
 
+// A lane's value of another lane of its row of 16, or of the row before, and 0 where there is
+// none: without the LDS round trip of a shuffle.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int from_lane(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false); }
+
+// Sums of the lanes up to and with each one.
+__device__ __forceinline__ int wave_scan(int v) {
+  v += from_lane<0x111, 0xf>(v);                 // one lane below, two, four, eight
+  v += from_lane<0x112, 0xf>(v);
+  v += from_lane<0x114, 0xf>(v);
+  v += from_lane<0x118, 0xf>(v);
+  v += from_lane<0x142, 0xa>(v);                 // the last lane of the row before, in rows 1 and 3
+  v += from_lane<0x143, 0xc>(v);                 // the last lane of row 1, in rows 2 and 3
+  return v;
+}
+
+// Maximum and sum over the 32 lanes of a half of the wave, in all of them.
+template <typename Op>
+__device__ __forceinline__ float half_reduce(float v, Op op) {
+  auto turn = [&](auto ctrl) {                   // around the row of 16
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(ctrl)::value, 0xf, 0xf, false));
+  };
+  v = op(v, turn(std::integral_constant<int, 0x128>{}));
+  v = op(v, turn(std::integral_constant<int, 0x124>{}));
+  v = op(v, turn(std::integral_constant<int, 0x122>{}));
+  v = op(v, turn(std::integral_constant<int, 0x121>{}));
+  return op(v, __shfl_xor(v, 16, kWave));
+}
+
 // Keys of a part: the parts of a request are equal, whole blocks of 64 keys, `least` or more.
 __device__ __forceinline__ int part_keys(const WeightsParams& p, int nk, int least = 1) {
   const int blocks = ((nk + 63) / 64 + p.parts - 1) / p.parts;
@@ -171,12 +200,7 @@ __device__ __forceinline__ Line line_of(const WeightsParams& p, int* lds, Units 
     n += units(s, l.chunk);
     m += s.used;
   }
-  int in = n, im = m;
-#pragma unroll
-  for (int off = 1; off < kWave; off <<= 1) {
-    const int a = __shfl_up(in, off, kWave), c = __shfl_up(im, off, kWave);
-    if (lane >= off) { in += a; im += c; }
-  }
+  const int in = wave_scan(n), im = wave_scan(m);
   if (lane == kWave - 1) { sums[0][wave] = in; sums[1][wave] = im; }
   __syncthreads();
   int on = in - n, om = im - m;
@@ -766,13 +790,8 @@ __global__ __launch_bounds__(NT) void weights_scores_kernel(WeightsParams p) {
       // over the 32 keys of a half of the wave
 #pragma unroll
       for (int r = 0; r < NR; ++r) {
-        float top = m[r];
-#pragma unroll
-        for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, kWave));
-        const float ref = top == -INFINITY ? 0.0f : top;
-        float sum = l[r] * __builtin_amdgcn_exp2f(m[r] - ref);
-#pragma unroll
-        for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor(sum, off, kWave);
+        const float top = half_reduce(m[r], [](float a, float b) { return fmaxf(a, b); }), ref = top == -INFINITY ? 0.0f : top;
+        const float sum = half_reduce(l[r] * __builtin_amdgcn_exp2f(m[r] - ref), [](float a, float b) { return a + b; });
         if ((lane & 31) == 0) found[wave][8 * (r >> 2) + 4 * half + (r & 3)] = f32x2_t{top, sum};
       }
     };
@@ -792,51 +811,67 @@ __global__ __launch_bounds__(NT) void weights_scores_kernel(WeightsParams p) {
   }
 }
 
-// Maximum and sum of the rows of a tile over a part of the keys: a wave a unit.
+// fp32.  Maximum and sum of the rows of a tile over a part of the keys: a wave a unit, the
+// next tile's keys on their way.
 template <typename Tile>
 __global__ __launch_bounds__(NT) void weights_stats_kernel(WeightsParams p) {
   extern __shared__ int lds[];
   constexpr int T = Tile::T;
-  auto units = [&](const Seq& s, int) { return s.nk > 0 ? (s.rows + T - 1) / T * p.n_kv * p.parts : 0; };
-  const Line line = line_of<false>(p, lds, units);
-  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6;
+  const Line line = line_of<false>(
+      p, lds, [&](const Seq& s, int) { return s.nk > 0 ? (s.rows + T - 1) / T * p.n_kv * p.parts : 0; });
+  const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const float c = scale_of(p);
   for (int u = blockIdx.x * WAVES + wave; u < line.all; u += gridDim.x * WAVES) {
     int at;
-    const int b = request_of(line, p.B, u, at);
+    const int b = __builtin_amdgcn_readfirstlane(request_of(line, p.B, u, at));
+    at = __builtin_amdgcn_readfirstlane(at);
     const Seq s = line.seq(p, b);
     const int tiles = (s.rows + T - 1) / T;
     const int t = at % tiles, part = at / tiles % p.parts, hk = at / tiles / p.parts;
     const int row = t * T + Tile::row(lane), src = row < s.rows ? row : s.rows - 1;
     const int tok = token_of(p, src), head = hk * p.group + src - tok * p.group;
-    typename Tile::Frag q, k;
+    typename Tile::Frag q, k[2];
     Tile::load(q, p.q, (long long)(s.row0 + tok) * p.q_stride + (long long)head * p.head_dim, p.head_dim, lane);
     const int keys = part_keys(p, s.nk);
     const long long begin = (long long)part * keys, end = begin + keys;
     const int lo = begin < s.nk ? (int)begin : s.nk, hi = end < s.nk ? (int)end : s.nk;
+    const int open = p.mask == kMaskCausal ? s.past + s.index0 + token_of(p, t * T) + 1 : (p.mask == kMaskTree ? s.past : s.nk);
     const int* table = p.table + (size_t)b * p.width;
     float m = -INFINITY, l = 0.0f;
-    for (int k0 = lo; k0 < hi; k0 += T) {
+    bool held[2] = {true, true};
+    auto load = [&](int k0, int i) {
       const int key = k0 + Tile::row(lane) < s.nk ? k0 + Tile::row(lane) : s.nk - 1;
-      bool held;
-      Tile::load(k, p.pool, key_row(p, table, hk, key, held), p.head_dim, lane);
-      const unsigned long long lost = ~__ballot(held);
+      Tile::load(k[i], p.pool, key_row(p, table, hk, key, held[i]), p.head_dim, lane);
+    };
+    auto step = [&](int k0, int i) {
+      if (k0 + T < hi) load(k0 + T, i ^ 1);
+      const unsigned long long lost = ~__ballot(held[i]);
       typename Tile::acc_t a;
-      Tile::mul(a, k, q);
-      float x[Tile::ACC], top = -INFINITY;
+      Tile::mul(a, k[i], q);
+      float x[Tile::ACC], top = m;
 #pragma unroll
-      for (int r = 0; r < Tile::ACC; ++r) {
-        const int i = Tile::of(lane, r);
-        const bool see = sees(p, s, s.row0 + tok, s.index0 + tok, k0 + i) && !(lost >> i & 1);
-        x[r] = see ? a[r] * c : -INFINITY;
-        top = fmaxf(top, x[r]);
+      for (int r = 0; r < Tile::ACC; ++r) x[r] = a[r] * c;
+      if (k0 + T > open || k0 + T > s.nk || lost) {
+#pragma unroll
+        for (int r = 0; r < Tile::ACC; ++r) {
+          const int j = Tile::of(lane, r);
+          const bool see = sees(p, s, s.row0 + tok, s.index0 + tok, k0 + j) && !(lost >> j & 1);
+          x[r] = see ? x[r] : -INFINITY;
+        }
       }
-      const float to = fmaxf(m, top), ref = to == -INFINITY ? 0.0f : to;
+#pragma unroll
+      for (int r = 0; r < Tile::ACC; ++r) top = fmaxf(top, x[r]);
+      const float ref = top == -INFINITY ? 0.0f : top;
       float sum = 0.0f;
 #pragma unroll
       for (int r = 0; r < Tile::ACC; ++r) sum += __builtin_amdgcn_exp2f(x[r] - ref);
       l = l * __builtin_amdgcn_exp2f(m - ref) + sum;
-      m = to;
+      m = top;
+    };
+    if (lo < hi) load(lo, 0);
+    for (int k0 = lo; k0 < hi; k0 += 2 * T) {
+      step(k0, 0);
+      if (k0 + T < hi) step(k0 + T, 1);
     }
     const float top = Tile::max(m), ref = top == -INFINITY ? 0.0f : top;
     l = Tile::sum(l * __builtin_amdgcn_exp2f(m - ref));
@@ -921,51 +956,72 @@ __global__ __launch_bounds__(NT) void weights_few_kernel(WeightsParams p) {
   }
 }
 
-// The weights of a tile of keys: a wave a unit.
+// fp32.  The weights of a tile of keys, from every fourth tile of rows a wave, whose
+// logarithms it makes from the parts, the next tile's rows on their way.
 template <typename Tile>
 __global__ __launch_bounds__(NT) void weights_sum_kernel(WeightsParams p) {
   extern __shared__ int lds[];
+  __shared__ float sums[WAVES][Tile::T];
   constexpr int T = Tile::T;
-  auto units = [&](const Seq& s, int) { return s.used > 0 ? (s.nk + T - 1) / T * p.n_kv : 0; };
-  const Line line = line_of<false>(p, lds, units);
-  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6;
+  const Line line = line_of<false>(p, lds, [&](const Seq& s, int) { return s.used > 0 ? (s.nk + T - 1) / T * p.n_kv : 0; });
+  const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const float c = scale_of(p);
-  for (int u = blockIdx.x * WAVES + wave; u < line.all; u += gridDim.x * WAVES) {
+  for (int u = blockIdx.x; u < line.all; u += gridDim.x) {
     int at;
-    const int b = request_of(line, p.B, u, at);
+    const int b = __builtin_amdgcn_readfirstlane(request_of(line, p.B, u, at));
+    at = __builtin_amdgcn_readfirstlane(at);
     const Seq s = line.seq(p, b);
     const int tiles = (s.nk + T - 1) / T;
     const int hk = at / tiles, k0 = (at - hk * tiles) * T;
     const int* table = p.table + (size_t)b * p.width;
     const int key = k0 + Tile::row(lane), src = key < s.nk ? key : s.nk - 1;
     bool held;
-    typename Tile::Frag k, q;
+    typename Tile::Frag k, q[2];
+    float lse[2];                                // of the lane's row
     const long long krow = key_row(p, table, hk, src, held);
     Tile::load(k, p.pool, krow, p.head_dim, lane);
-    const float* lse = p.lse + stat_row(p, line, s, b, hk);
-    float sum = 0.0f;
-    for (int r0 = 0; r0 < s.rows; r0 += T) {
+    const long long stat = stat_row(p, line, s, b, hk);
+    auto load = [&](int r0, int i) {
       const int row = r0 + Tile::row(lane) < s.rows ? r0 + Tile::row(lane) : s.rows - 1;
       const int tok = token_of(p, row), head = row - tok * p.group;
-      Tile::load(q, p.q, (long long)(s.row0 + tok) * p.q_stride + (long long)(hk * p.group + head) * p.head_dim, p.head_dim,
+      Tile::load(q[i], p.q, (long long)(s.row0 + tok) * p.q_stride + (long long)(hk * p.group + head) * p.head_dim, p.head_dim,
                  lane);
+      lse[i] = join(p, stat + row, p.parts);
+    };
+    float sum = 0.0f;
+    auto step = [&](int r0, int i) {
+      if (r0 + WAVES * T < s.rows) load(r0 + WAVES * T, i ^ 1);
       typename Tile::acc_t a;
-      Tile::mul(a, q, k);
+      Tile::mul(a, q[i], k);
+      const int sure = p.mask == kMaskCausal ? s.past + s.index0 + token_of(p, r0) + 1 : (p.mask == kMaskTree ? s.past : s.nk);
+      const bool masked = k0 + T > sure || r0 + T > s.rows;
 #pragma unroll
       for (int r = 0; r < Tile::ACC; ++r) {
-        const int i = r0 + Tile::of(lane, r);
-        if (i >= s.rows) continue;
-        const int it = token_of(p, i);
-        if (!sees(p, s, s.row0 + it, s.index0 + it, key)) continue;
-        sum += __builtin_amdgcn_exp2f(a[r] * c - lse[i]);
+        float w = __builtin_amdgcn_exp2f(a[r] * c - __shfl(lse[i], Tile::of(lane, r), kWave));
+        if (masked) {
+          const int j = r0 + Tile::of(lane, r), it = token_of(p, j < s.rows ? j : s.rows - 1);
+          const bool see = j < s.rows && sees(p, s, s.row0 + it, s.index0 + it, key);
+          w = see ? w : 0.0f;
+        }
+        sum += w;
       }
+    };
+    if (wave * T < s.rows) load(wave * T, 0);
+    for (int r0 = wave * T; r0 < s.rows; r0 += 2 * WAVES * T) {
+      step(r0, 0);
+      if (r0 + WAVES * T < s.rows) step(r0 + WAVES * T, 1);
     }
     sum = Tile::sum(sum);
-    if (lane < T && key < s.nk && held) {
+    if (lane < T) sums[wave][lane] = sum;
+    __syncthreads();
+    if (wave == 0 && lane < T && key < s.nk && held) {
+#pragma unroll
+      for (int w = 1; w < WAVES; ++w) sum += sums[w][lane];
       const long long id = table[key >> p.shift];
       const long long mark = (((id * p.n_kv) + hk) << p.shift) + (key & ((1 << p.shift) - 1));
       p.weight[mark] = p.prev ? __builtin_fmaf(p.decay, p.prev[mark], sum) : sum;
     }
+    __syncthreads();
   }
 }
 
@@ -974,7 +1030,6 @@ int launch_weights(const WeightsParams& p, hipStream_t s) {
   auto go = [&](auto tile) {
     using Tile = decltype(tile);
     hipLaunchKernelGGL((weights_stats_kernel<Tile>), dim3(2048), dim3(NT), lds, s, p);
-    hipLaunchKernelGGL(weights_lse_kernel, dim3(256), dim3(NT), lds, s, p);
     hipLaunchKernelGGL((weights_sum_kernel<Tile>), dim3(2048), dim3(NT), lds, s, p);
   };
   auto tiles = [&](auto dh) {

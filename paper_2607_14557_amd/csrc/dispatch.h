@@ -339,7 +339,8 @@ inline int weights_parts(long long rows, int batch, int heads, int n_kv, bool bf
   const int tile = few ? 32 : weights_tile(bf16);
   const long long tiles = ((rows * (heads / n_kv) + tile - 1) / tile + batch - 1) * n_kv;
   const long long parts = (few ? 4096 : weights_want(bf16)) / tiles;
-  return parts < 1 ? 1 : (parts > kWeightsParts ? kWeightsParts : (int)parts);
+  const int most = bf16 ? kWeightsParts : 8;
+  return parts < 1 ? 1 : (parts > most ? most : (int)parts);
 }
 
 // The most (row, head, part) that any call with up to so many rows has: as tiles are at
