@@ -111,22 +111,6 @@ __device__ __forceinline__ Seq seq_of(const WeightsParams& p, int b) {
   return s;
 }
 
-// A lane's value of another lane of its row of 16, or of the row before, and 0 where there is
-// none: without the LDS round trip of a shuffle.
-template <int CTRL, int ROWS>
-__device__ __forceinline__ int from_lane(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false); }
-
-// Sums of the lanes up to and with each one.
-__device__ __forceinline__ int wave_scan(int v) {
-  v += from_lane<0x111, 0xf>(v);                 // one lane below, two, four, eight
-  v += from_lane<0x112, 0xf>(v);
-  v += from_lane<0x114, 0xf>(v);
-  v += from_lane<0x118, 0xf>(v);
-  v += from_lane<0x142, 0xa>(v);                 // the last lane of the row before, in rows 1 and 3
-  v += from_lane<0x143, 0xc>(v);                 // the last lane of row 1, in rows 2 and 3
-  return v;
-}
-
 // Maximum and sum over the 32 lanes of a half of the wave, in all of them.
 template <typename Op>
 __device__ __forceinline__ float half_reduce(float v, Op op) {
@@ -314,11 +298,9 @@ struct Stream {
 #pragma unroll
     for (int ks = 0; ks < DH / 16; ++ks) a = __builtin_amdgcn_mfma_f32_32x32x16_bf16(st[ks], f[ks], a, 0, 0, 0);
   }
-  // products of the tile's rows 32 i .. 32 i + 31 with SETS sets of 32 rows in registers; the
-  // fragments are read AHEAD products before they are used
-  template <int SETS>
-  __device__ __forceinline__ static void mul(f32x16_t (&a)[SETS], const uint8_t* tile, int i,
-                                             const bf16x8_t (&st)[SETS][DH / 16], int lane) {
+  // products of the tile's rows 32 i .. 32 i + 31 with 32 rows in registers; the fragments
+  // are read AHEAD products before they are used
+  __device__ __forceinline__ static void mul(f32x16_t& a, const uint8_t* tile, int i, const bf16x8_t (&st)[DH / 16], int lane) {
     constexpr int KS = DH / 16, AHEAD = 3;
     const int fr = lane & 31;
     const uint8_t* row = tile + (32 * i + fr) * ROW;
@@ -331,17 +313,14 @@ struct Stream {
 #pragma unroll
     for (int ks = 0; ks < AHEAD; ++ks) f[ks] = read(ks);
 #pragma unroll
-    for (int s = 0; s < SETS; ++s)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) a[s][r] = 0.0f;
+    for (int r = 0; r < 16; ++r) a[r] = 0.0f;
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
       if (ks + AHEAD < KS) f[(ks + AHEAD) % (AHEAD + 1)] = read(ks + AHEAD);
-#pragma unroll
-      for (int s = 0; s < SETS; ++s) a[s] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[ks % (AHEAD + 1)], st[s][ks], a[s], 0, 0, 0);
+      a = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[ks % (AHEAD + 1)], st[ks], a, 0, 0, 0);
       if (ks + AHEAD < KS) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x008, SETS, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
     }
     __builtin_amdgcn_sched_barrier(0);
   }
@@ -356,17 +335,17 @@ __device__ __forceinline__ void load_row(bf16x8_t (&f)[DH / 16], const uint16_t*
 
 }  // namespace
 
-// Maximum and sum of 128 SETS rows over a part of the keys, which pass by: a lane owns
-// SETS rows, half of each tile's keys, and needs no other lane before the end.  The
+// Maximum and sum of 128 rows over a part of the keys, which pass by: a lane owns
+// a row, half of each tile's keys, and needs no other lane before the end.  The
 // reference of a row's exponentials is the maximum of the first tile in which it sees a
 // key and moves only where a later tile adds up to 2^40 of it: any reference gives the
 // same sum, and the common tile takes no maximum.
-template <int DH, int SETS>
+template <int DH>
 __global__ __launch_bounds__(NT, 4) void weights_stats_tile_kernel(WeightsParams p) {
   extern __shared__ int lds[];
   __shared__ __attribute__((aligned(1024))) uint8_t tile0[TILE * DH * 2];
   __shared__ __attribute__((aligned(1024))) uint8_t tile1[TILE * DH * 2];
-  constexpr int RT = 128 * SETS;
+  constexpr int RT = 128;
   const Share share(p.n_kv);
   auto units = [&](const Seq& s, int) { return s.nk > 0 ? (s.rows + RT - 1) / RT * share.heads * p.parts : 0; };
   const Line line = line_of<false>(p, lds, units);
@@ -381,19 +360,13 @@ __global__ __launch_bounds__(NT, 4) void weights_stats_tile_kernel(WeightsParams
     const Seq s = line.seq(p, b);
     const int tiles = (s.rows + RT - 1) / RT;
     const int t = at % tiles, part = at / tiles % p.parts, hk = share.head0 + at / tiles / p.parts;
-    const int row0 = t * RT + wave * 32 * SETS;
-    bf16x8_t st[SETS][DH / 16];
-    int index[SETS];                             // of the lane's rows among the request's rows of the call
-    float m[SETS], l[SETS];
-#pragma unroll
-    for (int e = 0; e < SETS; ++e) {
-      const int row = row0 + 32 * e + (lane & 31), src = row < s.rows ? row : s.rows - 1;
-      const int tok = token_of(p, src), head = hk * p.group + src - tok * p.group;
-      load_row<DH>(st[e], q + (long long)(s.row0 + tok) * p.q_stride + (long long)head * DH, lane);
-      index[e] = s.index0 + tok;
-      m[e] = -INFINITY;
-      l[e] = 0.0f;
-    }
+    const int row0 = t * RT + 32 * wave;
+    bf16x8_t st[DH / 16];
+    float m = -INFINITY, l = 0.0f;
+    const int row = row0 + (lane & 31), src = row < s.rows ? row : s.rows - 1;
+    const int tok = token_of(p, src), head = hk * p.group + src - tok * p.group;
+    load_row<DH>(st, q + (long long)(s.row0 + tok) * p.q_stride + (long long)head * DH, lane);
+    const int index = s.index0 + tok;            // of the lane's row among the request's rows of the call
     const int keys = part_keys(p, s.nk);
     const long long begin = (long long)part * keys, end = begin + keys;
     const int lo = begin < s.nk ? (int)begin : s.nk;
@@ -453,58 +426,50 @@ __global__ __launch_bounds__(NT, 4) void weights_stats_tile_kernel(WeightsParams
       }
       if (row0 < s.rows) {
         const bool masked = k0 + TILE > open || k0 + TILE > hi || lost != 0;
-        float x[SETS][2][16];
+        float x[2][16];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          f32x16_t a[SETS];
-          Stream<DH>::template mul<SETS>(a, B ? tile1 : tile0, i, st, lane);
+          f32x16_t a;
+          Stream<DH>::mul(a, B ? tile1 : tile0, i, st, lane);
 #pragma unroll
-          for (int e = 0; e < SETS; ++e)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) x[e][i][r] = a[e][r];
+          for (int r = 0; r < 16; ++r) x[i][r] = a[r];
         }
         if (masked) {
+          int lim = hi;
+          if (p.mask == kMaskCausal && s.past + index + 1 < lim) lim = s.past + index + 1;
+          const GqaSight<true> sight(lim, s.past, p.mask == kMaskTree ? p.bits + (size_t)(s.row0 - s.index0 + index) * p.words
+                                                                     : nullptr, p.words);
+          const unsigned long long seen = (sight.seen(k0) & ~lost) >> (4 * (lane >> 5));
 #pragma unroll
-          for (int e = 0; e < SETS; ++e) {
-            int lim = hi;
-            if (p.mask == kMaskCausal && s.past + index[e] + 1 < lim) lim = s.past + index[e] + 1;
-            const GqaSight<true> sight(lim, s.past, p.mask == kMaskTree ? p.bits + (size_t)(s.row0 - s.index0 + index[e]) * p.words
-                                                                       : nullptr, p.words);
-            const unsigned long long seen = (sight.seen(k0) & ~lost) >> (4 * (lane >> 5));
+          for (int i = 0; i < 2; ++i) {
+            const uint32_t half = (uint32_t)(seen >> (32 * i));
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              const uint32_t half = (uint32_t)(seen >> (32 * i));
-#pragma unroll
-              for (int r = 0; r < 16; ++r)
-                if (!(half >> (8 * (r >> 2) + (r & 3)) & 1)) x[e][i][r] = -INFINITY;
-            }
+            for (int r = 0; r < 16; ++r)
+              if (!(half >> (8 * (r >> 2) + (r & 3)) & 1)) x[i][r] = -INFINITY;
           }
         }
+        float sum;
+        auto add = [&](float ref) {
+          float s0 = 0.0f, s1 = 0.0f;
+          const float mc = ref * c;
 #pragma unroll
-        for (int e = 0; e < SETS; ++e) {
-          float sum;
-          auto add = [&](float ref) {
-            float s0 = 0.0f, s1 = 0.0f;
-            const float mc = ref * c;
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-              s0 += __builtin_amdgcn_exp2f(__builtin_fmaf(x[e][0][r], c, -mc));
-              s1 += __builtin_amdgcn_exp2f(__builtin_fmaf(x[e][1][r], c, -mc));
-            }
-            sum = s0 + s1;
-          };
-          add(m[e]);
-          // (no key seen yet: the reference is -inf, and -inf + inf or x + inf ask for a maximum too)
-          if (__any(!(sum < 0x1p40f))) {
-            float top = m[e];
-#pragma unroll
-            for (int r = 0; r < 16; ++r) top = fmaxf(top, fmaxf(x[e][0][r], x[e][1][r]));
-            l[e] *= m[e] == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m[e] - top) * c);
-            m[e] = top;
-            add(top == -INFINITY ? 0.0f : top);
+          for (int r = 0; r < 16; ++r) {
+            s0 += __builtin_amdgcn_exp2f(__builtin_fmaf(x[0][r], c, -mc));
+            s1 += __builtin_amdgcn_exp2f(__builtin_fmaf(x[1][r], c, -mc));
           }
-          l[e] += sum;
+          sum = s0 + s1;
+        };
+        add(m);
+        // (no key seen yet: the reference is -inf, and -inf + inf or x + inf ask for a maximum too)
+        if (__any(!(sum < 0x1p40f))) {
+          float top = m;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) top = fmaxf(top, fmaxf(x[0][r], x[1][r]));
+          l *= m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m - top) * c);
+          m = top;
+          add(top == -INFINITY ? 0.0f : top);
         }
+        l += sum;
       }
       lost = lost_next;
       __builtin_amdgcn_s_waitcnt(0x0f70);
@@ -514,30 +479,25 @@ __global__ __launch_bounds__(NT, 4) void weights_stats_tile_kernel(WeightsParams
       step(kt, std::integral_constant<int, 0>{});
       if (kt + 1 < n) step(kt + 1, std::integral_constant<int, 1>{});
     }
-#pragma unroll
-    for (int e = 0; e < SETS; ++e) {
-      const int row = row0 + 32 * e + (lane & 31);
-      const float top = fmaxf(m[e], __shfl_xor(m[e], 32, kWave)), ref = top == -INFINITY ? 0.0f : top;
-      const float part_l = l[e] * __builtin_amdgcn_exp2f((m[e] - ref) * c);
-      const float all = part_l + __shfl_xor(part_l, 32, kWave);
-      if (row < s.rows && lane < 32) {
-        const long long r = stat_row(p, line, s, b, hk) + row;
-        if (p.parts == 1) p.lse[r] = top * c + __builtin_amdgcn_logf(all);
-        else p.stats[r * p.parts + part] = f32x2_t{top * c, all};
-      }
+    const float top = fmaxf(m, __shfl_xor(m, 32, kWave)), ref = top == -INFINITY ? 0.0f : top;
+    const float part_l = l * __builtin_amdgcn_exp2f((m - ref) * c);
+    const float all = part_l + __shfl_xor(part_l, 32, kWave);
+    if (row < s.rows && lane < 32) {
+      const long long r = stat_row(p, line, s, b, hk) + row;
+      if (p.parts == 1) p.lse[r] = top * c + __builtin_amdgcn_logf(all);
+      else p.stats[r * p.parts + part] = f32x2_t{top * c, all};
     }
   }
 }
 
-// The weights of 128 SETS keys, which stay, from all rows, which pass by.
-template <int DH, int SETS>
+// The weights of 128 keys, which stay, from all rows, which pass by.
+template <int DH>
 __global__ __launch_bounds__(NT, 4) void weights_sum_tile_kernel(WeightsParams p) {
   extern __shared__ int lds[];
   __shared__ __attribute__((aligned(1024))) uint8_t tile0[TILE * DH * 2];
   __shared__ __attribute__((aligned(1024))) uint8_t tile1[TILE * DH * 2];
   __shared__ __attribute__((aligned(16))) float lse_lds[2][TILE];
-  __shared__ __attribute__((aligned(16))) int lim_lds[2][TILE];        // the keys before it are seen
-  constexpr int KT = 128 * SETS;
+  constexpr int KT = 128;
   const Share share(p.n_kv);
   auto units = [&](const Seq& s, int) { return s.used > 0 ? (s.nk + KT - 1) / KT * share.heads : 0; };
   const Line line = line_of<false>(p, lds, units);
@@ -551,20 +511,16 @@ __global__ __launch_bounds__(NT, 4) void weights_sum_tile_kernel(WeightsParams p
     at = __builtin_amdgcn_readfirstlane(at);
     const Seq s = line.seq(p, b);
     const int tiles = (s.nk + KT - 1) / KT;
-    const int quot = at / tiles, hk = share.head0 + quot, key0 = (at - quot * tiles) * KT, k0 = key0 + wave * 32 * SETS;
+    const int quot = at / tiles, hk = share.head0 + quot, key0 = (at - quot * tiles) * KT, k0 = key0 + 32 * wave;
     const int* table = p.table + (size_t)b * p.width;
-    bf16x8_t st[SETS][DH / 16];
-    long long mark[SETS];                        // where the lane's keys' weights are, -1: nowhere
-    float sum[SETS];
-#pragma unroll
-    for (int e = 0; e < SETS; ++e) {
-      const int key = k0 + 32 * e + (lane & 31), src = key < s.nk ? key : s.nk - 1;
-      bool held;
-      load_row<DH>(st[e], pool + key_row(p, table, hk, src, held), lane);
-      const long long id = table[src >> p.shift];
-      mark[e] = key < s.nk && held ? (((id * p.n_kv) + hk) << p.shift) + (key & ((1 << p.shift) - 1)) : -1;
-      sum[e] = 0.0f;
-    }
+    bf16x8_t st[DH / 16];
+    float sum = 0.0f;
+    const int key = k0 + (lane & 31), src = key < s.nk ? key : s.nk - 1;
+    bool held;
+    load_row<DH>(st, pool + key_row(p, table, hk, src, held), lane);
+    // rows that do not see the lane's key (causal): those before the first that does
+    const int behind = key - s.past - s.index0;
+    const int blind = behind > 0 ? (behind < s.used ? behind * p.group : s.rows) : 0;
     // the first row that sees a key of the workgroup's, in whole tiles
     int from = 0;
     if (p.mask == kMaskCausal) {
@@ -574,7 +530,6 @@ __global__ __launch_bounds__(NT, 4) void weights_sum_tile_kernel(WeightsParams p
     const float* lse = p.lse + stat_row(p, line, s, b, hk);
     const int n = (s.rows - from + TILE - 1) / TILE;
     float next_lse = 0.0f;
-    int next_lim = 0;
     auto load = [&](int r0, uint8_t* to) {
       int row = r0 + 16 * wave;
       row = row < s.rows ? row : s.rows - 1;     // rows past the end are the last one again
@@ -587,15 +542,12 @@ __global__ __launch_bounds__(NT, 4) void weights_sum_tile_kernel(WeightsParams p
       });
       if (wave == 0) {
         const int i = r0 + lane;
-        next_lse = i < s.rows ? lse[i] : INFINITY;
-        next_lim = p.mask == kMaskCausal ? s.past + s.index0 + token_of(p, i < s.rows ? i : s.rows - 1) + 1 : s.nk;
+        const float x = i < s.rows ? lse[i] : INFINITY;
+        next_lse = x == -INFINITY ? INFINITY : x;          // a row that sees no key
       }
     };
     auto keep = [&](int B) {
-      if (wave == 0) {
-        lse_lds[B][lane] = next_lse;
-        lim_lds[B][lane] = next_lim;
-      }
+      if (wave == 0) lse_lds[B][lane] = next_lse;
     };
     if (n > 0) {
       load(from, tile0);
@@ -610,33 +562,39 @@ __global__ __launch_bounds__(NT, 4) void weights_sum_tile_kernel(WeightsParams p
       if (k0 < s.nk) {
         const int sure = p.mask == kMaskCausal ? s.past + s.index0 + token_of(p, r0) + 1
                                                : (p.mask == kMaskTree ? s.past : s.nk);
-        const bool masked = p.mask != kMaskNone && k0 + 32 * SETS > sure;
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          f32x16_t a[SETS];
-          Stream<DH>::template mul<SETS>(a, B ? tile1 : tile0, i, st, lane);
-#pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            const int at = 32 * i + 8 * g + 4 * (lane >> 5);
-            const f32x4_t x = *reinterpret_cast<const f32x4_t*>(&lse_lds[B][at]);
-#pragma unroll
-            for (int e = 0; e < SETS; ++e)
-#pragma unroll
-              for (int r = 0; r < 4; ++r) {
-                float w = __builtin_amdgcn_exp2f(__builtin_fmaf(a[e][4 * g + r], c, -x[r]));
-                if (masked) {
-                  const int key = k0 + 32 * e + (lane & 31);
-                  bool see = key < lim_lds[B][at + r];
-                  if (p.mask == kMaskTree && key >= s.past) {
-                    const int j = key - s.past, tok = token_of(p, r0 + at + r < s.rows ? r0 + at + r : s.rows - 1);
-                    see = j >> 6 < p.words && (p.bits[(size_t)(s.row0 + tok) * p.words + (j >> 6)] >> (j & 63) & 1);
-                  }
-                  w = see ? w : 0.0f;
-                }
-                sum[e] += w;
-              }
+        const bool masked = p.mask != kMaskNone && k0 + 32 > sure;
+        unsigned long long seen = 0;             // which rows see the lane's key, in the order of its elements
+        if (masked && p.mask == kMaskCausal) {
+          const int hidden = blind - r0;
+          seen = hidden <= 0 ? ~0ull : (hidden >= TILE ? 0ull : ~0ull << hidden);
+        } else if (masked) {
+#pragma unroll 1
+          for (int r = 0; r < TILE; ++r) {
+            const int i = r0 + r < s.rows ? r0 + r : s.rows - 1;
+            seen |= (unsigned long long)sees(p, s, s.row0 + token_of(p, i), 0, key) << r;
           }
         }
+        seen >>= 4 * (lane >> 5);
+        // (two copies, so that a half's sums do not wait for the branch)
+        auto add = [&](auto blinded) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            f32x16_t a;
+            Stream<DH>::mul(a, B ? tile1 : tile0, i, st, lane);
+            const uint32_t half = (uint32_t)(seen >> (32 * i));
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+              const f32x4_t x = *reinterpret_cast<const f32x4_t*>(&lse_lds[B][32 * i + 8 * g + 4 * (lane >> 5)]);
+#pragma unroll
+              for (int r = 0; r < 4; ++r) {
+                const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(a[4 * g + r], c, -x[r]));
+                sum += !decltype(blinded)::value || (half >> (8 * g + r) & 1) ? w : 0.0f;
+              }
+            }
+          }
+        };
+        if (masked) add(std::true_type{});
+        else add(std::false_type{});
       }
       if (rt + 1 < n) keep(B ^ 1);
       __builtin_amdgcn_s_waitcnt(0x0f70);
@@ -646,11 +604,11 @@ __global__ __launch_bounds__(NT, 4) void weights_sum_tile_kernel(WeightsParams p
       step(rt, std::integral_constant<int, 0>{});
       if (rt + 1 < n) step(rt + 1, std::integral_constant<int, 1>{});
     }
-#pragma unroll
-    for (int e = 0; e < SETS; ++e) {
-      const float all = sum[e] + __shfl_xor(sum[e], 32, kWave);
-      if (lane < 32 && mark[e] >= 0)
-        p.weight[mark[e]] = p.prev ? __builtin_fmaf(p.decay, p.prev[mark[e]], all) : all;
+    const float all = sum + __shfl_xor(sum, 32, kWave);
+    const long long id = key < s.nk ? table[key >> p.shift] : -1;
+    if (lane < 32 && id >= 0 && id < p.n_pages) {
+      const long long mark = ((id * p.n_kv + hk) << p.shift) + (key & ((1 << p.shift) - 1));
+      p.weight[mark] = p.prev ? __builtin_fmaf(p.decay, p.prev[mark], all) : all;
     }
   }
 }
@@ -1039,9 +997,9 @@ int launch_weights(const WeightsParams& p, hipStream_t s) {
       hipLaunchKernelGGL(weights_few_kernel, dim3(2048), dim3(NT), lds, s, p);
       return;
     }
-    hipLaunchKernelGGL((weights_stats_tile_kernel<DH, 1>), dim3(1024), dim3(NT), lds, s, p);
+    hipLaunchKernelGGL((weights_stats_tile_kernel<DH>), dim3(1024), dim3(NT), lds, s, p);
     if (p.parts > 1) hipLaunchKernelGGL(weights_lse_kernel, dim3(256), dim3(NT), lds, s, p);
-    hipLaunchKernelGGL((weights_sum_tile_kernel<DH, 1>), dim3(1024), dim3(NT), lds, s, p);
+    hipLaunchKernelGGL((weights_sum_tile_kernel<DH>), dim3(1024), dim3(NT), lds, s, p);
   };
   if (p.bf16) {
     if (p.head_dim == 128) tiles(std::integral_constant<int, 128>{});

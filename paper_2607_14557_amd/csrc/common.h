@@ -77,6 +77,22 @@ __device__ __forceinline__ float wave_sum(float v) {
   return v;
 }
 
+// A lane's value of another lane of its row of 16, or of the row before, and 0 where there is
+// none: without the LDS round trip of a shuffle.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int from_lane(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false); }
+
+// Sums of the lanes up to and with each one.
+__device__ __forceinline__ int wave_scan(int v) {
+  v += from_lane<0x111, 0xf>(v);                 // one lane below, two, four, eight
+  v += from_lane<0x112, 0xf>(v);
+  v += from_lane<0x114, 0xf>(v);
+  v += from_lane<0x118, 0xf>(v);
+  v += from_lane<0x142, 0xa>(v);                 // the last lane of the row before, in rows 1 and 3
+  v += from_lane<0x143, 0xc>(v);                 // the last lane of row 1, in rows 2 and 3
+  return v;
+}
+
 __device__ __forceinline__ float wave_max(float v) {
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) v = fmaxf(v, __shfl_xor(v, off, kWave));

@@ -113,12 +113,7 @@ __device__ __forceinline__ uint32_t threshold(Shared<NT>& sh, int& left, Each ea
       n[i] = hist[tid * PER + i];
       own += n[i];
     }
-    int inc = own;
-#pragma unroll
-    for (int off = 1; off < kWave; off <<= 1) {
-      const int v = __shfl_up(inc, off, kWave);
-      if (lane >= off) inc += v;
-    }
+    const int inc = wave_scan(own);
     if (lane == kWave - 1) sh.part[wave] = inc;
     __syncthreads();
     int before = inc - own;
@@ -246,12 +241,7 @@ __global__ __launch_bounds__(NT) void evict_kernel(EvictParams p) {
 #pragma unroll
       for (int i = 0; i < K * NW; i += kWave) {
         const int own = i + lane < K * NW ? c[i + lane] : 0;
-        int inc = own;
-#pragma unroll
-        for (int off = 1; off < kWave; off <<= 1) {
-          const int v = __shfl_up(inc, off, kWave);
-          if (lane >= off) inc += v;
-        }
+        const int inc = wave_scan(own);
         if (i + lane < K * NW) c[i + lane] = base + inc - own;
         base += __builtin_amdgcn_readlane(inc, kWave - 1);
       }
@@ -299,7 +289,7 @@ __global__ __launch_bounds__(NT) void evict_kernel(EvictParams p) {
         if (k * NT + tid < r.N && (stays >> k & 1) && m[k].slot >= 0) {
           const long long at = mark_of(p, m[k].slot, h);
           p.weight_out[at] = m[k].w;
-          p.number_out[at] = m[k].number;
+          p.number_out[at] = p.number[at];         // (read again: held, it would cost K registers)
         }
     } else {
       unsigned long long* gone_bits = p.bits + (size_t)blockIdx.x * (p.room / 32);
