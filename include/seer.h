@@ -755,9 +755,10 @@ size_t seer_attn_weights_workspace_bytes(const seer_attn_desc* desc, const seer_
  * summed in one order: the same call gives the same bits; with other bounds
  * (rows_ub, batch, table_width) or another `last` they may differ by roundings.
  * workspace: seer_attn_weights_workspace_bytes, 256-byte aligned; it holds
- * nothing between calls.
+ * nothing between calls.  In bf16 up to 2^25 scores (128 MB) are part of it.
+ * Offsets in cu_seqlens that fall are no call: nothing is written then.
  * Errors: as seer_attn_paged; EINVAL (last < 0, decay negative or not finite),
- * EUNSUPPORTED (batch > 4096; batch * n_kv_heads * table_width * page_size of
+ * EUNSUPPORTED (rows_ub * n_heads >= 2^30; batch > 4096; batch * n_kv_heads * table_width * page_size of
  * 2^35 (bf16), 2^34 (fp32) or more). */
 int seer_attn_weights(const seer_attn_desc* desc, const seer_page_desc* pages, int32_t mask, const void* q,
                       int64_t q_stride, int32_t rows_ub, const int32_t* cu_seqlens, const int32_t* seqused,

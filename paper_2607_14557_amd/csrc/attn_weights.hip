@@ -151,6 +151,8 @@ struct Line {
 
 // units(seq, chunk): units of a request.  CHUNK: whether all blocks of keys are counted
 // first, so that units of `chunk` of them are about two for each workgroup that runs at once.
+// Row offsets that fall are no call: there are no units then, as rows would be counted twice
+// and the workspace has room for each once.
 template <bool CHUNK, typename Units>
 __device__ __forceinline__ Line line_of(const WeightsParams& p, int* lds, Units units) {
   __shared__ int sums[2][WAVES];
@@ -179,20 +181,25 @@ __device__ __forceinline__ Line line_of(const WeightsParams& p, int* lds, Units 
     if (want > 2.0f) l.chunk = __builtin_amdgcn_readfirstlane((int)want + 1);
   }
   int n = 0, m = 0;
+  bool falls = false;
   for (int b = b0; b < b1; ++b) {
     const Seq s = b == b0 ? only : seq_of(p, b);
     n += units(s, l.chunk);
     m += s.used;
+    falls |= p.cu[b + 1] < p.cu[b];
   }
+  const bool none = __any(falls);
   const int in = wave_scan(n), im = wave_scan(m);
-  if (lane == kWave - 1) { sums[0][wave] = in; sums[1][wave] = im; }
+  if (lane == kWave - 1) { sums[0][wave] = in; sums[1][wave] = none ? -1 : im; }
   __syncthreads();
-  int on = in - n, om = im - m;
+  int on = in - n, om = im - m, all = 0;
 #pragma unroll
   for (int w = 0; w < WAVES; ++w) {
     if (w < wave) { on += sums[0][w]; om += sums[1][w]; }
-    l.all += sums[0][w];
+    all += sums[0][w];
+    falls |= sums[1][w] < 0;
   }
+  l.all = falls ? 0 : all;
   for (int b = b0; b < b1; ++b) {
     const Seq s = b == b0 ? only : seq_of(p, b);
     on += units(s, l.chunk);
@@ -862,7 +869,7 @@ __device__ __forceinline__ float join(const WeightsParams& p, long long r, int p
 __global__ __launch_bounds__(NT) void weights_lse_kernel(WeightsParams p) {
   extern __shared__ int lds[];
   const Line line = line_of<false>(p, lds, [&](const Seq& s, int) { return s.nk > 0 ? s.used : 0; });
-  const long long all = (long long)line.rows[p.B - 1] * p.n_heads;
+  const long long all = line.all ? (long long)line.rows[p.B - 1] * p.n_heads : 0;
   for (long long r = (long long)blockIdx.x * NT + threadIdx.x; r < all; r += (long long)gridDim.x * NT) p.lse[r] = join(p, r, p.parts);
 }
 

@@ -1041,8 +1041,8 @@ static size_t weights_bytes(const seer_attn_desc* d, const seer_page_desc* pages
 size_t seer_attn_weights_workspace_bytes(const seer_attn_desc* desc, const seer_page_desc* pages, int32_t rows_ub,
                                          int32_t batch) {
   if (check_heads(desc) != SEER_OK || check_pages(pages) != SEER_OK) return 0;
-  if (rows_ub < 1 || batch < 1 || (long long)rows_ub * desc->n_heads >= (1ll << 31)) {
-    fail(SEER_EINVAL, "rows_ub and batch must be positive, rows_ub * n_heads below 2^31");
+  if (rows_ub < 1 || batch < 1 || (long long)rows_ub * desc->n_heads >= (1ll << 30)) {
+    fail(SEER_EINVAL, "rows_ub and batch must be positive, rows_ub * n_heads below 2^30");
     return 0;
   }
   size_t lse, scores;
@@ -1071,8 +1071,8 @@ int seer_attn_weights(const seer_attn_desc* desc, const seer_page_desc* pages, i
   if (mask == SEER_MASK_TREE && (!tree_bits || tree_words < 1))
     return fail(SEER_EINVAL, "SEER_MASK_TREE needs tree_bits and tree_words >= 1");
   if (!(decay >= 0.0f) || !isfinite(decay)) return fail(SEER_EINVAL, "decay must be finite and >= 0");
-  if ((long long)rows_ub * desc->n_heads >= (1ll << 31))
-    return fail(SEER_EUNSUPPORTED, "rows_ub * n_heads must stay below 2^31 (got %d * %d)", rows_ub, desc->n_heads);
+  if ((long long)rows_ub * desc->n_heads >= (1ll << 30))
+    return fail(SEER_EUNSUPPORTED, "rows_ub * n_heads must stay below 2^30 (got %d * %d)", rows_ub, desc->n_heads);
   const int T = desc->dtype == SEER_DTYPE_BF16 ? 32 : 16;
   // tiles of keys are counted in 31 bits
   if ((((long long)pages->table_width * pages->page_size + T - 1) / T) * desc->n_kv_heads * batch >= (1ll << 30))
