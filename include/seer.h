@@ -789,8 +789,8 @@ size_t seer_kv_evict_workspace_bytes(const seer_attn_desc* desc, const seer_page
  * between calls.
  * Errors: EINVAL (descriptions, null pointers, flags, batch < 1, first or recent
  * < 0, only one of weight_out and number_out in place, kept equal to kv_len or
- * seen, alignment), EUNSUPPORTED (desc, page_size, batch * n_kv_heads >= 2^20),
- * EWORKSPACE. */
+ * seen, alignment), EUNSUPPORTED (desc, page_size, batch * n_kv_heads >= 2^20,
+ * n_pages * n_kv_heads >= 2^31), EWORKSPACE. */
 int seer_kv_evict(const seer_attn_desc* desc, const seer_page_desc* pages, int32_t flags, const int32_t* kv_len,
                   const int32_t* budget, const int32_t* seen, int32_t batch, int32_t first, int32_t recent,
                   const int32_t* table, void* pool, const float* weight, const int32_t* number, float* weight_out,

@@ -45,7 +45,8 @@ __device__ __forceinline__ int slot_of(const EvictParams& p, const Request& r, i
 }
 // Where a slot's marks for head h are.
 __device__ __forceinline__ long long mark_of(const EvictParams& p, int slot, int h) {
-  return (((long long)(slot >> p.shift) * p.n_kv + h) << p.shift) + (slot & ((1 << p.shift) - 1));
+  // (pages times heads stay below 2^31)
+  return ((long long)((slot >> p.shift) * p.n_kv + h) << p.shift) + (slot & ((1 << p.shift) - 1));
 }
 
 struct Mark {
@@ -169,37 +170,97 @@ __device__ __forceinline__ void move_rows(const EvictParams& p, const int* from,
 
 }  // namespace
 
-// Lists of at most NT * K places.  p.fused: the workgroup moves its list's rows too;
-// otherwise it leaves the slots of what moves, and of shared lists which places below N
-// are given up, for evict_move_kernel.
+// Lanes whose place, `first` and the lane's number, lies before `end`.
+__device__ __forceinline__ unsigned long long before(int end, int first) {
+  const int n = end - first;
+  return n <= 0 ? 0ull : (n >= kWave ? ~0ull : (1ull << n) - 1);
+}
+
+// Lists of at most NT * K places, place k * NT + tid a thread's k-th.  p.fused: the workgroup
+// moves its list's rows too; otherwise it leaves the slots of what moves, and of shared lists
+// which places below N are given up, for evict_move_kernel.  All reads are on their way
+// together (one after the other they took 8 of 23 us of a list of 16 per thread); what stays
+// and moves is held as a bit a place, 64 places in two scalar registers.
 template <int NT, int K>
 __global__ __launch_bounds__(NT) void evict_kernel(EvictParams p) {
-  constexpr int NW = NT / kWave, MOST = NT * K <= 8192 ? NT * K / 2 : 1;
+  constexpr int NW = NT / kWave, MOST = NT * K / 2;
+  typedef unsigned long long bits_t;
   __shared__ Shared<NT> sh;
   __shared__ int counts[K][NW];                  // of what moves, per 64 places, then their sums before
-  __shared__ int from_lds[MOST], to_lds[MOST];
-  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6;
+  __shared__ int moving;
+  __shared__ int from[2 * MOST];                 // slots of what moves, and from MOST on those where it goes
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int b = blockIdx.x / p.lists, h = blockIdx.x % p.lists;
   const Request r = request(p, b);
   const int seen = p.seen[b];
+  const auto start = [&](int k) { return k * NT + wave * kWave; };         // the wave's first place of the k-th
+  int slot[K];
+#pragma unroll
+  for (int k = 0; k < K; ++k) slot[k] = slot_of(p, r, k * NT + tid < r.L ? k * NT + tid : 0);
   for (int i = tid; i < 3 * 2048; i += NT) (&sh.hist[0][0])[i] = 0;
   if (tid == 0) sh.guarded = 0;
-  Mark m[K];
-  uint32_t kinds = 0;                            // bit k: place k * NT + tid is protected
+  uint32_t order[K];
+  uint32_t kinds = 0;                            // bit k: the k-th place is protected
+  {
+    // of a place without a page the first slot's marks, which are not looked at
+    auto at = [&](int k) { return mark_of(p, slot[k] < 0 ? 0 : slot[k], h); };
+    auto take = [&](int k, float w, int number) {
+      const Mark m{w, number, slot[k]};
+      order[k] = order_of(m);
+      kinds |= (uint32_t)(k * NT + tid < r.L && guarded(p, m, seen)) << k;
+    };
+    constexpr int A = K <= 8 ? K : 8;            // places on their way together
+    if (!p.shared) {
 #pragma unroll
-  for (int k = 0; k < K; ++k) {
-    const int j = k * NT + tid;
-    m[k] = Mark{0.0f, 0, -1};
-    if (j < r.L) m[k] = look(p, r, h, j);
+      for (int k0 = 0; k0 < K; k0 += A) {
+        float w[A];
+        int number[A];
+#pragma unroll
+        for (int k = 0; k < A; ++k) {
+          const long long mark = at(k0 + k);
+          w[k] = p.weight[mark];
+          number[k] = p.number[mark];
+        }
+#pragma unroll
+        for (int k = 0; k < A; ++k) take(k0 + k, w[k], number[k]);
+      }
+    } else {
+      constexpr int G = 16 / A;                  // and heads of each
+#pragma unroll
+      for (int k0 = 0; k0 < K; k0 += A) {
+        double sum[A];
+        long long mark[A];
+        int number[A];
+#pragma unroll
+        for (int k = 0; k < A; ++k) {
+          mark[k] = at(k0 + k);
+          number[k] = p.number[mark[k]];
+          sum[k] = 0.0;
+        }
+        int i = 0;
+        for (; i + G <= p.n_kv; i += G) {
+          float x[A][G];
+#pragma unroll
+          for (int k = 0; k < A; ++k)
+#pragma unroll
+            for (int e = 0; e < G; ++e) x[k][e] = p.weight[mark[k] + ((long long)(i + e) << p.shift)];
+#pragma unroll
+          for (int k = 0; k < A; ++k)
+#pragma unroll
+            for (int e = 0; e < G; ++e) sum[k] += (double)x[k][e];
+        }
+        for (; i < p.n_kv; ++i)
+#pragma unroll
+          for (int k = 0; k < A; ++k) sum[k] += (double)p.weight[mark[k] + ((long long)i << p.shift)];
+#pragma unroll
+        for (int k = 0; k < A; ++k) take(k0 + k, (float)sum[k], number[k]);
+      }
+    }
   }
   __syncthreads();
   int mine = 0;
 #pragma unroll
-  for (int k = 0; k < K; ++k) {
-    const bool g = k * NT + tid < r.L && guarded(p, m[k], seen);
-    kinds |= (uint32_t)g << k;
-    mine += __popcll(__ballot(g));
-  }
+  for (int k = 0; k < K; ++k) mine += __popcll(__ballot(kinds >> k & 1));
   if (lane == 0 && mine) atomicAdd(&sh.guarded, mine);
   __syncthreads();
   // the kind of which some stay, and how many of them
@@ -208,105 +269,104 @@ __global__ __launch_bounds__(NT) void evict_kernel(EvictParams p) {
   const int members = of_guarded ? guarded_all : r.L - guarded_all;
   int left = of_guarded ? r.N : r.N - guarded_all;
   const bool some = left > 0 && left < members;
-  uint32_t least = 0;
-  if (some)
+  // members above the least order stay, and with `equal` those with exactly it
+  uint32_t least = left > 0 ? 0u : 0xffffffffu;
+  bool equal = left > 0;
+  if (some) {
     least = threshold<NT>(sh, left, [&](auto f) {
 #pragma unroll
       for (int k = 0; k < K; ++k)
-        if (k * NT + tid < r.L && (kinds >> k & 1) == of_guarded) f(order_of(m[k]));
+        if (k * NT + tid < r.L && (kinds >> k & 1) == of_guarded) f(order[k]);
     });
-  // which stay: of the places with exactly the least order, the first `left`
-  uint32_t stays = 0, ties = 0;
+    equal = left < 0;
+  }
+  // which stay
+  bits_t stays[K];
 #pragma unroll
   for (int k = 0; k < K; ++k) {
-    const bool in = k * NT + tid < r.L, member = (kinds >> k & 1) == of_guarded;
-    const uint32_t order = order_of(m[k]);
-    const bool stay = in && (member ? (some ? order > least || (left < 0 && order == least) : left > 0) : !of_guarded);
-    const bool tie = in && member && some && left > 0 && order == least;
-    stays |= (uint32_t)stay << k;
-    ties |= (uint32_t)tie << k;
+    const bits_t in = before(r.L, start(k)), kind = __ballot(kinds >> k & 1);
+    const bits_t member = of_guarded ? kind : in & ~kind;
+    const bits_t above = __ballot(order[k] > least) | (equal ? __ballot(order[k] == least) : 0ull);
+    stays[k] = (member & above) | (of_guarded ? 0ull : kind);
   }
-  // ranks in the order of the places: counts of each 64, their sums, and the ballots
-  auto rank = [&](uint32_t bits, auto use) {
-    __syncthreads();
+  // ranks in the order of the places: counts of each 64, their sums, and the bits before
+  auto rank = [&](auto set, auto use) {
+    int own = 0;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const unsigned long long set = __ballot(bits >> k & 1);
-      if (lane == 0) counts[k][wave] = __popcll(set);
+      const int n = __popcll(set(k));            // (all lanes' ballots, before one lane takes it)
+      own = lane == k ? n : own;
     }
+    __syncthreads();
+    if (lane < K) counts[lane][wave] = own;
     __syncthreads();
     if (wave == 0) {
       int* c = &counts[0][0];
       int base = 0;
 #pragma unroll
       for (int i = 0; i < K * NW; i += kWave) {
-        const int own = i + lane < K * NW ? c[i + lane] : 0;
-        const int inc = wave_scan(own);
-        if (i + lane < K * NW) c[i + lane] = base + inc - own;
+        const int n = i + lane < K * NW ? c[i + lane] : 0;
+        const int inc = wave_scan(n);
+        if (i + lane < K * NW) c[i + lane] = base + inc - n;
         base += __builtin_amdgcn_readlane(inc, kWave - 1);
       }
+      if (lane == 0) moving = base;
     }
     __syncthreads();
+    const int first = counts[lane < K ? lane : 0][wave];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const unsigned long long set = __ballot(bits >> k & 1);
-      if (bits >> k & 1) use(k, counts[k][wave] + __popcll(set & ((1ull << lane) - 1)));
+      const bits_t bits = set(k);
+      if (bits)
+        use(k, bits >> lane & 1, __builtin_amdgcn_mbcnt_hi((uint32_t)(bits >> 32), __builtin_amdgcn_mbcnt_lo(
+                                     (uint32_t)bits, __builtin_amdgcn_readlane(first, k))));
     }
   };
   if (some && left > 0) {
-    rank(ties, [&](int k, int at) {
-      if (at < left) stays |= 1u << k;
-    });
+    // of the places with exactly the least order, the first `left`
+    auto ties = [&](int k) {
+      const bits_t kind = __ballot(kinds >> k & 1);
+      return __ballot(order[k] == least) & (of_guarded ? kind : before(r.L, start(k)) & ~kind);
+    };
+    rank(ties, [&](int k, bool is, int at) { stays[k] |= __ballot(is && at < left); });
   }
   // places below N that are given up, and kept ones from N on: as many of either
-  uint32_t moves = 0;
-#pragma unroll
-  for (int k = 0; k < K; ++k) {
-    const int j = k * NT + tid;
-    if (j < r.L) moves |= (uint32_t)((j < r.N) != (bool)(stays >> k & 1)) << k;
-  }
-  int gone = 0;
-#pragma unroll
-  for (int k = 0; k < K; ++k) gone += __popcll(__ballot((moves >> k & 1) && k * NT + tid < r.N));
-  __syncthreads();
-  if (lane == 0) sh.part[wave] = gone;
-  __syncthreads();
-  int n = 0;
-#pragma unroll
-  for (int w = 0; w < NW; ++w) n += sh.part[w];
-  int* from = p.fused ? from_lds : p.moves + (size_t)blockIdx.x * 2 * p.room;
-  int* to = p.fused ? to_lds : from + p.room;
-  if (n > 0)
-    rank(moves, [&](int k, int at) {
-      if (at < n) to[at] = m[k].slot;
-      else from[at - n] = m[k].slot;
-    });
+  auto moves = [&](int k) { return (stays[k] ^ before(r.N, start(k))) & before(r.L, start(k)); };
+  // the first half of the ranks are those of places below N
+  rank(moves, [&](int k, bool is, int at) {
+    if (is) from[at < moving / 2 ? MOST + at : at - moving / 2] = slot[k];
+  });
+  const int n = moving / 2;
   if (p.weight_out != p.weight) {
     if (!p.shared) {
-      // marks that stay where they are, in another pool
+      // marks that stay where they are, in another pool (read again: held, they would cost registers)
 #pragma unroll
       for (int k = 0; k < K; ++k)
-        if (k * NT + tid < r.N && (stays >> k & 1) && m[k].slot >= 0) {
-          const long long at = mark_of(p, m[k].slot, h);
-          p.weight_out[at] = m[k].w;
-          p.number_out[at] = p.number[at];         // (read again: held, it would cost K registers)
+        if ((stays[k] & before(r.N, start(k))) >> lane & 1 && slot[k] >= 0) {
+          const long long at = mark_of(p, slot[k], h);
+          p.weight_out[at] = p.weight[at];
+          p.number_out[at] = p.number[at];
         }
     } else {
       unsigned long long* gone_bits = p.bits + (size_t)blockIdx.x * (p.room / 32);
 #pragma unroll
-      for (int k = 0; k < K; ++k) {
-        const unsigned long long set = __ballot(!(stays >> k & 1));
-        if (lane == 0 && k * NT + wave * kWave < r.N) gone_bits[(k * NT >> 6) + wave] = set;
-      }
+      for (int k = 0; k < K; ++k)
+        if (lane == 0 && start(k) < r.N) gone_bits[(k * NT >> 6) + wave] = ~stays[k];
     }
   }
   if (tid == 0) {
     if (h == 0) p.kept[b] = r.N;
     if (!p.fused) p.counts[blockIdx.x] = n;
   }
-  if (p.fused && n > 0) {
-    __syncthreads();
-    move_rows(p, from, to, n, h, 1, tid, NT);
+  __syncthreads();
+  if (p.fused) {
+    if (n > 0) move_rows(p, from, from + MOST, n, h, 1, tid, NT);
+  } else {
+    int* moves = p.moves + (size_t)blockIdx.x * 2 * p.room;
+    for (int i = tid; i < n; i += NT) {
+      moves[i] = from[i];
+      moves[p.room + i] = from[MOST + i];
+    }
   }
 }
 

@@ -1144,6 +1144,8 @@ int seer_kv_evict(const seer_attn_desc* desc, const seer_page_desc* pages, int32
   p.lists = p.shared ? 1 : desc->n_kv_heads;
   if ((long long)batch * p.lists >= 1 << 20)
     return fail(SEER_EUNSUPPORTED, "batch * n_kv_heads must stay below 2^20 (got %d * %d)", batch, p.lists);
+  if ((long long)pages->n_pages * desc->n_kv_heads >= (1ll << 31))
+    return fail(SEER_EUNSUPPORTED, "n_pages * n_kv_heads must stay below 2^31 (got %d * %d)", pages->n_pages, desc->n_kv_heads);
   p.table = table; p.n_kv = desc->n_kv_heads;
   p.head_pieces = desc->head_dim * (desc->dtype == SEER_DTYPE_BF16 ? 2 : 4) / 16;
   p.pool = static_cast<uint8_t*>(pool); p.weight = weight; p.number = number;
