@@ -899,11 +899,16 @@ __global__ __launch_bounds__(NT) void weights_few_kernel(WeightsParams p) {
       __syncthreads();
       if (key < s.nk) {
         const float* from = p.scores + (first + r0) * p.places + key;
-        for (int r = 0; r < n; ++r, from += p.places) {
-          f32x4_t x = *reinterpret_cast<const f32x4_t*>(from);
-          const float l = lse[r];
+        for (int r = 0; r < n; r += 8) {
+          f32x4_t x[8];                          // on their way together; rows past the last are the last again
 #pragma unroll
-          for (int e = 0; e < 4; ++e) sum[e] += __builtin_amdgcn_exp2f(x[e] * scale_of(p) - l);
+          for (int i = 0; i < 8; ++i) x[i] = *reinterpret_cast<const f32x4_t*>(from + (r + i < n ? r + i : n - 1) * p.places);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const float l = r + i < n ? lse[r + i] : INFINITY;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum[e] += __builtin_amdgcn_exp2f(x[i][e] * scale_of(p) - l);
+          }
         }
       }
       __syncthreads();
@@ -992,21 +997,25 @@ __global__ __launch_bounds__(NT) void weights_sum_kernel(WeightsParams p) {
 
 int launch_weights(const WeightsParams& p, hipStream_t s) {
   const size_t lds = 2 * (size_t)p.B * sizeof(int) + (p.B <= kKept ? p.B * sizeof(Seq) : 0);
+  // no more workgroups than there can be units, where a call is small (one token: 16 -> 12 us); a multiple of 8
+  auto grid = [](long long units, int most) { return dim3(units < most ? (units + 7) / 8 * 8 : most); };
+  auto tiles_of = [&](int rows) { return (p.rows * p.group / rows + p.B) * p.n_kv * p.parts; };
+  auto keys_of = [&](int keys) { return ((p.places + keys - 1) / keys) * p.B * p.n_kv; };
   auto go = [&](auto tile) {
     using Tile = decltype(tile);
-    hipLaunchKernelGGL((weights_stats_kernel<Tile>), dim3(2048), dim3(NT), lds, s, p);
-    hipLaunchKernelGGL((weights_sum_kernel<Tile>), dim3(2048), dim3(NT), lds, s, p);
+    hipLaunchKernelGGL((weights_stats_kernel<Tile>), grid(tiles_of(Tile::T) / WAVES + 1, 2048), dim3(NT), lds, s, p);
+    hipLaunchKernelGGL((weights_sum_kernel<Tile>), grid(keys_of(Tile::T), 2048), dim3(NT), lds, s, p);
   };
   auto tiles = [&](auto dh) {
     constexpr int DH = decltype(dh)::value;
     if (p.scores) {
-      hipLaunchKernelGGL((weights_scores_kernel<DH>), dim3(2048), dim3(NT), lds, s, p);
-      hipLaunchKernelGGL(weights_few_kernel, dim3(2048), dim3(NT), lds, s, p);
+      hipLaunchKernelGGL((weights_scores_kernel<DH>), grid(tiles_of(32), 2048), dim3(NT), lds, s, p);
+      hipLaunchKernelGGL(weights_few_kernel, grid(keys_of(4 * NT), 2048), dim3(NT), lds, s, p);
       return;
     }
-    hipLaunchKernelGGL((weights_stats_tile_kernel<DH>), dim3(1024), dim3(NT), lds, s, p);
-    if (p.parts > 1) hipLaunchKernelGGL(weights_lse_kernel, dim3(256), dim3(NT), lds, s, p);
-    hipLaunchKernelGGL((weights_sum_tile_kernel<DH>), dim3(1024), dim3(NT), lds, s, p);
+    hipLaunchKernelGGL((weights_stats_tile_kernel<DH>), grid(tiles_of(128), 1024), dim3(NT), lds, s, p);
+    if (p.parts > 1) hipLaunchKernelGGL(weights_lse_kernel, grid(p.rows * p.n_heads / NT + 1, 256), dim3(NT), lds, s, p);
+    hipLaunchKernelGGL((weights_sum_tile_kernel<DH>), grid(keys_of(128), 1024), dim3(NT), lds, s, p);
   };
   if (p.bf16) {
     if (p.head_dim == 128) tiles(std::integral_constant<int, 128>{});

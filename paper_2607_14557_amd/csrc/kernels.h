@@ -413,6 +413,7 @@ struct WeightsParams {
   const int* used;             // [B] or null
   int B, rows_ub;
   int last;                    // rows of a request that count, 0: all
+  long long rows;              // the most that count in all
   int n_heads, n_kv, head_dim;
   int group;                   // n_heads / n_kv, and what divides by it
   unsigned group_mul;

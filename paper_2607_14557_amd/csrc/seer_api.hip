@@ -1093,6 +1093,7 @@ int seer_attn_weights(const seer_attn_desc* desc, const seer_page_desc* pages, i
   p.decay = decay; p.prev = decay != 0.0f ? prev : nullptr; p.weight = weight;
   long long rows = rows_ub;
   if (last > 0 && (long long)last * batch < rows) rows = (long long)last * batch;
+  p.rows = rows;
   p.places = weights_places(pages);
   const bool few = seer::weights_few(rows, batch, p.n_heads, p.n_kv, p.places, p.bf16);
   p.parts = seer::weights_parts(rows, batch, p.n_heads, p.n_kv, p.bf16, few);
