@@ -331,8 +331,11 @@ inline size_t gqa_workspace(GqaLaunch g) {
 // Rows (token, head of the group) of a workgroup that makes their statistics (bf16) or of a wave (fp32).
 inline int weights_tile(bool bf16) { return bf16 ? 128 : 16; }
 
-// Parts that a request's keys are cut in for the rows' statistics: what fills the chip
-// with tiles, but no more than 32 to join.
+// Parts that a request's keys are cut in for the rows' statistics: what gives each of 1024
+// workgroups (bf16) or 4096 waves (fp32) about two tiles or one, as more parts than rows need
+// to be joined.  bf16: 64 rows of each of 7 prompts take 61 us with up to 2048 tiles, 62 with
+// 8192; windows of 16 requests 107 uncut, 116 cut in three.  fp32, trees over 1198 keys: 24 us
+// with at most 8 or 16 parts, which the second launch joins for each of its tiles, 28 with 32.
 inline int weights_want(bool bf16) { return bf16 ? 2048 : 4096; }
 constexpr int kWeightsParts = 32;
 inline int weights_parts(long long rows, int batch, int heads, int n_kv, bool bf16, bool few) {
@@ -353,31 +356,43 @@ inline long long weights_stats(long long rows, int heads, bool bf16) {
 
 // Whether the scores of the statistics' launch are kept for the sums (bf16): 8 bytes a row,
 // head and key, written and read, instead of the head's key again, 2 * head_dim; not for more
-// than 32 rows of a head on average, nor for more scores than this in all.
-constexpr long long kWeightsScores = 1 << 25;
+// than 16 rows of a head on average, nor for more scores than this in all.  Tiles and kept
+// scores, us: 64 requests over 4000 keys, 32 heads on 8, of 1 row 227 and 132, 4 rows (16 of a
+// head) 234 and 165, 8 rows 240 and 239; 16 requests over 1000 keys, 32 heads, of 16 rows 62
+// and 67, 32 rows 61 and 84; 64 requests over 2000 keys, 8 heads of 64, of 8 rows 71 and 53, 32
+// rows 72 and 93.
+constexpr long long kWeightsScores = 1 << 25, kWeightsFew = 16;
 inline bool weights_few(long long rows, int batch, int heads, int n_kv, long long places, bool bf16) {
-  return bf16 && rows * (heads / n_kv) <= 32ll * batch && rows * heads <= kWeightsScores / places;
+  return bf16 && rows * (heads / n_kv) <= kWeightsFew * batch && rows * heads <= kWeightsScores / places;
 }
 // The most that a call with up to so many rows and requests keeps.
 inline long long weights_scores(long long rows, int batch, int heads, int n_kv, long long places, bool bf16) {
-  const long long few = 32ll * batch / (heads / n_kv);       // rows of that many requests
+  const long long few = kWeightsFew * batch / (heads / n_kv);          // rows of that many requests
   const long long most = (rows < few ? rows : few) * heads;
   return bf16 ? (most < kWeightsScores / places ? most : kWeightsScores / places) * places : 0;
 }
 
 // ---- eviction ---------------------------------------------------------------------
 
+// Lists of up to 2048 places move their own rows, longer ones leave that to a second launch
+// of many workgroups; 1024 threads a list where there are fewer than two lists a CU, 256 or 512
+// otherwise.  us, lists of 1500 places in a launch of their own with 1024 and 256 threads, then
+// in two: one token over, 32 lists 12.1 and 11.2, 15.4 and 15.6; 384 lists 12.6 and 11.3, 16.2
+// and 15.6; 528 lists 16.0 and 12.3, 19.9 and 16.9; cut to 700, 32 lists 16 and 32, 15 and 17;
+// 384 lists 37 and 50, 42 and 41; 528 lists 65 and 72, 65 and 62.  Lists of 6000 cut to 1024 in
+// one launch and two: 32 lists 33 and 21, 288 lists 102 and 79, 528 lists 179 and 145 (one
+// token over 5000, 32 lists: 13 and 17).
 struct EvictRule {
   int places;            // the most of a list that a workgroup keeps in registers; 0: any number, read again
-  bool few;              // fewer lists than CUs: more threads each
+  bool few;              // few lists: more threads each
   bool fused;            // whether it moves the list's rows too, instead of a second launch
   int parts;             // workgroups of a list in that
 };
 inline EvictRule evict_rule(int lists, bool shared, long long places) {
   EvictRule r{};
   r.places = places <= 2048 ? 2048 : (places <= 8192 ? 8192 : (places <= 16384 ? 16384 : 0));
-  r.few = lists < 256;
-  r.fused = !shared && (r.places == 2048 || r.places == 8192) && lists >= 512;
+  r.few = lists < 512;
+  r.fused = !shared && r.places == 2048;
   r.parts = lists >= 4096 ? 1 : (4096 / lists > 128 ? 128 : 4096 / lists);
   return r;
 }

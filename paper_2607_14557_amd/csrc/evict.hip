@@ -8,6 +8,13 @@
 // A list is what one head keeps of a request, or all of them together.  A workgroup
 // reads a list's marks once, into registers, finds the order of the last token that
 // stays by histograms of 11, 11 and 10 bits, and ranks what moves by ballots.
+//
+// Bound by the latency of one list's steps where little moves, by bytes where much does.
+// Measured (MI355X, us): 96 requests, 8 heads, 700 to 1500 tokens, one of each evicted 12.4
+// (a launch is 5); 24 prompts of 1500 to 16,000 tokens, 4 heads, cut to 1024 40, of which the
+// choice 21 and the move of 78 MB 15 (5.2 TB/s); 16 prefixes of 32 heads, shared choice, 44, of
+// which the choice 9.5 and the move of 105 MB 25 (4.2 TB/s).  Of the 21 us of a list of 16,000,
+// the clocks say: marks 5, histograms 4.5, what stays 1.5, ranks 5, slots out 1.
 #include "common.h"
 #include "dispatch.h"
 #include "kernels.h"

@@ -45,7 +45,7 @@ int answer(const long long* v) {
 def test_form_of_weights(tmp_path):
     """Scores are kept where a request has few rows, and not where they would be many."""
     rows = [(1, 1, 32, 8, 4096, 1), (64, 64, 32, 8, 4096, 1), (1, 1, 32, 8, 4096, 0), (64, 4, 32, 8, 4096, 1),
-            (32, 4, 32, 8, 4096, 1), (33, 4, 32, 8, 4096, 1), (64, 64, 32, 8, 1 << 20, 1), (1, 1, 16, 1, 1 << 20, 1)]
+            (16, 4, 32, 8, 4096, 1), (17, 4, 32, 8, 4096, 1), (64, 64, 32, 8, 1 << 20, 1), (1, 1, 16, 1, 1 << 20, 1)]
     body = """int answer(const long long* v) { return weights_few(v[0], (int)v[1], (int)v[2], (int)v[3], v[4], v[5]); }"""
     assert _ask(tmp_path, body, rows) == [1, 1, 0, 0, 1, 0, 0, 1]
 
@@ -62,7 +62,7 @@ int answer(const long long* v) {
   const EvictRule r = evict_rule((int)v[0], v[1], v[2]);
   if (r.places && r.places < v[2]) return 1;
   if (!r.places && v[2] <= 16384) return 2;
-  if (r.fused && (v[1] || r.places > 8192 || r.places == 0)) return 3;
+  if (r.fused && (v[1] || r.places != 2048)) return 3;
   if (r.parts < 1 || r.parts * v[0] >= 1ll << 24) return 4;
   if (2 * evict_room(v[2]) < (size_t)v[2] || evict_room(v[2]) % 64) return 5;
   // slots from and to, then a bit of each place in whole words
