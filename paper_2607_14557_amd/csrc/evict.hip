@@ -13,8 +13,8 @@
 // Measured (MI355X, us): 96 requests, 8 heads, 700 to 1500 tokens, one of each evicted 12.4
 // (a launch is 5); 24 prompts of 1500 to 16,000 tokens, 4 heads, cut to 1024 40, of which the
 // choice 21 and the move of 78 MB 15 (5.2 TB/s); 16 prefixes of 32 heads, shared choice, 44, of
-// which the choice 9.5 and the move of 105 MB 25 (4.2 TB/s).  Of the 21 us of a list of 16,000,
-// the clocks say: marks 5, histograms 4.5, what stays 1.5, ranks 5, slots out 1.
+// which the choice 9.5 and the move of 105 MB 25 (4.2 TB/s).  Of the 21 us, by the
+// clocks of a list of 16,000, its marks take about 5, the histograms 4.5, what stays 1.5.
 #include "common.h"
 #include "dispatch.h"
 #include "kernels.h"
