@@ -233,6 +233,10 @@ __device__ __forceinline__ long long key_row(const WeightsParams& p, const int* 
   return ((held ? id : 0) * 2 * half + ((long long)hk << p.shift) + (key & ((1 << p.shift) - 1))) * p.head_dim;
 }
 
+__device__ __forceinline__ int token_of(const WeightsParams& p, int x) {
+  return (int)((__umulhi((unsigned)x, p.group_mul) + (unsigned)x) >> p.group_shift);
+}
+
 // Whether the row with this index among its request's rows of the call sees a key.
 __device__ __forceinline__ bool sees(const WeightsParams& p, const Seq& s, int b_row, int index, int key) {
   if (key >= s.nk) return false;
@@ -245,11 +249,24 @@ __device__ __forceinline__ bool sees(const WeightsParams& p, const Seq& s, int b
   return true;
 }
 
-__device__ __forceinline__ float scale_of(const WeightsParams& p) { return p.scale * 1.4426950408889634f; }
-
-__device__ __forceinline__ int token_of(const WeightsParams& p, int x) {
-  return (int)((__umulhi((unsigned)x, p.group_mul) + (unsigned)x) >> p.group_shift);
+// Which of the 32 keys from k0 on a row of the request (with its heads) sees, a lane a row, so
+// that the tree's words of all rows are on their way together.
+__device__ __forceinline__ uint32_t window(const WeightsParams& p, const Seq& s, int row, int k0) {
+  const int tok = token_of(p, row < s.rows ? row : s.rows - 1);
+  auto first = [](int n) { return n <= 0 ? 0u : (n >= 32 ? ~0u : (1u << n) - 1); };
+  uint32_t x = first(s.nk - k0);
+  if (p.mask == kMaskCausal) x &= first(s.past + s.index0 + tok + 1 - k0);
+  if (p.mask == kMaskTree) {
+    const int before = s.past - k0, at = before < 0 ? -before : 0, word = at >> 6, shift = at & 63;
+    const unsigned long long* bits = p.bits + (size_t)(s.row0 + tok) * p.words;
+    const unsigned long long b0 = word < p.words ? bits[word] : 0, b1 = word + 1 < p.words ? bits[word + 1] : 0;
+    const uint32_t own = (uint32_t)(b0 >> shift | (shift ? b1 << (64 - shift) : 0));
+    if (before < 32) x &= first(before) | (before > 0 ? own << before : own);
+  }
+  return x;
 }
+
+__device__ __forceinline__ float scale_of(const WeightsParams& p) { return p.scale * 1.4426950408889634f; }
 
 // Where the statistics of a request's rows for a key/value head begin: request after request, in each head
 // after head, in each row after row.
@@ -500,7 +517,7 @@ __global__ __launch_bounds__(NT, 4) void weights_sum_tile_kernel(WeightsParams p
   __shared__ __attribute__((aligned(16))) float lse_lds[2][TILE];
   constexpr int KT = 128;
   const Share share(p.n_kv);
-  auto units = [&](const Seq& s, int) { return s.used > 0 ? (s.nk + KT - 1) / KT * share.heads : 0; };
+  auto units = [&](const Seq& s, int) { return s.used > 0 ? (s.nk + KT - 1) / KT * share.heads * p.sums : 0; };
   const Line line = line_of<false>(p, lds, units);
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const float c = scale_of(p);
@@ -512,7 +529,8 @@ __global__ __launch_bounds__(NT, 4) void weights_sum_tile_kernel(WeightsParams p
     at = __builtin_amdgcn_readfirstlane(at);
     const Seq s = line.seq(p, b);
     const int tiles = (s.nk + KT - 1) / KT;
-    const int quot = at / tiles, hk = share.head0 + quot, key0 = (at - quot * tiles) * KT, k0 = key0 + 32 * wave;
+    const int quot = at / tiles, key0 = (at - quot * tiles) * KT, k0 = key0 + 32 * wave;
+    const int hk = share.head0 + quot / p.sums, part = quot % p.sums;
     const int* table = p.table + (size_t)b * p.width;
     bf16x8_t st[DH / 16];
     float sum = 0.0f;
@@ -529,7 +547,12 @@ __global__ __launch_bounds__(NT, 4) void weights_sum_tile_kernel(WeightsParams p
       if (token > 0) from = token < s.used ? token * p.group / TILE * TILE : s.rows;
     }
     const float* lse = p.lse + stat_row(p, line, s, b, hk);
-    const int n = (s.rows - from + TILE - 1) / TILE;
+    int n = (s.rows - from + TILE - 1) / TILE;
+    if (p.sums > 1) {                            // an equal share of them
+      const int per = (n + p.sums - 1) / p.sums, skip = part * per < n ? part * per : n;
+      from += skip * TILE;
+      n = n - skip < per ? n - skip : per;
+    }
     float next_lse = 0.0f;
     auto load = [&](int r0, uint8_t* to) {
       int row = r0 + 16 * wave;
@@ -569,10 +592,12 @@ __global__ __launch_bounds__(NT, 4) void weights_sum_tile_kernel(WeightsParams p
           const int hidden = blind - r0;
           seen = hidden <= 0 ? ~0ull : (hidden >= TILE ? 0ull : ~0ull << hidden);
         } else if (masked) {
-#pragma unroll 1
-          for (int r = 0; r < TILE; ++r) {
-            const int i = r0 + r < s.rows ? r0 + r : s.rows - 1;
-            seen |= (unsigned long long)sees(p, s, s.row0 + token_of(p, i), 0, key) << r;
+          const uint32_t keys = window(p, s, r0 + lane, k0);
+#pragma unroll
+          for (int r = 0; r < 32; ++r) {
+            const uint32_t low = __builtin_amdgcn_readlane(keys, r) >> (lane & 31) & 1;
+            const uint32_t high = __builtin_amdgcn_readlane(keys, r + 32) >> (lane & 31) & 1;
+            seen |= low << r | (unsigned long long)(high << r) << 32;
           }
         }
         seen >>= 4 * (lane >> 5);
@@ -606,11 +631,35 @@ __global__ __launch_bounds__(NT, 4) void weights_sum_tile_kernel(WeightsParams p
       if (rt + 1 < n) step(rt + 1, std::integral_constant<int, 1>{});
     }
     const float all = sum + __shfl_xor(sum, 32, kWave);
+    if (p.sums > 1) {
+      if (lane < 32 && key < s.nk) p.partial[(((long long)b * p.n_kv + hk) * p.places + key) * p.sums + part] = all;
+      continue;
+    }
     const long long id = key < s.nk ? table[key >> p.shift] : -1;
     if (lane < 32 && id >= 0 && id < p.n_pages) {
       const long long mark = ((id * p.n_kv + hk) << p.shift) + (key & ((1 << p.shift) - 1));
       p.weight[mark] = p.prev ? __builtin_fmaf(p.decay, p.prev[mark], all) : all;
     }
+  }
+}
+
+// The weights from the sums of parts of the rows, in their order.
+__global__ __launch_bounds__(NT) void weights_join_kernel(WeightsParams p) {
+  extern __shared__ int lds[];
+  const Line line = line_of<false>(p, lds, [&](const Seq& s, int) { return s.used > 0 ? (s.nk + NT - 1) / NT * p.n_kv : 0; });
+  for (int u = blockIdx.x; u < line.all; u += gridDim.x) {
+    int at;
+    const int b = request_of(line, p.B, u, at);
+    const Seq s = line.seq(p, b);
+    const int tiles = (s.nk + NT - 1) / NT, hk = at / tiles, key = (at - hk * tiles) * NT + threadIdx.x;
+    if (key >= s.nk) continue;
+    const long long id = p.table[(size_t)b * p.width + (key >> p.shift)];
+    if (id < 0 || id >= p.n_pages) continue;
+    const float* from = p.partial + (((long long)b * p.n_kv + hk) * p.places + key) * p.sums;
+    float sum = 0.0f;
+    for (int i = 0; i < p.sums; ++i) sum += from[i];
+    const long long mark = ((id * p.n_kv + hk) << p.shift) + (key & ((1 << p.shift) - 1));
+    p.weight[mark] = p.prev ? __builtin_fmaf(p.decay, p.prev[mark], sum) : sum;
   }
 }
 
@@ -712,14 +761,14 @@ __global__ __launch_bounds__(NT) void weights_scores_kernel(WeightsParams p) {
         f32x16_t a;
         Stream<DH>::mul_by(a, (B ? tile1 : tile0) + wave * FT, st, lane);
         if (k0 + 32 > open || __any(lost[B])) {
-          uint32_t own = 0;                      // bit r: the row of element r sees the key
-#pragma unroll 1
-          for (int r = 0; r < NR; ++r) {
-            const int i = r0 + 8 * (r >> 2) + 4 * half + (r & 3), tok = token_of(p, i < s.rows ? i : s.rows - 1);
-            own |= (uint32_t)(!lost[B] && sees(p, s, s.row0 + tok, s.index0 + tok, key)) << r;
-          }
+          const uint32_t keys = window(p, s, r0 + (lane & 31), k0);
 #pragma unroll
-          for (int r = 0; r < NR; ++r) a[r] = own >> r & 1 ? a[r] : -INFINITY;
+          for (int r = 0; r < NR; ++r) {
+            const int row = 8 * (r >> 2) + (r & 3);
+            const uint32_t low = __builtin_amdgcn_readlane(keys, row), high = __builtin_amdgcn_readlane(keys, row + 4);
+            const bool see = (half ? high : low) >> (lane & 31) & 1;
+            a[r] = see && !lost[B] ? a[r] : -INFINITY;
+          }
         }
 #pragma unroll
         for (int r = 0; r < NR; ++r) {
@@ -1009,7 +1058,8 @@ int launch_weights(const WeightsParams& p, hipStream_t s) {
     }
     hipLaunchKernelGGL((weights_stats_tile_kernel<DH>), grid(tiles_of(128), 1024), dim3(NT), lds, s, p);
     if (p.parts > 1) hipLaunchKernelGGL(weights_lse_kernel, grid(p.rows * p.n_heads / NT + 1, 256), dim3(NT), lds, s, p);
-    hipLaunchKernelGGL((weights_sum_tile_kernel<DH>), grid(keys_of(128), 1024), dim3(NT), lds, s, p);
+    hipLaunchKernelGGL((weights_sum_tile_kernel<DH>), grid(keys_of(128) * p.sums, 1024), dim3(NT), lds, s, p);
+    if (p.sums > 1) hipLaunchKernelGGL(weights_join_kernel, grid(keys_of(NT), 1024), dim3(NT), lds, s, p);
   };
   if (p.bf16) {
     if (p.head_dim == 128) tiles(std::integral_constant<int, 128>{});

@@ -372,6 +372,22 @@ inline long long weights_scores(long long rows, int batch, int heads, int n_kv, 
   return bf16 ? (most < kWeightsScores / places ? most : kWeightsScores / places) * places : 0;
 }
 
+// Parts that a request's rows are cut in for the sums (bf16, tiles): where the tiles of keys are
+// few and the rows many, as with one or two key/value heads; 4 tiles of 64 rows each if one
+// request has twice what all have on average.  Uncut and cut, us: 256 rows over 1056 keys, 32
+// heads on 8, 45 and 35; 512 rows 66 and 41; 64 rows over 4064 keys, 16 heads on 1, 37 and 26;
+// 8 requests of 150 rows over 450 keys, 14 heads on 2 of 64, 43 and 34; 5 of up to 400 rows over up
+// to 900 keys 66 and 32; 8 of 64 rows over 564 keys, 32 heads on 8, 28 and 31 (not cut by this).
+constexpr int kWeightsSums = 16, kWeightsSumTiles = 1024;
+inline int weights_sums(long long rows, int batch, int heads, int n_kv, long long places) {
+  const long long tiles = (places + 127) / 128 * batch * n_kv;
+  long long parts = 2 * rows * (heads / n_kv) / (64 * 4 * (batch + 1ll));
+  parts = parts < kWeightsSumTiles / tiles ? parts : kWeightsSumTiles / tiles;
+  return parts < 2 ? 1 : (parts > kWeightsSums ? kWeightsSums : (int)parts);
+}
+// The most floats of them: parts * tiles * 128.
+constexpr long long kWeightsPartial = kWeightsSumTiles * 128;
+
 // ---- eviction ---------------------------------------------------------------------
 
 // Lists of up to 2048 places move their own rows, longer ones leave that to a second launch

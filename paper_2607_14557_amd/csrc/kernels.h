@@ -431,9 +431,11 @@ struct WeightsParams {
   const float* prev;           // or null
   float* weight;
   int parts;                   // of a request's keys, whose statistics are joined
+  int sums;                    // parts of a request's rows, whose sums are joined
   f32x2_t* stats;              // [rows that count][n_heads][parts] maximum, sum
   float* lse;                  // [rows that count][n_heads] log2 of the sum
   float* scores;               // [rows that count][n_heads][places] q . k, or null
+  float* partial;              // [B][n_kv][places][sums]
   long long places;            // of a request, in whole 64
 };
 int launch_weights(const WeightsParams& p, hipStream_t s);

@@ -1035,7 +1035,9 @@ static size_t weights_bytes(const seer_attn_desc* d, const seer_page_desc* pages
   const bool bf16 = d->dtype == SEER_DTYPE_BF16;
   *lse = up256((size_t)seer::weights_stats(rows_ub, d->n_heads, bf16) * 8);
   *scores = *lse + up256((size_t)rows_ub * d->n_heads * 4);
-  return *scores + (size_t)seer::weights_scores(rows_ub, batch, d->n_heads, d->n_kv_heads, weights_places(pages), bf16) * 4;
+  // scores, or sums of parts of the rows: a call has the ones or the others
+  const long long kept = seer::weights_scores(rows_ub, batch, d->n_heads, d->n_kv_heads, weights_places(pages), bf16);
+  return *scores + (size_t)(bf16 && kept < seer::kWeightsPartial ? seer::kWeightsPartial : kept) * 4;
 }
 
 size_t seer_attn_weights_workspace_bytes(const seer_attn_desc* desc, const seer_page_desc* pages, int32_t rows_ub,
@@ -1102,7 +1104,9 @@ int seer_attn_weights(const seer_attn_desc* desc, const seer_page_desc* pages, i
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   p.stats = reinterpret_cast<seer::f32x2_t*>(ws);
   p.lse = reinterpret_cast<float*>(ws + lse);
+  p.sums = p.bf16 && !few ? seer::weights_sums(rows, batch, p.n_heads, p.n_kv, p.places) : 1;
   if (few) p.scores = reinterpret_cast<float*>(ws + scores);
+  else if (p.sums > 1) p.partial = reinterpret_cast<float*>(ws + scores);
   if (seer::launch_weights(p, stream)) return hip_fail("attention weights launch");
   return ok();
 }

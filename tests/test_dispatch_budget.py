@@ -36,6 +36,8 @@ int answer(const long long* v) {
   if (v[0] * heads * parts > weights_stats(v[2], heads, bf16)) return 2;
   if (few && v[0] * heads * places > weights_scores(v[2], batch, heads, kv, places, bf16)) return 3;
   if (few && !bf16) return 4;
+  const int sums = weights_sums(v[0], b, heads, kv, places);
+  if (sums < 1 || sums > kWeightsSums || (sums > 1 && sums * (long long)b * kv * places > kWeightsPartial)) return 6;
   return weights_scores(v[2], batch, heads, kv, places, bf16) > kWeightsScores ? 5 : 0;
 }
 """

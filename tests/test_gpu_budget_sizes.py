@@ -64,6 +64,33 @@ def test_rows_of_a_tile(S, rows):
         c.check(mask, last=8)
 
 
+@pytest.mark.parametrize("kind,H,KV,D", [("bf16", 16, 1, 128), ("v16", 14, 2, 64), ("bf16", 8, 8, 64)])
+@pytest.mark.parametrize("mask", ["causal", "none", "tree"])
+def test_rows_in_parts(S, kind, H, KV, D, mask):
+    """Many rows over few keys: each tile of keys adds its rows up in parts, some of which have none."""
+    for past, lens, last in (([300], [100], 0), ([70, 0, 5], [3, 130, 0], 0), ([0, 200], [150, 90], 70), ([0], [600], 0)):
+        if KV == 8:
+            past, lens = past[:1], [8 * n for n in lens[:1]]
+        if mask == "tree" and max(lens) > 200:
+            continue
+        c = Call(S, kind, H, KV, D, past, lens, bits=_bits(lens) if mask == "tree" else None, page=64)
+        for decay in (1.0, 0.0):
+            c.run(mask, last=last, decay=decay)
+            c.check(mask, last=last, decay=decay)
+
+
+@pytest.mark.parametrize("kind,H,KV,D", [("bf16", 4, 1, 128), ("bf16", 8, 8, 64), ("bf16", 16, 1, 64)])
+def test_trees_across_words(S, kind, H, KV, D):
+    """Trees whose first key lies at several places of a tile of 32 keys, and whose rows pass a word of 64."""
+    for past in (0, 1, 31, 32, 33, 63, 64, 95, 100, 127):
+        lens = [70, 1, 9, 2]
+        c = Call(S, kind, H, KV, D, [past, past + 1, past, 0], lens, bits=_bits(lens, past))
+        c.run("tree")
+        c.check("tree")
+        c.run("tree", last=2)
+        c.check("tree", last=2)
+
+
 def test_most_requests(S):
     """As many as a call takes, most of one token: the requests' line is at its longest beside the scores' tiles."""
     r = np.random.default_rng(9)
