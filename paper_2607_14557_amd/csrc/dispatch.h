@@ -336,14 +336,18 @@ inline int weights_tile(bool bf16) { return bf16 ? 128 : 16; }
 // to be joined.  bf16: 64 rows of each of 7 prompts take 61 us with up to 2048 tiles, 62 with
 // 8192; windows of 16 requests 107 uncut, 116 cut in three.  fp32, trees over 1198 keys: 24 us
 // with at most 8 or 16 parts, which the second launch joins for each of its tiles, 28 with 32.
+// bf16 parts are of 256 keys or more, as their join is a launch: with at least 64, 256 and 1024,
+// 100 rows over 2000 keys, 28 heads on 4, take 31, 28 and 38 us, 4 requests of 64 rows over 264
+// keys 20, 19 and 19, over 964 keys 25, 22 and 30, over 3964 39, 39 and 45.
 inline int weights_want(bool bf16) { return bf16 ? 2048 : 4096; }
-constexpr int kWeightsParts = 32;
-inline int weights_parts(long long rows, int batch, int heads, int n_kv, bool bf16, bool few) {
+constexpr int kWeightsParts = 32, kWeightsPart = 256;
+inline int weights_parts(long long rows, int batch, int heads, int n_kv, long long places, bool bf16, bool few) {
   const int tile = few ? 32 : weights_tile(bf16);
   const long long tiles = ((rows * (heads / n_kv) + tile - 1) / tile + batch - 1) * n_kv;
   const long long parts = (few ? 4096 : weights_want(bf16)) / tiles;
-  const int most = bf16 ? kWeightsParts : 8;
-  return parts < 1 ? 1 : (parts > most ? most : (int)parts);
+  long long most = bf16 ? kWeightsParts : 8;
+  if (bf16 && !few && places / kWeightsPart < most) most = places / kWeightsPart;
+  return parts < 1 || most < 1 ? 1 : (int)(parts > most ? most : parts);
 }
 
 // The most (row, head, part) that any call with up to so many rows has: as tiles are at

@@ -1098,7 +1098,7 @@ int seer_attn_weights(const seer_attn_desc* desc, const seer_page_desc* pages, i
   p.rows = rows;
   p.places = weights_places(pages);
   const bool few = seer::weights_few(rows, batch, p.n_heads, p.n_kv, p.places, p.bf16);
-  p.parts = seer::weights_parts(rows, batch, p.n_heads, p.n_kv, p.bf16, few);
+  p.parts = seer::weights_parts(rows, batch, p.n_heads, p.n_kv, p.places, p.bf16, few);
   size_t lse, scores;
   weights_bytes(desc, pages, rows_ub, batch, &lse, &scores);
   uint8_t* ws = static_cast<uint8_t*>(workspace);

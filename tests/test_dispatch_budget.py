@@ -31,7 +31,7 @@ int answer(const long long* v) {
   const long long places = v[6];
   const bool bf16 = v[7];
   const bool few = weights_few(v[0], b, heads, kv, places, bf16);
-  const int parts = weights_parts(v[0], b, heads, kv, bf16, few);
+  const int parts = weights_parts(v[0], b, heads, kv, places, bf16, few);
   if (parts < 1 || parts > kWeightsParts) return 1;
   if (v[0] * heads * parts > weights_stats(v[2], heads, bf16)) return 2;
   if (few && v[0] * heads * places > weights_scores(v[2], batch, heads, kv, places, bf16)) return 3;
