@@ -4,14 +4,16 @@
 //   p_ihj = exp(s_ihj - lse_ih),  s = scale q . k,  lse_ih = log sum_j exp(s_ihj) over the keys that row i sees
 //
 // per key/value head.  A row's sum is known when all its keys have been seen, so there are
-// two passes; each weight is written once, by one wave that adds in one order: no atomics,
-// the same bits every time.  Three forms, by the call's bounds (dispatch.h):
+// two passes; each weight is added up by one wave, or by one for each part of the rows and
+// then part after part: no atomics, the same bits every time.  Three forms, by the call's bounds (dispatch.h):
 //
 //   bf16, many rows   weights_stats_tile_kernel: 128 rows stay in registers, keys pass by in
 //                     LDS tiles of 64 (S^T = K Q^T, a lane owns a row); where the rows' tiles
 //                     are few, each takes a part of the keys and weights_lse_kernel joins the
 //                     parts.  weights_sum_tile_kernel: 128 keys stay, rows pass by (S = Q K^T,
-//                     a lane owns a key and adds up its rows in a register).  The scores are
+//                     a lane owns a key and adds up its rows in a register); where those
+//                     tiles are few, each takes a part of the rows and weights_join_kernel
+//                     adds the parts.  The scores are
 //                     made twice: 4 bytes a score, written and read, would take 170 us of the
 //                     windows below where the second product takes 30.
 //   bf16, few rows    weights_scores_kernel reads the keys once and keeps the scores, which are
@@ -19,10 +21,10 @@
 //   fp32              weights_stats_kernel and weights_sum_kernel, tiles of 16 x 16 a wave.
 //
 // Measured (MI355X, us): 3076 rows of 16 requests over 793 cached keys each and their own, 32
-// heads: 107, of which the first pass 50 and the second 60; 64 rows each of 7 prompts of 1500 to
+// heads: 104, of which the first pass 50 and the second 60; 64 rows each of 7 prompts of 1500 to
 // 8192 tokens, 32 heads on 8: 61; a token of 64 requests over 294,950 keys, 28 heads on 4: 89,
 // of which 67 read the keys at 4.6 TB/s; one token over 794 keys: 12; trees of drafted tokens in
-// fp32 over 1198 keys: 24.
+// fp32 over 1198 keys: 18.6.
 #include <limits.h>
 
 #include <type_traits>
@@ -819,17 +821,18 @@ __global__ __launch_bounds__(NT) void weights_scores_kernel(WeightsParams p) {
   }
 }
 
-// fp32.  Maximum and sum of the rows of a tile over a part of the keys: a wave a unit, the
-// next tile's keys on their way.
+// fp32.  Maximum and sum of the rows of a tile over a part of the keys, every fourth tile of
+// keys a wave, the next one on its way.  Bound by latency: trees of 54 rows over 1198 keys.
 template <typename Tile>
 __global__ __launch_bounds__(NT) void weights_stats_kernel(WeightsParams p) {
   extern __shared__ int lds[];
-  constexpr int T = Tile::T;
+  constexpr int T = Tile::T, STEP = WAVES * T;
+  __shared__ f32x2_t found[WAVES][T];
   const Line line = line_of<false>(
       p, lds, [&](const Seq& s, int) { return s.nk > 0 ? (s.rows + T - 1) / T * p.n_kv * p.parts : 0; });
   const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const float c = scale_of(p);
-  for (int u = blockIdx.x * WAVES + wave; u < line.all; u += gridDim.x * WAVES) {
+  for (int u = blockIdx.x; u < line.all; u += gridDim.x) {
     int at;
     const int b = __builtin_amdgcn_readfirstlane(request_of(line, p.B, u, at));
     at = __builtin_amdgcn_readfirstlane(at);
@@ -852,7 +855,7 @@ __global__ __launch_bounds__(NT) void weights_stats_kernel(WeightsParams p) {
       Tile::load(k[i], p.pool, key_row(p, table, hk, key, held[i]), p.head_dim, lane);
     };
     auto step = [&](int k0, int i) {
-      if (k0 + T < hi) load(k0 + T, i ^ 1);
+      if (k0 + STEP < hi) load(k0 + STEP, i ^ 1);
       const unsigned long long lost = ~__ballot(held[i]);
       typename Tile::acc_t a;
       Tile::mul(a, k[i], q);
@@ -863,6 +866,7 @@ __global__ __launch_bounds__(NT) void weights_stats_kernel(WeightsParams p) {
 #pragma unroll
         for (int r = 0; r < Tile::ACC; ++r) {
           const int j = Tile::of(lane, r);
+          // (a choice, not a branch around an assignment: the compiler lost that one here)
           const bool see = sees(p, s, s.row0 + tok, s.index0 + tok, k0 + j) && !(lost >> j & 1);
           x[r] = see ? x[r] : -INFINITY;
         }
@@ -876,14 +880,25 @@ __global__ __launch_bounds__(NT) void weights_stats_kernel(WeightsParams p) {
       l = l * __builtin_amdgcn_exp2f(m - ref) + sum;
       m = top;
     };
-    if (lo < hi) load(lo, 0);
-    for (int k0 = lo; k0 < hi; k0 += 2 * T) {
+    if (lo + wave * T < hi) load(lo + wave * T, 0);
+    for (int k0 = lo + wave * T; k0 < hi; k0 += 2 * STEP) {
       step(k0, 0);
-      if (k0 + T < hi) step(k0 + T, 1);
+      if (k0 + STEP < hi) step(k0 + STEP, 1);
     }
     const float top = Tile::max(m), ref = top == -INFINITY ? 0.0f : top;
     l = Tile::sum(l * __builtin_amdgcn_exp2f(m - ref));
-    if (row < s.rows && lane < T) p.stats[(stat_row(p, line, s, b, hk) + row) * p.parts + part] = f32x2_t{top, l};
+    if (lane < T) found[wave][lane] = f32x2_t{top, l};
+    __syncthreads();
+    if (wave == 0 && lane < T && row < s.rows) {
+      float all = -INFINITY, sum = 0.0f;
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) all = fmaxf(all, found[w][lane][0]);
+      const float to = all == -INFINITY ? 0.0f : all;
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) sum += found[w][lane][1] * __builtin_amdgcn_exp2f(found[w][lane][0] - to);
+      p.stats[(stat_row(p, line, s, b, hk) + row) * p.parts + part] = f32x2_t{all, sum};
+    }
+    __syncthreads();
   }
 }
 
@@ -1046,7 +1061,7 @@ int launch_weights(const WeightsParams& p, hipStream_t s) {
   auto keys_of = [&](int keys) { return ((p.places + keys - 1) / keys) * p.B * p.n_kv; };
   auto go = [&](auto tile) {
     using Tile = decltype(tile);
-    hipLaunchKernelGGL((weights_stats_kernel<Tile>), grid(tiles_of(Tile::T) / WAVES + 1, 2048), dim3(NT), lds, s, p);
+    hipLaunchKernelGGL((weights_stats_kernel<Tile>), grid(tiles_of(Tile::T), 2048), dim3(NT), lds, s, p);
     hipLaunchKernelGGL((weights_sum_kernel<Tile>), grid(keys_of(Tile::T), 2048), dim3(NT), lds, s, p);
   };
   auto tiles = [&](auto dh) {

@@ -328,18 +328,19 @@ inline size_t gqa_workspace(GqaLaunch g) {
 
 // ---- attention weight of cached tokens --------------------------------------------
 
-// Rows (token, head of the group) of a workgroup that makes their statistics (bf16) or of a wave (fp32).
+// Rows (token, head of the group) of a workgroup that makes their statistics.
 inline int weights_tile(bool bf16) { return bf16 ? 128 : 16; }
 
 // Parts that a request's keys are cut in for the rows' statistics: what gives each of 1024
-// workgroups (bf16) or 4096 waves (fp32) about two tiles or one, as more parts than rows need
-// to be joined.  bf16: 64 rows of each of 7 prompts take 61 us with up to 2048 tiles, 62 with
-// 8192; windows of 16 requests 107 uncut, 116 cut in three.  fp32, trees over 1198 keys: 24 us
-// with at most 8 or 16 parts, which the second launch joins for each of its tiles, 28 with 32.
+// workgroups about two tiles (bf16) or one (fp32), as more parts than rows need to be joined.
+// bf16: 64 rows of each of 7 prompts take 60 us with up to 2048 tiles, 62 with 8192; windows of
+// 16 requests 104 uncut, 112 cut in three.  fp32, with at most 4, 8 and 16 parts, which the second
+// launch joins for each of its tiles: trees over 1198 keys 20.5, 18.7 and 21.4 us; 800 rows over
+// 4800 keys, 8 heads on 2, 119 with up to 4 parts, 126 with 8, which 1024 tiles cut to 2.
 // bf16 parts are of 256 keys or more, as their join is a launch: with at least 64, 256 and 1024,
 // 100 rows over 2000 keys, 28 heads on 4, take 31, 28 and 38 us, 4 requests of 64 rows over 264
 // keys 20, 19 and 19, over 964 keys 25, 22 and 30, over 3964 39, 39 and 45.
-inline int weights_want(bool bf16) { return bf16 ? 2048 : 4096; }
+inline int weights_want(bool bf16) { return bf16 ? 2048 : 1024; }
 constexpr int kWeightsParts = 32, kWeightsPart = 256;
 inline int weights_parts(long long rows, int batch, int heads, int n_kv, long long places, bool bf16, bool few) {
   const int tile = few ? 32 : weights_tile(bf16);
