@@ -845,7 +845,12 @@ __global__ __launch_bounds__(NT) void weights_stats_kernel(WeightsParams p) {
     Tile::load(q, p.q, (long long)(s.row0 + tok) * p.q_stride + (long long)head * p.head_dim, p.head_dim, lane);
     const int keys = part_keys(p, s.nk);
     const long long begin = (long long)part * keys, end = begin + keys;
-    const int lo = begin < s.nk ? (int)begin : s.nk, hi = end < s.nk ? (int)end : s.nk;
+    const int lo = begin < s.nk ? (int)begin : s.nk;
+    int hi = end < s.nk ? (int)end : s.nk;
+    if (p.mask == kMaskCausal) {                 // where the tile's rows see no more
+      const int stop = s.past + s.index0 + token_of(p, t * T + T < s.rows ? t * T + T - 1 : s.rows - 1) + 1;
+      hi = stop < hi ? (stop > lo ? stop : lo) : hi;
+    }
     const int open = p.mask == kMaskCausal ? s.past + s.index0 + token_of(p, t * T) + 1 : (p.mask == kMaskTree ? s.past : s.nk);
     const int* table = p.table + (size_t)b * p.width;
     float m = -INFINITY, l = 0.0f;
@@ -902,23 +907,31 @@ __global__ __launch_bounds__(NT) void weights_stats_kernel(WeightsParams p) {
   }
 }
 
-// log2 of a row's sum, from its parts.
-__device__ __forceinline__ float join(const WeightsParams& p, long long r, int parts) {
-  const f32x2_t* from = p.stats + r * p.parts;
-  float top = -INFINITY, sum = 0.0f;
-  for (int k0 = 0; k0 < parts; k0 += 8) {
-    f32x2_t x[8];                                // on their way together
+// log2 of a row's sum, from its parts, eight of which are on their way together.
+struct Parts {
+  f32x2_t x[8];
+  __device__ __forceinline__ void load(const f32x2_t* from, int parts) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) x[k] = from[k0 + k < parts ? k0 + k : parts - 1];
+    for (int k = 0; k < 8; ++k) x[k] = from[k < parts ? k : parts - 1];
+  }
+  __device__ __forceinline__ void add(int parts, float& top, float& sum) const {
     float to = top;
 #pragma unroll
     for (int k = 0; k < 8; ++k) to = fmaxf(to, x[k][0]);
     const float ref = to == -INFINITY ? 0.0f : to;
     sum *= __builtin_amdgcn_exp2f(top - ref);
 #pragma unroll
-    for (int k = 0; k < 8; ++k)
-      if (k0 + k < parts) sum += x[k][1] * __builtin_amdgcn_exp2f(x[k][0] - ref);
+    for (int k = 0; k < 8; ++k) sum += k < parts ? x[k][1] * __builtin_amdgcn_exp2f(x[k][0] - ref) : 0.0f;
     top = to;
+  }
+};
+__device__ __forceinline__ float join(const WeightsParams& p, long long r, int parts) {
+  const f32x2_t* from = p.stats + r * p.parts;
+  float top = -INFINITY, sum = 0.0f;
+  for (int k = 0; k < parts; k += 8) {
+    Parts x;
+    x.load(from + k, parts - k);
+    x.add(parts - k, top, sum);
   }
   return top + __builtin_amdgcn_logf(sum);
 }
@@ -1005,7 +1018,7 @@ __global__ __launch_bounds__(NT) void weights_sum_kernel(WeightsParams p) {
     const int key = k0 + Tile::row(lane), src = key < s.nk ? key : s.nk - 1;
     bool held;
     typename Tile::Frag k, q[2];
-    float lse[2];                                // of the lane's row
+    Parts part[2];                               // of the lane's row's sum, at most 8
     const long long krow = key_row(p, table, hk, src, held);
     Tile::load(k, p.pool, krow, p.head_dim, lane);
     const long long stat = stat_row(p, line, s, b, hk);
@@ -1014,18 +1027,21 @@ __global__ __launch_bounds__(NT) void weights_sum_kernel(WeightsParams p) {
       const int tok = token_of(p, row), head = row - tok * p.group;
       Tile::load(q[i], p.q, (long long)(s.row0 + tok) * p.q_stride + (long long)(hk * p.group + head) * p.head_dim, p.head_dim,
                  lane);
-      lse[i] = join(p, stat + row, p.parts);
+      part[i].load(p.stats + (stat + row) * p.parts, p.parts);
     };
     float sum = 0.0f;
     auto step = [&](int r0, int i) {
       if (r0 + WAVES * T < s.rows) load(r0 + WAVES * T, i ^ 1);
       typename Tile::acc_t a;
       Tile::mul(a, q[i], k);
+      float top = -INFINITY, all = 0.0f;
+      part[i].add(p.parts, top, all);
+      const float lse = top + __builtin_amdgcn_logf(all);
       const int sure = p.mask == kMaskCausal ? s.past + s.index0 + token_of(p, r0) + 1 : (p.mask == kMaskTree ? s.past : s.nk);
       const bool masked = k0 + T > sure || r0 + T > s.rows;
 #pragma unroll
       for (int r = 0; r < Tile::ACC; ++r) {
-        float w = __builtin_amdgcn_exp2f(a[r] * c - __shfl(lse[i], Tile::of(lane, r), kWave));
+        float w = __builtin_amdgcn_exp2f(a[r] * c - __shfl(lse, Tile::of(lane, r), kWave));
         if (masked) {
           const int j = r0 + Tile::of(lane, r), it = token_of(p, j < s.rows ? j : s.rows - 1);
           const bool see = j < s.rows && sees(p, s, s.row0 + it, s.index0 + it, key);
@@ -1034,8 +1050,14 @@ __global__ __launch_bounds__(NT) void weights_sum_kernel(WeightsParams p) {
         sum += w;
       }
     };
-    if (wave * T < s.rows) load(wave * T, 0);
-    for (int r0 = wave * T; r0 < s.rows; r0 += 2 * WAVES * T) {
+    // the first row that sees a key of the tile, in whole tiles
+    int from = wave * T;
+    if (p.mask == kMaskCausal) {
+      const int behind = k0 - s.past - s.index0;
+      if (behind > 0) from += behind < s.used ? behind * p.group / T * T : s.rows;
+    }
+    if (from < s.rows) load(from, 0);
+    for (int r0 = from; r0 < s.rows; r0 += 2 * WAVES * T) {
       step(r0, 0);
       if (r0 + WAVES * T < s.rows) step(r0 + WAVES * T, 1);
     }
