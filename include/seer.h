@@ -755,7 +755,7 @@ size_t seer_attn_weights_workspace_bytes(const seer_attn_desc* desc, const seer_
  * summed in one order: the same call gives the same bits; with other bounds
  * (rows_ub, batch, table_width) or another `last` they may differ by roundings.
  * workspace: seer_attn_weights_workspace_bytes, 256-byte aligned; it holds
- * nothing between calls.  In bf16 up to 2^25 scores (128 MB) are part of it.
+ * nothing between calls.  In bf16 up to 2^26 scores (256 MB) are part of it.
  * Offsets in cu_seqlens that fall are no call: nothing is written then.
  * Errors: as seer_attn_paged; EINVAL (last < 0, decay negative or not finite),
  * EUNSUPPORTED (rows_ub * n_heads >= 2^30; batch > 4096; batch * n_kv_heads * table_width * page_size of

@@ -366,7 +366,7 @@ inline long long weights_stats(long long rows, int heads, bool bf16) {
 // head) 234 and 165, 8 rows 240 and 239; 16 requests over 1000 keys, 32 heads, of 16 rows 62
 // and 67, 32 rows 61 and 84; 64 requests over 2000 keys, 8 heads of 64, of 8 rows 71 and 53, 32
 // rows 72 and 93.
-constexpr long long kWeightsScores = 1 << 25, kWeightsFew = 16;
+constexpr long long kWeightsScores = 1 << 26, kWeightsFew = 16;
 inline bool weights_few(long long rows, int batch, int heads, int n_kv, long long places, bool bf16) {
   return bf16 && rows * (heads / n_kv) <= kWeightsFew * batch && rows * heads <= kWeightsScores / places;
 }

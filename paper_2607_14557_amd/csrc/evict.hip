@@ -95,7 +95,7 @@ struct Shared {
   static constexpr int NW = NT / kWave;
   uint32_t hist[3][2048];
   int part[NW];
-  int guarded, digit, left;
+  int guarded, digit, left, moving;
 };
 
 // The `left` largest members of a kind stay: those above the order that is returned, and
@@ -183,22 +183,19 @@ __device__ __forceinline__ unsigned long long before(int end, int first) {
   return n <= 0 ? 0ull : (n >= kWave ? ~0ull : (1ull << n) - 1);
 }
 
-// Lists of at most NT * K places, place k * NT + tid a thread's k-th.  p.fused: the workgroup
+// A list of at most NT * K places, place k * NT + tid a thread's k-th.  p.fused: the workgroup
 // moves its list's rows too; otherwise it leaves the slots of what moves, and of shared lists
 // which places below N are given up, for evict_move_kernel.  All reads are on their way
 // together (one after the other they took 8 of 23 us of a list of 16 per thread); what stays
 // and moves is held as a bit a place, 64 places in two scalar registers.
+// counts [K][NT / 64]: of what moves, per 64 places, then their sums before; from [NT * K]:
+// slots of what moves, and in its second half those where it goes.
 template <int NT, int K>
-__global__ __launch_bounds__(NT) void evict_kernel(EvictParams p) {
+__device__ __forceinline__ void evict_list(const EvictParams& p, const Request& r, int b, int h, Shared<NT>& sh, int* counts,
+                                           int* from) {
   constexpr int NW = NT / kWave, MOST = NT * K / 2;
   typedef unsigned long long bits_t;
-  __shared__ Shared<NT> sh;
-  __shared__ int counts[K][NW];                  // of what moves, per 64 places, then their sums before
-  __shared__ int moving;
-  __shared__ int from[2 * MOST];                 // slots of what moves, and from MOST on those where it goes
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int b = blockIdx.x / p.lists, h = blockIdx.x % p.lists;
-  const Request r = request(p, b);
   const int seen = p.seen[b];
   const auto start = [&](int k) { return k * NT + wave * kWave; };         // the wave's first place of the k-th
   int slot[K];
@@ -305,10 +302,10 @@ __global__ __launch_bounds__(NT) void evict_kernel(EvictParams p) {
       own = lane == k ? n : own;
     }
     __syncthreads();
-    if (lane < K) counts[lane][wave] = own;
+    if (lane < K) counts[lane * NW + wave] = own;
     __syncthreads();
     if (wave == 0) {
-      int* c = &counts[0][0];
+      int* c = counts;
       int base = 0;
 #pragma unroll
       for (int i = 0; i < K * NW; i += kWave) {
@@ -317,10 +314,10 @@ __global__ __launch_bounds__(NT) void evict_kernel(EvictParams p) {
         if (i + lane < K * NW) c[i + lane] = base + inc - n;
         base += __builtin_amdgcn_readlane(inc, kWave - 1);
       }
-      if (lane == 0) moving = base;
+      if (lane == 0) sh.moving = base;
     }
     __syncthreads();
-    const int first = counts[lane < K ? lane : 0][wave];
+    const int first = counts[(lane < K ? lane : 0) * NW + wave];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       const bits_t bits = set(k);
@@ -341,9 +338,9 @@ __global__ __launch_bounds__(NT) void evict_kernel(EvictParams p) {
   auto moves = [&](int k) { return (stays[k] ^ before(r.N, start(k))) & before(r.L, start(k)); };
   // the first half of the ranks are those of places below N
   rank(moves, [&](int k, bool is, int at) {
-    if (is) from[at < moving / 2 ? MOST + at : at - moving / 2] = slot[k];
+    if (is) from[at < sh.moving / 2 ? MOST + at : at - sh.moving / 2] = slot[k];
   });
-  const int n = moving / 2;
+  const int n = sh.moving / 2;
   if (p.weight_out != p.weight) {
     if (!p.shared) {
       // marks that stay where they are, in another pool (read again: held, they would cost registers)
@@ -377,14 +374,42 @@ __global__ __launch_bounds__(NT) void evict_kernel(EvictParams p) {
   }
 }
 
-// Lists of any length, whose marks are read again for each histogram.
+// Lists of at most NT * K places; short ones among them, as in a table that is wider than the
+// requests are long, take the steps of theirs.
+template <int NT, int K>
+__global__ __launch_bounds__(NT) void evict_kernel(EvictParams p) {
+  __shared__ Shared<NT> sh;
+  __shared__ int counts[K * NT / kWave], from[NT * K];
+  const int b = blockIdx.x / p.lists, h = blockIdx.x % p.lists;
+  const Request r = request(p, b);
+  constexpr int SHORT = 2048 / NT;
+  if constexpr (K > SHORT) {
+    if (r.L <= NT * SHORT) {
+      evict_list<NT, SHORT>(p, r, b, h, sh, counts, from);
+      return;
+    }
+  }
+  evict_list<NT, K>(p, r, b, h, sh, counts, from);
+}
+
+// Lists of any length; the marks of those of more than 8192 places are read again for each
+// histogram.
 __global__ __launch_bounds__(1024) void evict_long_kernel(EvictParams p) {
-  constexpr int NT = 1024, NW = NT / kWave;
+  constexpr int NT = 1024, NW = NT / kWave, K = 8;
   __shared__ Shared<NT> sh;
   __shared__ int part[3][NW];
+  __shared__ int counts[K * NW], from_lds[NT * K];
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6;
   const int b = blockIdx.x / p.lists, h = blockIdx.x % p.lists;
   const Request r = request(p, b);
+  if (r.L <= 2 * NT) {
+    evict_list<NT, 2>(p, r, b, h, sh, counts, from_lds);
+    return;
+  }
+  if (r.L <= K * NT) {
+    evict_list<NT, K>(p, r, b, h, sh, counts, from_lds);
+    return;
+  }
   const int seen = p.seen[b];
   for (int i = tid; i < 3 * 2048; i += NT) (&sh.hist[0][0])[i] = 0;
   if (tid == 0) sh.guarded = 0;

@@ -32,6 +32,18 @@ def test_lists(S, shared, lists, most):
         c.run([int(n * f) for n, f in zip(lens, r.random(len(lens)))], 2, 7, shared, apart)
 
 
+@pytest.mark.parametrize("places", [3000, 9000, 20000])
+@pytest.mark.parametrize("shared", [False, True])
+def test_wide_tables(S, places, shared):
+    """Lists of which all but one are much shorter than their row of the table, few and many of them."""
+    r = np.random.default_rng(places)
+    for n in (4, 140):
+        lens = [2047, 2048, 2049, places - 40][: 4 if n == 4 else 3] + [int(x) for x in r.integers(0, 300, n)]
+        c = Cache(S, "f32", 4, 4, lens, page=64, order="same", width=-(-places // 64))
+        c.run([int(m * f) for m, f in zip(lens, r.random(len(lens)))], 2, 7, shared)
+        c.run([max(0, m - 1) for m in lens], 2, 7, shared, True)
+
+
 @pytest.mark.parametrize("kind,KV,D", [("bf16", 9, 64), ("bf16", 8, 128), ("f32", 11, 4), ("f32", 8, 80)])
 def test_heads_of_lists_that_move_themselves(S, kind, KV, D):
     r = np.random.default_rng(KV)
