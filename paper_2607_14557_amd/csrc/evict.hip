@@ -11,7 +11,7 @@
 //
 // Bound by the latency of one list's steps where little moves, by bytes where much does.
 // Measured (MI355X, us): 96 requests, 8 heads, 700 to 1500 tokens, one of each evicted 12.4
-// (a launch is 5); 24 prompts of 1500 to 16,000 tokens, 4 heads, cut to 1024 40, of which the
+// (a launch is 5); 24 prompts of 1500 to 16,000 tokens, 4 heads, cut to 1024 41, of which the
 // choice 21 and the move of 78 MB 15 (5.2 TB/s); 16 prefixes of 32 heads, shared choice, 44, of
 // which the choice 9.5 and the move of 105 MB 25 (4.2 TB/s).  Of the 21 us, by the
 // clocks of a list of 16,000, its marks take about 5, the histograms 4.5, what stays 1.5.
@@ -31,7 +31,7 @@ __device__ __forceinline__ uint32_t order_of(float w) {
 }
 
 struct Request {
-  int L, N;
+  int L, N, seen;
   const int* table;
 };
 
@@ -39,6 +39,7 @@ __device__ __forceinline__ Request request(const EvictParams& p, int b) {
   Request r;
   const long long most = (long long)p.width << p.shift;
   const int L = p.kv_len[b], N = p.budget[b];
+  r.seen = p.seen[b];                            // on its way with the others
   r.L = L < 0 ? 0 : (L > most ? (int)most : L);
   r.N = N < 0 ? 0 : (N < r.L ? N : r.L);
   r.table = p.table + (size_t)b * p.width;
@@ -196,7 +197,7 @@ __device__ __forceinline__ void evict_list(const EvictParams& p, const Request& 
   constexpr int NW = NT / kWave, MOST = NT * K / 2;
   typedef unsigned long long bits_t;
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int seen = p.seen[b];
+  const int seen = r.seen;
   const auto start = [&](int k) { return k * NT + wave * kWave; };         // the wave's first place of the k-th
   int slot[K];
 #pragma unroll
@@ -317,13 +318,13 @@ __device__ __forceinline__ void evict_list(const EvictParams& p, const Request& 
       if (lane == 0) sh.moving = base;
     }
     __syncthreads();
-    const int first = counts[(lane < K ? lane : 0) * NW + wave];
+    const int first = counts[(lane < K ? lane : 0) * NW + wave], all = sh.moving;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       const bits_t bits = set(k);
       if (bits)
         use(k, bits >> lane & 1, __builtin_amdgcn_mbcnt_hi((uint32_t)(bits >> 32), __builtin_amdgcn_mbcnt_lo(
-                                     (uint32_t)bits, __builtin_amdgcn_readlane(first, k))));
+                                     (uint32_t)bits, __builtin_amdgcn_readlane(first, k))), all);
     }
   };
   if (some && left > 0) {
@@ -332,13 +333,13 @@ __device__ __forceinline__ void evict_list(const EvictParams& p, const Request& 
       const bits_t kind = __ballot(kinds >> k & 1);
       return __ballot(order[k] == least) & (of_guarded ? kind : before(r.L, start(k)) & ~kind);
     };
-    rank(ties, [&](int k, bool is, int at) { stays[k] |= __ballot(is && at < left); });
+    rank(ties, [&](int k, bool is, int at, int) { stays[k] |= __ballot(is && at < left); });
   }
   // places below N that are given up, and kept ones from N on: as many of either
   auto moves = [&](int k) { return (stays[k] ^ before(r.N, start(k))) & before(r.L, start(k)); };
   // the first half of the ranks are those of places below N
-  rank(moves, [&](int k, bool is, int at) {
-    if (is) from[at < sh.moving / 2 ? MOST + at : at - sh.moving / 2] = slot[k];
+  rank(moves, [&](int k, bool is, int at, int all) {
+    if (is) from[at < all / 2 ? MOST + at : at - all / 2] = slot[k];
   });
   const int n = sh.moving / 2;
   if (p.weight_out != p.weight) {
@@ -410,7 +411,7 @@ __global__ __launch_bounds__(1024) void evict_long_kernel(EvictParams p) {
     evict_list<NT, K>(p, r, b, h, sh, counts, from_lds);
     return;
   }
-  const int seen = p.seen[b];
+  const int seen = r.seen;
   for (int i = tid; i < 3 * 2048; i += NT) (&sh.hist[0][0])[i] = 0;
   if (tid == 0) sh.guarded = 0;
   __syncthreads();
