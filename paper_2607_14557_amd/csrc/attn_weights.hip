@@ -9,11 +9,10 @@
 //
 //   bf16, many rows   weights_stats_tile_kernel: 128 rows stay in registers, keys pass by in
 //                     LDS tiles of 64 (S^T = K Q^T, a lane owns a row); where the rows' tiles
-//                     are few, each takes a part of the keys and weights_lse_kernel joins the
-//                     parts.  weights_sum_tile_kernel: 128 keys stay, rows pass by (S = Q K^T,
-//                     a lane owns a key and adds up its rows in a register); where those
-//                     tiles are few, each takes a part of the rows and weights_join_kernel
-//                     adds the parts.  The scores are
+//                     are few, each takes a part of the keys.  weights_sum_tile_kernel: the
+//                     rows' parts joined, 128 keys stay, rows pass by (S = Q K^T, a lane owns
+//                     a key and adds up its rows in a register); where those tiles are few,
+//                     each takes a part of the rows and weights_join_kernel adds the parts.  The scores are
 //                     made twice: 4 bytes a score, written and read, would take 170 us of the
 //                     windows below where the second product takes 30.
 //   bf16, few rows    weights_scores_kernel reads the keys once and keeps the scores, which are
@@ -276,6 +275,35 @@ __device__ __forceinline__ long long stat_row(const WeightsParams& p, const Line
   return (long long)(l.rows[b] - s.used) * p.n_heads + (long long)hk * s.rows;
 }
 
+// log2 of a row's sum, from its parts, eight of which are on their way together.
+struct Parts {
+  f32x2_t x[8];
+  __device__ __forceinline__ void load(const f32x2_t* from, int parts) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) x[k] = from[k < parts ? k : parts - 1];
+  }
+  __device__ __forceinline__ void add(int parts, float& top, float& sum) const {
+    float to = top;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) to = fmaxf(to, x[k][0]);
+    const float ref = to == -INFINITY ? 0.0f : to;
+    sum *= __builtin_amdgcn_exp2f(top - ref);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sum += k < parts ? x[k][1] * __builtin_amdgcn_exp2f(x[k][0] - ref) : 0.0f;
+    top = to;
+  }
+};
+__device__ __forceinline__ float join(const WeightsParams& p, long long r, int parts) {
+  const f32x2_t* from = p.stats + r * p.parts;
+  float top = -INFINITY, sum = 0.0f;
+  for (int k = 0; k < parts; k += 8) {
+    Parts x;
+    x.load(from + k, parts - k);
+    x.add(parts - k, top, sum);
+  }
+  return top + __builtin_amdgcn_logf(sum);
+}
+
 // ---- tiles of 64 in LDS, for requests of many rows (bf16) -------------------------
 // Both launches keep one operand in registers and pass the other by it in tiles of 64
 // rows, which the four waves share: two buffers in LDS, filled by direct loads.  Rows
@@ -511,12 +539,15 @@ __global__ __launch_bounds__(NT, 4) void weights_stats_tile_kernel(WeightsParams
 // The weights of 128 keys, which stay, from all rows, which pass by.  A row that is blind to
 // a lane's key stands before the lane's first row that sees it (causal), so one number of a
 // key masks a tile; the tiles without a mask have a copy of the code of their own.
+// The parts of the rows' sums are joined here, 1024 rows at a time, by all threads (in a launch
+// of its own it took 5 us).
 template <int DH>
 __global__ __launch_bounds__(NT, 4) void weights_sum_tile_kernel(WeightsParams p) {
   extern __shared__ int lds[];
   __shared__ __attribute__((aligned(1024))) uint8_t tile0[TILE * DH * 2];
   __shared__ __attribute__((aligned(1024))) uint8_t tile1[TILE * DH * 2];
-  __shared__ __attribute__((aligned(16))) float lse_lds[2][TILE];
+  constexpr int ROWS = 1024;                     // whose logarithms are held at a time
+  __shared__ __attribute__((aligned(16))) float lse_lds[ROWS];
   constexpr int KT = 128;
   const Share share(p.n_kv);
   auto units = [&](const Seq& s, int) { return s.used > 0 ? (s.nk + KT - 1) / KT * share.heads * p.sums : 0; };
@@ -548,14 +579,22 @@ __global__ __launch_bounds__(NT, 4) void weights_sum_tile_kernel(WeightsParams p
       const int token = key0 - s.past - s.index0;
       if (token > 0) from = token < s.used ? token * p.group / TILE * TILE : s.rows;
     }
-    const float* lse = p.lse + stat_row(p, line, s, b, hk);
+    const long long stat = stat_row(p, line, s, b, hk);
     int n = (s.rows - from + TILE - 1) / TILE;
     if (p.sums > 1) {                            // an equal share of them
       const int per = (n + p.sums - 1) / p.sums, skip = part * per < n ? part * per : n;
       from += skip * TILE;
       n = n - skip < per ? n - skip : per;
     }
-    float next_lse = 0.0f;
+    // the logarithms of the sums of the rows of tile rt and those behind it
+    auto hold = [&](int rt) {
+      const int r0 = from + TILE * rt;
+      for (int t = tid; t < ROWS && r0 + (t & ~63) < s.rows; t += NT) {
+        float x = INFINITY;
+        if (r0 + t < s.rows) x = p.parts > 1 ? join(p, stat + r0 + t, p.parts) : p.lse[stat + r0 + t];
+        lse_lds[t] = x == -INFINITY ? INFINITY : x;          // a row that sees no key
+      }
+    };
     auto load = [&](int r0, uint8_t* to) {
       int row = r0 + 16 * wave;
       row = row < s.rows ? row : s.rows - 1;     // rows past the end are the last one again
@@ -566,18 +605,10 @@ __global__ __launch_bounds__(NT, 4) void weights_sum_tile_kernel(WeightsParams p
         const int i = row + (r < most ? r : most), tok = token_of(p, i);
         return (uint32_t)(tok - base) * (uint32_t)(p.q_stride * 2) + (uint32_t)(i - tok * p.group) * (DH * 2);
       });
-      if (wave == 0) {
-        const int i = r0 + lane;
-        const float x = i < s.rows ? lse[i] : INFINITY;
-        next_lse = x == -INFINITY ? INFINITY : x;          // a row that sees no key
-      }
-    };
-    auto keep = [&](int B) {
-      if (wave == 0) lse_lds[B][lane] = next_lse;
     };
     if (n > 0) {
       load(from, tile0);
-      keep(0);
+      hold(0);
     }
     __builtin_amdgcn_s_waitcnt(0x0f70);
     __syncthreads();
@@ -603,6 +634,7 @@ __global__ __launch_bounds__(NT, 4) void weights_sum_tile_kernel(WeightsParams p
           }
         }
         seen >>= 4 * (lane >> 5);
+        const float* lse = &lse_lds[rt % (ROWS / TILE) * TILE + 4 * (lane >> 5)];
         // (two copies, so that a half's sums do not wait for the branch)
         auto add = [&](auto blinded) {
 #pragma unroll
@@ -612,7 +644,7 @@ __global__ __launch_bounds__(NT, 4) void weights_sum_tile_kernel(WeightsParams p
             const uint32_t half = (uint32_t)(seen >> (32 * i));
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-              const f32x4_t x = *reinterpret_cast<const f32x4_t*>(&lse_lds[B][32 * i + 8 * g + 4 * (lane >> 5)]);
+              const f32x4_t x = *reinterpret_cast<const f32x4_t*>(lse + 32 * i + 8 * g);
 #pragma unroll
               for (int r = 0; r < 4; ++r) {
                 const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(a[4 * g + r], c, -x[r]));
@@ -624,9 +656,12 @@ __global__ __launch_bounds__(NT, 4) void weights_sum_tile_kernel(WeightsParams p
         if (masked) add(std::true_type{});
         else add(std::false_type{});
       }
-      if (rt + 1 < n) keep(B ^ 1);
       __builtin_amdgcn_s_waitcnt(0x0f70);
       __syncthreads();
+      if ((rt + 1) % (ROWS / TILE) == 0 && rt + 1 < n) {
+        hold(rt + 1);
+        __syncthreads();
+      }
     };
     for (int rt = 0; rt < n; rt += 2) {
       step(rt, std::integral_constant<int, 0>{});
@@ -907,43 +942,6 @@ __global__ __launch_bounds__(NT) void weights_stats_kernel(WeightsParams p) {
   }
 }
 
-// log2 of a row's sum, from its parts, eight of which are on their way together.
-struct Parts {
-  f32x2_t x[8];
-  __device__ __forceinline__ void load(const f32x2_t* from, int parts) {
-#pragma unroll
-    for (int k = 0; k < 8; ++k) x[k] = from[k < parts ? k : parts - 1];
-  }
-  __device__ __forceinline__ void add(int parts, float& top, float& sum) const {
-    float to = top;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) to = fmaxf(to, x[k][0]);
-    const float ref = to == -INFINITY ? 0.0f : to;
-    sum *= __builtin_amdgcn_exp2f(top - ref);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) sum += k < parts ? x[k][1] * __builtin_amdgcn_exp2f(x[k][0] - ref) : 0.0f;
-    top = to;
-  }
-};
-__device__ __forceinline__ float join(const WeightsParams& p, long long r, int parts) {
-  const f32x2_t* from = p.stats + r * p.parts;
-  float top = -INFINITY, sum = 0.0f;
-  for (int k = 0; k < parts; k += 8) {
-    Parts x;
-    x.load(from + k, parts - k);
-    x.add(parts - k, top, sum);
-  }
-  return top + __builtin_amdgcn_logf(sum);
-}
-
-// ... of all rows: a thread a row and head.
-__global__ __launch_bounds__(NT) void weights_lse_kernel(WeightsParams p) {
-  extern __shared__ int lds[];
-  const Line line = line_of<false>(p, lds, [&](const Seq& s, int) { return s.nk > 0 ? s.used : 0; });
-  const long long all = line.all ? (long long)line.rows[p.B - 1] * p.n_heads : 0;
-  for (long long r = (long long)blockIdx.x * NT + threadIdx.x; r < all; r += (long long)gridDim.x * NT) p.lse[r] = join(p, r, p.parts);
-}
-
 // The weights from scores that the statistics' launch has left: where a request has few
 // rows, those are fewer bytes than its keys.  A workgroup takes 1024 keys of a head and
 // all rows, whose logarithms it makes for itself: 14 us for the 33 MB of the 64 tokens.
@@ -1094,7 +1092,6 @@ int launch_weights(const WeightsParams& p, hipStream_t s) {
       return;
     }
     hipLaunchKernelGGL((weights_stats_tile_kernel<DH>), grid(tiles_of(128), 1024), dim3(NT), lds, s, p);
-    if (p.parts > 1) hipLaunchKernelGGL(weights_lse_kernel, grid(p.rows * p.n_heads / NT + 1, 256), dim3(NT), lds, s, p);
     hipLaunchKernelGGL((weights_sum_tile_kernel<DH>), grid(keys_of(128) * p.sums, 1024), dim3(NT), lds, s, p);
     if (p.sums > 1) hipLaunchKernelGGL(weights_join_kernel, grid(keys_of(NT), 1024), dim3(NT), lds, s, p);
   };

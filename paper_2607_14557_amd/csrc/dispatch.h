@@ -332,22 +332,25 @@ inline size_t gqa_workspace(GqaLaunch g) {
 inline int weights_tile(bool bf16) { return bf16 ? 128 : 16; }
 
 // Parts that a request's keys are cut in for the rows' statistics: what gives each of 1024
-// workgroups about two tiles (bf16) or one (fp32), as more parts than rows need to be joined.
-// bf16: 64 rows of each of 7 prompts take 60 us with up to 2048 tiles, 62 with 8192; windows of
-// 16 requests 104 uncut, 112 cut in three.  fp32, with at most 4, 8 and 16 parts, which the second
-// launch joins for each of its tiles: trees over 1198 keys 20.5, 18.7 and 21.4 us; 800 rows over
-// 4800 keys, 8 heads on 2, 119 with up to 4 parts, 126 with 8, which 1024 tiles cut to 2.
-// bf16 parts are of 256 keys or more, as their join is a launch: with at least 64, 256 and 1024,
-// 100 rows over 2000 keys, 28 heads on 4, take 31, 28 and 38 us, 4 requests of 64 rows over 264
-// keys 20, 19 and 19, over 964 keys 25, 22 and 30, over 3964 39, 39 and 45.
+// workgroups about two tiles (bf16) or one (fp32).  The second launch joins them for each of its
+// tiles, so no more than 8 up to 8192 places.  bf16, us with at most 4, 8 and 12 parts: 64
+// rows of each of 7 prompts of 1500 to 8192 74, 64 and 68; 4 requests of 64 rows over 4064
+// keys, 16 heads on 1, 40, 34 and 36; 2 of 12 to 20 rows over up to 11,600 keys 59, 38 and 33, with
+// 22 28.  Parts of 256 keys or more: with at least 64, 256 and 1024 100 rows over 2000 keys, 28
+// heads on 4, take 31, 28 and 38 us, 4 requests of 64 rows over 964 keys 25, 22 and 30.  fp32, with
+// at most 4, 8 and 16 parts: trees over 1198 keys 20.5, 18.7 and 21.4 us; 800 rows over 4800
+// keys, 8 heads on 2, 119 with up to 4 parts, 126 with 8, which 1024 tiles cut to 2.
 inline int weights_want(bool bf16) { return bf16 ? 2048 : 1024; }
 constexpr int kWeightsParts = 32, kWeightsPart = 256;
 inline int weights_parts(long long rows, int batch, int heads, int n_kv, long long places, bool bf16, bool few) {
   const int tile = few ? 32 : weights_tile(bf16);
   const long long tiles = ((rows * (heads / n_kv) + tile - 1) / tile + batch - 1) * n_kv;
   const long long parts = (few ? 4096 : weights_want(bf16)) / tiles;
-  long long most = bf16 ? kWeightsParts : 8;
-  if (bf16 && !few && places / kWeightsPart < most) most = places / kWeightsPart;
+  long long most = few ? kWeightsParts : 8;
+  if (bf16 && !few) {
+    if (places > 8192) most = places / 512 < kWeightsParts ? places / 512 : kWeightsParts;
+    if (places / kWeightsPart < most) most = places / kWeightsPart;
+  }
   return parts < 1 || most < 1 ? 1 : (int)(parts > most ? most : parts);
 }
 
