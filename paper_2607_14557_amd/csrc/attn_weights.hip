@@ -267,6 +267,10 @@ __device__ __forceinline__ uint32_t window(const WeightsParams& p, const Seq& s,
   return x;
 }
 
+// What the place of a score that its row does not see holds among the kept ones.  No product of bf16
+// rows gives these bits: a NaN of theirs has the upper 16 of an operand's, or the default ones.
+constexpr uint32_t kUnseen = 0xffffffffu;
+
 __device__ __forceinline__ float scale_of(const WeightsParams& p) { return p.scale * 1.4426950408889634f; }
 
 // Where the statistics of a request's rows for a key/value head begin: request after request, in each head
@@ -797,21 +801,26 @@ __global__ __launch_bounds__(NT) void weights_scores_kernel(WeightsParams p) {
         const int k0 = lo + k * 128 + 32 * wave, key = k0 + (lane & 31);
         f32x16_t a;
         Stream<DH>::mul_by(a, (B ? tile1 : tile0) + wave * FT, st, lane);
+        uint32_t score[NR];
+#pragma unroll
+        for (int r = 0; r < NR; ++r) score[r] = __float_as_uint(a[r]);
         if (k0 + 32 > open || __any(lost[B])) {
           const uint32_t keys = window(p, s, r0 + (lane & 31), k0);
 #pragma unroll
           for (int r = 0; r < NR; ++r) {
             const int row = 8 * (r >> 2) + (r & 3);
             const uint32_t low = __builtin_amdgcn_readlane(keys, row), high = __builtin_amdgcn_readlane(keys, row + 4);
-            const bool see = (half ? high : low) >> (lane & 31) & 1;
-            a[r] = see && !lost[B] ? a[r] : -INFINITY;
+            const bool see = ((half ? high : low) >> (lane & 31) & 1) && !lost[B];
+            score[r] = see ? score[r] : kUnseen;
+            a[r] = see ? a[r] : -INFINITY;
           }
         }
 #pragma unroll
         for (int r = 0; r < NR; ++r) {
           const int row = 8 * (r >> 2) + 4 * half + (r & 3);
           // past the caches: 2 to 3% of a large launch
-          __builtin_nontemporal_store(a[r], &p.scores[(stat + (row < left ? row : left - 1)) * p.places + key]);
+          __builtin_nontemporal_store(score[r], reinterpret_cast<uint32_t*>(p.scores) +
+                                                    (stat + (row < left ? row : left - 1)) * p.places + key);
         }
         if (k + 2 < n) {
           // this tile's fragments have been read
@@ -976,7 +985,11 @@ __global__ __launch_bounds__(NT) void weights_few_kernel(WeightsParams p) {
           for (int i = 0; i < 8; ++i) {
             const float l = r + i < n ? lse[r + i] : INFINITY;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) sum[e] += __builtin_amdgcn_exp2f(x[i][e] * scale_of(p) - l);
+            for (int e = 0; e < 4; ++e) {
+              // (by its bits: of a row whose logarithm is NaN, -inf would give NaN to keys that it does not see)
+              const float w = __builtin_amdgcn_exp2f(x[i][e] * scale_of(p) - l);
+              sum[e] += __float_as_uint(x[i][e]) == kUnseen ? 0.0f : w;
+            }
           }
         }
       }

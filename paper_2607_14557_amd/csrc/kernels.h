@@ -434,7 +434,7 @@ struct WeightsParams {
   int sums;                    // parts of a request's rows, whose sums are joined
   f32x2_t* stats;              // [rows that count][n_heads][parts] maximum, sum
   float* lse;                  // [rows that count][n_heads] log2 of the sum
-  float* scores;               // [rows that count][n_heads][places] q . k, or null
+  float* scores;               // [rows that count][n_heads][places] q . k, where it is seen, or null
   float* partial;              // [B][n_kv][places][sums]
   long long places;            // of a request, in whole 64
 };

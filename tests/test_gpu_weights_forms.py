@@ -1,0 +1,65 @@
+"""The three forms of the attention weights (bf16 tiles, bf16 with scores kept, fp32) on the cases where they could
+differ; the rule that chooses, compiled for the host, says which form a call takes."""
+import numpy as np
+import pytest
+
+from gpu_util import dev, host, log
+from test_dispatch import CXX, _ask
+from test_gpu_attn_weights import Call, _bits
+
+pytestmark = [pytest.mark.gpu, pytest.mark.skipif(CXX is None, reason="no host C++ compiler")]
+FORM = "int answer(const long long* v) { return v[5] ? 1 + weights_few(v[0], (int)v[1], (int)v[2], (int)v[3], v[4], true) : 0; }"
+
+
+@pytest.fixture(scope="module")
+def S():
+    from paper_2607_14557_amd import seer
+    seer.load_library()
+    return seer
+
+
+def form(tmp_path, c, last=0):
+    """The form that a call takes: tiles, scores (kept) or f32."""
+    H, KV, _ = c.shape
+    rows = min(c.rows, last * c.B) if last else c.rows
+    places = -(-c.W * c.page // 64) * 64
+    return ("f32", "tiles", "scores")[_ask(tmp_path, FORM, [(rows, c.B, H, KV, places, c.kind != "f32")])[0]]
+
+
+# rows that the call allows for behind its own, in each form
+PADS = [("bf16", "scores", 2), ("bf16", "tiles", 400), ("f32", "f32", 2)]
+
+
+@pytest.mark.parametrize("mask", ["causal", "tree"])
+@pytest.mark.parametrize("kind,want,pad", PADS)
+def test_rows_of_nan(S, tmp_path, kind, want, pad, mask):
+    """A row of NaN makes the weights of the keys that it sees NaN, and those of no other key; a key that it sees with a
+    score of -inf is one of them, and one that only other rows see, with -inf, gets nothing."""
+    lens, past = [6, 5], [70, 20]
+    bits = [0b1, 0b11, 0b101, 0b1001, 0b10001, 0b100001, 0b1, 0b11, 0b101, 0b1101, 0b11001] if mask == "tree" else None
+    c = Call(S, kind, 4, 2, 64, past, lens, pad=pad, bits=bits)
+    assert form(tmp_path, c) == want
+    c.q.copy_(c.q.abs())                               # so that a key of -inf has the score -inf, not NaN
+
+    def key(b, j):
+        return c.pool[c.table[b, j // 16], 0, :, j % 16]
+
+    key(0, 9).fill_(float("-inf"))                     # seen by all rows
+    key(0, 75).fill_(float("-inf"))                    # the last row's own
+    c.run(mask)
+    clean = host(c.weight)
+    c.q[2] = float("nan")                              # sees 0 .. 69, and of the call's rows 0 .. 2, or 0 and 2
+    c.weight.fill_(7.0)
+    c.run(mask)
+    got = host(c.weight)
+    for j in range(76):
+        seen = j < 70 or (j - 70 in (0, 1, 2) if mask == "causal" else j - 70 in (0, 2))
+        w, before = got[c.table[0, j // 16], :, j % 16], clean[c.table[0, j // 16], :, j % 16]
+        if seen:
+            assert np.isnan(w).all(), "token %d" % j
+        else:
+            assert np.array_equal(w, before), "token %d: %r for %r" % (j, w, before)
+    assert np.array_equal(clean[c.table[0, 4], :, 11], host(c.prev)[c.table[0, 4], :, 11]), "-inf gives nothing"
+    for j in range(25):
+        at = (c.table[1, j // 16], slice(None), j % 16)
+        assert np.array_equal(got[at], clean[at]), "the other request, token %d" % j
