@@ -32,7 +32,7 @@
  *                              over packed prompts with grouped heads
  *   seer_rope_rows,            rotary positions of rows, alone and on the way
  *   seer_kv_store_rope,        into pages; the attention weight of each cached
- *   seer_row_positions,        token, and eviction by it: a paged cache that
+ *   seer_row_positions(_kept), token, and eviction by it: a paged cache that
  *   seer_attn_weights,         stays within a budget
  *   seer_kv_evict
  *
@@ -735,6 +735,16 @@ int seer_kv_store_rope(const seer_attn_desc* desc, const seer_page_desc* pages, 
 int seer_row_positions(const int32_t* cu_seqlens, const int32_t* seqused, int32_t batch, const int32_t* seen,
                        const int32_t* base, const int32_t* status, int32_t rows_ub, int32_t* positions, int32_t* next,
                        hipStream_t stream);
+
+/* seer_row_positions, where kept[b] also becomes kv_len[b], the plan's; where the
+ * plan was refused, kept stays.  The next plan's `keep` is then this one array
+ * whether an eviction comes before it (which writes kept) or not, so that steps
+ * can be recorded and replayed from either state.
+ * Errors: as seer_row_positions; EINVAL (kv_len or kept NULL, kept equal to
+ * another argument). */
+int seer_row_positions_kept(const int32_t* cu_seqlens, const int32_t* seqused, int32_t batch, const int32_t* seen,
+                            const int32_t* base, const int32_t* status, int32_t rows_ub, int32_t* positions,
+                            int32_t* next, const int32_t* kv_len, int32_t* kept, hipStream_t stream);
 
 /* Workspace bytes of seer_attn_weights for up to rows_ub rows, whatever `last`;
  * 0 for a bad description. */

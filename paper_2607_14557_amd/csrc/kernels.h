@@ -400,6 +400,8 @@ struct RowPositionsParams {
   int rows_ub;
   int* positions;
   int* next;                   // [B] or null
+  const int* kv_len;           // [B] of the plan, to kept where it was not refused
+  int* kept;                   // or null
 };
 int launch_row_positions(const RowPositionsParams& p, hipStream_t s);
 

@@ -235,6 +235,8 @@ __global__ __launch_bounds__(NT) void row_positions_kernel(RowPositionsParams p)
   if (p.next)
     for (long long b = first; b < p.B; b += step)
       p.next[b] = refused ? (p.seen ? p.seen[b] : 0) : (base ? base[b] : 0) + real((int)b);
+  if (p.kept && !refused)
+    for (long long b = first; b < p.B; b += step) p.kept[b] = p.kv_len[b];
 }
 
 int launch_row_positions(const RowPositionsParams& p, hipStream_t s) {

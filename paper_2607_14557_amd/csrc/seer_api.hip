@@ -1010,18 +1010,33 @@ int seer_kv_store_rope(const seer_attn_desc* desc, const seer_page_desc* pages, 
   return ok();
 }
 
-int seer_row_positions(const int32_t* cu_seqlens, const int32_t* seqused, int32_t batch, const int32_t* seen,
-                       const int32_t* base, const int32_t* status, int32_t rows_ub, int32_t* positions, int32_t* next,
-                       hipStream_t stream) {
+static int row_positions(const int32_t* cu_seqlens, const int32_t* seqused, int32_t batch, const int32_t* seen,
+                         const int32_t* base, const int32_t* status, int32_t rows_ub, int32_t* positions, int32_t* next,
+                         const int32_t* kv_len, int32_t* kept, hipStream_t stream) {
   if (!cu_seqlens || (rows_ub > 0 && !positions)) return fail(SEER_EINVAL, "a required pointer is NULL");
   if (batch < 1 || rows_ub < 0) return fail(SEER_EINVAL, "batch must be >= 1, rows_ub >= 0 (got %d, %d)", batch, rows_ub);
   if (next && (next == seen || next == base)) return fail(SEER_EINVAL, "next may be neither seen nor base");
-  if (rows_ub == 0 && !next) return ok();
+  if (rows_ub == 0 && !next && !kept) return ok();
   seer::RowPositionsParams p{};
   p.cu = cu_seqlens; p.used = seqused; p.B = batch; p.seen = seen; p.base = base; p.status = status;
-  p.rows_ub = rows_ub; p.positions = positions; p.next = next;
+  p.rows_ub = rows_ub; p.positions = positions; p.next = next; p.kv_len = kv_len; p.kept = kept;
   if (seer::launch_row_positions(p, stream)) return hip_fail("row positions launch");
   return ok();
+}
+
+int seer_row_positions(const int32_t* cu_seqlens, const int32_t* seqused, int32_t batch, const int32_t* seen,
+                       const int32_t* base, const int32_t* status, int32_t rows_ub, int32_t* positions, int32_t* next,
+                       hipStream_t stream) {
+  return row_positions(cu_seqlens, seqused, batch, seen, base, status, rows_ub, positions, next, nullptr, nullptr, stream);
+}
+
+int seer_row_positions_kept(const int32_t* cu_seqlens, const int32_t* seqused, int32_t batch, const int32_t* seen,
+                            const int32_t* base, const int32_t* status, int32_t rows_ub, int32_t* positions,
+                            int32_t* next, const int32_t* kv_len, int32_t* kept, hipStream_t stream) {
+  if (!kv_len || !kept) return fail(SEER_EINVAL, "a required pointer is NULL");
+  for (const int32_t* x : {cu_seqlens, seqused, seen, base, status, (const int32_t*)positions, (const int32_t*)next, kv_len})
+    if (x == kept) return fail(SEER_EINVAL, "kept may be no other argument");
+  return row_positions(cu_seqlens, seqused, batch, seen, base, status, rows_ub, positions, next, kv_len, kept, stream);
 }
 
 // places of a request, in whole tiles of 64

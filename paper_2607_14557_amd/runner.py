@@ -422,6 +422,13 @@ class BudgetCache(PagedCache):
     one cut: ValueError.  Calls after a refused plan mean nothing until check()
     has raised it.
 
+    What stays of each request is counted on the device (kept: the tokens after
+    the last plan, or what evict() has left of them), so that a recording may
+    begin and end before a cut or behind one, and be replayed among eager steps.
+    The ValueErrors go by the order in which calls are made, and a recorded call
+    is made when it is recorded: behind a recording that ends with a cut, eager
+    calls go on with plan().
+
     rows, types and streams as for PagedCache; budget, base int32 [max_batch]."""
 
     def __init__(self, n_heads, n_kv_heads, head_dim, n_layers, n_pages, page_size, max_batch, max_len, max_rows,
@@ -439,7 +446,7 @@ class BudgetCache(PagedCache):
         self.numbers = [torch.zeros(marks, dtype=torch.int32, device=device) for _ in range(n_layers)]
         self._seen = [torch.zeros(max_batch, dtype=torch.int32, device=device) for _ in range(2)]
         self.positions = torch.zeros(max_rows, dtype=torch.int32, device=device)
-        self.kept = torch.zeros(max_batch, dtype=torch.int32, device=device)
+        self.kept = torch.zeros(max_batch, dtype=torch.int32, device=device)      # what the next plan keeps
         self._cut = set()                             # layers that are cut since the last plan
         self._cut_before = set()                      # and before it
         need = max(S.seer_attn_weights_workspace_bytes(self.desc, self.pages, max_rows, max_batch),
@@ -457,20 +464,29 @@ class BudgetCache(PagedCache):
         if layer in self._cut:
             raise ValueError("layer %d is cut: the next call is plan()" % layer)
 
+    @staticmethod
+    def _apart(name, x, written):
+        """Refuse an argument that shares memory with what the same call writes."""
+        if x is not None:
+            a, b = x.data_ptr(), written.data_ptr()
+            if a < b + 4 * written.numel() and b < a + x.numel() * x.element_size():
+                raise ValueError("%s may not be in a buffer that the plan writes" % name)
+
     def plan(self, cu, rows_ub, keep=None, seqused=None, base=None, stream=None):
         """The pages, slots and positions of a step; returns the slots of its rows."""
         if base is not None:
             self._ints("base", base, self.max_batch)
             if base is self._seen[1]:
                 raise ValueError("base may not be the buffer that the plan writes")
+        for name, x in (("cu", cu), ("seqused", seqused), ("base", base)):
+            self._apart(name, x, self.kept)
         if self._cut:
             if len(self._cut) < len(self.pools):
                 raise ValueError("%d of %d layers are cut: a plan comes after all or none" % (len(self._cut), len(self.pools)))
-            keep = self.kept if keep is None else keep
-        slots = super().plan(cu, rows_ub, keep, seqused, stream=stream)
+        slots = super().plan(cu, rows_ub, self.kept if keep is None else keep, seqused, stream=stream)
         self._cut_before, self._cut = self._cut, set()
         S.seer_row_positions(cu, seqused, self.max_batch, self._seen[0], base, self.status, rows_ub, self.positions,
-                             self._seen[1], stream=stream)
+                             self._seen[1], stream=stream, kv_len=self._lens[0], kept=self.kept)
         self._seen.reverse()
         return slots
 

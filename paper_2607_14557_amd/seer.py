@@ -35,7 +35,7 @@ EXPORTED = ("seer_prepacked_bytes", "seer_prepack_weights", "seer_layer_workspac
             "seer_graph_launch", "seer_graph_destroy", "seer_lm_head_workspace_bytes", "seer_lm_head_prepack",
             "seer_lm_head_predict", "seer_remask_step", "seer_page_pool_bytes", "seer_page_plan", "seer_page_plan_latched", "seer_kv_store",
             "seer_attn_workspace_bytes", "seer_attn_prompt", "seer_attn_paged", "seer_rope_turns", "seer_rope_rows",
-            "seer_kv_store_rope", "seer_row_positions", "seer_attn_weights_workspace_bytes", "seer_attn_weights",
+            "seer_kv_store_rope", "seer_row_positions", "seer_row_positions_kept", "seer_attn_weights_workspace_bytes", "seer_attn_weights",
             "seer_kv_evict_workspace_bytes", "seer_kv_evict", "seer_last_error",
             "seer_abi_version")
 
@@ -193,6 +193,8 @@ def load_library():
     L.seer_kv_store_rope.restype = ctypes.c_int
     L.seer_row_positions.argtypes = [_P, _P, _I, _P, _P, _P, _I, _P, _P, _P]
     L.seer_row_positions.restype = ctypes.c_int
+    L.seer_row_positions_kept.argtypes = [_P, _P, _I, _P, _P, _P, _I, _P, _P, _P, _P, _P]
+    L.seer_row_positions_kept.restype = ctypes.c_int
     L.seer_attn_weights_workspace_bytes.argtypes = [heads, pages, _I, _I]
     L.seer_attn_weights_workspace_bytes.restype = ctypes.c_size_t
     L.seer_attn_weights.argtypes = [heads, pages, _I, _P, _L, _I, _P, _P, _I, _I, _P, _P, _P, _P, _I, ctypes.c_float, _P,
@@ -468,10 +470,15 @@ def seer_kv_store_rope(desc, pages, rope, turns, q, q_stride, q_out, q_out_strid
         _ptr(pool), _ptr(weight), _ptr(number), _stream(stream)))
 
 
-def seer_row_positions(cu_seqlens, seqused, batch, seen, base, status, rows_ub, positions, next, stream=None):
-    _check(load_library().seer_row_positions(
-        _ptr(cu_seqlens), _ptr(seqused), int(batch), _ptr(seen), _ptr(base), _ptr(status), int(rows_ub), _ptr(positions),
-        _ptr(next), _stream(stream)))
+def seer_row_positions(cu_seqlens, seqused, batch, seen, base, status, rows_ub, positions, next, stream=None, kv_len=None,
+                       kept=None):
+    """With kept: seer_row_positions_kept."""
+    args = (_ptr(cu_seqlens), _ptr(seqused), int(batch), _ptr(seen), _ptr(base), _ptr(status), int(rows_ub), _ptr(positions),
+            _ptr(next))
+    if kept is None:
+        _check(load_library().seer_row_positions(*args, _stream(stream)))
+    else:
+        _check(load_library().seer_row_positions_kept(*args, _ptr(kv_len), _ptr(kept), _stream(stream)))
 
 
 def seer_attn_weights_workspace_bytes(desc, pages, rows_ub, batch):

@@ -1,0 +1,86 @@
+"""What BudgetCache hands to its calls around a cut (no GPU): the lengths that a plan keeps, recorded or not, and what it
+refuses before anything is launched or changed."""
+import ctypes
+import os
+
+import pytest
+import torch
+
+from test_budget_host import B, CALLS, D, FAKE, H, KV, ROWS, _bf16, _i32, rope
+
+
+@pytest.fixture(scope="module")
+def S():
+    from paper_2607_14557_amd import seer
+    if not os.path.exists(seer.LIB_PATH):
+        pytest.skip("libseer.so not built")
+    seer.load_library()
+    return seer
+
+
+@pytest.fixture
+def calls(S, monkeypatch):
+    """The entry points' names, arguments and keywords as they are called, with no launch behind them."""
+    from paper_2607_14557_amd import runner
+    made = []
+    for name in CALLS:
+        monkeypatch.setattr(runner.S, name, lambda *a, _name=name, **kw: made.append((_name, a, kw)))
+    return made
+
+
+def _cache(S, layers=2, **kw):
+    from paper_2607_14557_amd.runner import BudgetCache
+    return BudgetCache(H, KV, D, layers, 4, 16, B, 32, ROWS, rope=rope(S), device="cpu", **kw)
+
+
+def _plans(calls):
+    return [(a, kw) for n, a, kw in calls if n == "seer_page_plan_latched"]
+
+
+def _positions(calls):
+    return [(a, kw) for n, a, kw in calls if n == "seer_row_positions"]
+
+
+def test_what_a_plan_keeps(S, calls):
+    """One array, whatever came before on the host: a call that is recorded is made once and replayed in other states."""
+    c, cu, budget = _cache(S), _i32(B + 1), _i32(B)
+    c.plan(cu, ROWS)                                    # nothing is cut
+    for _ in range(2):                                  # as two steps are recorded
+        c.plan(cu, ROWS)
+        for layer in range(2):
+            c.evict(layer, budget)
+    c.plan(cu, ROWS)                                    # behind the recording, of which nothing has run
+    plans, after = _plans(calls), _positions(calls)
+    assert len(plans) == 4 and all(a[2] is c.kept for a, _ in plans)
+    # and it is the lengths of an accepted plan from then on: each after its plan, with its status
+    order = [n for n, _, _ in calls if n in ("seer_page_plan_latched", "seer_row_positions")]
+    assert order == ["seer_page_plan_latched", "seer_row_positions"] * 4
+    for (a, _), (pa, pkw) in zip(plans, after):
+        assert pkw["kept"] is c.kept and pkw["kv_len"] is a[11] and pa[5] is a[13]
+
+
+def test_plan_keeps_apart_what_it_writes(S, calls):
+    c, cu, budget = _cache(S), _i32(B + 1), _i32(B)
+    whole = c.kept = _i32(3 * B)[:B]                    # kept within something larger
+    parts = whole.as_strided((B,), (1,), whole.storage_offset())
+    for kw in (dict(base=c.kept), dict(base=parts), dict(seqused=c.kept),
+               dict(base=whole.as_strided((B,), (1,), whole.storage_offset() + B - 1))):
+        before, lens, seen = len(calls), c._lens[0], c._seen[0]
+        with pytest.raises(ValueError, match="writes"):
+            c.plan(cu, ROWS, **kw)
+        assert len(calls) == before and c._lens[0] is lens and c._seen[0] is seen
+    c.plan(cu, ROWS, base=whole.as_strided((B,), (1,), whole.storage_offset() + B))
+    c.plan(cu, ROWS, c.kept)                            # read by the plan, written behind it
+
+
+def test_row_positions_kept_refusals(S):
+    def call(cu=FAKE, used=None, batch=2, seen=FAKE, base=None, status=None, rows=4, pos=FAKE, next=2 * FAKE, kv=3 * FAKE,
+             kept=4 * FAKE):
+        return S.load_library().seer_row_positions_kept(cu, used, batch, seen, base, status, rows, pos, next, kv, kept, None)
+
+    for kw in (dict(cu=None), dict(pos=None), dict(batch=0), dict(rows=-1), dict(next=FAKE), dict(kv=None), dict(kept=None)):
+        assert call(**kw) == S.SEER_EINVAL, kw
+    for kw in (dict(kept=FAKE), dict(kept=2 * FAKE), dict(kept=3 * FAKE), dict(used=4 * FAKE), dict(base=4 * FAKE),
+               dict(status=4 * FAKE)):
+        assert call(**kw) == S.SEER_EINVAL and "kept" in S.seer_last_error(), kw
+    assert ctypes.c_int(call(rows=0, pos=None, batch=0)).value == S.SEER_EINVAL

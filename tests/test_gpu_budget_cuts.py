@@ -1,0 +1,140 @@
+"""Cuts of a cache within a budget (BudgetCache) around recordings, refused plans and layers that are not cut alike,
+beside the same steps made eagerly on a cache of its own."""
+import numpy as np
+import pytest
+
+from gpu_util import dev, host
+
+pytestmark = pytest.mark.gpu
+H, KV, D, B, ROWS = 8, 2, 128, 3, 4
+
+
+@pytest.fixture(scope="module")
+def S():
+    from paper_2607_14557_amd import seer
+    seer.load_library()
+    return seer
+
+
+class Pair:
+    """Two caches that take the same steps."""
+
+    def __init__(self, S, layers=2, n_pages=60, budget=(20, 20, 20)):
+        import torch
+        from paper_2607_14557_amd.runner import BudgetCache
+        rope = S.seer_rope_desc(S.SEER_ROPE_HALF, 0, S.SEER_ROPE_PLAIN, 0, 10000.0, 1.0, 0.0, 0.0, 0.0)
+        self.caches = [BudgetCache(H, KV, D, layers, n_pages, 16, B, 96, 64, rope=rope) for _ in range(2)]
+        self.gen = torch.Generator(device="cuda")
+        self.gen.manual_seed(1)
+        self.cu0, self.cu = dev(np.array([0, 30, 31, 50])), dev(np.array([0, 1, 2, 3]))
+        self.budget, self.layers = dev(np.array(budget)), range(layers)
+        zeros = lambda n: torch.zeros(64, n * D, dtype=torch.bfloat16, device="cuda")
+        self.q, self.k, self.v = zeros(H), zeros(KV), zeros(KV)
+        self.outs, self.qo = [zeros(H) for _ in self.caches], [zeros(H) for _ in self.caches]
+        self.draw()
+
+    def draw(self):
+        import torch
+        for x in (self.q, self.k, self.v):
+            x.copy_(torch.empty(x.shape, device="cuda").normal_(0, 1, generator=self.gen).to(x.dtype))
+        torch.cuda.synchronize()
+
+    def step(self, i, cu, n, cut=True, stream=None):
+        c = self.caches[i]
+        slots = c.plan(cu, n, stream=stream)
+        for layer in self.layers:
+            c.store(layer, self.k, self.v, n, slots, stream=stream, q=self.q, q_out=self.qo[i])
+            c.attend(layer, self.qo[i], self.outs[i], cu, n, stream=stream)
+            c.weigh(layer, self.qo[i], cu, n, stream=stream)
+        if cut:
+            self.cut(i, stream)
+
+    def cut(self, i, stream=None):
+        for layer in self.layers:
+            self.caches[i].evict(layer, self.budget, 1, 2, stream=stream)
+
+    def same(self, what=""):
+        import torch
+        torch.cuda.synchronize()
+        a, b = self.caches
+        assert torch.equal(a.lens, b.lens) and torch.equal(a.seen, b.seen) and torch.equal(a.free, b.free), what
+        assert torch.equal(self.outs[0], self.outs[1]) and torch.equal(a.kept, b.kept), what
+        for x, y in ((a.weights, b.weights), (a.numbers, b.numbers), (a.pools, b.pools)):
+            assert all(torch.equal(s, t) for s, t in zip(x, y)), what
+
+
+@pytest.mark.parametrize("cut_before", [False, True])
+def test_recorded_from_either_state(S, cut_before):
+    """Two decoding steps, each with its cut, recorded behind a prompt that is cut or not: the first replay goes on from
+    the prompt, the later ones from the replay before, with eager steps and steps without a cut between."""
+    import torch
+    from paper_2607_14557_amd.runner import record
+    p = Pair(S)
+    for i in range(2):
+        p.step(i, p.cu0, 64, cut_before)
+    torch.cuda.synchronize()
+    st = torch.cuda.Stream()
+
+    def two():
+        for _ in range(2):
+            p.step(0, p.cu, ROWS, stream=st)
+
+    g = record(two, st)
+    for turn in range(5):
+        p.draw()
+        g.replay(st)
+        torch.cuda.synchronize()
+        for _ in range(2):
+            p.step(1, p.cu, ROWS)
+        p.same("replay %d" % turn)
+        if turn == 2:                                # eager steps between, an even number of plans
+            for i in range(2):
+                p.step(i, p.cu, ROWS, cut=False)
+                p.step(i, p.cu, ROWS, cut=False)
+            p.same("eager steps")
+    for c in p.caches:
+        c.check()
+    assert host(p.caches[0].lens).tolist() == [21, 13, 21]        # the budget and the step's row
+
+
+def test_eager_behind_a_recording(S):
+    """A recording of which nothing has run changes nothing; a recorded cut counts for the eager plan behind its replay,
+    and only there."""
+    import torch
+    from paper_2607_14557_amd.runner import record
+    p = Pair(S)
+    for i in range(2):
+        p.step(i, p.cu0, 64, cut=False)
+    torch.cuda.synchronize()
+    st = torch.cuda.Stream()
+    g = record(lambda: p.cut(0, st), st)
+    for i in range(2):                                # nothing was cut
+        p.step(i, p.cu, ROWS, cut=False)
+        p.step(i, p.cu, ROWS, cut=False)
+    p.same("before the first replay")
+    assert host(p.caches[0].lens).tolist() == [32, 3, 21]
+    for turn in range(3):
+        p.draw()
+        torch.cuda.synchronize()
+        g.replay(st)
+        torch.cuda.synchronize()
+        p.cut(1)
+        for i in range(2):
+            p.step(i, p.cu, ROWS, cut=False)
+            p.step(i, p.cu, ROWS, cut=False)
+        p.same("turn %d" % turn)
+        assert host(p.caches[0].lens).tolist()[0] == 22
+    for c in p.caches:
+        c.check()
+
+
+def test_row_positions_kept(S):
+    """kept becomes the plan's lengths, and stays where the plan was refused."""
+    import torch
+    for n in (1, 3, 300):
+        cu, seen, kv = dev(np.arange(n + 1)), dev(np.arange(n) * 5), dev(np.arange(n) + 9)
+        for status, rows in ((0, n + 3), (4, n + 3), (0, 0)):
+            kept, nxt, pos = dev(np.full(n, 77)), dev(np.full(n, 77)), dev(np.full(n + 3, 77))
+            S.seer_row_positions(cu, None, n, seen, None, dev(np.array([status])), rows, pos, nxt, kv_len=kv, kept=kept)
+            assert host(kept).tolist() == ([77] * n if status else host(kv).tolist())
+            assert host(nxt).tolist() == [5 * i + (0 if status else 1) for i in range(n)]
