@@ -779,6 +779,11 @@ int seer_attn_weights(const seer_attn_desc* desc, const seer_page_desc* pages, i
 /* seer_kv_evict flags: one choice for all key/value heads of a request, by the sum of
  * the heads' weights (taken in fp64, rounded to fp32) and head 0's numbers. */
 #define SEER_EVICT_SHARED 1
+/* And one for the layers of a cache after the first: kept holds what the layers that
+ * are cut already keep.  N is at most that; where budget[b] asks for another length,
+ * kept[b] becomes -1 - N: the layers were not cut alike, and a plan with this `keep`
+ * is refused. */
+#define SEER_EVICT_ALIKE 4
 
 /* Workspace bytes of seer_kv_evict; 0 for a bad description. */
 size_t seer_kv_evict_workspace_bytes(const seer_attn_desc* desc, const seer_page_desc* pages, int32_t batch);
@@ -792,7 +797,7 @@ size_t seer_kv_evict_workspace_bytes(const seer_attn_desc* desc, const seer_page
  * that are given up: K and V in the pool, weight and number to weight_out and
  * number_out.  These may be weight and number (in place: nothing else is
  * written), or other marks, which then get all of the N kept tokens'.
- * kept[b] = N: the `keep` of the next seer_page_plan.  Places on a page outside the pool hold
+ * kept[b] = N: the `keep` of the next seer_page_plan (and see SEER_EVICT_ALIKE).  Places on a page outside the pool hold
  * nothing: they count as unprotected and lighter than any weight, and nothing
  * is read from or written to them.
  * workspace: seer_kv_evict_workspace_bytes, 256-byte aligned; it holds nothing

@@ -32,6 +32,7 @@ __device__ __forceinline__ uint32_t order_of(float w) {
 
 struct Request {
   int L, N, seen;
+  int kept;              // N, or -1 - N where other layers keep another number
   const int* table;
 };
 
@@ -40,8 +41,15 @@ __device__ __forceinline__ Request request(const EvictParams& p, int b) {
   const long long most = (long long)p.width << p.shift;
   const int L = p.kv_len[b], N = p.budget[b];
   r.seen = p.seen[b];                            // on its way with the others
+  const int others = p.alike ? p.kept[b] : 0;
   r.L = L < 0 ? 0 : (L > most ? (int)most : L);
-  r.N = N < 0 ? 0 : (N < r.L ? N : r.L);
+  r.N = r.kept = N < 0 ? 0 : (N < r.L ? N : r.L);
+  if (p.alike) {
+    // (a workgroup that reads what another one of the request has written already finds the same N)
+    const int least = others < 0 ? -1 - others : others;
+    r.N = r.N < least ? r.N : least;
+    r.kept = r.kept == others ? r.kept : -1 - r.N;
+  }
   r.table = p.table + (size_t)b * p.width;
   return r;
 }
@@ -360,7 +368,7 @@ __device__ __forceinline__ void evict_list(const EvictParams& p, const Request& 
     }
   }
   if (tid == 0) {
-    if (h == 0) p.kept[b] = r.N;
+    if (h == 0) p.kept[b] = r.kept;
     if (!p.fused) p.counts[blockIdx.x] = n;
   }
   __syncthreads();
@@ -490,7 +498,7 @@ __global__ __launch_bounds__(1024) void evict_long_kernel(EvictParams p) {
   }
   if (tid == 0) {
     p.counts[blockIdx.x] = sources;
-    if (h == 0) p.kept[b] = r.N;
+    if (h == 0) p.kept[b] = r.kept;
   }
 }
 

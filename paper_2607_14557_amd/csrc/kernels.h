@@ -459,6 +459,7 @@ struct EvictParams {
   float* weight_out;
   int* number_out;
   int* kept;
+  bool alike;                  // kept is read too: what other layers keep
   bool fused;
   int* counts;                 // [B * lists] moves
   int* moves;                  // [B * lists][2][room] slots from, to

@@ -1145,7 +1145,7 @@ int seer_kv_evict(const seer_attn_desc* desc, const seer_page_desc* pages, int32
   int rc = check_heads(desc);
   if (rc) return rc;
   if ((rc = check_pages(pages))) return rc;
-  if (flags & ~SEER_EVICT_SHARED) return fail(SEER_EINVAL, "unknown flags %d", flags);
+  if (flags & ~(SEER_EVICT_SHARED | SEER_EVICT_ALIKE)) return fail(SEER_EINVAL, "unknown flags %d", flags);
   if (batch < 1) return fail(SEER_EINVAL, "batch must be >= 1 (got %d)", batch);
   if (first < 0 || recent < 0) return fail(SEER_EINVAL, "first and recent must be >= 0 (got %d, %d)", first, recent);
   if (!kv_len || !budget || !seen || !table || !pool || !weight || !number || !weight_out || !number_out || !kept || !workspace)
@@ -1161,6 +1161,7 @@ int seer_kv_evict(const seer_attn_desc* desc, const seer_page_desc* pages, int32
   p.shift = page_shift(pages); p.n_pages = pages->n_pages; p.width = pages->table_width;
   p.kv_len = kv_len; p.budget = budget; p.seen = seen; p.B = batch; p.first = first; p.recent = recent;
   p.shared = (flags & SEER_EVICT_SHARED) != 0;
+  p.alike = (flags & SEER_EVICT_ALIKE) != 0;
   p.lists = p.shared ? 1 : desc->n_kv_heads;
   if ((long long)batch * p.lists >= 1 << 20)
     return fail(SEER_EUNSUPPORTED, "batch * n_kv_heads must stay below 2^20 (got %d * %d)", batch, p.lists);

@@ -223,6 +223,8 @@ class PagedCache:
     (row strides are free), tree_bits [at least rows_ub, words] int64 and contiguous,
     cu, keep, seqused and slots int32 and contiguous; ValueError otherwise."""
 
+    _invalid = "keep exceeds what a request holds"
+
     def __init__(self, n_heads, n_kv_heads, head_dim, n_layers, n_pages, page_size, max_batch, max_len, max_rows,
                  dtype="bf16", v_f16=False, scale=0.0, device="cuda"):
         S.load_library()
@@ -348,7 +350,7 @@ class PagedCache:
                 torch.cuda.current_stream(self.status.device).synchronize()     # before plans on other streams
             why = [n for bit, n in ((S.SEER_PAGES_EXHAUSTED, "not enough free pages"),
                                     (S.SEER_PAGES_WIDTH, "a request longer than max_len"),
-                                    (S.SEER_PAGES_INVALID, "keep exceeds what a request holds")) if st & bit]
+                                    (S.SEER_PAGES_INVALID, self._invalid)) if st & bit]
             raise S.SeerError(S.SEER_EWORKSPACE, "; ".join(why))
 
     def store(self, layer, k, v, rows_ub, slots=None, stream=None):
@@ -419,7 +421,8 @@ class BudgetCache(PagedCache):
     request has ended (0).  After evict() has cut every layer alike, plan() keeps
     what it kept; a `keep` of the caller's may keep less, not more.  A cut layer
     takes no other call before that plan, and no plan comes between the layers of
-    one cut: ValueError.  Calls after a refused plan mean nothing until check()
+    one cut: ValueError.  Where layers were cut to different lengths that plan is
+    refused; a `keep` up to the least of them is taken then.  Calls after a refused plan mean nothing until check()
     has raised it.
 
     What stays of each request is counted on the device (kept: the tokens after
@@ -430,6 +433,8 @@ class BudgetCache(PagedCache):
     calls go on with plan().
 
     rows, types and streams as for PagedCache; budget, base int32 [max_batch]."""
+
+    _invalid = "keep exceeds what a request holds, or its layers were cut to different lengths"
 
     def __init__(self, n_heads, n_kv_heads, head_dim, n_layers, n_pages, page_size, max_batch, max_len, max_rows,
                  rope=None, dtype="bf16", v_f16=False, scale=0.0, device="cuda"):
@@ -562,13 +567,14 @@ class BudgetCache(PagedCache):
                             stream=stream)
 
     def evict(self, layer, budget, first=0, recent=0, shared=False, stream=None):
-        """Cut each request's cache in this layer to budget[b] tokens; returns the lengths kept.  Takes effect with the
-        next plan, and all layers are cut alike before it."""
+        """Cut each request's cache in this layer to budget[b] tokens; returns the lengths kept (-1 - the least of them
+        where layers were cut to different ones).  Takes effect with the next plan, and all layers are cut alike before it."""
         self._takes(0)
         self._whole(layer)
         self._ints("budget", budget, self.max_batch)
         w, n = self.weights[layer], self.numbers[layer]
-        S.seer_kv_evict(self.desc, self.pages, S.SEER_EVICT_SHARED if shared else 0, self._lens[0], budget, self._seen[0],
+        flags = (S.SEER_EVICT_SHARED if shared else 0) | (S.SEER_EVICT_ALIKE if self._cut else 0)
+        S.seer_kv_evict(self.desc, self.pages, flags, self._lens[0], budget, self._seen[0],
                         self.max_batch, first, recent, self.table, self.pools[layer], w, n, w, n, self.kept,
                         self.workspace, self.ws_bytes, stream=stream)
         self._cut.add(layer)

@@ -25,6 +25,7 @@ SEER_ROPE_HALF, SEER_ROPE_PAIRS = 0, 1
 SEER_ROPE_PLAIN, SEER_ROPE_LINEAR, SEER_ROPE_BASE, SEER_ROPE_BANDS, SEER_ROPE_RAMP = 0, 1, 2, 3, 4
 SEER_ROPE_INVERSE = 1
 SEER_EVICT_SHARED = 1
+SEER_EVICT_ALIKE = 4
 
 EXPORTED = ("seer_prepacked_bytes", "seer_prepack_weights", "seer_layer_workspace_bytes",
             "seer_layer_status_reset", "seer_layer_workspace_offsets", "seer_layer_forward_varlen",

@@ -84,3 +84,16 @@ def test_row_positions_kept_refusals(S):
                dict(status=4 * FAKE)):
         assert call(**kw) == S.SEER_EINVAL and "kept" in S.seer_last_error(), kw
     assert ctypes.c_int(call(rows=0, pos=None, batch=0)).value == S.SEER_EINVAL
+
+
+def test_layers_of_one_cut(S, calls):
+    """The layers after the first are held to what the first one keeps."""
+    c, cu, budget = _cache(S, layers=3), _i32(B + 1), _i32(B)
+    for shared in (False, True):
+        c.plan(cu, ROWS)
+        for layer in (1, 0, 2):
+            c.evict(layer, budget, shared=shared)
+        one = S.SEER_EVICT_SHARED if shared else 0
+        cuts = [a for n, a, _ in calls if n == "seer_kv_evict"][-3:]
+        assert [a[2] for a in cuts] == [one, one | S.SEER_EVICT_ALIKE, one | S.SEER_EVICT_ALIKE]
+        assert all(a[15] is c.kept for a in cuts)

@@ -138,3 +138,49 @@ def test_row_positions_kept(S):
             S.seer_row_positions(cu, None, n, seen, None, dev(np.array([status])), rows, pos, nxt, kv_len=kv, kept=kept)
             assert host(kept).tolist() == ([77] * n if status else host(kv).tolist())
             assert host(nxt).tolist() == [5 * i + (0 if status else 1) for i in range(n)]
+
+
+@pytest.mark.parametrize("shared", [False, True])
+@pytest.mark.parametrize("long", [1, 40, 150])
+def test_layers_cut_apart(S, shared, long):
+    """Layers cut to different lengths: each keeps its heaviest tokens, no more than the others keep; the plan behind them
+    is refused, and one that keeps the least is taken, with its tokens whole in every layer."""
+    import torch
+    from paper_2607_14557_amd.runner import BudgetCache
+    from oracle.budget import choose, moves
+    n = 60 * long                                      # lists in each kernel of the choice
+    c = BudgetCache(KV, KV, 64, 3, 2 * (n // 64 + 2), 64, 2, n + 64, n + 64, dtype="f32")
+    rng = np.random.default_rng(3)
+    rows = torch.from_numpy(rng.standard_normal((n + 5, KV * 64)).astype(np.float32)).cuda()
+    c.plan(dev(np.array([0, n, n + 5])), n + 5)
+    for layer in range(3):
+        c.store(layer, rows, rows, n + 5)
+        c.weights[layer].copy_(torch.from_numpy(rng.random(c.weights[layer].shape).astype(np.float32)))
+    table = host(c.table)
+    at = [[(int(table[b, j // 64]), j % 64) for j in range(L)] for b, L in ((0, n), (1, 5))]
+    budgets = [[n // 2, 3], [n // 2 + 7, 3], [n // 3, 4]]
+    least, want = [n, 5], []
+    for layer in range(3):
+        old, w = host(c.pools[layer][:, 0]), host(c.weights[layer])
+        kept = c.evict(layer, dev(np.array(budgets[layer])), shared=shared)
+        got = host(c.pools[layer][:, 0])
+        for b in range(2):
+            least[b] = min(least[b], budgets[layer][b])
+            score = np.array([w[p, :, s] for p, s in at[b]])
+            for h in range(KV):
+                by = score.sum(1).astype(np.float32) if shared else score[:, h].astype(np.float32)
+                src, dst = moves(choose(by, np.zeros(len(by), int) + 9, least[b], 0, 0, 10 ** 6), least[b])
+                come = dict(zip(dst, src))
+                for j in range(least[b]):
+                    (p, s), (fp, fs) = at[b][j], at[b][come.get(j, j)]
+                    assert np.array_equal(got[p, h, s], old[fp, h, fs]), (layer, b, h, j)
+        want.append(host(kept).tolist())
+    assert want == [[n // 2, 3], [-1 - n // 2, 3], [-1 - n // 3, -1 - 3]]
+    cu = dev(np.array([0, 1, 2]))
+    c.plan(cu, 2)
+    with pytest.raises(S.SeerError, match="different lengths"):
+        c.check()
+    assert host(c.lens).tolist() == [n, 5] and host(c.kept).tolist() == want[2]
+    c.plan(cu, 2, keep=dev(np.array(least)))
+    c.check()
+    assert host(c.lens).tolist() == [n // 3 + 1, 4] and host(c.kept).tolist() == [n // 3 + 1, 4]
