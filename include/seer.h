@@ -25,7 +25,7 @@
  *   seer_lm_head_prepack,      synthetic LM head (one-time weight layout;
  *   seer_lm_head_predict,      argmax + confidence) and
  *   seer_remask_step           low-confidence remasking between steps
- *   seer_page_plan, seer_page_plan_latched,
+ *   seer_page_plan(_latched, _kept),
  *   seer_kv_store,             paged keys and values: block tables and slot
  *   seer_attn_paged,           maps from the requests' lengths, rows into
  *   seer_attn_prompt           their pages, attention over the pages, and
@@ -568,6 +568,17 @@ int seer_page_plan_latched(const seer_page_desc* pages, const int32_t* held, con
                            const int32_t* cu_seqlens, const int32_t* seqused, int32_t batch, int32_t rows_ub,
                            int32_t* free_pages, const int32_t* free_in, int32_t* free_out, int32_t* table,
                            int32_t* kv_len, int32_t* slots, int32_t* status, int32_t* refused, hipStream_t stream);
+
+/* seer_page_plan_latched, where request b holds held[b] tokens of which an
+ * eviction has left the first kept[b] (seer_kv_evict): a keep[b] above that
+ * contradicts it (SEER_PAGES_INVALID), as the tokens behind them have moved.
+ * kept[b] < 0 means -1 - kept[b] (SEER_EVICT_ALIKE), and is refused as a keep.
+ * keep may be kept.  Errors: as seer_page_plan_latched; EINVAL (kept NULL, kv_len
+ * equal to kept). */
+int seer_page_plan_kept(const seer_page_desc* pages, const int32_t* held, const int32_t* kept, const int32_t* keep,
+                        const int32_t* cu_seqlens, const int32_t* seqused, int32_t batch, int32_t rows_ub,
+                        int32_t* free_pages, const int32_t* free_in, int32_t* free_out, int32_t* table,
+                        int32_t* kv_len, int32_t* slots, int32_t* status, int32_t* refused, hipStream_t stream);
 
 /* Copy key and value rows into their pages: row r < rows_ub of k and of v
  * (n_kv_heads * head_dim elements, rows k_stride and v_stride elements apart)

@@ -298,6 +298,7 @@ struct PagePlanParams {
   int width;             // entries of a row of the table
   const int* held;
   const int* keep;
+  const int* kept;       // [B] tokens that an eviction has left, or null
   const int* cu;
   const int* used;       // [B] or null
   int B;

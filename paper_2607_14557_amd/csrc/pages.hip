@@ -85,6 +85,10 @@ __global__ __launch_bounds__(PLAN_T) void page_plan_kernel(PagePlanParams p) {
     if (b == b0) first_l = l;
     const int H = pages_of(l.held, p.shift), N = pages_of((long long)l.keep + l.real, p.shift);
     if (l.bad) bad |= kPagesInvalid;
+    if (p.kept) {
+      const int kept = p.kept[b];
+      if (l.keep > (kept < 0 ? -1 - kept : kept)) bad |= kPagesInvalid;
+    }
     if ((long long)l.keep + l.real > (long long)p.width << p.shift || (long long)l.keep + l.real > INT_MAX)
       bad |= kPagesWidth;
     give += H > N ? H - N : 0;

@@ -325,11 +325,14 @@ class PagedCache:
 
     def plan(self, cu, rows_ub, keep=None, seqused=None, stream=None):
         """The pages and slots of a step; returns the slots of its rows."""
+        return self._plan(cu, rows_ub, keep, seqused, stream)
+
+    def _plan(self, cu, rows_ub, keep, seqused, stream, kept=None):
         self._takes(rows_ub, cu, keep, seqused)
         held = self._lens[0]
         S.seer_page_plan_latched(self.pages, held, held if keep is None else keep, cu, seqused, self.max_batch, rows_ub,
                                  self.free_pages, self._free[0], self._free[1], self.table, self._lens[1], self.slots,
-                                 self.status, self.refused, stream=stream)
+                                 self.status, self.refused, stream=stream, kept=kept)
         self._lens.reverse()
         self._free.reverse()
         self._planned = rows_ub
@@ -419,7 +422,8 @@ class BudgetCache(PagedCache):
     counts the tokens that each request has had; plan() goes on from it, or from
     `base` where drafts were refused (with the `keep` that goes with them) or a
     request has ended (0).  After evict() has cut every layer alike, plan() keeps
-    what it kept; a `keep` of the caller's may keep less, not more.  A cut layer
+    what it kept; a `keep` of the caller's may keep less; one that keeps more is
+    refused.  A cut layer
     takes no other call before that plan, and no plan comes between the layers of
     one cut: ValueError.  Where layers were cut to different lengths that plan is
     refused; a `keep` up to the least of them is taken then.  Calls after a refused plan mean nothing until check()
@@ -488,7 +492,7 @@ class BudgetCache(PagedCache):
         if self._cut:
             if len(self._cut) < len(self.pools):
                 raise ValueError("%d of %d layers are cut: a plan comes after all or none" % (len(self._cut), len(self.pools)))
-        slots = super().plan(cu, rows_ub, self.kept if keep is None else keep, seqused, stream=stream)
+        slots = self._plan(cu, rows_ub, self.kept if keep is None else keep, seqused, stream, self.kept)
         self._cut_before, self._cut = self._cut, set()
         S.seer_row_positions(cu, seqused, self.max_batch, self._seen[0], base, self.status, rows_ub, self.positions,
                              self._seen[1], stream=stream, kv_len=self._lens[0], kept=self.kept)

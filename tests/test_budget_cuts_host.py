@@ -97,3 +97,29 @@ def test_layers_of_one_cut(S, calls):
         cuts = [a for n, a, _ in calls if n == "seer_kv_evict"][-3:]
         assert [a[2] for a in cuts] == [one, one | S.SEER_EVICT_ALIKE, one | S.SEER_EVICT_ALIKE]
         assert all(a[15] is c.kept for a in cuts)
+
+
+def test_what_bounds_a_keep(S, calls):
+    """A plan knows what the cut has left, whoever says what stays."""
+    c, cu, keep = _cache(S, layers=1), _i32(B + 1), _i32(B)
+    for k in (None, keep):
+        c.plan(cu, ROWS, k)
+        c.evict(0, keep)
+    assert all(kw["kept"] is c.kept for _, kw in _plans(calls)) and _plans(calls)[1][0][2] is keep
+
+
+def test_page_plan_kept_refusals(S):
+    names = ("held", "kept", "keep", "cu", "used", "batch", "rows", "free", "free_in", "free_out", "table", "kv", "slots",
+             "status", "refused")
+
+    def call(**kw):
+        a = dict(held=FAKE, kept=2 * FAKE, keep=2 * FAKE, cu=FAKE, used=None, batch=2, rows=4, free=FAKE, free_in=FAKE,
+                 free_out=3 * FAKE, table=FAKE, kv=4 * FAKE, slots=FAKE, status=FAKE, refused=5 * FAKE)
+        a.update(kw)
+        return S.load_library().seer_page_plan_kept(ctypes.byref(S.seer_page_desc(64, 100, 10)), *[a[n] for n in names], None)
+
+    for n in ("held", "kept", "keep", "cu", "free", "free_in", "free_out", "table", "kv", "slots", "status", "refused"):
+        assert call(**{n: None}) == S.SEER_EINVAL, n
+    for kw in (dict(kv=2 * FAKE, keep=FAKE), dict(kv=FAKE), dict(free_out=FAKE), dict(refused=FAKE), dict(batch=0), dict(rows=-1)):
+        assert call(**kw) == S.SEER_EINVAL, kw
+    assert call(batch=4097) == S.SEER_EUNSUPPORTED

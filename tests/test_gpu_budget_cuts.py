@@ -184,3 +184,27 @@ def test_layers_cut_apart(S, shared, long):
     c.plan(cu, 2, keep=dev(np.array(least)))
     c.check()
     assert host(c.lens).tolist() == [n // 3 + 1, 4] and host(c.kept).tolist() == [n // 3 + 1, 4]
+
+
+def test_keep_more_than_was_kept(S):
+    """Behind a cut, a keep above what it left is refused, though that many tokens were held; one up to it is taken."""
+    p = Pair(S)
+    for i in range(2):
+        p.step(i, p.cu0, 64)
+    a, b = p.caches
+    assert host(a.lens).tolist() == [30, 1, 19] and host(a.kept).tolist() == [20, 1, 19]
+    for keep in ([21, 1, 19], [30, 1, 19], [20, 2, 19]):
+        a.plan(p.cu, ROWS, keep=dev(np.array(keep)))
+        with pytest.raises(S.SeerError, match="keep exceeds"):
+            a.check()
+        assert host(a.kept).tolist() == [20, 1, 19]
+    a.plan(p.cu, ROWS, keep=a.lens)                   # an even number of plans, as of the other cache: none
+    with pytest.raises(S.SeerError, match="keep exceeds"):
+        a.check()
+    p.same("refused plans change nothing")
+    for i, keep in enumerate((dev(np.array([20, 1, 19])), None)):
+        p.caches[i].plan(p.cu, ROWS, keep=keep)
+    p.same("as kept")
+    a.plan(p.cu, ROWS, keep=dev(np.array([7, 0, 20])))      # less of the tokens that are there
+    a.check()
+    assert host(a.lens).tolist() == [8, 1, 21] and host(a.kept).tolist() == [8, 1, 21]
