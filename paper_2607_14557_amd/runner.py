@@ -485,10 +485,10 @@ class BudgetCache(PagedCache):
         """The pages, slots and positions of a step; returns the slots of its rows."""
         if base is not None:
             self._ints("base", base, self.max_batch)
-            if base is self._seen[1]:
-                raise ValueError("base may not be the buffer that the plan writes")
+        # (before the pages are planned: the positions come behind them)
         for name, x in (("cu", cu), ("seqused", seqused), ("base", base)):
             self._apart(name, x, self.kept)
+            self._apart(name, x, self._seen[1])
         if self._cut:
             if len(self._cut) < len(self.pools):
                 raise ValueError("%d of %d layers are cut: a plan comes after all or none" % (len(self._cut), len(self.pools)))

@@ -123,3 +123,17 @@ def test_page_plan_kept_refusals(S):
     for kw in (dict(kv=2 * FAKE, keep=FAKE), dict(kv=FAKE), dict(free_out=FAKE), dict(refused=FAKE), dict(batch=0), dict(rows=-1)):
         assert call(**kw) == S.SEER_EINVAL, kw
     assert call(batch=4097) == S.SEER_EUNSUPPORTED
+
+
+def test_base_within_what_a_plan_writes(S, calls):
+    """A view of the buffer is the buffer: refused before the pages are planned and the lengths change places."""
+    c, cu = _cache(S), _i32(B + 1)
+    for n in range(2):
+        old = c._seen[1]
+        assert old is not c.seen
+        for kw in (dict(base=old), dict(base=old[:]), dict(base=old.view(B)), dict(seqused=old)):
+            before, lens, seen = len(calls), c._lens[0], c._seen[0]
+            with pytest.raises(ValueError, match="writes"):
+                c.plan(cu, ROWS, **kw)
+            assert len(calls) == before and c._lens[0] is lens and c._seen[0] is seen and c._planned == n * ROWS
+        c.plan(cu, ROWS, base=c.seen[:])
