@@ -34,7 +34,7 @@
  *   seer_kv_store_rope,        into pages; the attention weight of each cached
  *   seer_row_positions(_kept), token, and eviction by it: a paged cache that
  *   seer_attn_weights,         stays within a budget
- *   seer_kv_evict
+ *   seer_kv_evict(_planned)
  *
  * Conventions shared by every call:
  *   - Buffers are owned by the caller.  Pointers are device pointers unless a
@@ -821,6 +821,16 @@ int seer_kv_evict(const seer_attn_desc* desc, const seer_page_desc* pages, int32
                   const int32_t* budget, const int32_t* seen, int32_t batch, int32_t first, int32_t recent,
                   const int32_t* table, void* pool, const float* weight, const int32_t* number, float* weight_out,
                   int32_t* number_out, int32_t* kept, void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* seer_kv_evict behind a plan that may have been refused (status: the plan's, device):
+ * then nothing is cut, moved or written, kept[b] neither, as kv_len[b] is what was held
+ * before it and an earlier cut may have left less.
+ * Errors: as seer_kv_evict; EINVAL (status NULL or kept). */
+int seer_kv_evict_planned(const seer_attn_desc* desc, const seer_page_desc* pages, int32_t flags, const int32_t* kv_len,
+                          const int32_t* budget, const int32_t* seen, int32_t batch, int32_t first, int32_t recent,
+                          const int32_t* table, void* pool, const float* weight, const int32_t* number,
+                          float* weight_out, int32_t* number_out, int32_t* kept, const int32_t* status,
+                          void* workspace, size_t workspace_bytes, hipStream_t stream);
 
 /* ---- recorded launch sequences (Sec. 3.5) -------------------------------
  * The graph-compatible execution paths replay a fixed launch sequence.  Every

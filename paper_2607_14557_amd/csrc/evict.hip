@@ -33,6 +33,7 @@ __device__ __forceinline__ uint32_t order_of(float w) {
 struct Request {
   int L, N, seen;
   int kept;              // N, or -1 - N where other layers keep another number
+  bool refused;          // the plan was: no tokens then, and kept stays
   const int* table;
 };
 
@@ -42,7 +43,8 @@ __device__ __forceinline__ Request request(const EvictParams& p, int b) {
   const int L = p.kv_len[b], N = p.budget[b];
   r.seen = p.seen[b];                            // on its way with the others
   const int others = p.alike ? p.kept[b] : 0;
-  r.L = L < 0 ? 0 : (L > most ? (int)most : L);
+  r.refused = p.status && *p.status != 0;
+  r.L = L < 0 || r.refused ? 0 : (L > most ? (int)most : L);
   r.N = r.kept = N < 0 ? 0 : (N < r.L ? N : r.L);
   if (p.alike) {
     // (a workgroup that reads what another one of the request has written already finds the same N)
@@ -368,7 +370,7 @@ __device__ __forceinline__ void evict_list(const EvictParams& p, const Request& 
     }
   }
   if (tid == 0) {
-    if (h == 0) p.kept[b] = r.kept;
+    if (h == 0 && !r.refused) p.kept[b] = r.kept;
     if (!p.fused) p.counts[blockIdx.x] = n;
   }
   __syncthreads();
@@ -498,7 +500,7 @@ __global__ __launch_bounds__(1024) void evict_long_kernel(EvictParams p) {
   }
   if (tid == 0) {
     p.counts[blockIdx.x] = sources;
-    if (h == 0) p.kept[b] = r.kept;
+    if (h == 0) p.kept[b] = r.kept;              // (a refused plan's lists are short ones)
   }
 }
 

@@ -461,6 +461,7 @@ struct EvictParams {
   int* number_out;
   int* kept;
   bool alike;                  // kept is read too: what other layers keep
+  const int* status;           // of the plan, or null
   bool fused;
   int* counts;                 // [B * lists] moves
   int* moves;                  // [B * lists][2][room] slots from, to

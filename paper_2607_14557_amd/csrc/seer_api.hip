@@ -1148,10 +1148,11 @@ size_t seer_kv_evict_workspace_bytes(const seer_attn_desc* desc, const seer_page
   return up256(lists * 4) + lists * seer::evict_list_bytes(evict_places(pages));
 }
 
-int seer_kv_evict(const seer_attn_desc* desc, const seer_page_desc* pages, int32_t flags, const int32_t* kv_len,
-                  const int32_t* budget, const int32_t* seen, int32_t batch, int32_t first, int32_t recent,
-                  const int32_t* table, void* pool, const float* weight, const int32_t* number, float* weight_out,
-                  int32_t* number_out, int32_t* kept, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+static int kv_evict(const seer_attn_desc* desc, const seer_page_desc* pages, int32_t flags, const int32_t* kv_len,
+                    const int32_t* budget, const int32_t* seen, int32_t batch, int32_t first, int32_t recent,
+                    const int32_t* table, void* pool, const float* weight, const int32_t* number, float* weight_out,
+                    int32_t* number_out, int32_t* kept, const int32_t* status, void* workspace, size_t workspace_bytes,
+                    hipStream_t stream) {
   int rc = check_heads(desc);
   if (rc) return rc;
   if ((rc = check_pages(pages))) return rc;
@@ -1172,6 +1173,7 @@ int seer_kv_evict(const seer_attn_desc* desc, const seer_page_desc* pages, int32
   p.kv_len = kv_len; p.budget = budget; p.seen = seen; p.B = batch; p.first = first; p.recent = recent;
   p.shared = (flags & SEER_EVICT_SHARED) != 0;
   p.alike = (flags & SEER_EVICT_ALIKE) != 0;
+  p.status = status;
   p.lists = p.shared ? 1 : desc->n_kv_heads;
   if ((long long)batch * p.lists >= 1 << 20)
     return fail(SEER_EUNSUPPORTED, "batch * n_kv_heads must stay below 2^20 (got %d * %d)", batch, p.lists);
@@ -1191,6 +1193,24 @@ int seer_kv_evict(const seer_attn_desc* desc, const seer_page_desc* pages, int32
   p.bits = reinterpret_cast<unsigned long long*>(p.moves + lists * 2 * p.room);
   if (seer::launch_evict(p, rule, stream)) return hip_fail("eviction launch");
   return ok();
+}
+
+int seer_kv_evict(const seer_attn_desc* desc, const seer_page_desc* pages, int32_t flags, const int32_t* kv_len,
+                  const int32_t* budget, const int32_t* seen, int32_t batch, int32_t first, int32_t recent,
+                  const int32_t* table, void* pool, const float* weight, const int32_t* number, float* weight_out,
+                  int32_t* number_out, int32_t* kept, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  return kv_evict(desc, pages, flags, kv_len, budget, seen, batch, first, recent, table, pool, weight, number, weight_out,
+                  number_out, kept, nullptr, workspace, workspace_bytes, stream);
+}
+
+int seer_kv_evict_planned(const seer_attn_desc* desc, const seer_page_desc* pages, int32_t flags, const int32_t* kv_len,
+                          const int32_t* budget, const int32_t* seen, int32_t batch, int32_t first, int32_t recent,
+                          const int32_t* table, void* pool, const float* weight, const int32_t* number,
+                          float* weight_out, int32_t* number_out, int32_t* kept, const int32_t* status,
+                          void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  if (!status || status == kept) return fail(SEER_EINVAL, "status may be neither NULL nor kept");
+  return kv_evict(desc, pages, flags, kv_len, budget, seen, batch, first, recent, table, pool, weight, number, weight_out,
+                  number_out, kept, status, workspace, workspace_bytes, stream);
 }
 
 // ---- recorded launch sequences (Sec. 3.5, graph-compatible paths) ----------

@@ -422,12 +422,12 @@ class BudgetCache(PagedCache):
     counts the tokens that each request has had; plan() goes on from it, or from
     `base` where drafts were refused (with the `keep` that goes with them) or a
     request has ended (0).  After evict() has cut every layer alike, plan() keeps
-    what it kept; a `keep` of the caller's may keep less; one that keeps more is
-    refused.  A cut layer
-    takes no other call before that plan, and no plan comes between the layers of
-    one cut: ValueError.  Where layers were cut to different lengths that plan is
-    refused; a `keep` up to the least of them is taken then.  Calls after a refused plan mean nothing until check()
-    has raised it.
+    what it kept; a `keep` of the caller's may keep less, and one that keeps more is
+    refused.  A cut layer takes no other call before that plan, and no plan comes
+    between the layers of one cut: ValueError.  Where layers were cut to different
+    lengths that plan is refused; a `keep` up to the least of them is taken then.
+    Calls after a refused plan mean nothing until check() has raised it: nothing is
+    stored or cut, and what was cut before stays so (weigh() adds to the weights).
 
     What stays of each request is counted on the device (kept: the tokens after
     the last plan, or what evict() has left of them), so that a recording may
@@ -580,7 +580,7 @@ class BudgetCache(PagedCache):
         flags = (S.SEER_EVICT_SHARED if shared else 0) | (S.SEER_EVICT_ALIKE if self._cut else 0)
         S.seer_kv_evict(self.desc, self.pages, flags, self._lens[0], budget, self._seen[0],
                         self.max_batch, first, recent, self.table, self.pools[layer], w, n, w, n, self.kept,
-                        self.workspace, self.ws_bytes, stream=stream)
+                        self.workspace, self.ws_bytes, stream=stream, status=self.status)
         self._cut.add(layer)
         return self.kept
 

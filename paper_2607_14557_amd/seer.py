@@ -38,7 +38,7 @@ EXPORTED = ("seer_prepacked_bytes", "seer_prepack_weights", "seer_layer_workspac
             "seer_page_plan_kept", "seer_kv_store",
             "seer_attn_workspace_bytes", "seer_attn_prompt", "seer_attn_paged", "seer_rope_turns", "seer_rope_rows",
             "seer_kv_store_rope", "seer_row_positions", "seer_row_positions_kept", "seer_attn_weights_workspace_bytes", "seer_attn_weights",
-            "seer_kv_evict_workspace_bytes", "seer_kv_evict", "seer_last_error",
+            "seer_kv_evict_workspace_bytes", "seer_kv_evict", "seer_kv_evict_planned", "seer_last_error",
             "seer_abi_version")
 
 
@@ -209,6 +209,9 @@ def load_library():
     L.seer_kv_evict.argtypes = [heads, pages, _I, _P, _P, _P, _I, _I, _I, _P, _P, _P, _P, _P, _P, _P, _P, ctypes.c_size_t,
                                 _P]
     L.seer_kv_evict.restype = ctypes.c_int
+    L.seer_kv_evict_planned.argtypes = [heads, pages, _I, _P, _P, _P, _I, _I, _I, _P, _P, _P, _P, _P, _P, _P, _P, _P,
+                                        ctypes.c_size_t, _P]
+    L.seer_kv_evict_planned.restype = ctypes.c_int
     L.seer_last_error.argtypes = []
     L.seer_last_error.restype = ctypes.c_char_p
     L.seer_abi_version.argtypes = []
@@ -507,9 +510,12 @@ def seer_kv_evict_workspace_bytes(desc, pages, batch):
 
 
 def seer_kv_evict(desc, pages, flags, kv_len, budget, seen, batch, first, recent, table, pool, weight, number, weight_out,
-                  number_out, kept, workspace, workspace_bytes=None, stream=None):
+                  number_out, kept, workspace, workspace_bytes=None, stream=None, status=None):
+    """With status: seer_kv_evict_planned."""
     nbytes = workspace_bytes if workspace_bytes is not None else workspace.numel() * workspace.element_size()
-    _check(load_library().seer_kv_evict(
-        ctypes.byref(desc), ctypes.byref(pages), int(flags), _ptr(kv_len), _ptr(budget), _ptr(seen), int(batch), int(first),
-        int(recent), _ptr(table), _ptr(pool), _ptr(weight), _ptr(number), _ptr(weight_out), _ptr(number_out), _ptr(kept),
-        _ptr(workspace), nbytes, _stream(stream)))
+    args = (ctypes.byref(desc), ctypes.byref(pages), int(flags), _ptr(kv_len), _ptr(budget), _ptr(seen), int(batch), int(first),
+            int(recent), _ptr(table), _ptr(pool), _ptr(weight), _ptr(number), _ptr(weight_out), _ptr(number_out), _ptr(kept))
+    if status is None:
+        _check(load_library().seer_kv_evict(*args, _ptr(workspace), nbytes, _stream(stream)))
+    else:
+        _check(load_library().seer_kv_evict_planned(*args, _ptr(status), _ptr(workspace), nbytes, _stream(stream)))

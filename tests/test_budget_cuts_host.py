@@ -137,3 +137,27 @@ def test_base_within_what_a_plan_writes(S, calls):
                 c.plan(cu, ROWS, **kw)
             assert len(calls) == before and c._lens[0] is lens and c._seen[0] is seen and c._planned == n * ROWS
         c.plan(cu, ROWS, base=c.seen[:])
+
+
+def test_evict_knows_the_plan(S, calls):
+    c, cu, budget = _cache(S), _i32(B + 1), _i32(B)
+    c.plan(cu, ROWS)
+    c.evict(0, budget)
+    assert calls[-1][0] == "seer_kv_evict" and calls[-1][2]["status"] is c.status and calls[0][1][13] is c.status
+
+
+def test_evict_planned_refusals(S):
+    names = ("flags", "kv", "budget", "seen", "batch", "first", "recent", "table", "pool", "weight", "number", "wo", "no",
+             "kept", "status", "ws", "bytes")
+
+    def call(**kw):
+        a = dict(flags=0, kv=FAKE, budget=2 * FAKE, seen=3 * FAKE, batch=2, first=0, recent=0, table=FAKE, pool=FAKE,
+                 weight=FAKE, number=2 * FAKE, wo=FAKE, no=2 * FAKE, kept=4 * FAKE, status=5 * FAKE, ws=FAKE, bytes=1 << 40)
+        a.update(kw)
+        return S.load_library().seer_kv_evict_planned(ctypes.byref(S.seer_attn_desc(8, 2, 128, S.SEER_DTYPE_BF16, 0, 0.0)),
+                                                      ctypes.byref(S.seer_page_desc(64, 100, 10)), *[a[n] for n in names], None)
+
+    for n in ("kv", "budget", "seen", "table", "pool", "weight", "number", "wo", "no", "kept", "status", "ws"):
+        assert call(**{n: None}) == S.SEER_EINVAL, n
+    for kw in (dict(status=4 * FAKE), dict(flags=2), dict(flags=8), dict(batch=0), dict(kept=FAKE), dict(bytes=16, flags=4)):
+        assert call(**kw) in (S.SEER_EINVAL, S.SEER_EWORKSPACE), kw

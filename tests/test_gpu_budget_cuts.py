@@ -208,3 +208,76 @@ def test_keep_more_than_was_kept(S):
     a.plan(p.cu, ROWS, keep=dev(np.array([7, 0, 20])))      # less of the tokens that are there
     a.check()
     assert host(a.lens).tolist() == [8, 1, 21] and host(a.kept).tolist() == [8, 1, 21]
+
+
+@pytest.mark.parametrize("shared", [False, True])
+@pytest.mark.parametrize("max_len", [96, 3000, 9000, 20000])
+def test_evict_behind_a_refused_plan(S, shared, max_len):
+    """Nothing is cut or moved and kept stays, by each kernel of the choice, in a table as wide as it takes."""
+    import torch
+    from paper_2607_14557_amd.runner import BudgetCache
+    c = BudgetCache(KV, KV, 64, 2, 12, 16, 2, max_len, 200, dtype="f32")
+    rows = torch.randn(200, KV * 64, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1))
+    budget = dev(np.array([20, 20]))
+
+    def step(cu, weigh=False):
+        c.plan(dev(np.array(cu)), 200)
+        for layer in range(2):
+            c.store(layer, rows, rows, 200)
+            if weigh:
+                c.weights[layer].uniform_(generator=torch.Generator(device="cuda").manual_seed(layer))
+        for layer in range(2):
+            c.evict(layer, budget, shared=shared)
+
+    step([0, 90, 120], True)
+    torch.cuda.synchronize()
+    state = [x.clone() for x in c.pools + c.weights + c.numbers + [c.kept]]
+    step([0, 100, 200])                                # more pages than there are
+    torch.cuda.synchronize()
+    for x, y in zip(state, c.pools + c.weights + c.numbers + [c.kept]):
+        assert torch.equal(x, y)
+    with pytest.raises(S.SeerError):                   # free pages, or a request that is too long
+        c.check()
+    assert host(c.kept).tolist() == [20, 20] and host(c.lens).tolist() == [90, 30]
+    step([0, 1, 3])
+    c.check()
+    assert host(c.lens).tolist() == [21, 22] and host(c.kept).tolist() == [20, 20]
+
+
+def test_recorded_steps_behind_a_refused_plan(S):
+    """A recording goes on behind a plan that is refused: its cut leaves what was cut before, and the cache goes on as one
+    that took only the steps that were accepted."""
+    import torch
+    from paper_2607_14557_amd.runner import record
+    p = Pair(S, n_pages=7)                              # a step of a row each needs 2 + 1 + 2 pages, one of 20 each does not fit
+    cu, wide = p.cu.clone(), dev(np.array([0, 20, 40, 60]))
+    for i in range(2):
+        p.step(i, p.cu0, 64)
+    torch.cuda.synchronize()
+    st = torch.cuda.Stream()
+
+    def two():
+        for _ in range(2):
+            slots = p.caches[0].plan(cu, 64, stream=st)
+            for layer in p.layers:
+                p.caches[0].store(layer, p.k, p.v, 64, slots, stream=st, q=p.q, q_out=p.qo[0])
+            p.cut(0, st)
+
+    g = record(two, st)
+    for turn, fits in enumerate((True, False, False, True)):
+        p.draw()
+        cu.copy_(p.cu if fits else wide)
+        torch.cuda.synchronize()
+        g.replay(st)
+        torch.cuda.synchronize()
+        if not fits:
+            with pytest.raises(S.SeerError, match="free pages"):
+                p.caches[0].check()
+            continue
+        for _ in range(2):
+            slots = p.caches[1].plan(p.cu, 64)
+            for layer in p.layers:
+                p.caches[1].store(layer, p.k, p.v, 64, slots, q=p.q, q_out=p.qo[1])
+            p.cut(1)
+        p.same("replay %d" % turn)
+    p.caches[0].check()
