@@ -712,10 +712,11 @@ int seer_rope_turns(const seer_rope_desc* rope, int32_t head_dim, double* turns)
  * NULL).  Row r stands at positions[r] (device), 0 to 2^31 - 1; rows with a
  * negative position are left as they are, in the outputs too.  q_out may be q and
  * k_out k (with the same row stride); else outputs overlap no input.  q and k rows may lie in
- * one buffer beside each other.  turns: device.  The angle is taken in fp64 and
+ * one buffer beside each other.  turns: device.  rope NULL (and turns NULL): rows that
+ * do not turn, whose elements are copied bit for bit.  The angle is taken in fp64 and
  * reduced to half a turn, its sine and cosine and the products are fp32, and
  * the result is rounded once.
- * Errors: EINVAL (desc, rope, null pointers, rows or strides not aligned to 16
+ * Errors: EINVAL (desc, rope, only one of rope and turns, null pointers, rows or strides not aligned to 16
  * bytes, a stride below the row, rows_ub < 1, flags, the aliases above),
  * EUNSUPPORTED (desc). */
 int seer_rope_rows(const seer_attn_desc* desc, const seer_rope_desc* rope, const double* turns, int32_t flags,
@@ -724,7 +725,7 @@ int seer_rope_rows(const seer_attn_desc* desc, const seer_rope_desc* rope, const
 
 /* seer_kv_store with rotary positions: row r of k, rotated, and of v go to slot
  * slots[r] of the pool, and q is rotated to q_out as in seer_rope_rows (q and
- * q_out NULL: no queries).  The token's marks become weight 0 and number
+ * q_out NULL: no queries; rope and turns NULL: nothing turns, as there).  The token's marks become weight 0 and number
  * positions[r], in all heads (weight and number NULL: no marks).  Rows with a
  * negative position, a negative slot or one past the pool are skipped, their q
  * too.  The slots of one call are distinct.

@@ -377,7 +377,7 @@ struct RopeParams {
   size_t q_stride, k_stride, v_stride, q_out_stride, k_out_stride;
   int es;                      // bytes of an element
   int n_heads, n_kv, dim;
-  int rot;                     // dims that turn
+  int rot;                     // dims that turn, 0: none
   bool pairs, inverse;
   float magnitude;
   const double* turns;         // [rot / 2] turns a position

@@ -950,13 +950,15 @@ int seer_rope_turns(const seer_rope_desc* rope, int32_t head_dim, double* turns)
   return ok();
 }
 
-// what both rotary calls check and fill in; q may be NULL
+// what both rotary calls check and fill in; q may be NULL, and rope where nothing turns (in half layout, whose
+// dims behind the turned ones, here all, are copied as they are)
 static int rope_params(seer::RopeParams& p, const seer_attn_desc* desc, const seer_rope_desc* rope, const double* turns,
                        const void* q, int64_t q_stride, void* q_out, int64_t q_out_stride, int32_t rows_ub,
                        const int32_t* positions) {
   int rc = check_heads(desc);
   if (rc) return rc;
-  if ((rc = check_rope(rope, desc->head_dim))) return rc;
+  if (rope && (rc = check_rope(rope, desc->head_dim))) return rc;
+  if (!rope != !turns) return fail(SEER_EINVAL, "rope and turns go together");
   const int es = desc->dtype == SEER_DTYPE_BF16 ? 2 : 4;
   const int64_t width = (int64_t)desc->n_heads * desc->head_dim;
   if (!q != !q_out) return fail(SEER_EINVAL, "q and q_out go together");
@@ -964,13 +966,15 @@ static int rope_params(seer::RopeParams& p, const seer_attn_desc* desc, const se
     return rc;
   if (q && q == q_out && q_stride != q_out_stride) return fail(SEER_EINVAL, "q_out in q's place needs its row stride");
   if (rows_ub < 1) return fail(SEER_EINVAL, "rows_ub must be >= 1 (got %d)", rows_ub);
-  if (!turns || !positions) return fail(SEER_EINVAL, "a required pointer is NULL");
+  if (!positions) return fail(SEER_EINVAL, "positions is NULL");
   p.q = static_cast<const uint8_t*>(q); p.q_out = static_cast<uint8_t*>(q_out);
   p.q_stride = (size_t)q_stride * es; p.q_out_stride = (size_t)q_out_stride * es;
   p.es = es; p.n_heads = desc->n_heads; p.n_kv = desc->n_kv_heads; p.dim = desc->head_dim;
-  p.rot = rope_dims(rope, desc->head_dim); p.pairs = rope->layout == SEER_ROPE_PAIRS;
-  p.magnitude = rope->magnitude != 0.0f ? rope->magnitude
-                : rope->scaling == SEER_ROPE_RAMP ? (float)(0.1 * log((double)rope->factor) + 1.0) : 1.0f;
+  if (rope) {
+    p.rot = rope_dims(rope, desc->head_dim); p.pairs = rope->layout == SEER_ROPE_PAIRS;
+    p.magnitude = rope->magnitude != 0.0f ? rope->magnitude
+                  : rope->scaling == SEER_ROPE_RAMP ? (float)(0.1 * log((double)rope->factor) + 1.0) : 1.0f;
+  }
   p.turns = turns; p.positions = positions; p.rows_ub = rows_ub;
   return SEER_OK;
 }

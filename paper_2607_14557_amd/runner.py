@@ -444,11 +444,8 @@ class BudgetCache(PagedCache):
                  rope=None, dtype="bf16", v_f16=False, scale=0.0, device="cuda"):
         super().__init__(n_heads, n_kv_heads, head_dim, n_layers, n_pages, page_size, max_batch, max_len, max_rows,
                          dtype=dtype, v_f16=v_f16, scale=scale, device=device)
-        self._still = S.seer_rope_desc(S.SEER_ROPE_HALF, 2, S.SEER_ROPE_PLAIN, 0, 10000.0, 1.0, 0.0, 0.0, 0.0)
-        self._still_turns = torch.zeros(1, dtype=torch.float64, device=device)      # by no angle
-        self.rope, self.turns = self._still, self._still_turns
+        self.rope, self.turns = rope, None
         if rope is not None:
-            self.rope = rope
             self.turns = torch.tensor(S.seer_rope_turns(rope, head_dim), dtype=torch.float64, device=device)
         marks = (n_pages, n_kv_heads, page_size)
         self.weights = [torch.zeros(marks, dtype=torch.float32, device=device) for _ in range(n_layers)]
@@ -547,8 +544,8 @@ class BudgetCache(PagedCache):
         """As PagedCache.store_layer, with new marks: the layer's keys carry its own positions and are not rotated again."""
         self._whole(layer)
         k, d, es = self._layer_rows(layer, stack, rows_ub, slots)
-        S.seer_kv_store_rope(self.desc, self.pages, self._still, self._still_turns, None, 0, None, 0, k, 3 * d, k + d * es,
-                             3 * d, rows_ub, self._positions(rows_ub, None), self._slots(rows_ub, slots), self.pools[layer],
+        S.seer_kv_store_rope(self.desc, self.pages, None, None, None, 0, None, 0, k, 3 * d, k + d * es, 3 * d, rows_ub,
+                             self._positions(rows_ub, None), self._slots(rows_ub, slots), self.pools[layer],
                              self.weights[layer], self.numbers[layer], stream=stream)
 
     def attend(self, layer, q, out, cu, rows_ub, mask=S.SEER_MASK_CAUSAL, tree_bits=None, seqused=None, stream=None):

@@ -464,18 +464,22 @@ def seer_rope_turns(rope, head_dim):
     return list(out)[:(rope.rotary_dim or int(head_dim)) // 2]
 
 
+def _rope(rope):
+    return None if rope is None else ctypes.byref(rope)
+
+
 def seer_rope_rows(desc, rope, turns, flags, q, q_stride, k, k_stride, q_out, q_out_stride, k_out, k_out_stride, rows_ub,
                    positions, stream=None):
     """turns: fp64 device tensor of seer_rope_turns."""
     _check(load_library().seer_rope_rows(
-        ctypes.byref(desc), ctypes.byref(rope), _ptr(turns), int(flags), _ptr(q), int(q_stride), _ptr(k), int(k_stride),
+        ctypes.byref(desc), _rope(rope), _ptr(turns), int(flags), _ptr(q), int(q_stride), _ptr(k), int(k_stride),
         _ptr(q_out), int(q_out_stride), _ptr(k_out), int(k_out_stride), int(rows_ub), _ptr(positions), _stream(stream)))
 
 
 def seer_kv_store_rope(desc, pages, rope, turns, q, q_stride, q_out, q_out_stride, k, k_stride, v, v_stride, rows_ub,
                        positions, slots, pool, weight, number, stream=None):
     _check(load_library().seer_kv_store_rope(
-        ctypes.byref(desc), ctypes.byref(pages), ctypes.byref(rope), _ptr(turns), _ptr(q), int(q_stride), _ptr(q_out),
+        ctypes.byref(desc), ctypes.byref(pages), _rope(rope), _ptr(turns), _ptr(q), int(q_stride), _ptr(q_out),
         int(q_out_stride), _ptr(k), int(k_stride), _ptr(v), int(v_stride), int(rows_ub), _ptr(positions), _ptr(slots),
         _ptr(pool), _ptr(weight), _ptr(number), _stream(stream)))
 

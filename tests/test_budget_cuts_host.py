@@ -161,3 +161,25 @@ def test_evict_planned_refusals(S):
         assert call(**{n: None}) == S.SEER_EINVAL, n
     for kw in (dict(status=4 * FAKE), dict(flags=2), dict(flags=8), dict(batch=0), dict(kept=FAKE), dict(bytes=16, flags=4)):
         assert call(**kw) in (S.SEER_EINVAL, S.SEER_EWORKSPACE), kw
+
+
+def test_rope_that_is_none(S, calls):
+    """Rows that do not turn have neither a description nor frequencies; one without the other is refused."""
+    from paper_2607_14557_amd.runner import BudgetCache
+    c, cu = BudgetCache(H, KV, D, 1, 4, 16, B, 32, ROWS, device="cpu"), _i32(B + 1)
+    c.plan(cu, ROWS)
+    c.store(0, _bf16(ROWS, KV * D), _bf16(ROWS, KV * D), ROWS)
+    c.rotate(_bf16(ROWS, H * D), None, ROWS)
+    assert calls[-2][0] == "seer_kv_store_rope" and calls[-2][1][2:4] == (None, None)
+    assert calls[-1][0] == "seer_rope_rows" and calls[-1][1][1:3] == (None, None)
+    L, d, p = S.load_library(), S.seer_attn_desc(H, KV, D, S.SEER_DTYPE_BF16, 0, 0.0), S.seer_page_desc(16, 4, 2)
+    r = rope(S)
+    for desc, turns in ((None, FAKE), (ctypes.byref(r), None)):
+        assert L.seer_rope_rows(ctypes.byref(d), desc, turns, 0, FAKE, 256, None, 0, FAKE, 256, None, 0, 4, FAKE, None) == S.SEER_EINVAL
+        assert "go together" in S.seer_last_error()
+        assert L.seer_kv_store_rope(ctypes.byref(d), ctypes.byref(p), desc, turns, None, 0, None, 0, FAKE, 128, FAKE, 128, 4, FAKE,
+                                    FAKE, FAKE, FAKE, FAKE, None) == S.SEER_EINVAL
+    # without either, the other checks stand
+    assert L.seer_rope_rows(ctypes.byref(d), None, None, 0, FAKE, 256, None, 0, FAKE, 256, None, 0, 4, None, None) == S.SEER_EINVAL
+    assert L.seer_kv_store_rope(ctypes.byref(d), ctypes.byref(p), None, None, None, 0, None, 0, FAKE, 128, FAKE, 128, 4, FAKE,
+                                None, FAKE, FAKE, FAKE, None) == S.SEER_EINVAL
