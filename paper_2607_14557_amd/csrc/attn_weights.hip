@@ -5,7 +5,9 @@
 //
 // per key/value head.  A row's sum is known when all its keys have been seen, so there are
 // two passes; each weight is added up by one wave, or by one for each part of the rows and
-// then part after part: no atomics, the same bits every time.  Three forms, by the call's bounds (dispatch.h):
+// then part after part: no atomics, the same bits every time.  A lane adds a tile's rows up by
+// themselves and then to its sum: thousands of equal terms, one after the other, end off by as many
+// half steps to one side.  Three forms, by the call's bounds (dispatch.h):
 //
 //   bf16, many rows   weights_stats_tile_kernel: 128 rows stay in registers, keys pass by in
 //                     LDS tiles of 64 (S^T = K Q^T, a lane owns a row); where the rows' tiles
@@ -640,6 +642,7 @@ __global__ __launch_bounds__(NT, 4) void weights_sum_tile_kernel(WeightsParams p
         seen >>= 4 * (lane >> 5);
         const float* lse = &lse_lds[rt % (ROWS / TILE) * TILE + 4 * (lane >> 5)];
         // (two copies, so that a half's sums do not wait for the branch)
+        float own = 0.0f;                        // of this tile's rows
         auto add = [&](auto blinded) {
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
@@ -652,13 +655,14 @@ __global__ __launch_bounds__(NT, 4) void weights_sum_tile_kernel(WeightsParams p
 #pragma unroll
               for (int r = 0; r < 4; ++r) {
                 const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(a[4 * g + r], c, -x[r]));
-                sum += !decltype(blinded)::value || (half >> (8 * g + r) & 1) ? w : 0.0f;
+                own += !decltype(blinded)::value || (half >> (8 * g + r) & 1) ? w : 0.0f;
               }
             }
           }
         };
         if (masked) add(std::true_type{});
         else add(std::false_type{});
+        sum += own;
       }
       __builtin_amdgcn_s_waitcnt(0x0f70);
       __syncthreads();
@@ -981,6 +985,7 @@ __global__ __launch_bounds__(NT) void weights_few_kernel(WeightsParams p) {
           f32x4_t x[8];                          // on their way together; rows past the last are the last again
 #pragma unroll
           for (int i = 0; i < 8; ++i) x[i] = *reinterpret_cast<const f32x4_t*>(from + (r + i < n ? r + i : n - 1) * p.places);
+          f32x4_t own = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             const float l = r + i < n ? lse[r + i] : INFINITY;
@@ -988,9 +993,11 @@ __global__ __launch_bounds__(NT) void weights_few_kernel(WeightsParams p) {
             for (int e = 0; e < 4; ++e) {
               // (by its bits: of a row whose logarithm is NaN, -inf would give NaN to keys that it does not see)
               const float w = __builtin_amdgcn_exp2f(x[i][e] * scale_of(p) - l);
-              sum[e] += __float_as_uint(x[i][e]) == kUnseen ? 0.0f : w;
+              own[e] += __float_as_uint(x[i][e]) == kUnseen ? 0.0f : w;
             }
           }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sum[e] += own[e];
         }
       }
       __syncthreads();
@@ -1050,6 +1057,7 @@ __global__ __launch_bounds__(NT) void weights_sum_kernel(WeightsParams p) {
       const float lse = top + __builtin_amdgcn_logf(all);
       const int sure = p.mask == kMaskCausal ? s.past + s.index0 + token_of(p, r0) + 1 : (p.mask == kMaskTree ? s.past : s.nk);
       const bool masked = k0 + T > sure || r0 + T > s.rows;
+      float own = 0.0f;
 #pragma unroll
       for (int r = 0; r < Tile::ACC; ++r) {
         float w = __builtin_amdgcn_exp2f(a[r] * c - __shfl(lse, Tile::of(lane, r), kWave));
@@ -1058,8 +1066,9 @@ __global__ __launch_bounds__(NT) void weights_sum_kernel(WeightsParams p) {
           const bool see = j < s.rows && sees(p, s, s.row0 + it, s.index0 + it, key);
           w = see ? w : 0.0f;
         }
-        sum += w;
+        own += w;
       }
+      sum += own;
     };
     // the first row that sees a key of the tile, in whole tiles
     int from = wave * T;

@@ -63,3 +63,29 @@ def test_rows_of_nan(S, tmp_path, kind, want, pad, mask):
     for j in range(25):
         at = (c.table[1, j // 16], slice(None), j % 16)
         assert np.array_equal(got[at], clean[at]), "the other request, token %d" % j
+
+
+@pytest.mark.parametrize("kind,want,H,KV,D,rows,keys", [("bf16", "tiles", 64, 16, 64, 4096, 8000), ("bf16", "tiles", 4, 1, 128, 4000, 600),
+                                                        ("bf16", "scores", 4, 1, 128, 1000, 2100), ("f32", "f32", 8, 1, 4, 2000, 300)])
+def test_many_equal_rows(S, tmp_path, kind, want, H, KV, D, rows, keys):
+    """Thousands of equal probabilities: every key has n / keys, and the sum's error does not grow with n roundings to the
+    same side.
+
+    Bound, relative to n / keys: the logarithm of a row's sum, log2 keys < 13, is off by 2^-20 whatever the parts, so p by
+    2^-20 and the exponential's 2^-21 (ln 2 below 1).  Of the sum's additions, each at most 2^-24: up to 32 within a tile of
+    rows, one a tile, at most rows a lane / 64 tiles (scores: 8 and a / 8; fp32: 4 and a quarter of a / 16), a few to join
+    lanes and parts."""
+    import torch
+    n = rows * (H // KV)
+    fill = -(-n // 16) if want == "scores" else 1      # requests without rows, so that rows are few on average
+    c = Call(S, kind, H, KV, D, [keys - rows] + [0] * (fill - 1), [rows] + [0] * (fill - 1), pad=0, page=64)
+    assert form(tmp_path, c) == want
+    c.pool[:, 0] = 0.0                                 # every score is 0
+    c.run("none", prev=False)
+    got = host(c.weight).transpose(0, 2, 1).reshape(-1, KV)
+    at = np.array([int(c.table[0, j // 64]) * 64 + j % 64 for j in range(keys)])
+    in_tile, tiles = {"tiles": (32, n // 64 + 1), "scores": (8, n // 8 + 1), "f32": (4, n // 64 + 1)}[want]
+    tol = 2.0 ** -20 + 2.0 ** -21 + (in_tile + tiles + 24) * 2.0 ** -24
+    err = np.abs(got[at] * keys / n - 1.0).max()
+    log("  %s %d rows of %d: off by %.2e, bound %.2e" % (want, n, keys, err, tol))
+    assert err <= tol
