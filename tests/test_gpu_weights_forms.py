@@ -89,3 +89,100 @@ def test_many_equal_rows(S, tmp_path, kind, want, H, KV, D, rows, keys):
     err = np.abs(got[at] * keys / n - 1.0).max()
     log("  %s %d rows of %d: off by %.2e, bound %.2e" % (want, n, keys, err, tol))
     assert err <= tol
+
+
+@pytest.mark.parametrize("mask", ["causal", "none", "tree"])
+@pytest.mark.parametrize("H,KV,D", [(4, 2, 64), (7, 1, 128), (8, 8, 64)])
+def test_tiles_with_pages_that_are_none(S, tmp_path, H, KV, D, mask):
+    """Missing pages of 16 keys at each place of a tile of 64, whole tiles of them, the first and the last page of a
+    request, before the call's rows and among them: seen by no row, written by none."""
+    past, lens = [250, 64, 0, 33], [40, 70, 50, 3]
+    for lost in ([0], [1], [2], [3], [4, 5, 6, 7], [0, 5, 10, 15, 17], [3, 4], [16, 18, 19]):
+        for last in (0, 40) if len(lost) > 1 else (0,):
+            c = Call(S, "bf16", H, KV, D, past, lens, bits=_bits(lens) if mask == "tree" else None)
+            for b in range(c.B):
+                held = -(-c.kv_len[b] // 16)
+                for i, j in enumerate(lost):
+                    c.table[b, j % held] = (-1, c.P, 1 << 30, -(1 << 31))[i % 4]
+                if lost == [3, 4]:
+                    c.table[b, held - 1] = -1
+            c.table_d = dev(c.table)
+            assert form(tmp_path, c, last) == "tiles"
+            c.run(mask, last=last)
+            c.check(mask, last=last)
+
+
+def test_tiles_of_a_request_without_pages(S, tmp_path):
+    """Every page missing: nothing is written, beside requests that have theirs."""
+    for mask in ("causal", "none", "tree"):
+        past, lens = [130, 70, 5], [50, 60, 70]
+        c = Call(S, "bf16", 4, 2, 64, past, lens, bits=_bits(lens) if mask == "tree" else None)
+        c.table[1, :] = -1
+        c.table_d = dev(c.table)
+        assert form(tmp_path, c) == "tiles"
+        c.run(mask)
+        c.check(mask)
+
+
+@pytest.mark.parametrize("H,KV,D", [(4, 2, 64), (3, 3, 128), (16, 8, 64)])
+def test_tiles_of_rows_that_see_nothing(S, tmp_path, H, KV, D):
+    """Rows with empty bits, some and all of a tile; caches that are shorter than the call's rows, so that the first ones
+    stand before the first key (causal), among them more than a tile of rows, and all but one."""
+    lens = [70, 40, 90, 33]
+    r = np.random.default_rng(1)
+    some = [b if r.random() < 0.4 else 0 for b in _bits(lens)]
+    for past, bits in (([0, 0, 0, 0], some), ([20, 0, 64, 1], some), ([0, 100, 0, 3], [0] * sum(lens))):
+        c = Call(S, "bf16", H, KV, D, past, lens, bits=bits)
+        assert form(tmp_path, c) == "tiles"
+        c.run("tree")
+        c.check("tree")
+    for past in ([-3, -39, -70, 0], [-69, -1, -89, -32], [-64, 5, -65, -31]):
+        c = Call(S, "bf16", H, KV, D, past, lens, pad=90)
+        assert form(tmp_path, c) == "tiles"
+        for mask in ("causal", "none"):
+            c.run(mask)
+            c.check(mask)
+        assert form(tmp_path, c, 60) == "tiles"
+        c.run("causal", last=60)
+        c.check("causal", last=60)
+
+
+@pytest.mark.parametrize("B", [129, 300])
+@pytest.mark.parametrize("H,KV,D,lens", [(8, 1, 64, (0, 12)), (2, 2, 128, (10, 40)), (8, 8, 64, (10, 40))])
+def test_tiles_of_many_requests(S, tmp_path, B, H, KV, D, lens):
+    """More requests than are kept beside the line, and more than threads: ragged, some without rows."""
+    r = np.random.default_rng(B)
+    n = [int(x) for x in r.integers(*lens, B)]
+    past = [int(x) for x in r.integers(0, 90, B)]
+    for mask in ("causal", "tree"):
+        c = Call(S, "bf16", H, KV, D, past, n, bits=_bits(n) if mask == "tree" else None)
+        assert form(tmp_path, c) == "tiles"
+        c.run(mask, decay=0.5)
+        c.check(mask, decay=0.5, requests=set(range(0, B, 13)) | {B - 1})
+
+
+def test_tiles_of_most_requests(S, tmp_path):
+    """As many requests as a call takes, with rows enough for tiles, most in one of them: the line is at its longest beside
+    the tiles and the logarithms."""
+    r = np.random.default_rng(9)
+    lens = [int(x) for x in r.integers(0, 3, 4096)]
+    lens[77] = 400
+    past = [int(x) for x in r.integers(0, 20, 4096)]
+    c = Call(S, "bf16", 16, 1, 128, past, lens)
+    assert form(tmp_path, c) == "tiles"
+    c.run("causal")
+    c.check("causal", requests=set(range(0, 4096, 61)) | {77})
+
+
+def test_tiles_in_parts_of_many_requests(S, tmp_path):
+    """Rows cut in parts for more than 128 requests: the launch that joins them finds its line by itself."""
+    B = 140
+    lens = [28] * B
+    lens[0], lens[139] = 200, 120
+    c = Call(S, "bf16", 16, 1, 64, [int(x) for x in np.random.default_rng(2).integers(0, 20, B)], lens, page=64)
+    assert form(tmp_path, c) == "tiles"
+    body = "int answer(const long long* v) { return weights_sums(v[0], (int)v[1], (int)v[2], (int)v[3], v[4]); }"
+    places = -(-c.W * c.page // 64) * 64
+    assert _ask(tmp_path, body, [(c.rows, B, 16, 1, places)])[0] > 1
+    c.run("causal")
+    c.check("causal", requests={0, 5, 138, 139})
