@@ -471,11 +471,13 @@ class BudgetCache(PagedCache):
             raise ValueError("layer %d is cut: the next call is plan()" % layer)
 
     @staticmethod
-    def _apart(name, x, written):
+    def _apart(name, x, *written):
         """Refuse an argument that shares memory with what the same call writes."""
-        if x is not None:
-            a, b = x.data_ptr(), written.data_ptr()
-            if a < b + 4 * written.numel() and b < a + x.numel() * x.element_size():
+        a = x.data_ptr()
+        end = a + x.numel() * x.element_size()
+        for w in written:
+            b = w.data_ptr()
+            if a < b + 4 * w.numel() and b < end:
                 raise ValueError("%s may not be in a buffer that the plan writes" % name)
 
     def plan(self, cu, rows_ub, keep=None, seqused=None, base=None, stream=None):
@@ -484,8 +486,8 @@ class BudgetCache(PagedCache):
             self._ints("base", base, self.max_batch)
         # (before the pages are planned: the positions come behind them)
         for name, x in (("cu", cu), ("seqused", seqused), ("base", base)):
-            self._apart(name, x, self.kept)
-            self._apart(name, x, self._seen[1])
+            if x is not None:
+                self._apart(name, x, self.kept, self._seen[1])
         if self._cut:
             if len(self._cut) < len(self.pools):
                 raise ValueError("%d of %d layers are cut: a plan comes after all or none" % (len(self._cut), len(self.pools)))
