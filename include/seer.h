@@ -794,7 +794,7 @@ int seer_attn_weights(const seer_attn_desc* desc, const seer_page_desc* pages, i
 /* And one for the layers of a cache after the first: kept holds what the layers that
  * are cut already keep.  N is at most that; where budget[b] asks for another length,
  * kept[b] becomes -1 - N: the layers were not cut alike, and a plan with this `keep`
- * is refused. */
+ * is refused.  budget may be kept: as many as they keep. */
 #define SEER_EVICT_ALIKE 4
 
 /* Workspace bytes of seer_kv_evict; 0 for a bad description. */

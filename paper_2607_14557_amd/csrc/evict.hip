@@ -42,17 +42,17 @@ struct Request {
 __device__ __forceinline__ Request request(const EvictParams& p, int b) {
   Request r;
   const long long most = (long long)p.width << p.shift;
-  const int L = p.kv_len[b], N = p.budget[b];
+  const int L = p.kv_len[b];
   r.seen = p.seen[b];                            // on its way with the others
-  const int others = p.alike ? p.kept[b] : 0;
+  const int others = p.alike ? p.kept[b] : 0, least = others < 0 ? -1 - others : others;
+  const int N = p.budget ? p.budget[b] : least;
   r.refused = p.status && *p.status != 0;
   r.L = L < 0 || r.refused ? 0 : (L > most ? (int)most : L);
   r.N = r.kept = N < 0 ? 0 : (N < r.L ? N : r.L);
   if (p.alike) {
-    // (a workgroup that reads what another one of the request has written already finds the same N)
-    const int least = others < 0 ? -1 - others : others;
+    // (who reads what another workgroup of the request has written already finds the same N)
     r.N = r.N < least ? r.N : least;
-    r.kept = r.kept == others ? r.kept : -1 - r.N;
+    r.kept = r.kept == others ? others : -1 - r.N;
   }
   r.table = p.table + (size_t)b * p.width;
   return r;

@@ -447,7 +447,7 @@ int launch_weights(const WeightsParams& p, hipStream_t s);
 struct EvictParams {
   int shift, n_pages, width;
   const int* kv_len;
-  const int* budget;
+  const int* budget;           // or null (alike): what other layers keep
   const int* seen;
   int B, first, recent;
   bool shared;

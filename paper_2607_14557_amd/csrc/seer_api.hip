@@ -1177,6 +1177,7 @@ static int kv_evict(const seer_attn_desc* desc, const seer_page_desc* pages, int
   p.kv_len = kv_len; p.budget = budget; p.seen = seen; p.B = batch; p.first = first; p.recent = recent;
   p.shared = (flags & SEER_EVICT_SHARED) != 0;
   p.alike = (flags & SEER_EVICT_ALIKE) != 0;
+  if (p.alike && budget == kept) p.budget = nullptr;
   p.status = status;
   p.lists = p.shared ? 1 : desc->n_kv_heads;
   if ((long long)batch * p.lists >= 1 << 20)

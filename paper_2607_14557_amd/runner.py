@@ -478,7 +478,7 @@ class BudgetCache(PagedCache):
         for w in written:
             b = w.data_ptr()
             if a < b + 4 * w.numel() and b < end:
-                raise ValueError("%s may not be in a buffer that the plan writes" % name)
+                raise ValueError("%s may not be in a buffer that the call writes" % name)
 
     def plan(self, cu, rows_ub, keep=None, seqused=None, base=None, stream=None):
         """The pages, slots and positions of a step; returns the slots of its rows."""
@@ -575,6 +575,8 @@ class BudgetCache(PagedCache):
         self._takes(0)
         self._whole(layer)
         self._ints("budget", budget, self.max_batch)
+        if budget.data_ptr() != self.kept.data_ptr():
+            self._apart("budget", budget, self.kept)
         w, n = self.weights[layer], self.numbers[layer]
         flags = (S.SEER_EVICT_SHARED if shared else 0) | (S.SEER_EVICT_ALIKE if self._cut else 0)
         S.seer_kv_evict(self.desc, self.pages, flags, self._lens[0], budget, self._seen[0],

@@ -183,3 +183,17 @@ def test_rope_that_is_none(S, calls):
     assert L.seer_rope_rows(ctypes.byref(d), None, None, 0, FAKE, 256, None, 0, FAKE, 256, None, 0, 4, None, None) == S.SEER_EINVAL
     assert L.seer_kv_store_rope(ctypes.byref(d), ctypes.byref(p), None, None, None, 0, None, 0, FAKE, 128, FAKE, 128, 4, FAKE,
                                 None, FAKE, FAKE, FAKE, None) == S.SEER_EINVAL
+
+
+def test_budget_within_kept(S, calls):
+    """The lengths that the layers before keep may be the budget of the next one; part of them, moved, may not."""
+    c, cu = _cache(S), _i32(B + 1)
+    whole = c.kept = _i32(3 * B)[:B]
+    c.plan(cu, ROWS)
+    c.evict(0, _i32(B))
+    c.evict(1, c.kept)
+    assert calls[-1][1][4] is c.kept and calls[-1][1][2] == S.SEER_EVICT_ALIKE
+    c.plan(cu, ROWS)
+    with pytest.raises(ValueError, match="budget"):
+        c.evict(0, whole.as_strided((B,), (1,), whole.storage_offset() + 1))
+    c.evict(0, whole.as_strided((B,), (1,), whole.storage_offset() + B))

@@ -281,3 +281,30 @@ def test_recorded_steps_behind_a_refused_plan(S):
             p.cut(1)
         p.same("replay %d" % turn)
     p.caches[0].check()
+
+
+@pytest.mark.parametrize("shared", [False, True])
+@pytest.mark.parametrize("n", [60, 2400, 9000, 17000])
+def test_budget_of_the_layers_before(S, shared, n):
+    """kept as the budget of the next layer: cut as with a copy of it, whatever it says, in each kernel of the choice and by
+    many workgroups of a request."""
+    import torch
+    kv, page, D = 8, 64, 4
+    P = -(-n // page)
+    d, pages = S.seer_attn_desc(kv, kv, D, S.SEER_DTYPE_F32, 0, 0.0), S.seer_page_desc(page, P, P)
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    pool0 = torch.randn(P, 2, kv, page, D, device="cuda", generator=gen)
+    w0 = torch.rand(P, kv, page, device="cuda", generator=gen)
+    table, lens, seen = dev(np.arange(P)[None]), dev(np.array([n])), dev(np.array([n]))
+    ws = torch.empty(S.seer_kv_evict_workspace_bytes(d, pages, 1), dtype=torch.uint8, device="cuda")
+    flags = S.SEER_EVICT_ALIKE | (S.SEER_EVICT_SHARED if shared else 0)
+    for kept0, want, left in ((n // 3, n // 3, n // 3), (-1 - n // 4, -1 - n // 4, n // 4), (n + 9, -1 - n, n), (0, 0, 0), (-1, -1, 0)):
+        got = []
+        for alias in (False, True):
+            pool, w, number = pool0.clone(), w0.clone(), torch.zeros(P, kv, page, dtype=torch.int32, device="cuda")
+            kept = dev(np.array([kept0]))
+            budget = kept if alias else dev(np.array([kept0 if kept0 >= 0 else -1 - kept0]))
+            S.seer_kv_evict(d, pages, flags, lens, budget, seen, 1, 0, 0, table, pool, w, number, w, number, kept, ws)
+            got.append((pool, w, host(kept).tolist()))
+        assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+        assert got[1][2] == [want] and got[0][2] == [left if kept0 == left else -1 - left], (kept0, got)
