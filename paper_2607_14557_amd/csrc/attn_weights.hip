@@ -22,12 +22,12 @@
 //   fp32              weights_stats_kernel and weights_sum_kernel, tiles of 16 x 16 a wave.
 //
 // Measured (MI355X, us a call among others; in brackets its kernels, medians of 30 passes in the
-// profiler, together up to a tenth more): 3076 rows of 16 requests over 793 cached keys
-// each and their own, 32 heads: 105 (53 and 65, at least 50 and 60); 64 rows each of 7 prompts of
-// 1500 to 8192 tokens, 32 heads on 8: 58 (30 and 33); a token of 64 requests over 294,950 keys, 28
-// heads on 4: 90 (68, which read the keys at 4.4 TB/s, and 14); one token over 794 keys: 12 (7 and
-// 6); trees of drafted tokens in fp32 over 1198 keys: 18.3 (7.5 and 11.6); all 32,267 rows of 7
-// prompts, 32 heads on 8, 1.5 TFLOP: 2140 (700 TFLOP/s).
+// profiler, together up to a tenth more): 3076 rows of 16 requests over 793 cached keys each and
+// their own, 32 heads: 103 to 111 over machines (53 and 65, at least 50 and 60); 64 rows each of 7
+// prompts of 1500 to 8192 tokens, 32 heads on 8: 58 (30 and 33); a token of 64 requests over 294,950
+// keys, 28 heads on 4: 90 (68, which read the keys at 4.4 TB/s, and 14); one token over 794 keys: 12
+// (7 and 6); trees of drafted tokens in fp32 over 1198 keys: 18.3 (7.5 and 11.6); all 32,267 rows of
+// 7 prompts, 32 heads on 8, 1.5 TFLOP: 2140 (700 TFLOP/s).
 #include <limits.h>
 
 #include <type_traits>

@@ -298,7 +298,6 @@ struct PagePlanParams {
   int width;             // entries of a row of the table
   const int* held;
   const int* keep;
-  const int* kept;       // [B] tokens that an eviction has left, or null
   const int* cu;
   const int* used;       // [B] or null
   int B;
@@ -312,7 +311,8 @@ struct PagePlanParams {
   int* status;
   int* refused;          // or null
 };
-int launch_page_plan(const PagePlanParams& p, hipStream_t s);
+// kept: [B] tokens that an eviction has left, or null
+int launch_page_plan(const PagePlanParams& p, const int* kept, hipStream_t s);
 
 struct KvStoreParams {
   const uint8_t* k;

@@ -733,10 +733,10 @@ static int page_plan(const seer_page_desc* pages, const int32_t* held, const int
     return fail(SEER_EINVAL, "free_out may not be free_in, kv_len neither held nor keep");
   seer::PagePlanParams p{};
   p.shift = page_shift(pages); p.n_pages = pages->n_pages; p.width = pages->table_width;
-  p.held = held; p.kept = kept; p.keep = keep; p.cu = cu_seqlens; p.used = seqused; p.B = batch; p.rows_ub = rows_ub;
+  p.held = held; p.keep = keep; p.cu = cu_seqlens; p.used = seqused; p.B = batch; p.rows_ub = rows_ub;
   p.free_pages = free_pages; p.free_in = free_in; p.free_out = free_out;
   p.table = table; p.kv_len = kv_len; p.slots = slots; p.status = status; p.refused = refused;
-  if (seer::launch_page_plan(p, stream)) return hip_fail("page plan launch");
+  if (seer::launch_page_plan(p, kept, stream)) return hip_fail("page plan launch");
   return ok();
 }
 
