@@ -308,3 +308,44 @@ def test_budget_of_the_layers_before(S, shared, n):
             got.append((pool, w, host(kept).tolist()))
         assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
         assert got[1][2] == [want] and got[0][2] == [left if kept0 == left else -1 - left], (kept0, got)
+
+
+@pytest.mark.parametrize("n", [1, 3, 300, 4096])
+def test_plan_of_what_is_kept(S, n):
+    """With all tokens kept, or just those that are asked for, the plan is the plan; a keep above kept of one request, or a
+    kept below zero as the keep, refuses it whole."""
+    import torch
+    r = np.random.default_rng(n)
+    page, width = 16, 6
+    held = r.integers(0, page * width - 3, n)
+    keep = (held * r.random(n)).astype(int)
+    cu = np.concatenate([[0], np.cumsum(r.integers(0, 4, n))])
+    rows, need = int(cu[-1]) + 5, -(-held // page)
+    P = int(need.sum()) + n
+    table0, at = np.full((n, width), -1), 0
+    for b in range(n):
+        table0[b, :need[b]] = np.arange(at, at + need[b])
+        at += need[b]
+    free0 = np.full(P, -1)
+    free0[:P - at] = np.arange(at, P)
+
+    def plan(keep, kept):
+        free, table, f_in, f_out = dev(free0), dev(table0), dev(np.array([P - at])), dev(np.array([0]))
+        kv, slots, status, refused = dev(np.zeros(n, int)), dev(np.full(rows, 77)), dev(np.array([9])), dev(np.array([0]))
+        S.seer_page_plan_latched(S.seer_page_desc(page, P, width), dev(held), dev(keep), dev(cu), None, n, rows, free, f_in, f_out,
+                                 table, kv, slots, status, refused, kept=None if kept is None else dev(kept))
+        return [free, table, f_out, kv, slots, status, refused]
+
+    want = plan(keep, None)
+    assert host(want[5]).item() == 0
+    for kept in (held, keep, -1 - held, -1 - keep):
+        assert all(torch.equal(x, y) for x, y in zip(want, plan(keep, kept)))
+    one = np.flatnonzero(keep)
+    if one.size:
+        b = one[-1]
+        for kept in (np.where(np.arange(n) == b, keep - 1, held), np.where(np.arange(n) == b, -keep, -1 - held)):
+            free, table, f_out, kv, slots, status, refused = plan(keep, kept)
+            assert host(status).item() == host(refused).item() == S.SEER_PAGES_INVALID and (host(slots) == -1).all()
+            assert np.array_equal(host(table), table0) and np.array_equal(host(free), free0) and np.array_equal(host(kv), held)
+            assert host(f_out).item() == P - at
+    assert host(plan(-1 - keep, -1 - keep)[5]).item() == S.SEER_PAGES_INVALID
