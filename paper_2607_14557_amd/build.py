@@ -17,7 +17,7 @@ CSRC = os.path.join(PKG, "csrc")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libseer.so")
 SOURCES = ["seer_api.hip", "gemm_bf16.hip", "attn_bf16.hip", "attn_gqa.hip", "attn_gqa_f32.hip",
-           "f32_kernels.hip", "rows.hip", "pages.hip", "rope.hip", "attn_weights.hip", "evict.hip"]
+           "f32_kernels.hip", "rows.hip", "pages.hip", "pages_kept.hip", "rope.hip", "attn_weights.hip", "evict.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 CFLAGS = ["--offload-arch=" + ARCH, "-O3", "-std=c++17", "-fPIC",

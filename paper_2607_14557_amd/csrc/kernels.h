@@ -311,8 +311,8 @@ struct PagePlanParams {
   int* status;
   int* refused;          // or null
 };
-// kept: [B] tokens that an eviction has left, or null
-int launch_page_plan(const PagePlanParams& p, const int* kept, hipStream_t s);
+int launch_page_plan(const PagePlanParams& p, hipStream_t s);
+int launch_page_plan_kept(const PagePlanParams& p, const int* kept, hipStream_t s);
 
 struct KvStoreParams {
   const uint8_t* k;

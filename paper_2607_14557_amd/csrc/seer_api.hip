@@ -1,7 +1,7 @@
 // C ABI of the Seer hot path: argument checks, workspace layout and the launch
 // sequence of each entry point.  Kernels live in gemm_bf16.hip, attn_bf16.hip,
-// attn_gqa.hip, attn_gqa_f32.hip, f32_kernels.hip, rows.hip, pages.hip, rope.hip,
-// attn_weights.hip and evict.hip.
+// attn_gqa.hip, attn_gqa_f32.hip, f32_kernels.hip, rows.hip, pages.hip, pages_kept.hip,
+// rope.hip, attn_weights.hip and evict.hip.
 #include <math.h>
 #include <stdarg.h>
 #include <stdio.h>
@@ -736,7 +736,7 @@ static int page_plan(const seer_page_desc* pages, const int32_t* held, const int
   p.held = held; p.keep = keep; p.cu = cu_seqlens; p.used = seqused; p.B = batch; p.rows_ub = rows_ub;
   p.free_pages = free_pages; p.free_in = free_in; p.free_out = free_out;
   p.table = table; p.kv_len = kv_len; p.slots = slots; p.status = status; p.refused = refused;
-  if (seer::launch_page_plan(p, kept, stream)) return hip_fail("page plan launch");
+  if (kept ? seer::launch_page_plan_kept(p, kept, stream) : seer::launch_page_plan(p, stream)) return hip_fail("page plan launch");
   return ok();
 }
 
